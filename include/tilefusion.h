@@ -46,7 +46,8 @@ typedef enum {
     TF_EMISMATCH = 6      /* plan and call disagree (dtype, kind of B, shape of B)            */
 } tf_status;
 
-typedef enum { TF_F32 = 0, TF_F64 = 1 } tf_dtype;
+/* The chain D = A (B C) runs in fp32 and fp64, the routed operators (below) in fp32, bf16 and fp16. */
+typedef enum { TF_F32 = 0, TF_F64 = 1, TF_BF16 = 2, TF_F16 = 3 } tf_dtype;
 
 /* A CSR matrix.  Caller-owned, read-only.  on_device tells where the three arrays live
  * (all three in the same place). */
@@ -297,6 +298,124 @@ tf_status tf_plan_workspace_unfused(const tf_plan *plan, void **d1_device);
  * rowptr[0] = 0, rowptr monotone, rowptr[n_rows] = nnz, 0 <= column < n_cols.  TF_OK or
  * TF_EBADCSR.  Synchronous; meant for a CSR B before it is handed to tf_spmm_spmm. */
 tf_status tf_csr_validate(const tf_csr *M);
+
+/* ------------------------------------------------------------------------------------------------
+ * Routed operators: the chain in which every column of A has dense operands of its own.
+ *
+ * A is a routing matrix, tokens x experts, in CSR with a few entries in a row; a row of D is
+ *     D[t] = sum over the entries q of row t of  A_q f_e(X[t]),   e = column of q,
+ *     f_e(x) = ( act(x Wg_e^T) o (x Wu_e^T) ) Wd_e^T      or, without a gate,  act(x Wu_e^T) Wd_e^T
+ * (mixture of experts).  The calls are made for the few tokens of a decoding batch, where the weights
+ * that the tokens meet have to be read once and this is what takes the time; they are right for any
+ * number of tokens, but read an expert's weights again for every 64 entries that name it.
+ *
+ * Conventions besides those at the top of this file
+ *   - Element types are TF_F32, TF_BF16 and TF_F16.  Products of 16-bit numbers are summed in 32 bits;
+ *     results are rounded once, to nearest even.
+ *   - X, D, Y and scores may have rows that are further apart than they are wide (ldx, ldd, ...,
+ *     in elements).  Their pointers need the alignment of one element; weights and codes 16 bytes.
+ *   - A row's values never reach another row: infinities and NaN stay in the rows that hold them.
+ *   - Calls are asynchronous on `hip_stream`, allocate nothing and never synchronise, unless their
+ *     comment says so; they may be captured into a graph.  Results do not vary from run to run.
+ */
+
+/* Stacked matrices with weights of 4 bits: n_mats matrices of n_rows outputs x n_cols inputs.  A weight
+ * is the value of its code times the scale of its group, `group` consecutive inputs of one output:
+ *   TF_Q4_INT   codes -7 .. 7
+ *   TF_Q4_E2M1  0, 0.5, 1, 1.5, 2, 3, 4, 6 (codes 0 .. 7) and their negatives (codes 8 .. 15)
+ * Scales are bf16 (powers of two between 2^-126 and 2^127 are exact in it).  codes and scales are device
+ * arrays of the caller's, in the library's own order, of the sizes that tf_q4_sizes tells; tf_q4_pack and
+ * tf_q4_quantize write them. */
+#define TF_Q4_INT 0
+#define TF_Q4_E2M1 1
+typedef struct tf_q4 {
+    int64_t n_mats;
+    int64_t n_rows;
+    int64_t n_cols;
+    void *codes;      /* 16-byte aligned */
+    void *scales;     /* 16-byte aligned */
+    int32_t kind;     /* TF_Q4_* */
+    int32_t group;    /* 32, 64 or 128 */
+} tf_q4;
+
+/* Bytes of the two arrays; W->codes and W->scales are not looked at. */
+tf_status tf_q4_sizes(const tf_q4 *W, int64_t *codes_bytes, int64_t *scales_bytes);
+
+/* Fills the arrays of *W from codes, one int8 each (n_mats x n_rows x n_cols; E2M1 codes as 0 .. 15), and
+ * bf16 scales (n_mats x n_rows x ceil(n_cols / group)); both on the device.  Codes outside of the kind's
+ * range make the call fail with TF_EINVAL (the arrays are then not to be used).  Allocates a word for that
+ * and waits for the stream: for the time when weights are loaded. */
+tf_status tf_q4_pack(const tf_q4 *W, const int8_t *codes, const void *scales_bf16, void *hip_stream);
+
+/* Fills the arrays of *W from weights (n_mats x n_rows x n_cols, `dtype`, on the device): the scale of a group
+ * is its largest magnitude over the largest code value (7 or 6) rounded to bf16, a code is the value nearest
+ * to weight / scale (halfway cases to the even code) within the kind's range.  A group of zeros has scale 0.
+ * Weights are to be finite: a group with an infinity or a NaN comes out as NaN. */
+tf_status tf_q4_quantize(const tf_q4 *W, const void *weights, int32_t dtype, void *hip_stream);
+
+/* The weights that *W stands for, rounded to `dtype` (n_mats x n_rows x n_cols, contiguous). */
+tf_status tf_q4_unpack(const tf_q4 *W, int32_t dtype, void *weights, void *hip_stream);
+
+/* Y = X W^T for m rows of X (m x n_cols, rows ldx apart) and one matrix (n_mats = 1): Y is m x n_rows, rows ldy
+ * apart.  For a few rows: codes are read once for every 64. */
+tf_status tf_q4_matvec(const tf_q4 *W, const void *X, int64_t ldx, void *Y, int64_t ldy, int64_t m, int32_t dtype,
+                       void *hip_stream);
+
+/* Weights of the entries that tf_moe_route makes; all but the first row of the comment are taken of the scores
+ * without the bias, for the selected experts only. */
+#define TF_ROUTE_SOFTMAX 0      /* exp(l_e) / sum over all experts           */
+#define TF_ROUTE_SOFTMAX_TOP 1  /* exp(l_e) / sum over the selected experts  */
+#define TF_ROUTE_SIGMOID 2      /* 1 / (1 + exp(-l_e))                       */
+#define TF_ROUTE_SIGMOID_TOP 3  /* the same over its sum over the selected   */
+
+/* Router: from scores l (tokens x experts, rows ld apart, `dtype`) to the routing matrix A.  Each token gets the
+ * k = A->nnz / A->n_rows experts with the largest l + bias (32-bit sums; bias: n_cols floats on the device or
+ * NULL), in falling order, equal ones by their number; their weights (see above) are multiplied by `scale`.
+ * Scores of -inf and NaN are never selected (a NaN counts as -inf in every sum): a row with fewer than k others is
+ * filled up with entries of column -1 and value 0, which tf_moe_layer passes over.
+ * A describes the result: n_rows tokens, n_cols experts (1024 at most), nnz = k n_rows (k 64 at most), device
+ * arrays, dtype TF_F32.  The call WRITES its three arrays. */
+tf_status tf_moe_route(const void *scores, int64_t ld, int32_t dtype, const float *bias, int32_t scoring, float scale,
+                       const tf_csr *A, void *hip_stream);
+
+/* Activations act(x) */
+#define TF_ACT_IDENTITY 0
+#define TF_ACT_RELU 1
+#define TF_ACT_SILU 2           /* x / (1 + exp(-x))           */
+#define TF_ACT_GELU 3           /* x (1 + erf(x / sqrt 2)) / 2 */
+
+typedef struct tf_moe_desc {
+    int64_t n_experts;
+    int64_t n_in;         /* columns of X                                                     */
+    int64_t n_hidden;     /* columns between the two products                                 */
+    int64_t n_out;        /* columns of D                                                     */
+    int64_t max_tokens;   /* largest number of rows of X                                      */
+    int64_t max_entries;  /* largest number of stored entries of A                            */
+    int32_t dtype;        /* of X, D and dense weights                                        */
+    int32_t activation;   /* TF_ACT_*                                                         */
+    int32_t gated;        /* 1: W1 holds the n_hidden rows of the gate, then those it multiplies */
+    int32_t reserved0;
+} tf_moe_desc;
+
+typedef struct tf_moe tf_moe; /* opaque, library-owned: the sizes above and a workspace */
+
+/* Allocates the workspace (max_entries rows between the products).  On failure *out is NULL. */
+tf_status tf_moe_create(const tf_moe_desc *desc, tf_moe **out);
+/* Frees it.  NULL is accepted. */
+tf_status tf_moe_destroy(tf_moe *plan);
+
+/* D = the layer of X (A->n_rows x n_in, rows ldx apart; D: A->n_rows x n_out, rows ldd apart).  W1 is n_experts x
+ * (2 n_hidden or n_hidden) x n_in, W2 n_experts x n_out x n_hidden, both contiguous, each row the weights of one
+ * output.  A: device arrays, values TF_F32, at most max_tokens rows and max_entries entries, any number of them
+ * in a row; entries whose column is not one of the experts are passed over, whatever their value; a row without
+ * entries gives a row of zeros.  A's arrays are not validated (see tf_spmm_spmm).  What lies between the products is
+ * held in 16 bits or more of precision (TF_F16: magnitudes up to 2^28, larger ones become infinite).
+ * Two executions of one plan must not overlap (they share its workspace). */
+tf_status tf_moe_layer(const tf_moe *plan, const tf_csr *A, const void *X, int64_t ldx, const void *W1, const void *W2,
+                       void *D, int64_t ldd, void *hip_stream);
+/* The same with weights of 4 bits: W1 and W2 hold n_experts matrices each, of the shapes above. */
+tf_status tf_moe_layer_q4(const tf_moe *plan, const tf_csr *A, const void *X, int64_t ldx, const tf_q4 *W1,
+                          const tf_q4 *W2, void *D, int64_t ldd, void *hip_stream);
 
 /* Message for the most recent failure on the calling thread ("" if none). */
 const char *tf_last_error(void);

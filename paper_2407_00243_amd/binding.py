@@ -11,7 +11,7 @@ from typing import Optional
 
 import numpy as np
 
-TF_F32, TF_F64 = 0, 1
+TF_F32, TF_F64, TF_BF16, TF_F16 = 0, 1, 2, 3
 TF_FLAG_NO_SPLIT = 1
 TF_FLAG_SCHEDULE_ONLY = 2
 TF_FLAG_REORDER = 4
@@ -19,6 +19,10 @@ TF_FLAG_C_TRANSPOSED = 8
 TF_FLAG_SKIP_UNREAD = 16
 TF_FLAG_NO_BASELINE = 32
 TF_EXECUTE_WAVEFRONTS, TF_EXECUTE_ONE_PASS, TF_EXECUTE_GATHER_FIRST, TF_EXECUTE_PLAIN_PAIR = 0, 1, 2, 3
+
+TF_Q4_INT, TF_Q4_E2M1 = 0, 1
+TF_ROUTE_SOFTMAX, TF_ROUTE_SOFTMAX_TOP, TF_ROUTE_SIGMOID, TF_ROUTE_SIGMOID_TOP = 0, 1, 2, 3
+TF_ACT_IDENTITY, TF_ACT_RELU, TF_ACT_SILU, TF_ACT_GELU = 0, 1, 2, 3
 
 _STATUS = {0: "TF_OK", 1: "TF_EINVAL", 2: "TF_EBADCSR", 3: "TF_ENOMEM", 4: "TF_EHIP",
            5: "TF_EUNSUPPORTED", 6: "TF_EMISMATCH"}
@@ -81,10 +85,26 @@ class tf_schedule_view(ctypes.Structure):
                 ("far_rows", ctypes.c_int32), ("automatic", ctypes.c_int32)]
 
 
+class tf_q4(ctypes.Structure):
+    _fields_ = [("n_mats", ctypes.c_int64), ("n_rows", ctypes.c_int64), ("n_cols", ctypes.c_int64),
+                ("codes", ctypes.c_void_p), ("scales", ctypes.c_void_p),
+                ("kind", ctypes.c_int32), ("group", ctypes.c_int32)]
+
+
+class tf_moe_desc(ctypes.Structure):
+    _fields_ = [("n_experts", ctypes.c_int64), ("n_in", ctypes.c_int64), ("n_hidden", ctypes.c_int64),
+                ("n_out", ctypes.c_int64), ("max_tokens", ctypes.c_int64),
+                ("max_entries", ctypes.c_int64), ("dtype", ctypes.c_int32),
+                ("activation", ctypes.c_int32), ("gated", ctypes.c_int32),
+                ("reserved0", ctypes.c_int32)]
+
+
 EXPORTS = ["tf_plan_create", "tf_plan_destroy", "tf_plan_schedule", "tf_plan_workspace",
            "tf_gemm_spmm", "tf_gemm_spmm_static", "tf_spmm_spmm", "tf_unfused_gemm_spmm",
            "tf_unfused_spmm_spmm", "tf_run_wavefront", "tf_plan_prepare_unfused", "tf_plan_workspace_unfused",
-           "tf_csr_validate", "tf_last_error", "tf_version"]
+           "tf_csr_validate", "tf_q4_sizes", "tf_q4_pack", "tf_q4_quantize", "tf_q4_unpack", "tf_q4_matvec",
+           "tf_moe_route", "tf_moe_create", "tf_moe_destroy", "tf_moe_layer", "tf_moe_layer_q4",
+           "tf_last_error", "tf_version"]
 _INT_RETURNS = [e for e in EXPORTS if e not in ("tf_last_error", "tf_version")]
 
 
@@ -116,6 +136,18 @@ def load_library():
     lib.tf_plan_prepare_unfused.argtypes = [vp]
     lib.tf_plan_workspace_unfused.argtypes = [vp, ctypes.POINTER(vp)]
     lib.tf_csr_validate.argtypes = [ctypes.POINTER(tf_csr)]
+    q4 = ctypes.POINTER(tf_q4)
+    csr = ctypes.POINTER(tf_csr)
+    lib.tf_q4_sizes.argtypes = [q4, ctypes.POINTER(i64), ctypes.POINTER(i64)]
+    lib.tf_q4_pack.argtypes = [q4, vp, vp, vp]
+    lib.tf_q4_quantize.argtypes = [q4, vp, i32, vp]
+    lib.tf_q4_unpack.argtypes = [q4, i32, vp, vp]
+    lib.tf_q4_matvec.argtypes = [q4, vp, i64, vp, i64, i64, i32, vp]
+    lib.tf_moe_route.argtypes = [vp, i64, i32, vp, i32, ctypes.c_float, csr, vp]
+    lib.tf_moe_create.argtypes = [ctypes.POINTER(tf_moe_desc), ctypes.POINTER(vp)]
+    lib.tf_moe_destroy.argtypes = [vp]
+    lib.tf_moe_layer.argtypes = [vp, csr, vp, i64, vp, vp, vp, i64, vp]
+    lib.tf_moe_layer_q4.argtypes = [vp, csr, vp, i64, q4, q4, vp, i64, vp]
     for name in _INT_RETURNS:
         getattr(lib, name).restype = ctypes.c_int
     lib.tf_last_error.restype = ctypes.c_char_p
@@ -289,6 +321,190 @@ def tf_run_wavefront(plan: int, wavefront: int, B, C, D, stream=None) -> None:
         b = _csr_arg(B)
         _check(lib.tf_run_wavefront(plan, wavefront, None, ctypes.byref(b), _addr(C), _addr(D),
                                     _addr(stream)))
+
+
+# ------------------------------------------------------------------------------- routed operators
+
+_ROUTED = {"torch.float32": TF_F32, "float32": TF_F32, "torch.bfloat16": TF_BF16,
+           "torch.float16": TF_F16, "float16": TF_F16}
+
+
+def _routed_code(dt) -> int:
+    if isinstance(dt, int):
+        return dt
+    code = _ROUTED.get(str(dt))
+    if code is None:
+        raise TypeError(f"unsupported element type {dt}")
+    return code
+
+
+def _matrix(x, what: str, cols: Optional[int] = None):
+    """Rows, columns and distance of the rows (in elements) of a matrix whose rows are contiguous."""
+    if len(x.shape) != 2:
+        raise ValueError(f"{what} must be a matrix")
+    rows, n = x.shape
+    if cols is not None and n != cols:
+        raise ValueError(f"{what} must have {cols} columns, not {n}")
+    step, ld = x.stride(1), x.stride(0)
+    if n > 1 and step != 1:
+        raise ValueError(f"the rows of {what} must be contiguous")
+    if rows <= 1:
+        ld = max(ld, n)
+    return rows, n, ld
+
+
+def _contiguous(x, what: str, shape, dtype: Optional[int] = None):
+    if tuple(x.shape) != tuple(shape):
+        raise ValueError(f"{what} must have the shape {tuple(shape)}, not {tuple(x.shape)}")
+    if not x.is_contiguous():
+        raise ValueError(f"{what} must be contiguous")
+    if dtype is not None and _routed_code(x.dtype) != dtype:
+        raise TypeError(f"{what} has another element type than the call")
+
+
+class Q4Matrix:
+    """Stacked matrices with weights of 4 bits in device arrays of the caller's (kept alive by this object), of
+    the sizes that tf_q4_sizes tells."""
+
+    def __init__(self, n_rows: int, n_cols: int, kind: int, group: int, codes, scales, n_mats: int = 1):
+        self.n_mats, self.n_rows, self.n_cols = int(n_mats), int(n_rows), int(n_cols)
+        self.kind, self.group = int(kind), int(group)
+        self.codes, self.scales = codes, scales
+        need = tf_q4_sizes(n_rows, n_cols, kind, group, n_mats)
+        for what, x, n in (("codes", codes, need[0]), ("scales", scales, need[1])):
+            if hasattr(x, "numel") and x.numel() * x.element_size() < n:
+                raise ValueError(f"{what} must hold {n} bytes")
+        self.struct = tf_q4(self.n_mats, self.n_rows, self.n_cols, _addr(codes), _addr(scales), self.kind,
+                            self.group)
+
+
+def tf_q4_sizes(n_rows: int, n_cols: int, kind: int, group: int, n_mats: int = 1):
+    """Bytes of the codes and of the scales of n_mats matrices."""
+    w = tf_q4(n_mats, n_rows, n_cols, None, None, kind, group)
+    codes, scales = ctypes.c_int64(), ctypes.c_int64()
+    _check(load_library().tf_q4_sizes(ctypes.byref(w), ctypes.byref(codes), ctypes.byref(scales)))
+    return codes.value, scales.value
+
+
+def tf_q4_pack(W: Q4Matrix, codes, scales, stream=None) -> None:
+    """codes: int8, n_mats x n_rows x n_cols; scales: bf16, n_mats x n_rows x groups."""
+    for what, x, n, t in (("codes", codes, W.n_cols, "torch.int8"),
+                          ("scales", scales, -(-W.n_cols // W.group), "torch.bfloat16")):
+        if hasattr(x, "is_contiguous"):
+            _contiguous(x, what, (W.n_mats, W.n_rows, n))
+            if str(x.dtype) != t:
+                raise TypeError(f"{what} must be {t}")
+    _check(load_library().tf_q4_pack(ctypes.byref(W.struct), _addr(codes), _addr(scales), _addr(stream)))
+
+
+def tf_q4_quantize(W: Q4Matrix, weights, stream=None) -> None:
+    _contiguous(weights, "weights", (W.n_mats, W.n_rows, W.n_cols))
+    _check(load_library().tf_q4_quantize(ctypes.byref(W.struct), _addr(weights), _routed_code(weights.dtype),
+                                         _addr(stream)))
+
+
+def tf_q4_unpack(W: Q4Matrix, weights, stream=None) -> None:
+    _contiguous(weights, "weights", (W.n_mats, W.n_rows, W.n_cols))
+    _check(load_library().tf_q4_unpack(ctypes.byref(W.struct), _routed_code(weights.dtype), _addr(weights),
+                                       _addr(stream)))
+
+
+def tf_q4_matvec(W: Q4Matrix, X, Y, stream=None) -> None:
+    """Y = X W^T; X and Y are matrices of one element type, their rows may be further apart than they are wide."""
+    m, _, ldx = _matrix(X, "X", W.n_cols)
+    my, _, ldy = _matrix(Y, "Y", W.n_rows)
+    if m != my:
+        raise ValueError("X and Y must have the same number of rows")
+    if X.dtype != Y.dtype:
+        raise TypeError("X and Y must have the same element type")
+    _check(load_library().tf_q4_matvec(ctypes.byref(W.struct), _addr(X), ldx, _addr(Y), ldy, m,
+                                       _routed_code(X.dtype), _addr(stream)))
+
+
+def tf_moe_route(scores, A: DeviceCsr, scoring: int = TF_ROUTE_SOFTMAX_TOP, bias=None, scale: float = 1.0,
+                 stream=None) -> None:
+    """Writes the arrays of A (rowptr, colidx, vals): the nnz / n_rows best experts of each token."""
+    rows, _, ld = _matrix(scores, "scores", A.n_cols)
+    if rows != A.n_rows:
+        raise ValueError("A must have a row for each row of the scores")
+    if bias is not None and hasattr(bias, "shape"):
+        _contiguous(bias, "bias", (A.n_cols,), TF_F32)
+    a = A.as_struct()
+    _check(load_library().tf_moe_route(_addr(scores), ld, _routed_code(scores.dtype), _addr(bias), scoring, scale,
+                                       ctypes.byref(a), _addr(stream)))
+
+
+def tf_moe_create(n_experts: int, n_in: int, n_hidden: int, n_out: int, dtype, max_tokens: int,
+                  max_entries: int, activation: int = TF_ACT_SILU, gated: bool = True) -> int:
+    """Returns the opaque handle of a plan for mixture-of-experts layers of these sizes."""
+    d = tf_moe_desc(n_experts, n_in, n_hidden, n_out, max_tokens, max_entries, _routed_code(dtype), activation,
+                    1 if gated else 0, 0)
+    out = ctypes.c_void_p()
+    _check(load_library().tf_moe_create(ctypes.byref(d), ctypes.byref(out)))
+    return out.value
+
+
+def tf_moe_destroy(plan: Optional[int]) -> None:
+    _check(load_library().tf_moe_destroy(plan))
+
+
+def tf_moe_layer(plan: int, A: DeviceCsr, X, W1, W2, D, stream=None) -> None:
+    a = A.as_struct()
+    _check(load_library().tf_moe_layer(plan, ctypes.byref(a), _addr(X), _matrix(X, "X")[2], _addr(W1), _addr(W2),
+                                       _addr(D), _matrix(D, "D")[2], _addr(stream)))
+
+
+def tf_moe_layer_q4(plan: int, A: DeviceCsr, X, W1: Q4Matrix, W2: Q4Matrix, D, stream=None) -> None:
+    a = A.as_struct()
+    _check(load_library().tf_moe_layer_q4(plan, ctypes.byref(a), _addr(X), _matrix(X, "X")[2],
+                                          ctypes.byref(W1.struct), ctypes.byref(W2.struct), _addr(D),
+                                          _matrix(D, "D")[2], _addr(stream)))
+
+
+class MoePlan:
+    """Owns a plan for mixture-of-experts layers; checks the operands that it is given."""
+
+    def __init__(self, n_experts: int, n_in: int, n_hidden: int, dtype, max_tokens: int, max_entries: int,
+                 n_out: int = 0, activation: int = TF_ACT_SILU, gated: bool = True):
+        self.handle = None
+        self.n_experts, self.n_in, self.n_hidden, self.n_out = n_experts, n_in, n_hidden, n_out or n_in
+        self.dtype, self.gated = _routed_code(dtype), bool(gated)
+        self.handle = tf_moe_create(n_experts, n_in, n_hidden, self.n_out, self.dtype, max_tokens, max_entries,
+                                    activation, gated)
+
+    def run(self, A: DeviceCsr, X, W1, W2, D, stream=None) -> None:
+        """W1 and W2: both dense (n_experts x (2) n_hidden x n_in, n_experts x n_out x n_hidden) or both Q4Matrix."""
+        for what, x, cols in (("X", X, self.n_in), ("D", D, self.n_out)):
+            if _matrix(x, what, cols)[0] != A.n_rows:
+                raise ValueError(f"{what} must have a row for each row of A")
+            if _routed_code(x.dtype) != self.dtype:
+                raise TypeError(f"{what} has another element type than the plan")
+        if isinstance(W1, Q4Matrix) and isinstance(W2, Q4Matrix):
+            tf_moe_layer_q4(self.handle, A, X, W1, W2, D, stream)
+            return
+        if isinstance(W1, Q4Matrix) or isinstance(W2, Q4Matrix):
+            raise TypeError("W1 and W2 must both be dense or both have 4 bits")
+        first = self.n_hidden * (2 if self.gated else 1)
+        _contiguous(W1, "W1", (self.n_experts, first, self.n_in), self.dtype)
+        _contiguous(W2, "W2", (self.n_experts, self.n_out, self.n_hidden), self.dtype)
+        tf_moe_layer(self.handle, A, X, W1, W2, D, stream)
+
+    def close(self) -> None:
+        if self.handle:
+            tf_moe_destroy(self.handle)
+            self.handle = None
+
+    def __enter__(self):
+        return self
+
+    def __exit__(self, *exc):
+        self.close()
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
 
 
 class Plan:

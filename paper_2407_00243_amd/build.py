@@ -10,8 +10,9 @@ from concurrent.futures import ThreadPoolExecutor
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libtilefusion.so")
-SOURCES = ["tf_kernels.hip", "tf_gemm.hip", "tf_chain.hip", "tf_gather.hip", "tf_inspector.cpp", "tf_api.cpp"]
-HEADERS = ["tf_internal.h", "tf_device.h", os.path.join("..", "..", "include", "tilefusion.h")]
+SOURCES = ["tf_kernels.hip", "tf_gemm.hip", "tf_chain.hip", "tf_gather.hip", "tf_inspector.cpp", "tf_api.cpp",
+           "tf_experts_bf16.hip", "tf_experts_f16.hip", "tf_experts_f32.hip", "tf_q4.hip", "tf_route.hip", "tf_moe_api.cpp"]
+HEADERS = ["tf_internal.h", "tf_device.h", "tf_moe.h", "tf_moe_device.h", "tf_experts.h", os.path.join("..", "..", "include", "tilefusion.h")]
 
 # packed-fp32 instructions are switched off for all device code
 HIPCC_FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",

@@ -14,6 +14,7 @@
 #include <vector>
 
 #include "tf_internal.h"
+#include "tf_moe.h"
 
 namespace {
 
@@ -28,6 +29,15 @@ tf_status hip_fail(hipError_t e, const char *what) {
     g_err = std::string(what) + ": " + hipGetErrorString(e);
     return e == hipErrorOutOfMemory ? TF_ENOMEM : TF_EHIP;
 }
+
+}  // namespace
+
+namespace tf {
+tf_status report(tf_status st, const char *msg) { return fail(st, msg); }
+tf_status report_hip(int hip_error, const char *what) { return hip_fail((hipError_t)hip_error, what); }
+}  // namespace tf
+
+namespace {
 
 bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 

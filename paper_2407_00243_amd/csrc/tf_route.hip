@@ -1,0 +1,142 @@
+// Router: the largest scores of each token and their weights; and the weighted sum over a token's entries.
+#include <algorithm>
+
+#include "tf_moe_device.h"
+
+namespace tf {
+namespace {
+
+constexpr int kWaves = 4, kThreads = 64 * kWaves;
+
+__device__ __forceinline__ float wave_sum(float x) {
+#pragma unroll
+    for (int d = 32; d; d >>= 1) x += __shfl_xor(x, d, 64);
+    return x;
+}
+__device__ __forceinline__ float wave_max(float x) {
+#pragma unroll
+    for (int d = 32; d; d >>= 1) x = fmaxf(x, __shfl_xor(x, d, 64));
+    return x;
+}
+
+// One wave per token; lane l holds the scores of experts l, l + 64, ..., V of them.  k times the largest of those left.
+template <int EL, int V> __global__ __launch_bounds__(kThreads) void k_route(const RouteLaunch a) {
+    typedef typename El<EL>::T T;
+    const int lane = threadIdx.x & 63;
+    const int t = blockIdx.x * kWaves + (threadIdx.x >> 6);
+    if (t >= a.n_tokens) return;
+    const T *row = static_cast<const T *>(a.scores) + (int64_t)t * a.ld;
+    const float low = -__builtin_inff();
+    float l[V], key[V];
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+        const int e = lane + 64 * v;
+        l[v] = low;
+        key[v] = low;
+        if (e < a.n_experts) {
+            const float x = El<EL>::get(row[e]);
+            l[v] = __builtin_isnan(x) ? low : x;
+            const float y = a.bias ? l[v] + a.bias[e] : l[v];
+            key[v] = __builtin_isnan(y) ? low : y;
+        }
+    }
+    int mine = -1;             // the expert that this lane's rank selects, and its score
+    float score = low;
+    for (int i = 0; i < a.k; ++i) {
+        float best = low, best_l = low;
+        int at = 0x7fffffff;
+#pragma unroll
+        for (int v = 0; v < V; ++v)
+            if (key[v] > best) {
+                best = key[v];
+                best_l = l[v];
+                at = lane + 64 * v;
+            }
+#pragma unroll
+        for (int d = 32; d; d >>= 1) {
+            const float ob = __shfl_xor(best, d, 64), ol = __shfl_xor(best_l, d, 64);
+            const int oa = __shfl_xor(at, d, 64);
+            if (ob > best || (ob == best && oa < at)) {
+                best = ob;
+                best_l = ol;
+                at = oa;
+            }
+        }
+        if (!(best > low)) break;
+        if (lane == i) {
+            mine = at;
+            score = best_l;
+        }
+#pragma unroll
+        for (int v = 0; v < V; ++v)
+            if (at == lane + 64 * v) key[v] = low;
+    }
+    float w;
+    if (a.scoring == TF_ROUTE_SOFTMAX || a.scoring == TF_ROUTE_SOFTMAX_TOP) {
+        float top = score, sum = 0.0f;
+        if (a.scoring == TF_ROUTE_SOFTMAX) {
+#pragma unroll
+            for (int v = 0; v < V; ++v) top = fmaxf(top, l[v]);
+            top = wave_max(top);
+#pragma unroll
+            for (int v = 0; v < V; ++v) sum += l[v] > low ? expf(l[v] - top) : 0.0f;
+        } else {
+            top = wave_max(top);
+            sum = mine >= 0 ? expf(score - top) : 0.0f;
+        }
+        w = expf(score - top) / wave_sum(sum);
+    } else {
+        w = 1.0f / (1.0f + expf(-score));
+        // (all selected ones below 2^-126: the sum must not be zero)
+        if (a.scoring == TF_ROUTE_SIGMOID_TOP) w /= fmaxf(wave_sum(mine >= 0 ? w : 0.0f), 0x1p-126f);
+    }
+    if (lane < a.k) {
+        a.colidx[(int64_t)t * a.k + lane] = mine;
+        a.vals[(int64_t)t * a.k + lane] = mine >= 0 ? w * a.scale : 0.0f;
+    }
+    if (lane == 0) {
+        a.rowptr[t] = t * a.k;
+        if (t == a.n_tokens - 1) a.rowptr[t + 1] = (t + 1) * a.k;
+    }
+}
+
+// D[t] = sum of value times Y over the entries of row t, in their order.
+template <int EL> __global__ __launch_bounds__(kThreads) void k_combine(const CombineLaunch a, int col_blocks) {
+    typedef typename El<EL>::T T;
+    const int t = blockIdx.x / col_blocks, c = blockIdx.x % col_blocks * kThreads + threadIdx.x;
+    if (c >= a.n_out) return;
+    float d = 0.0f;
+    for (int q = a.rowptr[t]; q < a.rowptr[t + 1]; ++q)
+        if ((uint32_t)a.colidx[q] < (uint32_t)a.n_experts) d = fmaf(a.vals[q], a.Y[(int64_t)q * a.n_out + c], d);
+    static_cast<T *>(a.D)[(int64_t)t * a.ldd + c] = El<EL>::put(d);
+}
+
+template <int EL> void route_el(const RouteLaunch &a, hipStream_t st) {
+    const dim3 grid((a.n_tokens + kWaves - 1) / kWaves), block(kThreads);
+    if (a.n_experts <= 64) hipLaunchKernelGGL((k_route<EL, 1>), grid, block, 0, st, a);
+    else if (a.n_experts <= 128) hipLaunchKernelGGL((k_route<EL, 2>), grid, block, 0, st, a);
+    else if (a.n_experts <= 256) hipLaunchKernelGGL((k_route<EL, 4>), grid, block, 0, st, a);
+    else hipLaunchKernelGGL((k_route<EL, 16>), grid, block, 0, st, a);
+}
+
+}  // namespace
+
+int launch_route(const RouteLaunch &a, void *stream) {
+    const hipStream_t st = static_cast<hipStream_t>(stream);
+    if (a.dtype == TF_BF16) route_el<TF_BF16>(a, st);
+    else if (a.dtype == TF_F16) route_el<TF_F16>(a, st);
+    else route_el<TF_F32>(a, st);
+    return (int)hipGetLastError();
+}
+
+int launch_combine(const CombineLaunch &a, void *stream) {
+    const hipStream_t st = static_cast<hipStream_t>(stream);
+    const int col_blocks = (a.n_out + kThreads - 1) / kThreads;
+    const dim3 grid((unsigned)((int64_t)col_blocks * a.n_tokens));
+    if (a.dtype == TF_BF16) hipLaunchKernelGGL(k_combine<TF_BF16>, grid, dim3(kThreads), 0, st, a, col_blocks);
+    else if (a.dtype == TF_F16) hipLaunchKernelGGL(k_combine<TF_F16>, grid, dim3(kThreads), 0, st, a, col_blocks);
+    else hipLaunchKernelGGL(k_combine<TF_F32>, grid, dim3(kThreads), 0, st, a, col_blocks);
+    return (int)hipGetLastError();
+}
+
+}  // namespace tf
