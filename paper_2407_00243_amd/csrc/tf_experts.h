@@ -1,12 +1,17 @@
 // Products of a few rows with the weights of the experts that name them (or with one 4-bit matrix).
 #pragma once
+#include <algorithm>
+#include <type_traits>
+
 #include "tf_moe_device.h"
 
 namespace tf {
 namespace {
 
-constexpr int kExpertWaves = 8, kExpertThreads = 64 * kExpertWaves;
-constexpr int kExpertFrags = 2;       // blocks of sixteen rows of weights per workgroup
+constexpr int kExpertWaves = 4, kExpertThreads = 64 * kExpertWaves;
+constexpr int kExpertSpread = 512;    // workgroups of a launch that are enough
+constexpr int kNearRows = 256;        // row pointers that are held in LDS
+constexpr int kJoinTokens = 16;       // the most tokens whose entries the last workgroups add up
 
 // Hidden rows of TF_F16 are held in two parts, high * 2^12 + low: fp16 alone ends at 65504, which a gate times
 // what it gates passes easily.
@@ -79,9 +84,9 @@ __device__ __forceinline__ float activate(int act, float x) {
     }
 }
 
-// Row of A that entry q belongs to.  Where all rows have the same number of entries, as a router leaves them, the first
+// Row of A that entry q belongs to: where all rows have the same number of entries, as a router leaves them, the first
 // guess is right.
-__device__ __forceinline__ int row_of_entry(const int32_t *__restrict__ rowptr, int n_rows, int nnz, int q) {
+__device__ __forceinline__ int row_of_entry(const int32_t *rowptr, int n_rows, int nnz, int q) {
     const int guess = (int)((int64_t)q * n_rows / nnz);
     if (rowptr[guess] <= q && q < rowptr[guess + 1]) return guess;
     int lo = 0, hi = n_rows;              // the first row that ends beyond q
@@ -93,65 +98,517 @@ __device__ __forceinline__ int row_of_entry(const int32_t *__restrict__ rowptr, 
     return min(lo, n_rows - 1);
 }
 
-// EL: element type; KIND: 4-bit kind or -1; G: groups in 128 columns; HID: X are hidden rows; NT: blocks of sixteen
-// entries that are multiplied at a time.
+// Sixteen bytes of a row that ends at column n were loaded at min(k, n - piece) instead of column k: moved to their places,
+// zeros from the end of the row on.
+template <typename T> __device__ __forceinline__ Words4 set_right(Words4 x, int k, int n) {
+    constexpr int piece = 16 / (int)sizeof(T);
+    const int bits = min(max(k + piece - n, 0), piece) * 8 * (int)sizeof(T);
+    if constexpr (sizeof(T) == 2) {
+        const bool half = bits & 16;
+        x = Words4{half ? x[0] >> 16 | x[1] << 16 : x[0], half ? x[1] >> 16 | x[2] << 16 : x[1], half ? x[2] >> 16 | x[3] << 16 : x[2],
+                   half ? x[3] >> 16 : x[3]};
+    }
+    x = bits & 32 ? Words4{x[1], x[2], x[3], 0} : x;
+    x = bits & 64 ? Words4{x[2], x[3], 0, 0} : x;
+    return bits & 128 ? Words4{0, 0, 0, 0} : x;
+}
+// The same for a row of fewer than sixteen bytes, loaded element by element.
+template <typename T> __device__ __forceinline__ Words4 load_short(const char *p, int k, int n) {
+    Words4 y = {0, 0, 0, 0};
+#pragma unroll 1
+    for (int i = 0; i < 16 / (int)sizeof(T); ++i) {
+        const uint32_t e = k + i < n ? reinterpret_cast<const T *>(p)[k + i] : T(0);
+        if constexpr (sizeof(T) == 4) y = Words4{y[1], y[2], y[3], e};
+        else y = Words4{y[0] >> 16 | y[1] << 16, y[1] >> 16 | y[2] << 16, y[2] >> 16 | y[3] << 16, y[3] >> 16 | e << 16};
+    }
+    return y;
+}
+
+// EL: element type; KIND: 4-bit kind or -1; G: groups in 128 columns; HID: X are hidden rows; in their methods NT: blocks of
+// sixteen entries that are multiplied at a time.
 //
-// A workgroup multiplies kExpertFrags blocks of sixteen rows of one expert's weights (with a gate: sixteen of the gate and
-// the sixteen that it multiplies) with the rows of X of the entries that name the expert; its waves share the columns,
-// a group of steps in turn, and their sums are added up through LDS, wave after wave.  Weights are the first operand of the
-// matrix instructions, straight from memory: whatever the number of entries up to sixteen, what one instruction
-// multiplies was loaded by one instruction.
-template <int EL, int KIND, int G, bool HID, int NT>
-__global__ __launch_bounds__(kExpertThreads) void k_experts(const ExpertLaunch a) {
+// A wave multiplies NF blocks of sixteen rows of one expert's weights (with a gate: sixteen of the gate and the sixteen
+// that it multiplies) with the rows of X of the entries that name the expert.  a.k_waves waves of the workgroup share the
+// columns of the same rows, a step in turn, and their sums are added up through LDS, wave after wave.  Weights are the first
+// operand of the matrix instructions, straight from memory: whatever the number of entries up to sixteen, what one
+// instruction multiplies was loaded by one instruction.  X passes through LDS, chunk by chunk, in the order of the
+// instructions, and is read there by all waves.
+//
+// Dense weights are loaded by whole lines of 128 bytes: an instruction takes eight rows x 128 bytes, and two of them are
+// put in operand order (sixteen rows x 64 bytes) by exchanging halves of sixteen lanes (a read of 512 MiB by itself, rows of
+// 4 / 8 / 16 KiB: sixteen rows x 64 bytes 4.9 / 6.0 / 5.2 TB/s, eight rows x 128 bytes 6.2 / 6.4 / 5.8).
+template <int EL, int KIND, int G, bool HID, int NF> struct Expert {
     typedef typename El<EL>::T T;
-    constexpr int NF = kExpertFrags;
-    constexpr bool DENSE = KIND < 0, WIDE = EL == TF_F32;
-    constexpr int STEP = DENSE ? (WIDE ? 16 : 32) : kQ4Block;     // columns of a step
-    constexpr int SUB = DENSE ? 1 : 4;                            // operands of X in a step
-    constexpr int XE = DENSE && WIDE ? 4 : 8;                     // columns of X that a lane holds of an operand
-    constexpr int XR = !DENSE && WIDE ? 2 : HID && !WIDE ? 2 : 1; // sixteen-byte pieces of it
-    constexpr int U = DENSE ? (NT > 1 ? 2 : 4) : (NT > 1 ? 1 : 2);
-    constexpr int SETS = !DENSE && WIDE ? 2 : HID && EL == TF_F16 ? 2 : 1;   // sums of high and of low parts
+    typedef std::conditional_t<EL == TF_F32, uint32_t, uint16_t> Bits;
+    static constexpr int CHUNK = 32 << 10;                           // LDS of a chunk of X, of which there are two
+    static constexpr int MOST = 4;                                   // blocks of sixteen entries that are multiplied at a time
+    static constexpr bool DENSE = KIND < 0, WIDE = EL == TF_F32;
+    static constexpr int PIECE = 16 / (int)sizeof(T);                // elements of sixteen bytes
+    static constexpr int STEP = DENSE ? 8 * PIECE : kQ4Block;        // columns of a step
+    static constexpr int SUB = DENSE ? 2 : 4;                        // operands of X in a step
+    static constexpr int SUBK = STEP / SUB;                          // columns of an operand
+    static constexpr int XP = !DENSE && WIDE ? 3 : HID && !WIDE ? 2 : 1;   // parts of X
+    static constexpr int SETS = !DENSE && WIDE ? 2 : HID && EL == TF_F16 ? 2 : 1;   // sums of high and of low parts
+    static constexpr int WL = DENSE ? 2 : 1;                         // pieces of weights that a lane holds of a step and block
+    static constexpr int SW = DENSE ? 1 : 2 * G;                     // words of scales
+    static constexpr int AHEAD = 2;                      // steps whose weights are on their way
+    static constexpr int RING = AHEAD + 1;
+    static constexpr int XR = !DENSE && WIDE ? 2 : XP;               // sixteen-byte pieces that a lane loads of an operand
 
-    __shared__ int s_count[kExpertWaves], s_entry[16 * NT];
-    extern __shared__ __align__(16) unsigned char smem[];
-    Float4 *red = reinterpret_cast<Float4 *>(smem);
+    // Chunks of X for NT blocks of TOK entries (of fewer than sixteen only these are held; an operand is 4 TOK pieces then).
+    template <int NT, int TOK> struct Chunk {
+        static constexpr int LANES = 4 * TOK;
+        static constexpr int FIT = CHUNK / (SUB * NT * XP * LANES * 16);
+        static constexpr int STEPS = FIT >= 32 ? 32 : FIT >= 16 ? 16 : FIT >= 8 ? 8 : FIT >= 4 ? 4 : FIT >= 2 ? 2 : 1;
+        static constexpr int SLOTS = STEPS * SUB * NT;
+        static constexpr int MINE = (SLOTS * LANES + kExpertThreads - 1) / kExpertThreads;
+        static constexpr int PIECES = SLOTS * XP * LANES;            // of a buffer
+        Words4 x[MINE][XR];
+    };
 
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, g = lane >> 4, r = lane & 15;
-    const int rows_per = a.gated ? 16 : 16 * NF;
-    const int tiles = (a.n_rows + rows_per - 1) / rows_per;
-    const int tile = blockIdx.x % tiles, unit = blockIdx.x / tiles;
-
-    int expert = 0;
-    const bool by_entry = a.rowptr && a.n_entries <= a.n_experts;
-    if (a.rowptr) {
-        expert = by_entry ? a.colidx[unit] : unit;
-        if (expert < 0 || expert >= a.n_experts) return;
+    // LDS of a workgroup: two chunks of X, or one if that is all there is; the waves' sums in their place.
+    template <int NT, int TOK> static int bytes(int steps) {
+        typedef Chunk<NT, TOK> C;
+        const int x = steps > C::STEPS ? 2 * C::PIECES : (steps * SUB * NT * C::LANES + kExpertThreads - 1) / kExpertThreads * kExpertThreads * XP;
+        return std::max(x * 16, kExpertWaves * NF * NT * 1024);
     }
 
-    // weights
-    const char *wp[NF];
-    const char *sp[NF];
-    const int blocks = (a.n_cols + kQ4Block - 1) / kQ4Block;
+    struct Weights {
+        Words4 w[NF][WL];
+    };
+    struct Scales {
+        uint32_t s[DENSE ? 1 : NF][SW];
+    };
+
+    // Places of a wave's weights: of a block of sixteen rows one that is the same for all lanes, and a lane's offset from it
+    // (below 2^31: columns are limited, kMaxColumns).
+    const char *wb[NF], *sb[NF];
+    uint32_t w_at[WL], w_up, s_at, s_up;      // (4 bits: those of the rows behind a gate's begin anywhere in the layout's blocks)
+    int s_next, s_off;       // bytes to the scales of the next four of these rows, and how many of them belong to these
+    int n_cols, g, r, wave, lane, tid;
+
+    // row0: row of the first block of outputs
+    __device__ __forceinline__ void set(const ExpertLaunch &a, int expert, int row0) {
+        tid = threadIdx.x;
+        lane = tid & 63;
+        wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+        g = lane >> 4;
+        r = lane & 15;
+        n_cols = a.n_cols;
+        const int out_blocks = a.gated ? NF / 2 : NF;
+        const int64_t blocks = (n_cols + kQ4Block - 1) / kQ4Block;
+        const char *w = static_cast<const char *>(a.W) + expert * a.w_mat;
+        const char *sc = static_cast<const char *>(a.scales) + expert * a.s_mat;
+        s_off = !DENSE && a.gated ? a.n_rows & 3 : 0;
+        s_next = 0;
+        w_up = s_up = s_at = 0;
 #pragma unroll
-    for (int f = 0; f < NF; ++f) {
-        // (a block beyond the matrix reads its last row again; what comes of it is not stored)
-        const char *base = static_cast<const char *>(a.W) + expert * a.w_mat;
+        for (int f = 0; f < NF; ++f) {
+            const int up = f >= out_blocks;
+            const int first = block_row(a, row0, f - up * out_blocks) + up * a.n_rows;
+            if constexpr (DENSE) {
+                wb[f] = w + (int64_t)first * n_cols * (int)sizeof(T);
+                sb[f] = nullptr;
+            } else {
+                wb[f] = w + (first >> 4) * blocks * 1024;
+                sb[f] = sc + (first >> 4) * blocks * (32 * G);
+            }
+        }
         if constexpr (DENSE) {
-            int row = a.gated ? min(tile * 16 + r, a.n_rows - 1) + f * a.n_rows : min((tile * NF + f) * 16 + r, a.n_rows - 1);
-            wp[f] = base + ((int64_t)row * a.n_cols + XE * g) * (int)sizeof(T);
-            sp[f] = nullptr;
+            const int rows = min(a.n_rows, 16);       // (of a matrix with fewer rows than a block the last one is read again)
+#pragma unroll
+            for (int i = 0; i < 2; ++i) w_at[i] = (uint32_t)min(8 * i + (r & 7), rows - 1) * (uint32_t)n_cols * (uint32_t)sizeof(T);
         } else {
-            // with a gate n_rows is a multiple of sixteen or the second half begins inside a block: rows are looked up one by one
-            int row = a.gated ? min(tile * 16 + r, a.n_rows - 1) + f * a.n_rows : min((tile * NF + f) * 16 + r, a.n_rows - 1);
-            wp[f] = base + (int64_t)(row >> 4) * blocks * 1024 + (16 * g + (row & 15)) * 16;
-            sp[f] = static_cast<const char *>(a.scales) + expert * a.s_mat;
+            w_at[0] = lane * 16;
+            s_at = g * (8 * G);
+            // rows behind a gate's: block b's begin at row n_rows + 16 b, o rows into a block of the layout
+            const int o = a.n_rows & 15;
+            const uint32_t next = (uint32_t)blocks * 1024u;
+            // (the layout's next block exists where rows of it are used; those of the last block that are not are read again)
+            const int last = (2 * a.n_rows - 1) >> 4, b0 = (a.n_rows + block_row(a, row0, 0)) >> 4;
+            const int row = o + r, quad = (o + 4 * g) & ~3;
+            const bool over = NF > 2 || b0 < last;
+            w_up = (row >> 4 && over ? next : 0) + (16 * g + (row & 15)) * 16;
+            s_up = (quad >> 4 && over ? (uint32_t)blocks * (32 * G) : 0) + ((quad & 15) >> 2) * (8 * G);
+            const int quad2 = quad + 4;
+            s_next = (int)((quad2 >> 4 && over ? (uint32_t)blocks * (32 * G) : 0) + ((quad2 & 15) >> 2) * (8 * G)) - (int)s_up;
         }
     }
-    (void)sp;
+    // First row of a block of outputs: the last block of dense weights ends with the matrix (rows that two blocks hold are stored
+    // twice, the same), blocks beyond the matrix are its last one.
+    static __device__ __forceinline__ int block_row(const ExpertLaunch &a, int row0, int f) {
+        return max(0, min(row0 + 16 * f, DENSE ? a.n_rows - 16 : (a.n_rows - 1) & ~15));
+    }
+    static __device__ __forceinline__ void load_scales(uint32_t (&s)[SW], const char *p) {
+        if constexpr (SW == 2) {
+            const Words2 y = *reinterpret_cast<const Words2 *>(p);
+            s[0] = y[0];
+            s[1] = y[1];
+        } else {
+#pragma unroll
+            for (int q = 0; q < SW / 4; ++q) {
+                const Words4 y = reinterpret_cast<const Words4 *>(p)[q];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) s[4 * q + i] = y[i];
+            }
+        }
+    }
+    __device__ __forceinline__ int dense_column(int step) const { return step * STEP + PIECE * (g + 4 * (r >> 3)); }
+    __device__ __forceinline__ void load(Weights &x, int step, const ExpertLaunch &a) const {
+        if constexpr (DENSE) {
+            const uint32_t k = (uint32_t)min(dense_column(step), n_cols - PIECE) * (uint32_t)sizeof(T);
+#pragma unroll
+            for (int f = 0; f < NF; ++f)
+#pragma unroll
+                for (int i = 0; i < 2; ++i) x.w[f][i] = __builtin_nontemporal_load(reinterpret_cast<const AnyWords4 *>(wb[f] + (w_at[i] + k)));
+        } else {
+            const int out_blocks = a.gated ? NF / 2 : NF;
+#pragma unroll
+            for (int f = 0; f < NF; ++f)
+                x.w[f][0] = __builtin_nontemporal_load(
+                    reinterpret_cast<const Words4 *>(wb[f] + (int64_t)step * 1024 + (f >= out_blocks ? w_up : w_at[0])));
+        }
+    }
+    __device__ __forceinline__ void load(Scales &x, int step, const ExpertLaunch &a) const {
+        if constexpr (!DENSE) {
+            const int out_blocks = a.gated ? NF / 2 : NF;
+#pragma unroll
+            for (int f = 0; f < NF; ++f) {
+                const char *p = sb[f] + (int64_t)step * (32 * G) + (f >= out_blocks ? s_up : s_at);
+                load_scales(x.s[f], p);
+                if (f >= NF / 2 && s_off) {
+                    uint32_t y[SW];
+                    load_scales(y, p + s_next);
+#pragma unroll
+                    for (int q = 0; q < SW; q += 2) {
+                        const uint64_t lo = (uint64_t)x.s[f][q + 1] << 32 | x.s[f][q], hi = (uint64_t)y[q + 1] << 32 | y[q];
+                        const uint64_t z = lo >> (16 * s_off) | hi << (64 - 16 * s_off);
+                        x.s[f][q] = (uint32_t)z;
+                        x.s[f][q + 1] = (uint32_t)(z >> 32);
+                    }
+                }
+            }
+        }
+    }
+    // Operand j of the step, in the order of the instructions.
+    static __device__ __forceinline__ Words4 operand(const Weights &x, int f, int j) {
+        if constexpr (DENSE) {
+            constexpr int ror8 = 0x128;
+            Words4 y;
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                y[i] = j == 0 ? (uint32_t)__builtin_amdgcn_update_dpp((int)x.w[f][0][i], (int)x.w[f][WL - 1][i], ror8, 0xf, 0xc, false)
+                              : (uint32_t)__builtin_amdgcn_update_dpp((int)x.w[f][WL - 1][i], (int)x.w[f][0][i], ror8, 0xf, 0x3, false);
+            return y;
+        } else {
+            return q4_decode<EL, KIND>(x.w[f][0][j]);
+        }
+    }
 
-    for (int first = 0;; first += 16 * NT) {
-        // the entries first .. first + 16 NT - 1 of those that name the expert
+    template <int NT> struct Sums {
+        Float4 sum[NF][NT];
+        Float4 acc[SETS][NF][NT];
+    };
+    // xs: the step's operands of X in LDS, this lane's piece of the first.
+    template <int NT, int TOK> static __device__ __forceinline__ void multiply(Sums<NT> &c, const Weights &x, const Scales &sc, const Words4 *xs) {
+#pragma unroll
+        for (int j = 0; j < SUB; ++j) {
+            // (operands of later ones are not read ahead: there are no registers for them)
+            if (NT * XP > 1 && j) __builtin_amdgcn_sched_barrier(0);
+            Words4 w[NF];
+#pragma unroll
+            for (int f = 0; f < NF; ++f) w[f] = operand(x, f, j);
+#pragma unroll
+            for (int n = 0; n < NT; ++n) {
+                Words4 y[XP];
+#pragma unroll
+                for (int h = 0; h < XP; ++h) y[h] = xs[((j * NT + n) * XP + h) * (4 * TOK)];
+#pragma unroll
+                for (int f = 0; f < NF; ++f) {
+                    if constexpr (DENSE && WIDE) {
+                        const Float4 v = __builtin_bit_cast(Float4, w[f]), b = __builtin_bit_cast(Float4, y[0]);
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) c.acc[0][f][n] = mfma_f32(v[i], b[i], c.acc[0][f][n]);
+                    } else {
+#pragma unroll
+                        for (int h = 0; h < XP; ++h) {
+                            Float4 &d = c.acc[h < SETS ? h : SETS - 1][f][n];
+                            d = EL == TF_F16 ? mfma_f16(w[f], y[h], d) : mfma_bf16(w[f], y[h], d);
+                        }
+                    }
+                }
+            }
+            if constexpr (!DENSE) {
+                if ((j + 1) % (4 / G) == 0) {
+                    constexpr int per = 4 / G;
+#pragma unroll
+                    for (int f = 0; f < NF; ++f) {
+                        float s[4];
+#pragma unroll
+                        for (int v = 0; v < 4; ++v) s[v] = v & 1 ? bf16_high(sc.s[f][2 * (j / per) + v / 2]) : bf16_low(sc.s[f][2 * (j / per) + v / 2]);
+#pragma unroll
+                        for (int n = 0; n < NT; ++n)
+#pragma unroll
+                            for (int v = 0; v < 4; ++v) {
+                                float d = c.acc[0][f][n][v];
+                                c.acc[0][f][n][v] = 0.0f;
+                                if constexpr (SETS > 1) {
+                                    d = EL == TF_F16 ? fmaf(d, kHalfHigh, c.acc[SETS - 1][f][n][v]) : d + c.acc[SETS - 1][f][n][v];
+                                    c.acc[SETS - 1][f][n][v] = 0.0f;
+                                }
+                                c.sum[f][n][v] = fmaf(s[v], d, c.sum[f][n][v]);
+                            }
+                    }
+                }
+            }
+        }
+    }
+    // What the sums of an entry's four rows are for.  up: the sums that the gate multiplies.
+    static __device__ __forceinline__ void store(const ExpertLaunch &a, int entry, int row0, const Float4 &y, const Float4 &up) {
+#pragma unroll
+        for (int v = 0; v < 4; ++v) {
+            if (row0 + v >= a.n_rows) continue;
+            const int64_t at = (int64_t)entry * a.ldo + row0 + v;
+            if constexpr (HID) {
+                // (read by another workgroup of the launch: past the caches that it does not share)
+                __hip_atomic_store(static_cast<float *>(a.out) + at, y[v], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+            } else if (a.out_kind == kOutRows) {
+                static_cast<T *>(a.out)[at] = El<EL>::put(y[v]);
+            } else {
+                const float h = activate(a.activation, y[v]) * up[v];
+                T *hi = static_cast<T *>(a.out);
+                T *lo = reinterpret_cast<T *>(static_cast<char *>(a.out) + a.out_part);
+                if constexpr (EL == TF_F32) {
+                    hi[at] = h;
+                } else if constexpr (EL == TF_BF16) {
+                    const uint16_t top = El<EL>::put(h);
+                    const float rest = h - El<EL>::get(top);
+                    hi[at] = top;
+                    lo[at] = __builtin_isinf(El<EL>::get(top)) ? 0 : El<EL>::put(rest);
+                } else {
+                    const uint16_t top = El<EL>::put(h * (1.0f / kHalfHigh));
+                    const float rest = fmaf(-kHalfHigh, El<EL>::get(top), h);
+                    hi[at] = top;
+                    lo[at] = __builtin_isinf(El<EL>::get(top)) ? 0 : El<EL>::put(fminf(fmaxf(rest, -65504.0f), 65504.0f));
+                }
+            }
+        }
+    }
+
+    // This thread's pieces of a chunk of X: from memory, and into LDS when they have arrived.  s_row: rows of X of the entries.
+    // (Beyond the last entry: the first one again; what comes of it is not stored.)
+    template <int NT, int TOK> __device__ __forceinline__ int piece_column(int m, int chunk) const {
+        typedef Chunk<NT, TOK> C;
+        const int p = m * kExpertThreads + tid;
+        return chunk * (C::STEPS * STEP) + p / C::LANES / NT * SUBK + (WIDE && DENSE ? 4 : 8) * (p % C::LANES / TOK);
+    }
+    template <int NT, int TOK> __device__ __forceinline__ bool piece_needed(int m, int chunk) const {
+        typedef Chunk<NT, TOK> C;
+        return chunk * (C::STEPS * STEP) + m * kExpertThreads / C::LANES / NT * SUBK < steps() * STEP;      // (of the first thread)
+    }
+    template <int NT, int TOK>
+    __device__ __forceinline__ void fetch(Chunk<NT, TOK> &y, const ExpertLaunch &a, const int *s_row, int count, int chunk) const {
+        typedef Chunk<NT, TOK> C;
+#pragma unroll
+        for (int m = 0; m < C::MINE; ++m) {
+            if (!piece_needed<NT, TOK>(m, chunk)) break;
+            const int p = m * kExpertThreads + tid;
+            const int at = p / C::LANES % NT * 16 + p % TOK;
+            const char *row = static_cast<const char *>(a.X) + s_row[at < count ? at : 0] * a.ldx * (int64_t)sizeof(T);
+            const int k = piece_column<NT, TOK>(m, chunk);
+#pragma unroll
+            for (int h = 0; h < XR; ++h) {
+                const char *q = HID && !WIDE && h ? row + a.x_part : row;
+                const int kh = k + (WIDE && h ? 4 : 0);
+                y.x[m][h] = n_cols < PIECE ? load_short<Bits>(q, kh, n_cols)
+                                           : *reinterpret_cast<const AnyWords4 *>(q + (int64_t)min(kh, n_cols - PIECE) * (int)sizeof(T));
+            }
+        }
+    }
+    template <int NT, int TOK> __device__ __forceinline__ void put(Chunk<NT, TOK> &y, int chunk, Words4 *xs) const {
+        typedef Chunk<NT, TOK> C;
+        const bool cut = (chunk + 1) * (C::STEPS * STEP) > n_cols && n_cols >= PIECE;
+#pragma unroll
+        for (int m = 0; m < C::MINE; ++m) {
+            if (!piece_needed<NT, TOK>(m, chunk)) break;
+            const int p = m * kExpertThreads + tid;
+            if (C::SLOTS * C::LANES % kExpertThreads && p >= C::SLOTS * C::LANES) break;
+            Words4 *to = xs + p / C::LANES * (XP * C::LANES) + p % C::LANES;
+            if (cut) {
+                const int k = piece_column<NT, TOK>(m, chunk);
+#pragma unroll
+                for (int h = 0; h < XR; ++h) y.x[m][h] = set_right<Bits>(y.x[m][h], k + (WIDE && h ? 4 : 0), n_cols);
+            }
+            if constexpr (!DENSE && WIDE) {
+                Words4 part[3];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    uint32_t h, m1, l;
+                    cut_pair(h, m1, l, __uint_as_float(y.x[m][i / 2][2 * (i & 1)]), __uint_as_float(y.x[m][i / 2][2 * (i & 1) + 1]));
+                    part[0][i] = h;
+                    part[1][i] = m1;
+                    part[2][i] = l;
+                }
+#pragma unroll
+                for (int h = 0; h < 3; ++h) to[h * C::LANES] = part[h];
+            } else {
+#pragma unroll
+                for (int h = 0; h < XP; ++h) to[h * C::LANES] = y.x[m][h];
+            }
+        }
+    }
+
+    __device__ __forceinline__ int steps() const { return (n_cols + STEP - 1) / STEP; }
+    // The first weights are on their way.
+    __device__ __forceinline__ void start(Weights (&w)[RING], const ExpertLaunch &a, int k_wave) const {
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i) load(w[i], min(k_wave + i * a.k_waves, steps() - 1), a);
+    }
+
+    // The `count` entries (at most NT blocks of sixteen; TOK < 16: at most TOK) in s_entry, their rows of X in s_row.  row0: the
+    // wave's first row.  smem: LDS of bytes().
+    template <int NT, int TOK>
+    __device__ __forceinline__ void run(const ExpertLaunch &a, Weights (&w)[RING], int k_wave, int row0, int count, const int *s_entry,
+                                        const int *s_row, unsigned char *smem) {
+        typedef Chunk<NT, TOK> C;
+        asm volatile("" : "+v"(tid));          // (what follows from it is worked out here, not before all cases and kept)
+        Words4 *const xs = reinterpret_cast<Words4 *>(smem);
+        C y;
+        fetch<NT, TOK>(y, a, s_row, count, 0);
+        Sums<NT> c;
+#pragma unroll
+        for (int f = 0; f < NF; ++f)
+#pragma unroll
+            for (int n = 0; n < NT; ++n) {
+                c.sum[f][n] = Float4{0, 0, 0, 0};
+#pragma unroll
+                for (int s = 0; s < SETS; ++s) c.acc[s][f][n] = Float4{0, 0, 0, 0};
+            }
+        const int last = steps() - 1, turns = last / a.k_waves + 1, chunk_turns = C::STEPS / a.k_waves;
+        const int mine = row0 < a.n_rows ? last - k_wave : -1;       // (steps of this wave: those up to k_wave + mine)
+        for (int t0 = 0; t0 < turns; t0 += RING) {
+#pragma unroll
+            for (int i = 0; i < RING; ++i) {
+                const int t = t0 + i;
+                if (t >= turns) break;
+                const int chunk = t / chunk_turns;
+                if (t % chunk_turns == 0) {
+                    put<NT, TOK>(y, chunk, xs + (chunk & 1) * C::PIECES);
+                    __syncthreads();
+                    if (t + chunk_turns < turns) fetch<NT, TOK>(y, a, s_row, count, chunk + 1);
+                }
+                const int s = k_wave + t * a.k_waves;
+                Scales sc;
+                load(sc, min(s, last), a);
+                load(w[(i + AHEAD) % RING], min(s + AHEAD * a.k_waves, last), a);
+                if (t * a.k_waves <= mine) {
+                    if constexpr (DENSE) {
+                        if ((s + 1) * STEP > n_cols) {
+#pragma unroll
+                            for (int f = 0; f < NF; ++f)
+#pragma unroll
+                                for (int q = 0; q < WL; ++q) w[i].w[f][q] = set_right<Bits>(w[i].w[f][q], dense_column(s), n_cols);
+                        }
+                    }
+                    multiply<NT, TOK>(c, w[i], sc, xs + (chunk & 1) * C::PIECES + (s - chunk * C::STEPS) * (SUB * NT * XP * C::LANES) +
+                                                   g * TOK + r % TOK);
+                }
+            }
+        }
+        __syncthreads();
+        if constexpr (DENSE) {
+#pragma unroll
+            for (int f = 0; f < NF; ++f)
+#pragma unroll
+                for (int n = 0; n < NT; ++n)
+#pragma unroll
+                    for (int v = 0; v < 4; ++v)
+                        c.sum[f][n][v] = SETS > 1 ? fmaf(c.acc[0][f][n][v], kHalfHigh, c.acc[SETS - 1][f][n][v]) : c.acc[0][f][n][v];
+        }
+
+        const int out_blocks = a.gated ? NF / 2 : NF;
+        // sums of the waves that share rows, in their order (in the place of X, which all waves are done with)
+        Float4 *const red = reinterpret_cast<Float4 *>(smem);
+#pragma unroll
+        for (int f = 0; f < NF; ++f)
+#pragma unroll
+            for (int n = 0; n < NT; ++n) red[((wave * NF + f) * NT + n) * 64 + lane] = c.sum[f][n];
+        __syncthreads();
+        const int row_groups = kExpertWaves / a.k_waves, per_group = out_blocks * NT * 64;
+        for (int item = threadIdx.x; item < row_groups * per_group; item += kExpertThreads) {
+            const int rg = item / per_group, in = item % per_group;        // (in: block, sixteen entries, lane)
+            const Float4 *p = red + rg * a.k_waves * (NF * NT * 64) + in;
+            Float4 y = p[0];
+            for (int w = 1; w < a.k_waves; ++w) y += p[w * (NF * NT * 64)];
+            Float4 up = Float4{1, 1, 1, 1};
+            if (a.gated) {
+                p += NF / 2 * NT * 64;
+                up = p[0];
+                for (int w = 1; w < a.k_waves; ++w) up += p[w * (NF * NT * 64)];
+            }
+            const int f = in / (NT * 64), n = in / 64 % NT, il = in & 63;
+            const int slot = 16 * n + (il & 15);
+            // (row0 is that of this wave's group)
+            const int first = row0 + (rg - wave / a.k_waves) * (16 * out_blocks);
+            if (slot < count && first + 16 * f < a.n_rows) store(a, s_entry[slot], block_row(a, first, f) + 4 * (il >> 4), y, up);
+        }
+    }
+};
+
+// One element of D: the sum of value times result over the entries of a token, in their order.
+template <bool SHARED>
+__device__ __forceinline__ float combine_entries(const int32_t *__restrict__ rowptr, const int32_t *__restrict__ colidx,
+                                                 const float *__restrict__ vals, const float *Y, int64_t ldy, int n_experts, int t, int c) {
+    constexpr int batch = 4;          // entries whose loads go out together
+    const int q1 = rowptr[t + 1];
+    float d = 0.0f;
+    for (int q = rowptr[t]; q < q1; q += batch) {
+        float v[batch], y[batch];
+        bool in[batch];
+#pragma unroll
+        for (int i = 0; i < batch; ++i) {
+            const int e = min(q + i, q1 - 1);
+            in[i] = q + i < q1 && (uint32_t)colidx[e] < (uint32_t)n_experts;
+            v[i] = vals[e];
+            const float *p = Y + (int64_t)e * ldy + c;
+            y[i] = SHARED ? __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) : *p;
+        }
+#pragma unroll
+        for (int i = 0; i < batch; ++i)
+            if (in[i]) d = fmaf(v[i], y[i], d);
+    }
+    return d;
+}
+
+template <int EL, int KIND, int G, bool HID, int NF>
+__global__ __launch_bounds__(kExpertThreads, 2) void k_experts(const ExpertLaunch a) {
+    typedef Expert<EL, KIND, G, HID, NF> Ex;
+    constexpr int most = 16 * Ex::MOST;
+    __shared__ int s_count[kExpertWaves], s_entry[most], s_row[most], s_rowptr[HID ? 1 : kNearRows], s_last;
+    extern __shared__ __align__(16) unsigned char smem[];
+
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int wave_rows = 16 * (a.gated ? NF / 2 : NF), rows_per = kExpertWaves / a.k_waves * wave_rows;
+    const int tiles = (a.n_rows + rows_per - 1) / rows_per;
+    const int tile = blockIdx.x % tiles, unit = blockIdx.x / tiles;
+    const int row0 = tile * rows_per + wave / a.k_waves * wave_rows, k_wave = wave % a.k_waves;
+
+    const bool by_entry = a.rowptr && a.n_entries <= a.n_experts;
+    int expert = 0;
+    if (a.rowptr) expert = !by_entry ? unit : unit < a.n_entries ? a.colidx[unit] : -1;
+    const bool named = expert >= 0 && expert < a.n_experts;
+    Ex x;
+    typename Ex::Weights w[Ex::RING];
+    if (named) {
+        x.set(a, expert, row0);
+        x.start(w, a, k_wave);        // (before the entries are looked for: nearly always there are some)
+    }
+    // row pointers are looked at in LDS, as far as they fit
+    const bool near = !HID && a.rowptr && a.n_tokens < kNearRows;
+    if (near && named)
+        for (int i = threadIdx.x; i <= a.n_tokens; i += kExpertThreads) s_rowptr[i] = a.rowptr[i];
+    for (int first = 0; named; first += most) {
+        // the entries first .. first + most - 1 of those that name the expert
         int total = a.n_entries;
         if (a.rowptr) {
             total = 0;
@@ -168,247 +625,104 @@ __global__ __launch_bounds__(kExpertThreads) void k_experts(const ExpertLaunch a
                     total += s_count[w];
                 }
                 const int rank = before + __popcll(m & ((1ull << lane) - 1)) - first;
-                if (hit && rank >= 0 && rank < 16 * NT) s_entry[rank] = i;
+                if (hit && rank >= 0 && rank < most) {
+                    s_entry[rank] = i;
+                    if (HID) s_row[rank] = i;
+                    else if (near) s_row[rank] = row_of_entry(s_rowptr, a.n_tokens, a.n_entries, i);
+                    else s_row[rank] = row_of_entry(a.rowptr, a.n_tokens, a.n_entries, i);
+                }
                 __syncthreads();
             }
         }
-        if (total <= first) return;
+        total = __builtin_amdgcn_readfirstlane(total);
+        if (total <= first) break;
         // (by entry: the first that names the expert does the work of all)
-        if (by_entry && first == 0 && s_entry[0] != unit) return;
-        const int count = min(total - first, 16 * NT);
-
-        const char *xp[NT];
-#pragma unroll
-        for (int n = 0; n < NT; ++n) {
-            // (beyond the last entry: the first one again; what comes of it is not stored)
-            const int at = 16 * n + r < count ? 16 * n + r : 0;
-            int row = a.rowptr ? s_entry[at] : first + at;
-            if (a.rowptr && !HID) row = row_of_entry(a.rowptr, a.n_tokens, a.n_entries, row);
-            xp[n] = static_cast<const char *>(a.X) + (row * a.ldx + XE * g) * (int64_t)sizeof(T);
+        if (by_entry && first == 0 && __builtin_amdgcn_readfirstlane(s_entry[0]) != unit) break;
+        const int count = min(total - first, most);
+        if (first > 0) x.start(w, a, k_wave);
+        if (!a.rowptr) {
+            if ((int)threadIdx.x < count) s_entry[threadIdx.x] = s_row[threadIdx.x] = first + (int)threadIdx.x;
+            __syncthreads();
         }
-
-        Float4 sum[NF][NT], acc[SETS][NF][NT];
-#pragma unroll
-        for (int f = 0; f < NF; ++f)
-#pragma unroll
-            for (int n = 0; n < NT; ++n) {
-                sum[f][n] = Float4{0, 0, 0, 0};
-#pragma unroll
-                for (int s = 0; s < SETS; ++s) acc[s][f][n] = Float4{0, 0, 0, 0};
-            }
-
-        struct Step {
-            Words4 w[NF];
-            float scale[DENSE ? 1 : NF][DENSE ? 1 : G][DENSE ? 1 : 4];
-            Words4 x[SUB][NT][XR];
-        };
-        auto load = [&](Step &s, int step, bool whole) __attribute__((always_inline)) {
-            const int k0 = step * STEP;
-#pragma unroll
-            for (int f = 0; f < NF; ++f) {
-                if constexpr (DENSE) {
-                    const char *p = wp[f] + (int64_t)k0 * (int)sizeof(T);
-                    if (whole) {
-                        s.w[f] = __builtin_nontemporal_load(reinterpret_cast<const AnyWords4 *>(p));
-                    } else {
-                        T e[XE];
-#pragma unroll
-                        for (int i = 0; i < XE; ++i) e[i] = k0 + XE * g + i < a.n_cols ? reinterpret_cast<const T *>(p)[i] : T(0);
-                        s.w[f] = __builtin_bit_cast(Words4, e);
-                    }
-                } else {
-                    s.w[f] = __builtin_nontemporal_load(reinterpret_cast<const Words4 *>(wp[f] + (int64_t)step * 1024));
-#pragma unroll
-                    for (int q = 0; q < G; ++q)
-#pragma unroll
-                        for (int v = 0; v < 4; ++v) {
-                            const int out = a.gated ? min(tile * 16 + 4 * g + v, a.n_rows - 1) + f * a.n_rows
-                                                    : min((tile * NF + f) * 16 + 4 * g + v, a.n_rows - 1);
-                            const int64_t at = ((int64_t)(out >> 4) * blocks + step) * (16 * G) + ((out & 15) >> 2) * (4 * G) + 4 * q + (out & 3);
-                            s.scale[f][q][v] = El<TF_BF16>::get(reinterpret_cast<const uint16_t *>(sp[f])[at]);
-                        }
-                }
-            }
-#pragma unroll
-            for (int j = 0; j < SUB; ++j)
-#pragma unroll
-                for (int n = 0; n < NT; ++n)
-#pragma unroll
-                    for (int h = 0; h < XR; ++h) {
-                        constexpr int per = 16 / (int)sizeof(T);        // elements of a piece
-                        const int k = k0 + 32 * j + (WIDE && h ? 4 : 0);
-                        const char *p = xp[n] + (int64_t)k * (int)sizeof(T) + (HID && !WIDE && h ? a.x_part : 0);
-                        if (whole) {
-                            s.x[j][n][h] = *reinterpret_cast<const AnyWords4 *>(p);
-                        } else {
-                            T e[per];
-#pragma unroll
-                            for (int i = 0; i < per; ++i) e[i] = k + XE * g + i < a.n_cols ? reinterpret_cast<const T *>(p)[i] : T(0);
-                            s.x[j][n][h] = __builtin_bit_cast(Words4, e);
-                        }
-                    }
-        };
-        auto multiply = [&](const Step &s) __attribute__((always_inline)) {
-#pragma unroll
-            for (int j = 0; j < SUB; ++j) {
-                Words4 w[NF];
-#pragma unroll
-                for (int f = 0; f < NF; ++f)
-                    if constexpr (DENSE) w[f] = s.w[f];
-                    else w[f] = q4_decode<EL, KIND>(s.w[f][j]);
-#pragma unroll
-                for (int n = 0; n < NT; ++n) {
-                    if constexpr (DENSE && WIDE) {
-                        const Float4 x = __builtin_bit_cast(Float4, s.x[j][n][0]);
-#pragma unroll
-                        for (int f = 0; f < NF; ++f) {
-                            const Float4 y = __builtin_bit_cast(Float4, w[f]);
-#pragma unroll
-                            for (int i = 0; i < 4; ++i) acc[0][f][n] = mfma_f32(y[i], x[i], acc[0][f][n]);
-                        }
-                    } else if constexpr (WIDE) {
-                        Words4 part[3];
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) {
-                            uint32_t h, m, l;
-                            cut_pair(h, m, l, __uint_as_float(s.x[j][n][i / 2][2 * (i & 1)]), __uint_as_float(s.x[j][n][i / 2][2 * (i & 1) + 1]));
-                            part[0][i] = h;
-                            part[1][i] = m;
-                            part[2][i] = l;
-                        }
-#pragma unroll
-                        for (int f = 0; f < NF; ++f) {
-                            acc[0][f][n] = mfma_bf16(w[f], part[0], acc[0][f][n]);
-                            acc[1][f][n] = mfma_bf16(w[f], part[1], acc[1][f][n]);
-                            acc[1][f][n] = mfma_bf16(w[f], part[2], acc[1][f][n]);
-                        }
-                    } else {
-#pragma unroll
-                        for (int f = 0; f < NF; ++f)
-#pragma unroll
-                            for (int h = 0; h < XR; ++h) {
-                                Float4 &c = acc[SETS > 1 ? h : 0][f][n];
-                                c = EL == TF_F16 ? mfma_f16(w[f], s.x[j][n][h], c) : mfma_bf16(w[f], s.x[j][n][h], c);
-                            }
-                    }
-                }
-                if constexpr (!DENSE) {
-                    if ((j + 1) % (4 / G) == 0) {
-#pragma unroll
-                        for (int f = 0; f < NF; ++f)
-#pragma unroll
-                            for (int n = 0; n < NT; ++n)
-#pragma unroll
-                                for (int v = 0; v < 4; ++v) {
-                                    float c = acc[0][f][n][v];
-                                    acc[0][f][n][v] = 0.0f;
-                                    if constexpr (SETS > 1) {
-                                        c = EL == TF_F16 ? fmaf(c, kHalfHigh, acc[1][f][n][v]) : c + acc[1][f][n][v];
-                                        acc[1][f][n][v] = 0.0f;
-                                    }
-                                    sum[f][n][v] = fmaf(s.scale[f][j / (4 / G)][v], c, sum[f][n][v]);
-                                }
-                    }
-                }
-            }
-        };
-
-        const int whole_steps = a.n_cols / STEP, steps = (a.n_cols + STEP - 1) / STEP;
-        for (int s0 = wave * U; s0 < steps; s0 += kExpertWaves * U) {
-            if (s0 + U <= whole_steps) {
-                Step s[U];
-#pragma unroll
-                for (int u = 0; u < U; ++u) load(s[u], s0 + u, true);
-#pragma unroll
-                for (int u = 0; u < U; ++u) multiply(s[u]);
-            } else {
-                for (int u = s0; u < min(s0 + U, steps); ++u) {
-                    Step s;
-                    load(s, u, false);
-                    multiply(s);
-                }
-            }
-        }
-        if constexpr (DENSE) {
-#pragma unroll
-            for (int f = 0; f < NF; ++f)
-#pragma unroll
-                for (int n = 0; n < NT; ++n)
-#pragma unroll
-                    for (int v = 0; v < 4; ++v)
-                        sum[f][n][v] = SETS > 1 ? fmaf(acc[0][f][n][v], kHalfHigh, acc[SETS - 1][f][n][v]) : acc[0][f][n][v];
-        }
-
-        // sums of the waves, in their order
-#pragma unroll
-        for (int f = 0; f < NF; ++f)
-#pragma unroll
-            for (int n = 0; n < NT; ++n) red[((wave * NF + f) * NT + n) * 64 + lane] = sum[f][n];
+        if (count <= 4) x.template run<1, 4>(a, w, k_wave, row0, count, s_entry, s_row, smem);
+        else if (count <= 16) x.template run<1, 16>(a, w, k_wave, row0, count, s_entry, s_row, smem);
+        else if (Ex::MOST == 2 || count <= 32) x.template run<2, 16>(a, w, k_wave, row0, count, s_entry, s_row, smem);
+        else x.template run<Ex::MOST, 16>(a, w, k_wave, row0, count, s_entry, s_row, smem);
+        if (first + most >= total) break;
         __syncthreads();
-        const int items = (a.gated ? 1 : NF) * NT * 64;
-        for (int item = threadIdx.x; item < items; item += kExpertThreads) {
-            Float4 y = red[item];
-            for (int w = 1; w < kExpertWaves; ++w) y += red[w * (NF * NT * 64) + item];
-            Float4 up = Float4{1, 1, 1, 1};
-            if (a.gated) {
-                up = red[NT * 64 + item];
-                for (int w = 1; w < kExpertWaves; ++w) up += red[(w * NF + 1) * (NT * 64) + item];
-            }
-            const int f = item / (NT * 64), n = item / 64 % NT, il = item & 63;
-            const int slot = 16 * n + (il & 15);
-            const int row0 = (a.gated ? tile : tile * NF + f) * 16 + 4 * (il >> 4);
-            if (slot < count) {
-                const int entry = a.rowptr ? s_entry[slot] : first + slot;
-#pragma unroll
-                for (int v = 0; v < 4; ++v) {
-                    if (row0 + v >= a.n_rows) continue;
-                    const int64_t at = (int64_t)entry * a.ldo + row0 + v;
-                    if (a.out_kind == kOutSums) {
-                        static_cast<float *>(a.out)[at] = y[v];
-                    } else if (a.out_kind == kOutRows) {
-                        static_cast<T *>(a.out)[at] = El<EL>::put(y[v]);
-                    } else {
-                        const float h = activate(a.activation, y[v]) * up[v];
-                        T *hi = static_cast<T *>(a.out);
-                        T *lo = reinterpret_cast<T *>(static_cast<char *>(a.out) + a.out_part);
-                        if constexpr (EL == TF_F32) {
-                            hi[at] = h;
-                        } else if constexpr (EL == TF_BF16) {
-                            const uint16_t top = El<EL>::put(h);
-                            const float rest = h - El<EL>::get(top);
-                            hi[at] = top;
-                            lo[at] = __builtin_isinf(El<EL>::get(top)) ? 0 : El<EL>::put(rest);
-                        } else {
-                            const uint16_t top = El<EL>::put(h * (1.0f / kHalfHigh));
-                            const float rest = fmaf(-kHalfHigh, El<EL>::get(top), h);
-                            hi[at] = top;
-                            lo[at] = __builtin_isinf(El<EL>::get(top)) ? 0 : El<EL>::put(fminf(fmaxf(rest, -65504.0f), 65504.0f));
-                        }
-                    }
-                }
-            }
-        }
-        if (first + 16 * NT >= total) return;
+    }
+    if constexpr (HID) {
+        if (!a.arrived) return;
+        // this workgroup's sums are where all others see them, then it counts itself in; the last one for a block of columns
+        // adds up the entries of each token
+        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup");
+        __builtin_amdgcn_s_waitcnt(0);
         __syncthreads();
+        if (threadIdx.x == 0) s_last = atomicInc(a.arrived + tile, (unsigned)(gridDim.x / tiles - 1)) == gridDim.x / tiles - 1;
+        __syncthreads();
+        if (!s_last) return;
+        __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup");
+        const int cols = min(rows_per, a.n_rows - tile * rows_per);
+        for (int i = threadIdx.x; i < a.n_tokens * cols; i += kExpertThreads) {
+            const int t = i / cols, c = tile * rows_per + i % cols;
+            static_cast<typename El<EL>::T *>(a.D)[(int64_t)t * a.ldd + c] = El<EL>::put(
+                combine_entries<true>(a.rowptr, a.colidx, a.vals, static_cast<const float *>(a.out), a.ldo, a.n_experts, t, c));
+        }
     }
 }
 
-template <int EL, int KIND, int G, bool HID, int NT> int launch_experts_nt(const ExpertLaunch &a, hipStream_t st) {
-    const int rows_per = a.gated ? 16 : 16 * kExpertFrags;
+template <int EL> __global__ __launch_bounds__(256) void k_combine(const ExpertLaunch a, int col_blocks) {
+    const int t = blockIdx.x / col_blocks, c = blockIdx.x % col_blocks * 256 + threadIdx.x;
+    if (c >= a.n_rows) return;
+    static_cast<typename El<EL>::T *>(a.D)[(int64_t)t * a.ldd + c] =
+        El<EL>::put(combine_entries<false>(a.rowptr, a.colidx, a.vals, static_cast<const float *>(a.out), a.ldo, a.n_experts, t, c));
+}
+
+template <int EL, int KIND, int G, bool HID, int NF> int launch_experts_nf(ExpertLaunch a, int64_t units, int k_waves, hipStream_t st) {
+    typedef Expert<EL, KIND, G, HID, NF> Ex;
+    const int most = a.rowptr ? a.n_tokens : a.n_entries;      // entries of an expert, one a token
+    const int steps = (a.n_cols + Ex::STEP - 1) / Ex::STEP;
+    int lds = Ex::template bytes<1, 4>(steps);
+    if (most > 4) lds = std::max(lds, Ex::template bytes<1, 16>(steps));
+    if (most > 16) lds = std::max(lds, Ex::template bytes<2, 16>(steps));
+    if (most > 32) lds = std::max(lds, Ex::template bytes<Ex::MOST, 16>(steps));
+    const int rows_per = kExpertWaves / k_waves * 16 * (a.gated ? NF / 2 : NF);
     const int64_t tiles = (a.n_rows + rows_per - 1) / rows_per;
-    const int64_t units = !a.rowptr ? 1 : a.n_entries <= a.n_experts ? a.n_entries : a.n_experts;
-    const size_t lds = (size_t)kExpertWaves * kExpertFrags * NT * 64 * sizeof(Float4);
-    if (lds >= (64 << 10) - 1024) {          // (more than a launch may ask for by default, with the static LDS)
-        static const int raised = (int)hipFuncSetAttribute(reinterpret_cast<const void *>(&k_experts<EL, KIND, G, HID, NT>),
-                                                           hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
-        if (raised) return raised;
-    }
-    hipLaunchKernelGGL((k_experts<EL, KIND, G, HID, NT>), dim3((unsigned)(tiles * units)), dim3(kExpertThreads), lds, st, a);
+    a.k_waves = k_waves;
+    // (more than a launch may ask for by default)
+    static const int raised = (int)hipFuncSetAttribute(reinterpret_cast<const void *>(&k_experts<EL, KIND, G, HID, NF>),
+                                                       hipFuncAttributeMaxDynamicSharedMemorySize, 96 << 10);
+    if (raised) return raised;
+    hipLaunchKernelGGL((k_experts<EL, KIND, G, HID, NF>), dim3((unsigned)(tiles * units)), dim3(kExpertThreads), lds, st, a);
     return (int)hipGetLastError();
 }
-template <int EL, int KIND, int G, bool HID> int launch_experts_hid(const ExpertLaunch &a, hipStream_t st) {
-    const int most = a.rowptr ? a.n_tokens : a.n_entries;      // entries of an expert, one a token
-    return most <= 16 ? launch_experts_nt<EL, KIND, G, HID, 1>(a, st) : launch_experts_nt<EL, KIND, G, HID, 4>(a, st);
+// The most waves of a workgroup that may share columns: each has a step of every chunk.
+template <typename Ex> int most_k_waves(int most) {
+    const int steps = most <= 4 ? Ex::template Chunk<1, 4>::STEPS : most <= 16 ? Ex::template Chunk<1, 16>::STEPS
+                      : most <= 32 ? Ex::template Chunk<2, 16>::STEPS : Ex::template Chunk<Ex::MOST, 16>::STEPS;
+    return std::min(kExpertWaves, steps);
+}
+template <int EL, int KIND, int G, bool HID> int launch_experts_hid(ExpertLaunch a, hipStream_t st) {
+    const int most = a.rowptr ? a.n_tokens : a.n_entries;
+    const int64_t units = !a.rowptr ? 1 : a.n_entries < 1 ? 1 : a.n_entries <= a.n_experts ? a.n_entries : a.n_experts;
+    if (HID && a.n_tokens > kJoinTokens) a.arrived = nullptr;
+    const auto workgroups = [&](int rows) { return (a.n_rows + rows - 1) / rows * units; };
+    // Two blocks of rows a wave, so that what is read of X from LDS is used twice; one where workgroups would be too few otherwise.
+    // Waves share columns as long as workgroups are few.
+    const auto spread = [&](int out, int k_waves) {
+        while (k_waves > 1 && workgroups(kExpertWaves / k_waves * 2 * out) >= kExpertSpread) k_waves /= 2;
+        return k_waves;
+    };
+    int e;
+    const int k2 = most_k_waves<Expert<EL, KIND, G, HID, 2>>(most), out2 = a.gated ? 16 : 32;
+    if (!a.gated && workgroups(kExpertWaves / k2 * 32) < kExpertSpread)
+        e = launch_experts_nf<EL, KIND, G, HID, 1>(a, units, spread(16, most_k_waves<Expert<EL, KIND, G, HID, 1>>(most)), st);
+    else
+        e = launch_experts_nf<EL, KIND, G, HID, 2>(a, units, spread(out2, k2), st);
+    if (e || !HID || a.arrived) return e;
+    const int col_blocks = (a.n_rows + 255) / 256;
+    hipLaunchKernelGGL((k_combine<EL>), dim3((unsigned)(col_blocks * (int64_t)a.n_tokens)), dim3(256), 0, st, a, col_blocks);
+    return (int)hipGetLastError();
 }
 template <int EL, int KIND, int G> int launch_experts_g(const ExpertLaunch &a, hipStream_t st) {
     return a.x_hidden ? launch_experts_hid<EL, KIND, G, true>(a, st) : launch_experts_hid<EL, KIND, G, false>(a, st);

@@ -52,9 +52,11 @@ int launch_route(const RouteLaunch &a, void *stream);
 
 // ------------------------------------------------------------------------------ experts' products
 
-// What a launch does with the sums: the activated hidden row of an entry, fp32 sums of an entry, or rows of Y.
-enum ExpertOut { kOutHidden = 0, kOutSums = 1, kOutRows = 2 };
+// What a launch does with the sums of rows of tokens: the activated hidden row of an entry, or rows of Y.  (Those of hidden
+// rows are fp32 sums of entries, which the last workgroup adds up to rows of D.)
+enum ExpertOut { kOutHidden = 0, kOutRows = 2 };
 
+constexpr int64_t kMaxColumns = (int64_t)1 << 24;     // of weights: sixteen rows of them are below 2^31 bytes apart
 struct ExpertLaunch {
     const void *W, *scales;       // dense: row-major; 4 bits: codes and scales as above
     int64_t w_mat, s_mat;         // bytes from one expert's to the next one's
@@ -70,21 +72,16 @@ struct ExpertLaunch {
     int32_t out_kind, activation, gated;
     void *out;
     int64_t ldo, out_part;        // elements; bytes
+    const float *vals;            // hidden rows: values of the entries, rows of D
+    void *D;
+    int64_t ldd;
+    uint32_t *arrived;            // for each block of columns: workgroups that have stored their sums (all zero between launches)
+    int32_t k_waves;              // waves of a workgroup that share the columns of the same rows: 1, 2, 4 or 8
 };
 int launch_experts(const ExpertLaunch &a, void *stream);
 int launch_experts_bf16(const ExpertLaunch &a, void *stream);
 int launch_experts_f16(const ExpertLaunch &a, void *stream);
 int launch_experts_f32(const ExpertLaunch &a, void *stream);
-
-struct CombineLaunch {
-    const float *Y;               // n_entries x n_out
-    const int32_t *rowptr, *colidx;
-    const float *vals;
-    void *D;
-    int64_t ldd;
-    int32_t n_tokens, n_entries, n_experts, n_out, dtype;
-};
-int launch_combine(const CombineLaunch &a, void *stream);
 
 // Elements from one hidden row to the next: whole 4-bit blocks, zeros beyond n_hidden.
 inline int64_t hidden_ld(int64_t n_hidden) { return (n_hidden + kQ4Block - 1) / kQ4Block * kQ4Block; }

@@ -68,6 +68,7 @@ struct tf_moe {
     tf_moe_desc d{};
     Buffer hidden;            // rows between the products, high parts and behind them the low ones
     Buffer sums;              // results of the second product, entry by entry
+    Buffer arrived;           // a count for each block of columns of D
     int64_t hidden_part = 0;
 };
 
@@ -93,9 +94,12 @@ tf_status run_layer(const tf_moe *p, const tf_csr *A, const void *X, int64_t ldx
     second.ldx = tf::hidden_ld(d.n_hidden);
     second.x_hidden = 1;
     second.x_part = p->hidden_part;
-    second.out_kind = tf::kOutSums;
     second.out = p->sums.p;
     second.ldo = d.n_out;
+    second.vals = static_cast<const float *>(A->vals);
+    second.D = D;
+    second.ldd = ldd;
+    second.arrived = static_cast<uint32_t *>(p->arrived.p);
     for (tf::ExpertLaunch *a : {&first, &second}) {
         a->dtype = d.dtype;
         a->rowptr = A->rowptr;
@@ -103,24 +107,11 @@ tf_status run_layer(const tf_moe *p, const tf_csr *A, const void *X, int64_t ldx
         a->n_tokens = (int32_t)A->n_rows;
         a->n_entries = (int32_t)A->nnz;
         a->n_experts = (int32_t)d.n_experts;
-        if (A->nnz == 0) break;
+        if (A->nnz == 0 && a == &first) continue;        // (the second launch writes the zeros)
         const int e = tf::launch_experts(*a, stream);
         if (e) return report_hip(e, "launching the experts' products");
     }
-    tf::CombineLaunch c{};
-    c.Y = static_cast<const float *>(p->sums.p);
-    c.rowptr = A->rowptr;
-    c.colidx = A->colidx;
-    c.vals = static_cast<const float *>(A->vals);
-    c.D = D;
-    c.ldd = ldd;
-    c.n_tokens = (int32_t)A->n_rows;
-    c.n_entries = (int32_t)A->nnz;
-    c.n_experts = (int32_t)d.n_experts;
-    c.n_out = (int32_t)d.n_out;
-    c.dtype = d.dtype;
-    const int e = tf::launch_combine(c, stream);
-    return e ? report_hip(e, "launching the sum over the experts") : TF_OK;
+    return TF_OK;
 }
 
 tf_status check_layer(const tf_moe *p, const tf_csr *A, const void *X, int64_t ldx, const void *W1, const void *W2, void *D, int64_t ldd) {
@@ -211,6 +202,7 @@ tf_status tf_q4_matvec(const tf_q4 *W, const void *X, int64_t ldx, void *Y, int6
     const tf_status st = check_q4(W);
     if (st != TF_OK) return st;
     if (W->n_mats != 1) return report(TF_EMISMATCH, "a product takes one 4-bit matrix");
+    if (W->n_cols > tf::kMaxColumns) return report(TF_EUNSUPPORTED, "weights have rows of at most 2^24 columns");
     if (!routed_dtype(dtype)) return report(TF_EUNSUPPORTED, "element type must be fp32, bf16 or fp16");
     if (m < 0 || m > kMaxSize) return report(TF_EINVAL, "number of rows");
     if (m == 0) return TF_OK;
@@ -279,6 +271,7 @@ tf_status tf_moe_create(const tf_moe_desc *desc, tf_moe **out) {
     if (!routed_dtype(d.dtype)) return report(TF_EUNSUPPORTED, "element type must be fp32, bf16 or fp16");
     if (d.activation < TF_ACT_IDENTITY || d.activation > TF_ACT_GELU) return report(TF_EINVAL, "unknown activation");
     if (d.gated != 0 && d.gated != 1) return report(TF_EINVAL, "gated must be 0 or 1");
+    if (d.n_in > tf::kMaxColumns || d.n_hidden > tf::kMaxColumns) return report(TF_EUNSUPPORTED, "weights have rows of at most 2^24 columns");
     const int64_t most = kMaxSize / 4;
     if (d.n_experts > most || d.n_in > most || d.n_hidden > most || d.n_out > most || d.max_tokens > most || d.max_entries > most)
         return report(TF_EUNSUPPORTED, "a size is too large");
@@ -298,6 +291,9 @@ tf_status tf_moe_create(const tf_moe_desc *desc, tf_moe **out) {
         // columns beyond n_hidden stay zero
         if (e == hipSuccess) e = hipMemset(p->hidden.p, 0, hidden);
         if (e == hipSuccess) e = hipMalloc(&p->sums.p, (size_t)(d.max_entries * d.n_out) * 4);
+        const size_t counts = (size_t)((d.n_out + 15) / 16) * sizeof(uint32_t);
+        if (e == hipSuccess) e = hipMalloc(&p->arrived.p, counts);
+        if (e == hipSuccess) e = hipMemset(p->arrived.p, 0, counts);
         if (e == hipSuccess) e = hipDeviceSynchronize();
     }
     if (e != hipSuccess) {
@@ -319,6 +315,8 @@ tf_status tf_moe_layer(const tf_moe *p, const tf_csr *A, const void *X, int64_t 
     if (st != TF_OK) return st;
     if (!aligned(W1, 16) || !aligned(W2, 16)) return report(TF_EINVAL, "weights must be 16-byte aligned");
     const tf_moe_desc &d = p->d;
+    if (d.n_in * bytes_of(d.dtype) < 16 || d.n_hidden * bytes_of(d.dtype) < 16)
+        return report(TF_EUNSUPPORTED, "dense weights must have rows of 16 bytes or more");
     tf::ExpertLaunch first{}, second{};
     first.W = W1;
     first.w_mat = (d.gated ? 2 : 1) * d.n_hidden * d.n_in * bytes_of(d.dtype);

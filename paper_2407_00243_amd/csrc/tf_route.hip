@@ -1,6 +1,4 @@
-// Router: the largest scores of each token and their weights; and the weighted sum over a token's entries.
-#include <algorithm>
-
+// Router: the largest scores of each token and their weights.
 #include "tf_moe_device.h"
 
 namespace tf {
@@ -100,17 +98,6 @@ template <int EL, int V> __global__ __launch_bounds__(kThreads) void k_route(con
     }
 }
 
-// D[t] = sum of value times Y over the entries of row t, in their order.
-template <int EL> __global__ __launch_bounds__(kThreads) void k_combine(const CombineLaunch a, int col_blocks) {
-    typedef typename El<EL>::T T;
-    const int t = blockIdx.x / col_blocks, c = blockIdx.x % col_blocks * kThreads + threadIdx.x;
-    if (c >= a.n_out) return;
-    float d = 0.0f;
-    for (int q = a.rowptr[t]; q < a.rowptr[t + 1]; ++q)
-        if ((uint32_t)a.colidx[q] < (uint32_t)a.n_experts) d = fmaf(a.vals[q], a.Y[(int64_t)q * a.n_out + c], d);
-    static_cast<T *>(a.D)[(int64_t)t * a.ldd + c] = El<EL>::put(d);
-}
-
 template <int EL> void route_el(const RouteLaunch &a, hipStream_t st) {
     const dim3 grid((a.n_tokens + kWaves - 1) / kWaves), block(kThreads);
     if (a.n_experts <= 64) hipLaunchKernelGGL((k_route<EL, 1>), grid, block, 0, st, a);
@@ -126,16 +113,6 @@ int launch_route(const RouteLaunch &a, void *stream) {
     if (a.dtype == TF_BF16) route_el<TF_BF16>(a, st);
     else if (a.dtype == TF_F16) route_el<TF_F16>(a, st);
     else route_el<TF_F32>(a, st);
-    return (int)hipGetLastError();
-}
-
-int launch_combine(const CombineLaunch &a, void *stream) {
-    const hipStream_t st = static_cast<hipStream_t>(stream);
-    const int col_blocks = (a.n_out + kThreads - 1) / kThreads;
-    const dim3 grid((unsigned)((int64_t)col_blocks * a.n_tokens));
-    if (a.dtype == TF_BF16) hipLaunchKernelGGL(k_combine<TF_BF16>, grid, dim3(kThreads), 0, st, a, col_blocks);
-    else if (a.dtype == TF_F16) hipLaunchKernelGGL(k_combine<TF_F16>, grid, dim3(kThreads), 0, st, a, col_blocks);
-    else hipLaunchKernelGGL(k_combine<TF_F32>, grid, dim3(kThreads), 0, st, a, col_blocks);
     return (int)hipGetLastError();
 }
 
