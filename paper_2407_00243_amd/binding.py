@@ -327,30 +327,40 @@ def tf_run_wavefront(plan: int, wavefront: int, B, C, D, stream=None) -> None:
 
 _ROUTED = {"torch.float32": TF_F32, "float32": TF_F32, "torch.bfloat16": TF_BF16,
            "torch.float16": TF_F16, "float16": TF_F16}
+_codes: dict = {}          # of element types that have been seen, by the type itself
 
 
 def _routed_code(dt) -> int:
-    if isinstance(dt, int):
-        return dt
-    code = _ROUTED.get(str(dt))
+    code = _codes.get(dt)
     if code is None:
-        raise TypeError(f"unsupported element type {dt}")
+        code = dt if isinstance(dt, int) else _ROUTED.get(str(dt))
+        if code is None:
+            raise TypeError(f"unsupported element type {dt}")
+        _codes[dt] = code
     return code
 
 
 def _matrix(x, what: str, cols: Optional[int] = None):
     """Rows, columns and distance of the rows (in elements) of a matrix whose rows are contiguous."""
-    if len(x.shape) != 2:
+    shape = x.shape
+    if len(shape) != 2:
         raise ValueError(f"{what} must be a matrix")
-    rows, n = x.shape
+    rows, n = shape
     if cols is not None and n != cols:
         raise ValueError(f"{what} must have {cols} columns, not {n}")
-    step, ld = x.stride(1), x.stride(0)
-    if n > 1 and step != 1:
+    ld, step = x.stride()
+    if step != 1 and n > 1:
         raise ValueError(f"the rows of {what} must be contiguous")
-    if rows <= 1:
-        ld = max(ld, n)
-    return rows, n, ld
+    return rows, n, ld if rows > 1 else max(ld, n)
+
+
+def _routing(A) -> tf_csr:
+    """A routing matrix as the library takes it (values are fp32)."""
+    if isinstance(A, tf_csr):
+        return A
+    if _routed_code(A.vals.dtype) != TF_F32:
+        raise TypeError("the values of A must be fp32")
+    return tf_csr(A.n_rows, A.n_cols, A.nnz, A.rowptr.data_ptr(), A.colidx.data_ptr(), A.vals.data_ptr(), TF_F32, 1)
 
 
 def _contiguous(x, what: str, shape, dtype: Optional[int] = None):
@@ -376,6 +386,7 @@ class Q4Matrix:
                 raise ValueError(f"{what} must hold {n} bytes")
         self.struct = tf_q4(self.n_mats, self.n_rows, self.n_cols, _addr(codes), _addr(scales), self.kind,
                             self.group)
+        self.ref = ctypes.byref(self.struct)
 
 
 def tf_q4_sizes(n_rows: int, n_cols: int, kind: int, group: int, n_mats: int = 1):
@@ -417,8 +428,9 @@ def tf_q4_matvec(W: Q4Matrix, X, Y, stream=None) -> None:
         raise ValueError("X and Y must have the same number of rows")
     if X.dtype != Y.dtype:
         raise TypeError("X and Y must have the same element type")
-    _check(load_library().tf_q4_matvec(ctypes.byref(W.struct), _addr(X), ldx, _addr(Y), ldy, m,
-                                       _routed_code(X.dtype), _addr(stream)))
+    status = load_library().tf_q4_matvec(W.ref, X.data_ptr(), ldx, Y.data_ptr(), ldy, m, _routed_code(X.dtype), stream)
+    if status:
+        _check(status)
 
 
 def tf_moe_route(scores, A: DeviceCsr, scoring: int = TF_ROUTE_SOFTMAX_TOP, bias=None, scale: float = 1.0,
@@ -429,9 +441,10 @@ def tf_moe_route(scores, A: DeviceCsr, scoring: int = TF_ROUTE_SOFTMAX_TOP, bias
         raise ValueError("A must have a row for each row of the scores")
     if bias is not None and hasattr(bias, "shape"):
         _contiguous(bias, "bias", (A.n_cols,), TF_F32)
-    a = A.as_struct()
-    _check(load_library().tf_moe_route(_addr(scores), ld, _routed_code(scores.dtype), _addr(bias), scoring, scale,
-                                       ctypes.byref(a), _addr(stream)))
+    status = load_library().tf_moe_route(scores.data_ptr(), ld, _routed_code(scores.dtype), _addr(bias), scoring, scale,
+                                         ctypes.byref(_routing(A)), stream)
+    if status:
+        _check(status)
 
 
 def tf_moe_create(n_experts: int, n_in: int, n_hidden: int, n_out: int, dtype, max_tokens: int,
@@ -449,16 +462,13 @@ def tf_moe_destroy(plan: Optional[int]) -> None:
 
 
 def tf_moe_layer(plan: int, A: DeviceCsr, X, W1, W2, D, stream=None) -> None:
-    a = A.as_struct()
-    _check(load_library().tf_moe_layer(plan, ctypes.byref(a), _addr(X), _matrix(X, "X")[2], _addr(W1), _addr(W2),
-                                       _addr(D), _matrix(D, "D")[2], _addr(stream)))
+    _check(load_library().tf_moe_layer(plan, ctypes.byref(_routing(A)), X.data_ptr(), _matrix(X, "X")[2], W1.data_ptr(),
+                                       W2.data_ptr(), D.data_ptr(), _matrix(D, "D")[2], stream))
 
 
 def tf_moe_layer_q4(plan: int, A: DeviceCsr, X, W1: Q4Matrix, W2: Q4Matrix, D, stream=None) -> None:
-    a = A.as_struct()
-    _check(load_library().tf_moe_layer_q4(plan, ctypes.byref(a), _addr(X), _matrix(X, "X")[2],
-                                          ctypes.byref(W1.struct), ctypes.byref(W2.struct), _addr(D),
-                                          _matrix(D, "D")[2], _addr(stream)))
+    _check(load_library().tf_moe_layer_q4(plan, ctypes.byref(_routing(A)), X.data_ptr(), _matrix(X, "X")[2], W1.ref, W2.ref,
+                                          D.data_ptr(), _matrix(D, "D")[2], stream))
 
 
 class MoePlan:
@@ -474,20 +484,23 @@ class MoePlan:
 
     def run(self, A: DeviceCsr, X, W1, W2, D, stream=None) -> None:
         """W1 and W2: both dense (n_experts x (2) n_hidden x n_in, n_experts x n_out x n_hidden) or both Q4Matrix."""
-        for what, x, cols in (("X", X, self.n_in), ("D", D, self.n_out)):
-            if _matrix(x, what, cols)[0] != A.n_rows:
-                raise ValueError(f"{what} must have a row for each row of A")
-            if _routed_code(x.dtype) != self.dtype:
-                raise TypeError(f"{what} has another element type than the plan")
+        rows, _, ldx = _matrix(X, "X", self.n_in)
+        rows_d, _, ldd = _matrix(D, "D", self.n_out)
+        if rows != A.n_rows or rows_d != rows:
+            raise ValueError("X and D must have a row for each row of A")
+        if _routed_code(X.dtype) != self.dtype or _routed_code(D.dtype) != self.dtype:
+            raise TypeError("X and D must have the element type of the plan")
+        lib, a = load_library(), ctypes.byref(_routing(A))
         if isinstance(W1, Q4Matrix) and isinstance(W2, Q4Matrix):
-            tf_moe_layer_q4(self.handle, A, X, W1, W2, D, stream)
-            return
-        if isinstance(W1, Q4Matrix) or isinstance(W2, Q4Matrix):
+            status = lib.tf_moe_layer_q4(self.handle, a, X.data_ptr(), ldx, W1.ref, W2.ref, D.data_ptr(), ldd, stream)
+        elif isinstance(W1, Q4Matrix) or isinstance(W2, Q4Matrix):
             raise TypeError("W1 and W2 must both be dense or both have 4 bits")
-        first = self.n_hidden * (2 if self.gated else 1)
-        _contiguous(W1, "W1", (self.n_experts, first, self.n_in), self.dtype)
-        _contiguous(W2, "W2", (self.n_experts, self.n_out, self.n_hidden), self.dtype)
-        tf_moe_layer(self.handle, A, X, W1, W2, D, stream)
+        else:
+            _contiguous(W1, "W1", (self.n_experts, self.n_hidden * (2 if self.gated else 1), self.n_in), self.dtype)
+            _contiguous(W2, "W2", (self.n_experts, self.n_out, self.n_hidden), self.dtype)
+            status = lib.tf_moe_layer(self.handle, a, X.data_ptr(), ldx, W1.data_ptr(), W2.data_ptr(), D.data_ptr(), ldd, stream)
+        if status:
+            _check(status)
 
     def close(self) -> None:
         if self.handle:

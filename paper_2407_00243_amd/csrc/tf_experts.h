@@ -141,7 +141,7 @@ template <int EL, int KIND, int G, bool HID, int NF> struct Expert {
     typedef typename El<EL>::T T;
     typedef std::conditional_t<EL == TF_F32, uint32_t, uint16_t> Bits;
     static constexpr int CHUNK = 32 << 10;                           // LDS of a chunk of X, of which there are two
-    static constexpr int MOST = 4;                                   // blocks of sixteen entries that are multiplied at a time
+    static constexpr int MOST = KIND < 0 || NF == 1 ? 4 : 2;           // blocks of sixteen entries that are multiplied at a time
     static constexpr bool DENSE = KIND < 0, WIDE = EL == TF_F32;
     static constexpr int PIECE = 16 / (int)sizeof(T);                // elements of sixteen bytes
     static constexpr int STEP = DENSE ? 8 * PIECE : kQ4Block;        // columns of a step
@@ -150,9 +150,8 @@ template <int EL, int KIND, int G, bool HID, int NF> struct Expert {
     static constexpr int XP = !DENSE && WIDE ? 3 : HID && !WIDE ? 2 : 1;   // parts of X
     static constexpr int SETS = !DENSE && WIDE ? 2 : HID && EL == TF_F16 ? 2 : 1;   // sums of high and of low parts
     static constexpr int WL = DENSE ? 2 : 1;                         // pieces of weights that a lane holds of a step and block
-    static constexpr int SW = DENSE ? 1 : 2 * G;                     // words of scales
-    static constexpr int AHEAD = 2;                      // steps whose weights are on their way
-    static constexpr int RING = AHEAD + 1;
+    static constexpr int SW = G == 4 ? 2 : 1;                        // words of scales
+    static constexpr int AHEAD = 2, RING = AHEAD + 1;                // steps whose weights are on their way, and the one multiplied
     static constexpr int XR = !DENSE && WIDE ? 2 : XP;               // sixteen-byte pieces that a lane loads of an operand
 
     // Chunks of X for NT blocks of TOK entries (of fewer than sixteen only these are held; an operand is 4 TOK pieces then).
@@ -175,8 +174,6 @@ template <int EL, int KIND, int G, bool HID, int NF> struct Expert {
 
     struct Weights {
         Words4 w[NF][WL];
-    };
-    struct Scales {
         uint32_t s[DENSE ? 1 : NF][SW];
     };
 
@@ -184,7 +181,6 @@ template <int EL, int KIND, int G, bool HID, int NF> struct Expert {
     // (below 2^31: columns are limited, kMaxColumns).
     const char *wb[NF], *sb[NF];
     uint32_t w_at[WL], w_up, s_at, s_up;      // (4 bits: those of the rows behind a gate's begin anywhere in the layout's blocks)
-    int s_next, s_off;       // bytes to the scales of the next four of these rows, and how many of them belong to these
     int n_cols, g, r, wave, lane, tid;
 
     // row0: row of the first block of outputs
@@ -199,8 +195,6 @@ template <int EL, int KIND, int G, bool HID, int NF> struct Expert {
         const int64_t blocks = (n_cols + kQ4Block - 1) / kQ4Block;
         const char *w = static_cast<const char *>(a.W) + expert * a.w_mat;
         const char *sc = static_cast<const char *>(a.scales) + expert * a.s_mat;
-        s_off = !DENSE && a.gated ? a.n_rows & 3 : 0;
-        s_next = 0;
         w_up = s_up = s_at = 0;
 #pragma unroll
         for (int f = 0; f < NF; ++f) {
@@ -220,38 +214,19 @@ template <int EL, int KIND, int G, bool HID, int NF> struct Expert {
             for (int i = 0; i < 2; ++i) w_at[i] = (uint32_t)min(8 * i + (r & 7), rows - 1) * (uint32_t)n_cols * (uint32_t)sizeof(T);
         } else {
             w_at[0] = lane * 16;
-            s_at = g * (8 * G);
-            // rows behind a gate's: block b's begin at row n_rows + 16 b, o rows into a block of the layout
-            const int o = a.n_rows & 15;
-            const uint32_t next = (uint32_t)blocks * 1024u;
-            // (the layout's next block exists where rows of it are used; those of the last block that are not are read again)
-            const int last = (2 * a.n_rows - 1) >> 4, b0 = (a.n_rows + block_row(a, row0, 0)) >> 4;
-            const int row = o + r, quad = (o + 4 * g) & ~3;
-            const bool over = NF > 2 || b0 < last;
-            w_up = (row >> 4 && over ? next : 0) + (16 * g + (row & 15)) * 16;
-            s_up = (quad >> 4 && over ? (uint32_t)blocks * (32 * G) : 0) + ((quad & 15) >> 2) * (8 * G);
-            const int quad2 = quad + 4;
-            s_next = (int)((quad2 >> 4 && over ? (uint32_t)blocks * (32 * G) : 0) + ((quad2 & 15) >> 2) * (8 * G)) - (int)s_up;
+            s_at = r * (2 * G);
+            // rows behind a gate's: the first of a block is row o of a block of the layout, whose next one exists where rows of it
+            // are used (rows beyond the matrix: others are read)
+            const int row = (a.n_rows & 15) + r;
+            const bool next = row > 15 && (NF > 2 || (a.n_rows + block_row(a, row0, 0)) >> 4 < (2 * a.n_rows - 1) >> 4);
+            w_up = (next ? (uint32_t)blocks * 1024 : 0) + (16 * g + (row & 15)) * 16;
+            s_up = (next ? (uint32_t)blocks * (32 * G) : 0) + (row & 15) * (2 * G);
         }
     }
     // First row of a block of outputs: the last block of dense weights ends with the matrix (rows that two blocks hold are stored
     // twice, the same), blocks beyond the matrix are its last one.
     static __device__ __forceinline__ int block_row(const ExpertLaunch &a, int row0, int f) {
         return max(0, min(row0 + 16 * f, DENSE ? a.n_rows - 16 : (a.n_rows - 1) & ~15));
-    }
-    static __device__ __forceinline__ void load_scales(uint32_t (&s)[SW], const char *p) {
-        if constexpr (SW == 2) {
-            const Words2 y = *reinterpret_cast<const Words2 *>(p);
-            s[0] = y[0];
-            s[1] = y[1];
-        } else {
-#pragma unroll
-            for (int q = 0; q < SW / 4; ++q) {
-                const Words4 y = reinterpret_cast<const Words4 *>(p)[q];
-#pragma unroll
-                for (int i = 0; i < 4; ++i) s[4 * q + i] = y[i];
-            }
-        }
     }
     __device__ __forceinline__ int dense_column(int step) const { return step * STEP + PIECE * (g + 4 * (r >> 3)); }
     __device__ __forceinline__ void load(Weights &x, int step, const ExpertLaunch &a) const {
@@ -264,28 +239,15 @@ template <int EL, int KIND, int G, bool HID, int NF> struct Expert {
         } else {
             const int out_blocks = a.gated ? NF / 2 : NF;
 #pragma unroll
-            for (int f = 0; f < NF; ++f)
+            for (int f = 0; f < NF; ++f) {
                 x.w[f][0] = __builtin_nontemporal_load(
                     reinterpret_cast<const Words4 *>(wb[f] + (int64_t)step * 1024 + (f >= out_blocks ? w_up : w_at[0])));
-        }
-    }
-    __device__ __forceinline__ void load(Scales &x, int step, const ExpertLaunch &a) const {
-        if constexpr (!DENSE) {
-            const int out_blocks = a.gated ? NF / 2 : NF;
-#pragma unroll
-            for (int f = 0; f < NF; ++f) {
                 const char *p = sb[f] + (int64_t)step * (32 * G) + (f >= out_blocks ? s_up : s_at);
-                load_scales(x.s[f], p);
-                if (f >= NF / 2 && s_off) {
-                    uint32_t y[SW];
-                    load_scales(y, p + s_next);
+                if constexpr (G == 1) {
+                    x.s[f][0] = *reinterpret_cast<const uint16_t *>(p);
+                } else {
 #pragma unroll
-                    for (int q = 0; q < SW; q += 2) {
-                        const uint64_t lo = (uint64_t)x.s[f][q + 1] << 32 | x.s[f][q], hi = (uint64_t)y[q + 1] << 32 | y[q];
-                        const uint64_t z = lo >> (16 * s_off) | hi << (64 - 16 * s_off);
-                        x.s[f][q] = (uint32_t)z;
-                        x.s[f][q + 1] = (uint32_t)(z >> 32);
-                    }
+                    for (int i = 0; i < SW; ++i) x.s[f][i] = reinterpret_cast<const uint32_t *>(p)[i];
                 }
             }
         }
@@ -305,137 +267,150 @@ template <int EL, int KIND, int G, bool HID, int NF> struct Expert {
         }
     }
 
+    // Dense weights: sums of high and of low parts; 4 bits: sums that the scales are in.
     template <int NT> struct Sums {
-        Float4 sum[NF][NT];
-        Float4 acc[SETS][NF][NT];
+        Float4 v[DENSE ? SETS : 1][NF][NT];
     };
     // xs: the step's operands of X in LDS, this lane's piece of the first.
-    template <int NT, int TOK> static __device__ __forceinline__ void multiply(Sums<NT> &c, const Weights &x, const Scales &sc, const Words4 *xs) {
+    template <int NT, int TOK> static __device__ __forceinline__ void multiply(Sums<NT> &c, const Weights &x, const Words4 *xs) {
+        if constexpr (DENSE) {
 #pragma unroll
-        for (int j = 0; j < SUB; ++j) {
-            // (operands of later ones are not read ahead: there are no registers for them)
-            if (NT * XP > 1 && j) __builtin_amdgcn_sched_barrier(0);
-            Words4 w[NF];
+            for (int j = 0; j < SUB; ++j) multiply_operand<NT, TOK>(c.v, x, xs, j);
+        } else {
+            // a group's sums are multiplied by its scales when the instructions of the next group are on their way
+            constexpr int per = 4 / G;
+            Float4 acc[2][SETS][NF][NT];
 #pragma unroll
-            for (int f = 0; f < NF; ++f) w[f] = operand(x, f, j);
+            for (int q = 0; q <= G; ++q) {
+                if (q < G) {
 #pragma unroll
-            for (int n = 0; n < NT; ++n) {
-                Words4 y[XP];
+                    for (int h = 0; h < SETS; ++h)
 #pragma unroll
-                for (int h = 0; h < XP; ++h) y[h] = xs[((j * NT + n) * XP + h) * (4 * TOK)];
+                        for (int f = 0; f < NF; ++f)
 #pragma unroll
-                for (int f = 0; f < NF; ++f) {
-                    if constexpr (DENSE && WIDE) {
-                        const Float4 v = __builtin_bit_cast(Float4, w[f]), b = __builtin_bit_cast(Float4, y[0]);
+                            for (int n = 0; n < NT; ++n) acc[q & 1][h][f][n] = Float4{0, 0, 0, 0};
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) c.acc[0][f][n] = mfma_f32(v[i], b[i], c.acc[0][f][n]);
-                    } else {
-#pragma unroll
-                        for (int h = 0; h < XP; ++h) {
-                            Float4 &d = c.acc[h < SETS ? h : SETS - 1][f][n];
-                            d = EL == TF_F16 ? mfma_f16(w[f], y[h], d) : mfma_bf16(w[f], y[h], d);
-                        }
-                    }
+                    for (int j = q * per; j < (q + 1) * per; ++j) multiply_operand<NT, TOK>(acc[q & 1], x, xs, j);
                 }
-            }
-            if constexpr (!DENSE) {
-                if ((j + 1) % (4 / G) == 0) {
-                    constexpr int per = 4 / G;
+                if (q > 0) {
+                    const int p = q - 1;
 #pragma unroll
                     for (int f = 0; f < NF; ++f) {
-                        float s[4];
-#pragma unroll
-                        for (int v = 0; v < 4; ++v) s[v] = v & 1 ? bf16_high(sc.s[f][2 * (j / per) + v / 2]) : bf16_low(sc.s[f][2 * (j / per) + v / 2]);
+                        const float s = p & 1 ? bf16_high(x.s[f][p / 2]) : bf16_low(x.s[f][p / 2]);
 #pragma unroll
                         for (int n = 0; n < NT; ++n)
 #pragma unroll
                             for (int v = 0; v < 4; ++v) {
-                                float d = c.acc[0][f][n][v];
-                                c.acc[0][f][n][v] = 0.0f;
-                                if constexpr (SETS > 1) {
-                                    d = EL == TF_F16 ? fmaf(d, kHalfHigh, c.acc[SETS - 1][f][n][v]) : d + c.acc[SETS - 1][f][n][v];
-                                    c.acc[SETS - 1][f][n][v] = 0.0f;
-                                }
-                                c.sum[f][n][v] = fmaf(s[v], d, c.sum[f][n][v]);
+                                float d = acc[p & 1][0][f][n][v];
+                                if constexpr (SETS > 1)
+                                    d = EL == TF_F16 ? fmaf(d, kHalfHigh, acc[p & 1][SETS - 1][f][n][v]) : d + acc[p & 1][SETS - 1][f][n][v];
+                                c.v[0][f][n][v] = fmaf(s, d, c.v[0][f][n][v]);
                             }
                     }
                 }
             }
         }
     }
-    // What the sums of an entry's four rows are for.  up: the sums that the gate multiplies.
-    static __device__ __forceinline__ void store(const ExpertLaunch &a, int entry, int row0, const Float4 &y, const Float4 &up) {
+    template <int NT, int TOK, int S>
+    static __device__ __forceinline__ void multiply_operand(Float4 (&acc)[S][NF][NT], const Weights &x, const Words4 *xs, int j) {
+        Words4 w[NF];
 #pragma unroll
-        for (int v = 0; v < 4; ++v) {
-            if (row0 + v >= a.n_rows) continue;
-            const int64_t at = (int64_t)entry * a.ldo + row0 + v;
-            if constexpr (HID) {
-                // (read by another workgroup of the launch: past the caches that it does not share)
-                __hip_atomic_store(static_cast<float *>(a.out) + at, y[v], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-            } else if (a.out_kind == kOutRows) {
-                static_cast<T *>(a.out)[at] = El<EL>::put(y[v]);
-            } else {
-                const float h = activate(a.activation, y[v]) * up[v];
-                T *hi = static_cast<T *>(a.out);
-                T *lo = reinterpret_cast<T *>(static_cast<char *>(a.out) + a.out_part);
-                if constexpr (EL == TF_F32) {
-                    hi[at] = h;
-                } else if constexpr (EL == TF_BF16) {
-                    const uint16_t top = El<EL>::put(h);
-                    const float rest = h - El<EL>::get(top);
-                    hi[at] = top;
-                    lo[at] = __builtin_isinf(El<EL>::get(top)) ? 0 : El<EL>::put(rest);
+        for (int f = 0; f < NF; ++f) w[f] = operand(x, f, j);
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+            Words4 y[XP];
+#pragma unroll
+            for (int h = 0; h < XP; ++h) y[h] = xs[((j * NT + n) * XP + h) * (4 * TOK)];
+#pragma unroll
+            for (int f = 0; f < NF; ++f) {
+                if constexpr (DENSE && WIDE) {
+                    const Float4 v = __builtin_bit_cast(Float4, w[f]), b = __builtin_bit_cast(Float4, y[0]);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) acc[0][f][n] = mfma_f32(b[i], v[i], acc[0][f][n]);
                 } else {
-                    const uint16_t top = El<EL>::put(h * (1.0f / kHalfHigh));
-                    const float rest = fmaf(-kHalfHigh, El<EL>::get(top), h);
-                    hi[at] = top;
-                    lo[at] = __builtin_isinf(El<EL>::get(top)) ? 0 : El<EL>::put(fminf(fmaxf(rest, -65504.0f), 65504.0f));
+#pragma unroll
+                    for (int h = 0; h < XP; ++h) {
+                        Float4 &d = acc[h < SETS ? h : SETS - 1][f][n];
+                        d = EL == TF_F16 ? mfma_f16(y[h], w[f], d) : mfma_bf16(y[h], w[f], d);
+                    }
                 }
+            }
+        }
+    }
+    // What the sum of an entry and a row is for.  up: the sum that the gate multiplies.
+    static __device__ __forceinline__ void store(const ExpertLaunch &a, int entry, int row, float y, float up) {
+        const int64_t at = (int64_t)entry * a.ldo + row;
+        if constexpr (HID) {
+            // (read by another workgroup of the launch: past the caches that it does not share)
+            __hip_atomic_store(static_cast<float *>(a.out) + at, y, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        } else if (a.out_kind == kOutRows) {
+            static_cast<T *>(a.out)[at] = El<EL>::put(y);
+        } else {
+            const float h = activate(a.activation, y) * up;
+            T *hi = static_cast<T *>(a.out);
+            T *lo = reinterpret_cast<T *>(static_cast<char *>(a.out) + a.out_part);
+            if constexpr (EL == TF_F32) {
+                hi[at] = h;
+            } else if constexpr (EL == TF_BF16) {
+                const uint16_t top = El<EL>::put(h);
+                const float rest = h - El<EL>::get(top);
+                hi[at] = top;
+                lo[at] = __builtin_isinf(El<EL>::get(top)) ? 0 : El<EL>::put(rest);
+            } else {
+                const uint16_t top = El<EL>::put(h * (1.0f / kHalfHigh));
+                const float rest = fmaf(-kHalfHigh, El<EL>::get(top), h);
+                hi[at] = top;
+                lo[at] = __builtin_isinf(El<EL>::get(top)) ? 0 : El<EL>::put(fminf(fmaxf(rest, -65504.0f), 65504.0f));
             }
         }
     }
 
     // This thread's pieces of a chunk of X: from memory, and into LDS when they have arrived.  s_row: rows of X of the entries.
     // (Beyond the last entry: the first one again; what comes of it is not stored.)
-    template <int NT, int TOK> __device__ __forceinline__ int piece_column(int m, int chunk) const {
-        typedef Chunk<NT, TOK> C;
-        const int p = m * kExpertThreads + tid;
-        return chunk * (C::STEPS * STEP) + p / C::LANES / NT * SUBK + (WIDE && DENSE ? 4 : 8) * (p % C::LANES / TOK);
-    }
+    // A thread's pieces are all of one row, `row` with its first column k0 (k0: in the chunk).
+    template <int NT, int TOK> static constexpr int piece_columns(int m) { return m * (kExpertThreads / Chunk<NT, TOK>::LANES) / NT * SUBK; }
     template <int NT, int TOK> __device__ __forceinline__ bool piece_needed(int m, int chunk) const {
-        typedef Chunk<NT, TOK> C;
-        return chunk * (C::STEPS * STEP) + m * kExpertThreads / C::LANES / NT * SUBK < steps() * STEP;      // (of the first thread)
+        return chunk * (Chunk<NT, TOK>::STEPS * STEP) + piece_columns<NT, TOK>(m) < steps() * STEP;      // (of the first thread)
     }
+    template <int NT, int TOK> __device__ __forceinline__ bool cut(int chunk) const { return (chunk + 1) * (Chunk<NT, TOK>::STEPS * STEP) > n_cols; }
     template <int NT, int TOK>
-    __device__ __forceinline__ void fetch(Chunk<NT, TOK> &y, const ExpertLaunch &a, const int *s_row, int count, int chunk) const {
+    __device__ __forceinline__ void fetch(Chunk<NT, TOK> &y, const ExpertLaunch &a, const char *row, int k0, int chunk) const {
         typedef Chunk<NT, TOK> C;
+        static_assert(kExpertThreads / C::LANES % NT == 0, "all pieces of a thread are of one entry");
+        k0 += chunk * (C::STEPS * STEP);
+        if (!cut<NT, TOK>(chunk)) {
+            row += (int64_t)k0 * (int)sizeof(T);
+#pragma unroll
+            for (int m = 0; m < C::MINE; ++m)
+#pragma unroll
+                for (int h = 0; h < XR; ++h)
+                    y.x[m][h] = *reinterpret_cast<const AnyWords4 *>((HID && !WIDE && h ? row + a.x_part : row) +
+                                                                    (piece_columns<NT, TOK>(m) + (WIDE && h ? 4 : 0)) * (int)sizeof(T));
+            return;
+        }
 #pragma unroll
         for (int m = 0; m < C::MINE; ++m) {
             if (!piece_needed<NT, TOK>(m, chunk)) break;
-            const int p = m * kExpertThreads + tid;
-            const int at = p / C::LANES % NT * 16 + p % TOK;
-            const char *row = static_cast<const char *>(a.X) + s_row[at < count ? at : 0] * a.ldx * (int64_t)sizeof(T);
-            const int k = piece_column<NT, TOK>(m, chunk);
 #pragma unroll
             for (int h = 0; h < XR; ++h) {
                 const char *q = HID && !WIDE && h ? row + a.x_part : row;
-                const int kh = k + (WIDE && h ? 4 : 0);
-                y.x[m][h] = n_cols < PIECE ? load_short<Bits>(q, kh, n_cols)
-                                           : *reinterpret_cast<const AnyWords4 *>(q + (int64_t)min(kh, n_cols - PIECE) * (int)sizeof(T));
+                const int k = k0 + piece_columns<NT, TOK>(m) + (WIDE && h ? 4 : 0);
+                y.x[m][h] = n_cols < PIECE ? load_short<Bits>(q, k, n_cols)
+                                           : *reinterpret_cast<const AnyWords4 *>(q + (int64_t)min(k, n_cols - PIECE) * (int)sizeof(T));
             }
         }
     }
-    template <int NT, int TOK> __device__ __forceinline__ void put(Chunk<NT, TOK> &y, int chunk, Words4 *xs) const {
+    template <int NT, int TOK> __device__ __forceinline__ void put(Chunk<NT, TOK> &y, int k0, int chunk, Words4 *xs) const {
         typedef Chunk<NT, TOK> C;
-        const bool cut = (chunk + 1) * (C::STEPS * STEP) > n_cols && n_cols >= PIECE;
+        const bool move = cut<NT, TOK>(chunk) && n_cols >= PIECE;
 #pragma unroll
         for (int m = 0; m < C::MINE; ++m) {
             if (!piece_needed<NT, TOK>(m, chunk)) break;
             const int p = m * kExpertThreads + tid;
             if (C::SLOTS * C::LANES % kExpertThreads && p >= C::SLOTS * C::LANES) break;
             Words4 *to = xs + p / C::LANES * (XP * C::LANES) + p % C::LANES;
-            if (cut) {
-                const int k = piece_column<NT, TOK>(m, chunk);
+            if (move) {
+                const int k = k0 + chunk * (C::STEPS * STEP) + piece_columns<NT, TOK>(m);
 #pragma unroll
                 for (int h = 0; h < XR; ++h) y.x[m][h] = set_right<Bits>(y.x[m][h], k + (WIDE && h ? 4 : 0), n_cols);
             }
@@ -473,17 +448,17 @@ template <int EL, int KIND, int G, bool HID, int NF> struct Expert {
         typedef Chunk<NT, TOK> C;
         asm volatile("" : "+v"(tid));          // (what follows from it is worked out here, not before all cases and kept)
         Words4 *const xs = reinterpret_cast<Words4 *>(smem);
+        const int entry = tid / C::LANES % NT * 16 + tid % TOK, k0 = tid / C::LANES / NT * SUBK + (WIDE && DENSE ? 4 : 8) * (tid % C::LANES / TOK);
+        const char *const row = static_cast<const char *>(a.X) + s_row[entry < count ? entry : 0] * a.ldx * (int64_t)sizeof(T);
         C y;
-        fetch<NT, TOK>(y, a, s_row, count, 0);
+        fetch<NT, TOK>(y, a, row, k0, 0);
         Sums<NT> c;
 #pragma unroll
         for (int f = 0; f < NF; ++f)
 #pragma unroll
-            for (int n = 0; n < NT; ++n) {
-                c.sum[f][n] = Float4{0, 0, 0, 0};
+            for (int n = 0; n < NT; ++n)
 #pragma unroll
-                for (int s = 0; s < SETS; ++s) c.acc[s][f][n] = Float4{0, 0, 0, 0};
-            }
+                for (int h = 0; h < (DENSE ? SETS : 1); ++h) c.v[h][f][n] = Float4{0, 0, 0, 0};
         const int last = steps() - 1, turns = last / a.k_waves + 1, chunk_turns = C::STEPS / a.k_waves;
         const int mine = row0 < a.n_rows ? last - k_wave : -1;       // (steps of this wave: those up to k_wave + mine)
         for (int t0 = 0; t0 < turns; t0 += RING) {
@@ -492,38 +467,34 @@ template <int EL, int KIND, int G, bool HID, int NF> struct Expert {
                 const int t = t0 + i;
                 if (t >= turns) break;
                 const int chunk = t / chunk_turns;
+                Words4 *const x = xs + (chunk & 1) * C::PIECES;
                 if (t % chunk_turns == 0) {
-                    put<NT, TOK>(y, chunk, xs + (chunk & 1) * C::PIECES);
+                    put<NT, TOK>(y, k0, chunk, x);
                     __syncthreads();
-                    if (t + chunk_turns < turns) fetch<NT, TOK>(y, a, s_row, count, chunk + 1);
+                    if (t + chunk_turns < turns) fetch<NT, TOK>(y, a, row, k0, chunk + 1);
                 }
                 const int s = k_wave + t * a.k_waves;
-                Scales sc;
-                load(sc, min(s, last), a);
                 load(w[(i + AHEAD) % RING], min(s + AHEAD * a.k_waves, last), a);
-                if (t * a.k_waves <= mine) {
-                    if constexpr (DENSE) {
-                        if ((s + 1) * STEP > n_cols) {
+                if (t * a.k_waves > mine) continue;
+                if constexpr (DENSE) {
+                    if ((s + 1) * STEP > n_cols) {
 #pragma unroll
-                            for (int f = 0; f < NF; ++f)
+                        for (int f = 0; f < NF; ++f)
 #pragma unroll
-                                for (int q = 0; q < WL; ++q) w[i].w[f][q] = set_right<Bits>(w[i].w[f][q], dense_column(s), n_cols);
-                        }
+                            for (int q = 0; q < WL; ++q) w[i].w[f][q] = set_right<Bits>(w[i].w[f][q], dense_column(s), n_cols);
                     }
-                    multiply<NT, TOK>(c, w[i], sc, xs + (chunk & 1) * C::PIECES + (s - chunk * C::STEPS) * (SUB * NT * XP * C::LANES) +
-                                                   g * TOK + r % TOK);
                 }
+                multiply<NT, TOK>(c, w[i], x + s % C::STEPS * (SUB * NT * XP * C::LANES) + g * TOK + r % TOK);
             }
         }
         __syncthreads();
-        if constexpr (DENSE) {
+        if constexpr (DENSE && SETS > 1) {
 #pragma unroll
             for (int f = 0; f < NF; ++f)
 #pragma unroll
                 for (int n = 0; n < NT; ++n)
 #pragma unroll
-                    for (int v = 0; v < 4; ++v)
-                        c.sum[f][n][v] = SETS > 1 ? fmaf(c.acc[0][f][n][v], kHalfHigh, c.acc[SETS - 1][f][n][v]) : c.acc[0][f][n][v];
+                    for (int v = 0; v < 4; ++v) c.v[0][f][n][v] = fmaf(c.v[0][f][n][v], kHalfHigh, c.v[SETS - 1][f][n][v]);
         }
 
         const int out_blocks = a.gated ? NF / 2 : NF;
@@ -532,7 +503,7 @@ template <int EL, int KIND, int G, bool HID, int NF> struct Expert {
 #pragma unroll
         for (int f = 0; f < NF; ++f)
 #pragma unroll
-            for (int n = 0; n < NT; ++n) red[((wave * NF + f) * NT + n) * 64 + lane] = c.sum[f][n];
+            for (int n = 0; n < NT; ++n) red[((wave * NF + f) * NT + n) * 64 + lane] = c.v[0][f][n];
         __syncthreads();
         const int row_groups = kExpertWaves / a.k_waves, per_group = out_blocks * NT * 64;
         for (int item = threadIdx.x; item < row_groups * per_group; item += kExpertThreads) {
@@ -547,10 +518,14 @@ template <int EL, int KIND, int G, bool HID, int NF> struct Expert {
                 for (int w = 1; w < a.k_waves; ++w) up += p[w * (NF * NT * 64)];
             }
             const int f = in / (NT * 64), n = in / 64 % NT, il = in & 63;
-            const int slot = 16 * n + (il & 15);
+            const int slot = 16 * n + 4 * (il >> 4);
             // (row0 is that of this wave's group)
             const int first = row0 + (rg - wave / a.k_waves) * (16 * out_blocks);
-            if (slot < count && first + 16 * f < a.n_rows) store(a, s_entry[slot], block_row(a, first, f) + 4 * (il >> 4), y, up);
+            const int row = block_row(a, first, f) + (il & 15);
+            if (first + 16 * f >= a.n_rows || row >= a.n_rows) continue;
+#pragma unroll
+            for (int v = 0; v < 4; ++v)
+                if (slot + v < count) store(a, s_entry[slot + v], row, y[v], up[v]);
         }
     }
 };

@@ -10,10 +10,9 @@ namespace tf {
 //
 // A matrix is cut into blocks of 16 rows x 128 columns, 1 KiB each, block row after block row: what one wave
 // loads with one instruction, sixteen bytes a lane.  Lane 16 g + r holds in word j the eight columns
-// 128 kb + 32 j + 8 g + {0 .. 7} of row r: the first operand of the j-th 16 x 16 x 32 matrix instruction.
-// Scales follow the results instead: of a block and its 128 / group groups, lane group g holds those of rows
-// 4 g .. 4 g + 3 (where the instruction leaves its sums), group after group.  Columns beyond the matrix have
-// code 0 and scale 0, rows beyond it likewise.
+// 128 kb + 32 j + 8 g + {0 .. 7} of row r: an operand of the j-th 16 x 16 x 32 matrix instruction.  Scales are in blocks of
+// the same rows and columns, row after row, group after group.  Columns beyond the matrix have code 0 and scale 0, rows beyond
+// it likewise.
 constexpr int kQ4Block = 128;
 inline int64_t q4_tiles(int64_t rows) { return (rows + 15) / 16; }
 inline int64_t q4_blocks(int64_t cols) { return (cols + kQ4Block - 1) / kQ4Block; }

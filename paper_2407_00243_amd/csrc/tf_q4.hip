@@ -19,7 +19,7 @@ __device__ __forceinline__ Place place_of_word(int64_t w, int64_t tiles, int64_t
 }
 // Place of the scale of (row, group q of block kb) of a matrix, in elements from the matrix's first.
 __device__ __forceinline__ int64_t scale_at(int64_t row, int64_t kb, int q, int64_t blocks, int per_block) {
-    return ((row >> 4) * blocks + kb) * (16 * per_block) + ((row & 15) >> 2) * (4 * per_block) + 4 * q + (row & 3);
+    return ((row >> 4) * blocks + kb) * (16 * per_block) + (row & 15) * per_block + q;
 }
 
 template <int KIND> __global__ __launch_bounds__(kThreads) void k_q4_pack(const Q4Launch a, int64_t tiles, int64_t blocks) {
