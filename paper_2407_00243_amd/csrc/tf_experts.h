@@ -151,7 +151,8 @@ template <int EL, int KIND, int G, bool HID, int NF> struct Expert {
     static constexpr int SETS = !DENSE && WIDE ? 2 : HID && EL == TF_F16 ? 2 : 1;   // sums of high and of low parts
     static constexpr int WL = DENSE ? 2 : 1;                         // pieces of weights that a lane holds of a step and block
     static constexpr int SW = G == 4 ? 2 : 1;                        // words of scales
-    static constexpr int AHEAD = 2, RING = AHEAD + 1;                // steps whose weights are on their way, and the one multiplied
+    static constexpr int AHEAD = 1, RING = AHEAD + 1;                // steps whose weights are on their way, and the one multiplied
+    static constexpr int XE = DENSE && WIDE ? 4 : 8;                 // columns of X that a lane holds of an operand
     static constexpr int XR = !DENSE && WIDE ? 2 : XP;               // sixteen-byte pieces that a lane loads of an operand
 
     // Chunks of X for NT blocks of TOK entries (of fewer than sixteen only these are held; an operand is 4 TOK pieces then).
@@ -162,13 +163,14 @@ template <int EL, int KIND, int G, bool HID, int NF> struct Expert {
         static constexpr int SLOTS = STEPS * SUB * NT;
         static constexpr int MINE = (SLOTS * LANES + kExpertThreads - 1) / kExpertThreads;
         static constexpr int PIECES = SLOTS * XP * LANES;            // of a buffer
+        const char *row[MINE];                                       // where the thread's pieces begin
         Words4 x[MINE][XR];
     };
 
     // LDS of a workgroup: two chunks of X, or one if that is all there is; the waves' sums in their place.
     template <int NT, int TOK> static int bytes(int steps) {
         typedef Chunk<NT, TOK> C;
-        const int x = steps > C::STEPS ? 2 * C::PIECES : (steps * SUB * NT * C::LANES + kExpertThreads - 1) / kExpertThreads * kExpertThreads * XP;
+        const int x = steps > C::STEPS ? 2 * C::PIECES : steps * SUB * NT * C::LANES * XP;
         return std::max(x * 16, kExpertWaves * NF * NT * 1024);
     }
 
@@ -271,11 +273,11 @@ template <int EL, int KIND, int G, bool HID, int NF> struct Expert {
     template <int NT> struct Sums {
         Float4 v[DENSE ? SETS : 1][NF][NT];
     };
-    // xs: the step's operands of X in LDS, this lane's piece of the first.
-    template <int NT, int TOK> static __device__ __forceinline__ void multiply(Sums<NT> &c, const Weights &x, const Words4 *xs) {
+    // xs: operands of X in LDS, the step's from j0 on.
+    template <int NT, int TOK> __device__ __forceinline__ void multiply(Sums<NT> &c, const Weights &x, const Words4 *xs, int j0) const {
         if constexpr (DENSE) {
 #pragma unroll
-            for (int j = 0; j < SUB; ++j) multiply_operand<NT, TOK>(c.v, x, xs, j);
+            for (int j = 0; j < SUB; ++j) multiply_operand<NT, TOK>(c.v, x, xs, j0, j);
         } else {
             // a group's sums are multiplied by its scales when the instructions of the next group are on their way
             constexpr int per = 4 / G;
@@ -290,7 +292,7 @@ template <int EL, int KIND, int G, bool HID, int NF> struct Expert {
 #pragma unroll
                             for (int n = 0; n < NT; ++n) acc[q & 1][h][f][n] = Float4{0, 0, 0, 0};
 #pragma unroll
-                    for (int j = q * per; j < (q + 1) * per; ++j) multiply_operand<NT, TOK>(acc[q & 1], x, xs, j);
+                    for (int j = q * per; j < (q + 1) * per; ++j) multiply_operand<NT, TOK>(acc[q & 1], x, xs, j0, j);
                 }
                 if (q > 0) {
                     const int p = q - 1;
@@ -312,7 +314,8 @@ template <int EL, int KIND, int G, bool HID, int NF> struct Expert {
         }
     }
     template <int NT, int TOK, int S>
-    static __device__ __forceinline__ void multiply_operand(Float4 (&acc)[S][NF][NT], const Weights &x, const Words4 *xs, int j) {
+    __device__ __forceinline__ void multiply_operand(Float4 (&acc)[S][NF][NT], const Weights &x, const Words4 *xs, int j0, int j) const {
+        xs += (j0 + j) * (NT * XP * 4 * TOK) + place<NT, TOK>(j0 + j, g, r % TOK);
         Words4 w[NF];
 #pragma unroll
         for (int f = 0; f < NF; ++f) w[f] = operand(x, f, j);
@@ -320,7 +323,7 @@ template <int EL, int KIND, int G, bool HID, int NF> struct Expert {
         for (int n = 0; n < NT; ++n) {
             Words4 y[XP];
 #pragma unroll
-            for (int h = 0; h < XP; ++h) y[h] = xs[((j * NT + n) * XP + h) * (4 * TOK)];
+            for (int h = 0; h < XP; ++h) y[h] = xs[(n * XP + h) * (4 * TOK)];
 #pragma unroll
             for (int f = 0; f < NF; ++f) {
                 if constexpr (DENSE && WIDE) {
@@ -365,52 +368,67 @@ template <int EL, int KIND, int G, bool HID, int NF> struct Expert {
         }
     }
 
-    // This thread's pieces of a chunk of X: from memory, and into LDS when they have arrived.  s_row: rows of X of the entries.
-    // (Beyond the last entry: the first one again; what comes of it is not stored.)
-    // A thread's pieces are all of one row, `row` with its first column k0 (k0: in the chunk).
-    template <int NT, int TOK> static constexpr int piece_columns(int m) { return m * (kExpertThreads / Chunk<NT, TOK>::LANES) / NT * SUBK; }
-    template <int NT, int TOK> __device__ __forceinline__ bool piece_needed(int m, int chunk) const {
-        return chunk * (Chunk<NT, TOK>::STEPS * STEP) + piece_columns<NT, TOK>(m) < steps() * STEP;      // (of the first thread)
+    // This thread's pieces of a chunk of X: from memory, and into LDS when they have arrived.
+    // Pieces are dealt to the threads row by row: a wave loads a contiguous part of a row.  (With sixteen rows x 64 bytes a load all
+    // lines come from the same channel of the L2 where rows are a power of two apart: times of whole products up to three times as
+    // long.)  A piece's place among those of its operand is rotated with its column, so that neither the writes of a row
+    // nor the reads of an operand meet in the same banks.
+    template <int NT, int TOK> struct Piece {
+        static constexpr int ROW = Chunk<NT, TOK>::STEPS * SUB * 4;       // pieces of a row in a chunk
+        int e, c;                                                        // entry, piece of its row
+        __device__ __forceinline__ Piece(int m, int tid) : e((m * kExpertThreads + tid) / ROW), c((m * kExpertThreads + tid) % ROW) {}
+    };
+    template <int NT, int TOK> static __device__ __forceinline__ int place(int j, int g, int r) {       // operand j of the chunk
+        return TOK == 16 ? g * 16 + ((r + g + 4 * j) & 15) : (g * TOK + r + j) & (4 * TOK - 1);
     }
-    template <int NT, int TOK> __device__ __forceinline__ bool cut(int chunk) const { return (chunk + 1) * (Chunk<NT, TOK>::STEPS * STEP) > n_cols; }
+    template <int NT, int TOK> __device__ __forceinline__ int chunk_pieces(int chunk) const {          // of a row, as far as it goes
+        return min(Chunk<NT, TOK>::STEPS, steps() - chunk * Chunk<NT, TOK>::STEPS) * (SUB * 4);
+    }
     template <int NT, int TOK>
-    __device__ __forceinline__ void fetch(Chunk<NT, TOK> &y, const ExpertLaunch &a, const char *row, int k0, int chunk) const {
-        typedef Chunk<NT, TOK> C;
-        static_assert(kExpertThreads / C::LANES % NT == 0, "all pieces of a thread are of one entry");
-        k0 += chunk * (C::STEPS * STEP);
-        if (!cut<NT, TOK>(chunk)) {
-            row += (int64_t)k0 * (int)sizeof(T);
+    __device__ __forceinline__ void find_rows(Chunk<NT, TOK> &y, const ExpertLaunch &a, const int *s_row, int count) const {
 #pragma unroll
-            for (int m = 0; m < C::MINE; ++m)
-#pragma unroll
-                for (int h = 0; h < XR; ++h)
-                    y.x[m][h] = *reinterpret_cast<const AnyWords4 *>((HID && !WIDE && h ? row + a.x_part : row) +
-                                                                    (piece_columns<NT, TOK>(m) + (WIDE && h ? 4 : 0)) * (int)sizeof(T));
-            return;
+        for (int m = 0; m < Chunk<NT, TOK>::MINE; ++m) {
+            int at = s_row[min(Piece<NT, TOK>(m, tid).e, count - 1)];
+            if constexpr (Piece<NT, TOK>::ROW % 64 == 0) at = __builtin_amdgcn_readfirstlane(at);
+            y.row[m] = static_cast<const char *>(a.X) + at * a.ldx * (int64_t)sizeof(T);
         }
+    }
+    template <int NT, int TOK>
+    __device__ __forceinline__ void fetch(Chunk<NT, TOK> &y, const ExpertLaunch &a, int count, int chunk) const {
+        typedef Chunk<NT, TOK> C;
+        const int limit = chunk_pieces<NT, TOK>(chunk);
+        const bool cut = (chunk + 1) * (C::STEPS * STEP) > n_cols;
 #pragma unroll
         for (int m = 0; m < C::MINE; ++m) {
-            if (!piece_needed<NT, TOK>(m, chunk)) break;
+            if (m * kExpertThreads / Piece<NT, TOK>::ROW >= count) break;
+            const Piece<NT, TOK> p(m, tid);
+            if (p.e >= count || p.c >= limit) continue;
+            const int k0 = chunk * (C::STEPS * STEP) + XE * p.c;
 #pragma unroll
             for (int h = 0; h < XR; ++h) {
-                const char *q = HID && !WIDE && h ? row + a.x_part : row;
-                const int k = k0 + piece_columns<NT, TOK>(m) + (WIDE && h ? 4 : 0);
-                y.x[m][h] = n_cols < PIECE ? load_short<Bits>(q, k, n_cols)
-                                           : *reinterpret_cast<const AnyWords4 *>(q + (int64_t)min(k, n_cols - PIECE) * (int)sizeof(T));
+                const char *q = HID && !WIDE && h ? y.row[m] + a.x_part : y.row[m];
+                int k = k0 + (WIDE && h ? 4 : 0);
+                if (cut && n_cols < PIECE) {
+                    y.x[m][h] = load_short<Bits>(q, k, n_cols);
+                    continue;
+                }
+                if (cut) k = min(k, n_cols - PIECE);
+                y.x[m][h] = *reinterpret_cast<const AnyWords4 *>(q + (uint32_t)k * (uint32_t)sizeof(T));
             }
         }
     }
-    template <int NT, int TOK> __device__ __forceinline__ void put(Chunk<NT, TOK> &y, int k0, int chunk, Words4 *xs) const {
+    template <int NT, int TOK> __device__ __forceinline__ void put(Chunk<NT, TOK> &y, int count, int chunk, Words4 *xs) const {
         typedef Chunk<NT, TOK> C;
-        const bool move = cut<NT, TOK>(chunk) && n_cols >= PIECE;
+        const int limit = chunk_pieces<NT, TOK>(chunk);
+        const bool move = (chunk + 1) * (C::STEPS * STEP) > n_cols && n_cols >= PIECE;
 #pragma unroll
         for (int m = 0; m < C::MINE; ++m) {
-            if (!piece_needed<NT, TOK>(m, chunk)) break;
-            const int p = m * kExpertThreads + tid;
-            if (C::SLOTS * C::LANES % kExpertThreads && p >= C::SLOTS * C::LANES) break;
-            Words4 *to = xs + p / C::LANES * (XP * C::LANES) + p % C::LANES;
+            if (m * kExpertThreads / Piece<NT, TOK>::ROW >= count) break;
+            const Piece<NT, TOK> p(m, tid);
+            if (p.e >= count || p.c >= limit) continue;
+            Words4 *to = xs + (p.c / 4 * NT + p.e / 16) * (XP * C::LANES) + place<NT, TOK>(p.c / 4, p.c % 4, p.e % 16);
             if (move) {
-                const int k = k0 + chunk * (C::STEPS * STEP) + piece_columns<NT, TOK>(m);
+                const int k = chunk * (C::STEPS * STEP) + XE * p.c;
 #pragma unroll
                 for (int h = 0; h < XR; ++h) y.x[m][h] = set_right<Bits>(y.x[m][h], k + (WIDE && h ? 4 : 0), n_cols);
             }
@@ -448,10 +466,9 @@ template <int EL, int KIND, int G, bool HID, int NF> struct Expert {
         typedef Chunk<NT, TOK> C;
         asm volatile("" : "+v"(tid));          // (what follows from it is worked out here, not before all cases and kept)
         Words4 *const xs = reinterpret_cast<Words4 *>(smem);
-        const int entry = tid / C::LANES % NT * 16 + tid % TOK, k0 = tid / C::LANES / NT * SUBK + (WIDE && DENSE ? 4 : 8) * (tid % C::LANES / TOK);
-        const char *const row = static_cast<const char *>(a.X) + s_row[entry < count ? entry : 0] * a.ldx * (int64_t)sizeof(T);
         C y;
-        fetch<NT, TOK>(y, a, row, k0, 0);
+        find_rows<NT, TOK>(y, a, s_row, count);
+        fetch<NT, TOK>(y, a, count, 0);
         Sums<NT> c;
 #pragma unroll
         for (int f = 0; f < NF; ++f)
@@ -469,9 +486,9 @@ template <int EL, int KIND, int G, bool HID, int NF> struct Expert {
                 const int chunk = t / chunk_turns;
                 Words4 *const x = xs + (chunk & 1) * C::PIECES;
                 if (t % chunk_turns == 0) {
-                    put<NT, TOK>(y, k0, chunk, x);
+                    put<NT, TOK>(y, count, chunk, x);
                     __syncthreads();
-                    if (t + chunk_turns < turns) fetch<NT, TOK>(y, a, row, k0, chunk + 1);
+                    if (t + chunk_turns < turns) fetch<NT, TOK>(y, a, count, chunk + 1);
                 }
                 const int s = k_wave + t * a.k_waves;
                 load(w[(i + AHEAD) % RING], min(s + AHEAD * a.k_waves, last), a);
@@ -484,7 +501,7 @@ template <int EL, int KIND, int G, bool HID, int NF> struct Expert {
                             for (int q = 0; q < WL; ++q) w[i].w[f][q] = set_right<Bits>(w[i].w[f][q], dense_column(s), n_cols);
                     }
                 }
-                multiply<NT, TOK>(c, w[i], x + s % C::STEPS * (SUB * NT * XP * C::LANES) + g * TOK + r % TOK);
+                multiply<NT, TOK>(c, w[i], x, s % C::STEPS * SUB);
             }
         }
         __syncthreads();
