@@ -11,6 +11,7 @@ namespace {
 constexpr int kExpertWaves = 4, kExpertThreads = 64 * kExpertWaves;
 constexpr int kExpertSpread = 512;    // workgroups of a launch that are enough
 constexpr int kNearRows = 256;        // row pointers that are held in LDS
+constexpr int kNearEntries = kExpertThreads;      // entries whose sum finds columns and values in LDS
 constexpr int kJoinTokens = 16;       // the most tokens whose entries the last workgroups add up
 
 // Hidden rows of TF_F16 are held in two parts, high * 2^12 + low: fp16 alone ends at 65504, which a gate times
@@ -547,14 +548,14 @@ template <int EL, int KIND, int G, bool HID, int NF> struct Expert {
     }
 };
 
-// One element of D: the sum of value times result over the entries of a token, in their order.
+// One element of D: the sum of value times result over the entries q0 .. q1 - 1 of a token, in their order.  SHARED: results that
+// workgroups of this launch have stored.
 template <bool SHARED>
-__device__ __forceinline__ float combine_entries(const int32_t *__restrict__ rowptr, const int32_t *__restrict__ colidx,
-                                                 const float *__restrict__ vals, const float *Y, int64_t ldy, int n_experts, int t, int c) {
+__device__ __forceinline__ float combine_entries(int q0, int q1, const int32_t *colidx, const float *vals, const float *Y, int64_t ldy,
+                                                 int n_experts, int c) {
     constexpr int batch = 4;          // entries whose loads go out together
-    const int q1 = rowptr[t + 1];
     float d = 0.0f;
-    for (int q = rowptr[t]; q < q1; q += batch) {
+    for (int q = q0; q < q1; q += batch) {
         float v[batch], y[batch];
         bool in[batch];
 #pragma unroll
@@ -576,7 +577,9 @@ template <int EL, int KIND, int G, bool HID, int NF>
 __global__ __launch_bounds__(kExpertThreads, 2) void k_experts(const ExpertLaunch a) {
     typedef Expert<EL, KIND, G, HID, NF> Ex;
     constexpr int most = 16 * Ex::MOST;
-    __shared__ int s_count[kExpertWaves], s_entry[most], s_row[most], s_rowptr[HID ? 1 : kNearRows], s_last;
+    __shared__ int s_count[kExpertWaves], s_entry[most], s_row[most], s_rowptr[HID ? kJoinTokens + 1 : kNearRows], s_last;
+    __shared__ int s_col[HID ? kNearEntries : 1];
+    __shared__ float s_val[HID ? kNearEntries : 1];
     extern __shared__ __align__(16) unsigned char smem[];
 
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -589,20 +592,51 @@ __global__ __launch_bounds__(kExpertThreads, 2) void k_experts(const ExpertLaunc
     int expert = 0;
     if (a.rowptr) expert = !by_entry ? unit : unit < a.n_entries ? a.colidx[unit] : -1;
     const bool named = expert >= 0 && expert < a.n_experts;
+    // what the sum over the entries needs of A (its loads are ahead of those of the weights: what is loaded first is waited for first)
+    const bool join = HID && a.arrived, near_entries = join && a.n_entries <= kNearEntries;
+    int32_t col = -1, end = 0;
+    float val = 0.0f;
+    if (near_entries && (int)threadIdx.x < a.n_entries) {
+        col = a.colidx[threadIdx.x];
+        val = a.vals[threadIdx.x];
+    }
+    if (join && (int)threadIdx.x <= a.n_tokens) end = a.rowptr[threadIdx.x];
+    // few entries: every wave looks for those of its expert by itself
+    const bool few = a.rowptr && a.n_entries <= 64 && a.n_tokens <= kJoinTokens;
+    int here = -1, here_row = 0;
+    if (few) {
+        if (lane < a.n_entries) here = a.colidx[lane];
+        if (!HID)
+            for (int t = 1; t < a.n_tokens; ++t) here_row += a.rowptr[t] <= lane;
+    }
     Ex x;
     typename Ex::Weights w[Ex::RING];
     if (named) {
         x.set(a, expert, row0);
         x.start(w, a, k_wave);        // (before the entries are looked for: nearly always there are some)
     }
+    if (near_entries) {
+        s_col[threadIdx.x] = col;
+        s_val[threadIdx.x] = val;
+    }
+    if (join && threadIdx.x <= kJoinTokens) s_rowptr[threadIdx.x] = end;
     // row pointers are looked at in LDS, as far as they fit
-    const bool near = !HID && a.rowptr && a.n_tokens < kNearRows;
+    const bool near = !HID && !few && a.rowptr && a.n_tokens < kNearRows;
     if (near && named)
         for (int i = threadIdx.x; i <= a.n_tokens; i += kExpertThreads) s_rowptr[i] = a.rowptr[i];
     for (int first = 0; named; first += most) {
         // the entries first .. first + most - 1 of those that name the expert
-        int total = a.n_entries;
-        if (a.rowptr) {
+        int total = a.n_entries, leader = unit;
+        if (few) {
+            const uint64_t m = __builtin_amdgcn_ballot_w64(here == expert);
+            total = __popcll(m);
+            leader = __ffsll((unsigned long long)m) - 1;
+            const int rank = __popcll(m & ((1ull << lane) - 1)) - first;
+            if (here == expert && rank >= 0 && rank < most) {       // (all waves write the same)
+                s_entry[rank] = lane;
+                s_row[rank] = HID ? lane : here_row;
+            }
+        } else if (a.rowptr) {
             total = 0;
             for (int i0 = 0; i0 < a.n_entries; i0 += kExpertThreads) {
                 const int i = i0 + (int)threadIdx.x;
@@ -625,11 +659,12 @@ __global__ __launch_bounds__(kExpertThreads, 2) void k_experts(const ExpertLaunc
                 }
                 __syncthreads();
             }
+            if (first == 0 && total > 0) leader = s_entry[0];
         }
         total = __builtin_amdgcn_readfirstlane(total);
         if (total <= first) break;
         // (by entry: the first that names the expert does the work of all)
-        if (by_entry && first == 0 && __builtin_amdgcn_readfirstlane(s_entry[0]) != unit) break;
+        if (by_entry && first == 0 && __builtin_amdgcn_readfirstlane(leader) != unit) break;
         const int count = min(total - first, most);
         if (first > 0) x.start(w, a, k_wave);
         if (!a.rowptr) {
@@ -644,7 +679,7 @@ __global__ __launch_bounds__(kExpertThreads, 2) void k_experts(const ExpertLaunc
         __syncthreads();
     }
     if constexpr (HID) {
-        if (!a.arrived) return;
+        if (!join) return;
         // this workgroup's sums are where all others see them, then it counts itself in; the last one for a block of columns
         // adds up the entries of each token
         __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup");
@@ -657,8 +692,10 @@ __global__ __launch_bounds__(kExpertThreads, 2) void k_experts(const ExpertLaunc
         const int cols = min(rows_per, a.n_rows - tile * rows_per);
         for (int i = threadIdx.x; i < a.n_tokens * cols; i += kExpertThreads) {
             const int t = i / cols, c = tile * rows_per + i % cols;
-            static_cast<typename El<EL>::T *>(a.D)[(int64_t)t * a.ldd + c] = El<EL>::put(
-                combine_entries<true>(a.rowptr, a.colidx, a.vals, static_cast<const float *>(a.out), a.ldo, a.n_experts, t, c));
+            const float *Y = static_cast<const float *>(a.out);
+            const float d = near_entries ? combine_entries<true>(s_rowptr[t], s_rowptr[t + 1], s_col, s_val, Y, a.ldo, a.n_experts, c)
+                                         : combine_entries<true>(s_rowptr[t], s_rowptr[t + 1], a.colidx, a.vals, Y, a.ldo, a.n_experts, c);
+            static_cast<typename El<EL>::T *>(a.D)[(int64_t)t * a.ldd + c] = El<EL>::put(d);
         }
     }
 }
@@ -667,7 +704,7 @@ template <int EL> __global__ __launch_bounds__(256) void k_combine(const ExpertL
     const int t = blockIdx.x / col_blocks, c = blockIdx.x % col_blocks * 256 + threadIdx.x;
     if (c >= a.n_rows) return;
     static_cast<typename El<EL>::T *>(a.D)[(int64_t)t * a.ldd + c] =
-        El<EL>::put(combine_entries<false>(a.rowptr, a.colidx, a.vals, static_cast<const float *>(a.out), a.ldo, a.n_experts, t, c));
+        El<EL>::put(combine_entries<false>(a.rowptr[t], a.rowptr[t + 1], a.colidx, a.vals, static_cast<const float *>(a.out), a.ldo, a.n_experts, c));
 }
 
 template <int EL, int KIND, int G, bool HID, int NF> int launch_experts_nf(ExpertLaunch a, int64_t units, int k_waves, hipStream_t st) {
