@@ -1,6 +1,7 @@
 // Products of a few rows with the weights of the experts that name them (or with one 4-bit matrix).
 #pragma once
 #include <algorithm>
+#include <cmath>
 #include <type_traits>
 
 #include "tf_moe_device.h"
@@ -8,10 +9,10 @@
 namespace tf {
 namespace {
 
-constexpr int kExpertWaves = 4, kExpertThreads = 64 * kExpertWaves;
-constexpr int kExpertSpread = 512;    // workgroups of a launch that are enough
+// Waves of a workgroup by the blocks of rows that each multiplies.
+constexpr int expert_waves(int nf) { return nf == 1 ? 8 : 4; }
 constexpr int kNearRows = 256;        // row pointers that are held in LDS
-constexpr int kNearEntries = kExpertThreads;      // entries whose sum finds columns and values in LDS
+constexpr int kNearEntries = 256;     // entries whose sum finds columns and values in LDS
 constexpr int kJoinTokens = 16;       // the most tokens whose entries the last workgroups add up
 
 // Hidden rows of TF_F16 are held in two parts, high * 2^12 + low: fp16 alone ends at 65504, which a gate times
@@ -141,7 +142,8 @@ template <typename T> __device__ __forceinline__ Words4 load_short(const char *p
 template <int EL, int KIND, int G, bool HID, int NF> struct Expert {
     typedef typename El<EL>::T T;
     typedef std::conditional_t<EL == TF_F32, uint32_t, uint16_t> Bits;
-    static constexpr int CHUNK = 32 << 10;                           // LDS of a chunk of X, of which there are two
+    static constexpr int WAVES = expert_waves(NF), THREADS = 64 * WAVES;
+    static constexpr int CHUNK = WAVES * (8 << 10);                  // LDS of a chunk of X, of which there are two
     static constexpr int MOST = KIND < 0 || NF == 1 ? 4 : 2;           // blocks of sixteen entries that are multiplied at a time
     static constexpr bool DENSE = KIND < 0, WIDE = EL == TF_F32;
     static constexpr int PIECE = 16 / (int)sizeof(T);                // elements of sixteen bytes
@@ -162,7 +164,7 @@ template <int EL, int KIND, int G, bool HID, int NF> struct Expert {
         static constexpr int FIT = CHUNK / (SUB * NT * XP * LANES * 16);
         static constexpr int STEPS = FIT >= 32 ? 32 : FIT >= 16 ? 16 : FIT >= 8 ? 8 : FIT >= 4 ? 4 : FIT >= 2 ? 2 : 1;
         static constexpr int SLOTS = STEPS * SUB * NT;
-        static constexpr int MINE = (SLOTS * LANES + kExpertThreads - 1) / kExpertThreads;
+        static constexpr int MINE = (SLOTS * LANES + THREADS - 1) / THREADS;
         static constexpr int PIECES = SLOTS * XP * LANES;            // of a buffer
         const char *row[MINE];                                       // where the thread's pieces begin
         Words4 x[MINE][XR];
@@ -172,7 +174,7 @@ template <int EL, int KIND, int G, bool HID, int NF> struct Expert {
     template <int NT, int TOK> static int bytes(int steps) {
         typedef Chunk<NT, TOK> C;
         const int x = steps > C::STEPS ? 2 * C::PIECES : steps * SUB * NT * C::LANES * XP;
-        return std::max(x * 16, kExpertWaves * NF * NT * 1024);
+        return std::max(x * 16, WAVES * NF * NT * 1024);
     }
 
     struct Weights {
@@ -370,14 +372,13 @@ template <int EL, int KIND, int G, bool HID, int NF> struct Expert {
     }
 
     // This thread's pieces of a chunk of X: from memory, and into LDS when they have arrived.
-    // Pieces are dealt to the threads row by row: a wave loads a contiguous part of a row.  (With sixteen rows x 64 bytes a load all
-    // lines come from the same channel of the L2 where rows are a power of two apart: times of whole products up to three times as
-    // long.)  A piece's place among those of its operand is rotated with its column, so that neither the writes of a row
-    // nor the reads of an operand meet in the same banks.
+    // Pieces are dealt to the threads row by row: a wave loads a contiguous part of a row, and rows of no entry are not loaded at
+    // all.  A piece's place among those of its operand is rotated with its column, so that neither the writes of a row nor the
+    // reads of an operand meet in the same banks.
     template <int NT, int TOK> struct Piece {
         static constexpr int ROW = Chunk<NT, TOK>::STEPS * SUB * 4;       // pieces of a row in a chunk
         int e, c;                                                        // entry, piece of its row
-        __device__ __forceinline__ Piece(int m, int tid) : e((m * kExpertThreads + tid) / ROW), c((m * kExpertThreads + tid) % ROW) {}
+        __device__ __forceinline__ Piece(int m, int tid) : e((m * THREADS + tid) / ROW), c((m * THREADS + tid) % ROW) {}
     };
     template <int NT, int TOK> static __device__ __forceinline__ int place(int j, int g, int r) {       // operand j of the chunk
         return TOK == 16 ? g * 16 + ((r + g + 4 * j) & 15) : (g * TOK + r + j) & (4 * TOK - 1);
@@ -401,7 +402,7 @@ template <int EL, int KIND, int G, bool HID, int NF> struct Expert {
         const bool cut = (chunk + 1) * (C::STEPS * STEP) > n_cols;
 #pragma unroll
         for (int m = 0; m < C::MINE; ++m) {
-            if (m * kExpertThreads / Piece<NT, TOK>::ROW >= count) break;
+            if (m * THREADS / Piece<NT, TOK>::ROW >= count) break;
             const Piece<NT, TOK> p(m, tid);
             if (p.e >= count || p.c >= limit) continue;
             const int k0 = chunk * (C::STEPS * STEP) + XE * p.c;
@@ -424,7 +425,7 @@ template <int EL, int KIND, int G, bool HID, int NF> struct Expert {
         const bool move = (chunk + 1) * (C::STEPS * STEP) > n_cols && n_cols >= PIECE;
 #pragma unroll
         for (int m = 0; m < C::MINE; ++m) {
-            if (m * kExpertThreads / Piece<NT, TOK>::ROW >= count) break;
+            if (m * THREADS / Piece<NT, TOK>::ROW >= count) break;
             const Piece<NT, TOK> p(m, tid);
             if (p.e >= count || p.c >= limit) continue;
             Words4 *to = xs + (p.c / 4 * NT + p.e / 16) * (XP * C::LANES) + place<NT, TOK>(p.c / 4, p.c % 4, p.e % 16);
@@ -523,8 +524,8 @@ template <int EL, int KIND, int G, bool HID, int NF> struct Expert {
 #pragma unroll
             for (int n = 0; n < NT; ++n) red[((wave * NF + f) * NT + n) * 64 + lane] = c.v[0][f][n];
         __syncthreads();
-        const int row_groups = kExpertWaves / a.k_waves, per_group = out_blocks * NT * 64;
-        for (int item = threadIdx.x; item < row_groups * per_group; item += kExpertThreads) {
+        const int row_groups = WAVES / a.k_waves, per_group = out_blocks * NT * 64;
+        for (int item = threadIdx.x; item < row_groups * per_group; item += THREADS) {
             const int rg = item / per_group, in = item % per_group;        // (in: block, sixteen entries, lane)
             const Float4 *p = red + rg * a.k_waves * (NF * NT * 64) + in;
             Float4 y = p[0];
@@ -574,16 +575,16 @@ __device__ __forceinline__ float combine_entries(int q0, int q1, const int32_t *
 }
 
 template <int EL, int KIND, int G, bool HID, int NF>
-__global__ __launch_bounds__(kExpertThreads, 2) void k_experts(const ExpertLaunch a) {
+__global__ __launch_bounds__(64 * expert_waves(NF), 2) void k_experts(const ExpertLaunch a) {
     typedef Expert<EL, KIND, G, HID, NF> Ex;
     constexpr int most = 16 * Ex::MOST;
-    __shared__ int s_count[kExpertWaves], s_entry[most], s_row[most], s_rowptr[HID ? kJoinTokens + 1 : kNearRows], s_last;
+    __shared__ int s_count[Ex::WAVES], s_entry[most], s_row[most], s_rowptr[HID ? kJoinTokens + 1 : kNearRows], s_last;
     __shared__ int s_col[HID ? kNearEntries : 1];
     __shared__ float s_val[HID ? kNearEntries : 1];
     extern __shared__ __align__(16) unsigned char smem[];
 
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int wave_rows = 16 * (a.gated ? NF / 2 : NF), rows_per = kExpertWaves / a.k_waves * wave_rows;
+    const int wave_rows = 16 * (a.gated ? NF / 2 : NF), rows_per = Ex::WAVES / a.k_waves * wave_rows;
     const int tiles = (a.n_rows + rows_per - 1) / rows_per;
     const int tile = blockIdx.x % tiles, unit = blockIdx.x / tiles;
     const int row0 = tile * rows_per + wave / a.k_waves * wave_rows, k_wave = wave % a.k_waves;
@@ -615,7 +616,7 @@ __global__ __launch_bounds__(kExpertThreads, 2) void k_experts(const ExpertLaunc
         x.set(a, expert, row0);
         x.start(w, a, k_wave);        // (before the entries are looked for: nearly always there are some)
     }
-    if (near_entries) {
+    if (near_entries && threadIdx.x < kNearEntries) {
         s_col[threadIdx.x] = col;
         s_val[threadIdx.x] = val;
     }
@@ -623,7 +624,7 @@ __global__ __launch_bounds__(kExpertThreads, 2) void k_experts(const ExpertLaunc
     // row pointers are looked at in LDS, as far as they fit
     const bool near = !HID && !few && a.rowptr && a.n_tokens < kNearRows;
     if (near && named)
-        for (int i = threadIdx.x; i <= a.n_tokens; i += kExpertThreads) s_rowptr[i] = a.rowptr[i];
+        for (int i = threadIdx.x; i <= a.n_tokens; i += Ex::THREADS) s_rowptr[i] = a.rowptr[i];
     for (int first = 0; named; first += most) {
         // the entries first .. first + most - 1 of those that name the expert
         int total = a.n_entries, leader = unit;
@@ -638,7 +639,7 @@ __global__ __launch_bounds__(kExpertThreads, 2) void k_experts(const ExpertLaunc
             }
         } else if (a.rowptr) {
             total = 0;
-            for (int i0 = 0; i0 < a.n_entries; i0 += kExpertThreads) {
+            for (int i0 = 0; i0 < a.n_entries; i0 += Ex::THREADS) {
                 const int i = i0 + (int)threadIdx.x;
                 const bool hit = i < a.n_entries && a.colidx[i] == expert;
                 const uint64_t m = __builtin_amdgcn_ballot_w64(hit);
@@ -646,7 +647,7 @@ __global__ __launch_bounds__(kExpertThreads, 2) void k_experts(const ExpertLaunc
                 __syncthreads();
                 int before = total;
 #pragma unroll
-                for (int w = 0; w < kExpertWaves; ++w) {
+                for (int w = 0; w < Ex::WAVES; ++w) {
                     if (w < wave) before += s_count[w];
                     total += s_count[w];
                 }
@@ -690,7 +691,7 @@ __global__ __launch_bounds__(kExpertThreads, 2) void k_experts(const ExpertLaunc
         if (!s_last) return;
         __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup");
         const int cols = min(rows_per, a.n_rows - tile * rows_per);
-        for (int i = threadIdx.x; i < a.n_tokens * cols; i += kExpertThreads) {
+        for (int i = threadIdx.x; i < a.n_tokens * cols; i += Ex::THREADS) {
             const int t = i / cols, c = tile * rows_per + i % cols;
             const float *Y = static_cast<const float *>(a.out);
             const float d = near_entries ? combine_entries<true>(s_rowptr[t], s_rowptr[t + 1], s_col, s_val, Y, a.ldo, a.n_experts, c)
@@ -715,39 +716,54 @@ template <int EL, int KIND, int G, bool HID, int NF> int launch_experts_nf(Exper
     if (most > 4) lds = std::max(lds, Ex::template bytes<1, 16>(steps));
     if (most > 16) lds = std::max(lds, Ex::template bytes<2, 16>(steps));
     if (most > 32) lds = std::max(lds, Ex::template bytes<Ex::MOST, 16>(steps));
-    const int rows_per = kExpertWaves / k_waves * 16 * (a.gated ? NF / 2 : NF);
+    const int rows_per = Ex::WAVES / k_waves * 16 * (a.gated ? NF / 2 : NF);
     const int64_t tiles = (a.n_rows + rows_per - 1) / rows_per;
     a.k_waves = k_waves;
     // (more than a launch may ask for by default)
     static const int raised = (int)hipFuncSetAttribute(reinterpret_cast<const void *>(&k_experts<EL, KIND, G, HID, NF>),
-                                                       hipFuncAttributeMaxDynamicSharedMemorySize, 96 << 10);
+                                                       hipFuncAttributeMaxDynamicSharedMemorySize, 144 << 10);
     if (raised) return raised;
-    hipLaunchKernelGGL((k_experts<EL, KIND, G, HID, NF>), dim3((unsigned)(tiles * units)), dim3(kExpertThreads), lds, st, a);
+    hipLaunchKernelGGL((k_experts<EL, KIND, G, HID, NF>), dim3((unsigned)(tiles * units)), dim3(Ex::THREADS), lds, st, a);
     return (int)hipGetLastError();
 }
 // The most waves of a workgroup that may share columns: each has a step of every chunk.
 template <typename Ex> int most_k_waves(int most) {
     const int steps = most <= 4 ? Ex::template Chunk<1, 4>::STEPS : most <= 16 ? Ex::template Chunk<1, 16>::STEPS
                       : most <= 32 ? Ex::template Chunk<2, 16>::STEPS : Ex::template Chunk<Ex::MOST, 16>::STEPS;
-    return std::min(kExpertWaves, steps);
+    return std::min(Ex::WAVES, steps);
+}
+// How a launch is cut: k_waves and an estimate of its time, in steps of a wave that multiplies two blocks of rows.
+struct ExpertCut {
+    int k_waves;
+    double cost;
+};
+// Workgroups run in rounds of as many as the card holds (two of four waves a compute unit, or one of eight), each as long
+// as its waves' steps and some four more for what comes before and after them.  A step of one block of rows takes 0.6 of one of
+// two.  More waves on the same columns make shorter workgroups, and more of them.
+template <typename Ex, int NF> ExpertCut cut_experts(const ExpertLaunch &a, int most, double units) {
+    const int steps = (a.n_cols + Ex::STEP - 1) / Ex::STEP;
+    const double slots = NF == 1 ? 256.0 : 512.0, step = NF == 1 ? 0.6 : 1.0;
+    const int passes = a.rowptr ? 1 : (most + 16 * Ex::MOST - 1) / (16 * Ex::MOST);
+    ExpertCut best{0, 0.0};
+    for (int k = most_k_waves<Ex>(most); k >= 1; k /= 2) {
+        const int rows = Ex::WAVES / k * 16 * (a.gated ? NF / 2 : NF);
+        const double rounds = std::ceil((a.n_rows + rows - 1) / rows * units / slots);
+        const double cost = rounds * passes * (step * ((steps + k - 1) / k) + 4.0);
+        if (!best.k_waves || cost < best.cost) best = ExpertCut{k, cost};
+    }
+    return best;
 }
 template <int EL, int KIND, int G, bool HID> int launch_experts_hid(ExpertLaunch a, hipStream_t st) {
     const int most = a.rowptr ? a.n_tokens : a.n_entries;
     const int64_t units = !a.rowptr ? 1 : a.n_entries < 1 ? 1 : a.n_entries <= a.n_experts ? a.n_entries : a.n_experts;
     if (HID && a.n_tokens > kJoinTokens) a.arrived = nullptr;
-    const auto workgroups = [&](int rows) { return (a.n_rows + rows - 1) / rows * units; };
+    // experts that entries name, if any is as likely as the other
+    const double named = !a.rowptr ? 1.0 : std::max(1.0, a.n_experts * -std::expm1(a.n_entries * std::log1p(-1.0 / (a.n_experts + 1.0))));
     // Two blocks of rows a wave, so that what is read of X from LDS is used twice; one where workgroups would be too few otherwise.
-    // Waves share columns as long as workgroups are few.
-    const auto spread = [&](int out, int k_waves) {
-        while (k_waves > 1 && workgroups(kExpertWaves / k_waves * 2 * out) >= kExpertSpread) k_waves /= 2;
-        return k_waves;
-    };
-    int e;
-    const int k2 = most_k_waves<Expert<EL, KIND, G, HID, 2>>(most), out2 = a.gated ? 16 : 32;
-    if (!a.gated && workgroups(kExpertWaves / k2 * 32) < kExpertSpread)
-        e = launch_experts_nf<EL, KIND, G, HID, 1>(a, units, spread(16, most_k_waves<Expert<EL, KIND, G, HID, 1>>(most)), st);
-    else
-        e = launch_experts_nf<EL, KIND, G, HID, 2>(a, units, spread(out2, k2), st);
+    const ExpertCut two = cut_experts<Expert<EL, KIND, G, HID, 2>, 2>(a, most, named);
+    const ExpertCut one = a.gated ? ExpertCut{0, 0.0} : cut_experts<Expert<EL, KIND, G, HID, 1>, 1>(a, most, named);
+    const int e = one.k_waves && one.cost < two.cost ? launch_experts_nf<EL, KIND, G, HID, 1>(a, units, one.k_waves, st)
+                                                     : launch_experts_nf<EL, KIND, G, HID, 2>(a, units, two.k_waves, st);
     if (e || !HID || a.arrived) return e;
     const int col_blocks = (a.n_rows + 255) / 256;
     hipLaunchKernelGGL((k_combine<EL>), dim3((unsigned)(col_blocks * (int64_t)a.n_tokens)), dim3(256), 0, st, a, col_blocks);
