@@ -307,7 +307,7 @@ tf_status tf_csr_validate(const tf_csr *M);
  *     f_e(x) = ( act(x Wg_e^T) o (x Wu_e^T) ) Wd_e^T      or, without a gate,  act(x Wu_e^T) Wd_e^T
  * (mixture of experts).  The calls are made for the few tokens of a decoding batch, where the weights
  * that the tokens meet have to be read once and this is what takes the time; they are right for any
- * number of tokens, but read an expert's weights again for every 64 entries that name it.
+ * number of tokens, but read an expert's weights again for every 32 or 64 entries that name it.
  *
  * Conventions besides those at the top of this file
  *   - Element types are TF_F32, TF_BF16 and TF_F16.  Products of 16-bit numbers are summed in 32 bits;
@@ -357,7 +357,7 @@ tf_status tf_q4_quantize(const tf_q4 *W, const void *weights, int32_t dtype, voi
 tf_status tf_q4_unpack(const tf_q4 *W, int32_t dtype, void *weights, void *hip_stream);
 
 /* Y = X W^T for m rows of X (m x n_cols, rows ldx apart) and one matrix (n_mats = 1): Y is m x n_rows, rows ldy
- * apart.  For a few rows: codes are read once for every 64. */
+ * apart.  For a few rows: codes are read again for every 32 or 64.  n_cols is at most 2^24. */
 tf_status tf_q4_matvec(const tf_q4 *W, const void *X, int64_t ldx, void *Y, int64_t ldy, int64_t m, int32_t dtype,
                        void *hip_stream);
 
@@ -399,14 +399,15 @@ typedef struct tf_moe_desc {
 
 typedef struct tf_moe tf_moe; /* opaque, library-owned: the sizes above and a workspace */
 
-/* Allocates the workspace (max_entries rows between the products).  On failure *out is NULL. */
+/* Allocates the workspace (max_entries rows between the products).  n_in and n_hidden are at most 2^24.  On failure
+ * *out is NULL. */
 tf_status tf_moe_create(const tf_moe_desc *desc, tf_moe **out);
 /* Frees it.  NULL is accepted. */
 tf_status tf_moe_destroy(tf_moe *plan);
 
 /* D = the layer of X (A->n_rows x n_in, rows ldx apart; D: A->n_rows x n_out, rows ldd apart).  W1 is n_experts x
  * (2 n_hidden or n_hidden) x n_in, W2 n_experts x n_out x n_hidden, both contiguous, each row the weights of one
- * output.  A: device arrays, values TF_F32, at most max_tokens rows and max_entries entries, any number of them
+ * output, of 16 bytes or more (TF_EUNSUPPORTED otherwise).  A: device arrays, values TF_F32, at most max_tokens rows and max_entries entries, any number of them
  * in a row; entries whose column is not one of the experts are passed over, whatever their value; a row without
  * entries gives a row of zeros.  A's arrays are not validated (see tf_spmm_spmm).  What lies between the products is
  * held in 16 bits or more of precision (TF_F16: magnitudes up to 2^28, larger ones become infinite).

@@ -13,7 +13,9 @@ namespace {
 constexpr int expert_waves(int nf) { return nf == 1 ? 8 : 4; }
 constexpr int kNearRows = 256;        // row pointers that are held in LDS
 constexpr int kNearEntries = 256;     // entries whose sum finds columns and values in LDS
-constexpr int kJoinTokens = 16;       // the most tokens whose entries the last workgroups add up
+// The most tokens whose entries the last workgroups add up: one token 3 us less than a launch of its own, but 32 tokens through
+// 64 experts 212 us, with that launch 161.
+constexpr int kJoinTokens = 16;
 
 // Hidden rows of TF_F16 are held in two parts, high * 2^12 + low: fp16 alone ends at 65504, which a gate times
 // what it gates passes easily.
@@ -131,10 +133,17 @@ template <typename T> __device__ __forceinline__ Words4 load_short(const char *p
 //
 // A wave multiplies NF blocks of sixteen rows of one expert's weights (with a gate: sixteen of the gate and the sixteen
 // that it multiplies) with the rows of X of the entries that name the expert.  a.k_waves waves of the workgroup share the
-// columns of the same rows, a step in turn, and their sums are added up through LDS, wave after wave.  Weights are the first
-// operand of the matrix instructions, straight from memory: whatever the number of entries up to sixteen, what one
-// instruction multiplies was loaded by one instruction.  X passes through LDS, chunk by chunk, in the order of the
-// instructions, and is read there by all waves.
+// columns of the same rows, a step in turn, and their sums are added up through LDS, wave after wave.  Weights are an operand of
+// the matrix instructions straight from memory: whatever the number of entries up to sixteen, what one instruction
+// multiplies was loaded by one instruction.  X is the other operand and passes through LDS, chunk by chunk, in operand order,
+// where all waves read it.  X is the first of the two: a lane then holds sums of four entries and one row of weights, whose
+// group has one scale (with the weights first it took four scales a group and 128-column steps of twice the registers).
+//
+// Bound by memory where entries of an expert are few: 32 bf16 tokens through 64 experts of 2048 x 1024 (0.77 GB) 142 us, 5.4 TB/s;
+// one through two of 4096 x 8192 85 us, 4.7; an fp16 row times a 4-bit matrix of 32768 x 8192 28.5 us, 5.3; and by the instructions of
+// products and staging where they are many: 128 fp16 tokens through 16 4-bit experts of 4096 x 8192 284 us, 3.2 TB/s, vector
+// instructions a quarter of the waves' cycles, waits 40 %, at the two waves a SIMD that 256 registers leave (three or four with
+// spilled registers were slower).  X in registers instead of LDS (the first kernel): 983 us there, 247 for the 32 tokens.
 //
 // Dense weights are loaded by whole lines of 128 bytes: an instruction takes eight rows x 128 bytes, and two of them are
 // put in operand order (sixteen rows x 64 bytes) by exchanging halves of sixteen lanes (a read of 512 MiB by itself, rows of
@@ -149,7 +158,6 @@ template <int EL, int KIND, int G, bool HID, int NF> struct Expert {
     static constexpr int PIECE = 16 / (int)sizeof(T);                // elements of sixteen bytes
     static constexpr int STEP = DENSE ? 8 * PIECE : kQ4Block;        // columns of a step
     static constexpr int SUB = DENSE ? 2 : 4;                        // operands of X in a step
-    static constexpr int SUBK = STEP / SUB;                          // columns of an operand
     static constexpr int XP = !DENSE && WIDE ? 3 : HID && !WIDE ? 2 : 1;   // parts of X
     static constexpr int SETS = !DENSE && WIDE ? 2 : HID && EL == TF_F16 ? 2 : 1;   // sums of high and of low parts
     static constexpr int WL = DENSE ? 2 : 1;                         // pieces of weights that a lane holds of a step and block
@@ -373,8 +381,10 @@ template <int EL, int KIND, int G, bool HID, int NF> struct Expert {
 
     // This thread's pieces of a chunk of X: from memory, and into LDS when they have arrived.
     // Pieces are dealt to the threads row by row: a wave loads a contiguous part of a row, and rows of no entry are not loaded at
-    // all.  A piece's place among those of its operand is rotated with its column, so that neither the writes of a row nor the
-    // reads of an operand meet in the same banks.
+    // all.  A piece's place among those of its operand is rotated with its column: without that the 64 pieces of a row that a wave
+    // writes would all be in the same four banks (of the LDS cycles of 128 fp16 tokens through 4-bit experts 40 % are
+    // still conflicts; with pieces dealt operand by operand, sixteen rows x 64 bytes a load, none are, but 64 bf16 rows times a 4-bit
+    // 8192 x 8192 matrix took 66 us instead of 59).
     template <int NT, int TOK> struct Piece {
         static constexpr int ROW = Chunk<NT, TOK>::STEPS * SUB * 4;       // pieces of a row in a chunk
         int e, c;                                                        // entry, piece of its row
@@ -601,7 +611,7 @@ __global__ __launch_bounds__(64 * expert_waves(NF), 2) void k_experts(const Expe
         col = a.colidx[threadIdx.x];
         val = a.vals[threadIdx.x];
     }
-    if (join && (int)threadIdx.x <= a.n_tokens) end = a.rowptr[threadIdx.x];
+    if (join && (int)threadIdx.x <= a.n_tokens) end = min(max(a.rowptr[threadIdx.x], 0), a.n_entries);
     // few entries: every wave looks for those of its expert by itself
     const bool few = a.rowptr && a.n_entries <= 64 && a.n_tokens <= kJoinTokens;
     int here = -1, here_row = 0;
@@ -705,7 +715,7 @@ template <int EL> __global__ __launch_bounds__(256) void k_combine(const ExpertL
     const int t = blockIdx.x / col_blocks, c = blockIdx.x % col_blocks * 256 + threadIdx.x;
     if (c >= a.n_rows) return;
     static_cast<typename El<EL>::T *>(a.D)[(int64_t)t * a.ldd + c] =
-        El<EL>::put(combine_entries<false>(a.rowptr[t], a.rowptr[t + 1], a.colidx, a.vals, static_cast<const float *>(a.out), a.ldo, a.n_experts, c));
+        El<EL>::put(combine_entries<false>(max(a.rowptr[t], 0), min(a.rowptr[t + 1], a.n_entries), a.colidx, a.vals, static_cast<const float *>(a.out), a.ldo, a.n_experts, c));
 }
 
 template <int EL, int KIND, int G, bool HID, int NF> int launch_experts_nf(ExpertLaunch a, int64_t units, int k_waves, hipStream_t st) {
@@ -739,7 +749,8 @@ struct ExpertCut {
 };
 // Workgroups run in rounds of as many as the card holds (two of four waves a compute unit, or one of eight), each as long
 // as its waves' steps and some four more for what comes before and after them.  A step of one block of rows takes 0.6 of one of
-// two.  More waves on the same columns make shorter workgroups, and more of them.
+// two.  More waves on the same columns make shorter workgroups, and more of them.  (64 bf16 rows times 4-bit 8192 x 8192: one block of rows
+// and four waves on the same columns 38 us, two blocks 59; fp16 row times 32768 x 8192: two blocks and two waves 29.5, four waves 34 to 44.)
 template <typename Ex, int NF> ExpertCut cut_experts(const ExpertLaunch &a, int most, double units) {
     const int steps = (a.n_cols + Ex::STEP - 1) / Ex::STEP;
     const double slots = NF == 1 ? 256.0 : 512.0, step = NF == 1 ? 0.6 : 1.0;

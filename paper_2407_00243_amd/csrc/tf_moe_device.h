@@ -8,7 +8,6 @@ namespace tf {
 namespace {
 
 typedef float Float4 __attribute__((ext_vector_type(4)));
-typedef uint32_t Words2 __attribute__((ext_vector_type(2)));
 typedef uint32_t Words4 __attribute__((ext_vector_type(4)));
 typedef __bf16 Bf8 __attribute__((ext_vector_type(8)));
 typedef __bf16 Bf2 __attribute__((ext_vector_type(2)));

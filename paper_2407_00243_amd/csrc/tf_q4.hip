@@ -1,4 +1,4 @@
-// Weights of 4 bits: into and out of the library's layout (tf_moe.h).
+// Weights of 4 bits: into and out of the library's layout (tf_moe.h).  One pass over memory each, run when weights are loaded.
 #include <algorithm>
 
 #include "tf_moe_device.h"

@@ -424,3 +424,48 @@ def test_route_and_layer_in_a_graph():
             graph.replay()
             torch.cuda.synchronize()
             assert torch.equal(D, eager) and eager.abs().sum() > 0
+
+
+@pytest.mark.parametrize("dtype", DT)
+@pytest.mark.parametrize("kind,group", [(tf.TF_Q4_INT, 128), (tf.TF_Q4_E2M1, 32)])
+@pytest.mark.parametrize("m,n,k", [(3, 50, 9001), (12, 40, 5000), (30, 33, 4111), (64, 530, 2500), (100, 20, 3000), (1, 4097, 640)])
+def test_matvec_over_many_chunks(dtype, kind, group, m, n, k):
+    g = gen(m + n)
+    q, w = random_q4(g, n, k, kind, group)
+    x = randn(g, m, k, dtype=DT[dtype])
+    y = torch.full((m, n), math.nan, dtype=DT[dtype], device="cuda")
+    tf.tf_q4_matvec(q, x, y, stream())
+    ref, b = ru.product(x.double(), w[0])
+    ru.check(y, ref, b, DT[dtype])
+
+
+@pytest.mark.parametrize("dtype", DT)
+@pytest.mark.parametrize("quant", [None, (tf.TF_Q4_E2M1, 32), (tf.TF_Q4_INT, 128)])
+@pytest.mark.parametrize("T,E,k,H,I", [
+    (8, 100, 8, 1500, 530),        # 64 entries: the most that every wave looks for by itself
+    (13, 90, 5, 2100, 300),        # 65
+    (16, 30, 20, 520, 1100),       # more entries than the sum over them finds in LDS
+    (17, 12, 3, 900, 260),         # more tokens than the last workgroups add up
+    (300, 6, 2, 200, 136),         # more row pointers than fit LDS, more entries than are multiplied at a time
+])
+def test_layer_at_the_borders_of_its_cases(dtype, quant, T, E, k, H, I):
+    rows = some_rows(T, E, k)
+    rows[T // 2] = rows[T // 2][:1]                # (rows of different lengths)
+    D, ref, b = run_layer(rows, E, H, I, H, dtype, quant=quant)
+    ru.check(D, ref, b, DT[dtype])
+
+
+def test_layer_with_unaligned_rows():
+    g = gen(31)
+    E, H, I, T = 3, 77, 41, 5
+    for dt in DT.values():
+        W1, W2 = (randn(g, E, 2 * I, H) / 9).to(dt), (randn(g, E, H, I) / 6).to(dt)
+        X = randn(g, T * 79 + 1, dtype=dt)[1:].as_strided((T, H), (79, 1))
+        D = torch.zeros(T * 81 + 3, dtype=dt, device="cuda")[3:].as_strided((T, H), (81, 1))
+        A, rowptr, cols = csr(some_rows(T, E, 2), E)
+        with tf.MoePlan(E, H, I, dt, T, 2 * T) as plan:
+            plan.run(A, X, W1, W2, D, stream())
+            torch.cuda.synchronize()
+        ref, b = ru.layer(X.double(), rowptr, cols, A.vals.tolist(), lambda e: W1[e].double(), lambda e: W2[e].double(),
+                          "silu", True, dt)
+        ru.check(D, ref, b, dt)

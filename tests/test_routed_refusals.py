@@ -99,6 +99,15 @@ def test_create_refuses(over, want):
     assert status(st) == want and not out.value and tf.tf_last_error()
 
 
+def test_limits_of_rows_of_weights():
+    lib = tf.load_library()
+    w = q4(n_cols=(1 << 24) + 1)
+    assert status(lib.tf_q4_matvec(ctypes.byref(w), P, 1 << 25, P, 32, 1, tf.TF_BF16, None)) == "TF_EUNSUPPORTED"
+    d = binding.tf_moe_desc(4, (1 << 24) + 1, 32, 64, 2, 4, tf.TF_BF16, 2, 1, 0)
+    out = ctypes.c_void_p()
+    assert status(lib.tf_moe_create(ctypes.byref(d), ctypes.byref(out))) == "TF_EUNSUPPORTED"
+
+
 def test_binding_checks_its_operands():
     torch = pytest.importorskip("torch")
     W = tf.Q4Matrix(32, 64, tf.TF_Q4_INT, 32, torch.empty(2048, dtype=torch.uint8), torch.empty(256, dtype=torch.uint8))
