@@ -307,7 +307,8 @@ tf_status tf_csr_validate(const tf_csr *M);
  *     f_e(x) = ( act(x Wg_e^T) o (x Wu_e^T) ) Wd_e^T      or, without a gate,  act(x Wu_e^T) Wd_e^T
  * (mixture of experts).  The calls are made for the few tokens of a decoding batch, where the weights
  * that the tokens meet have to be read once and this is what takes the time; they are right for any
- * number of tokens, but read an expert's weights again for every 32 or 64 entries that name it.
+ * number of tokens, but read an expert's weights again for every 32 or 64 entries that name it (for every 4 or 16
+ * of up to 4 or 16 tokens, where rows name an expert more than once).
  *
  * Conventions besides those at the top of this file
  *   - Element types are TF_F32, TF_BF16 and TF_F16.  Products of 16-bit numbers are summed in 32 bits;

@@ -185,6 +185,22 @@ template <int EL, int KIND, int G, bool HID, int NF> struct Expert {
         return std::max(x * 16, WAVES * NF * NT * 1024);
     }
 
+    // Entries that a pass multiplies at the most, in the case of run() that holds `entries` of them: what a launch's LDS and the waves
+    // that share columns are chosen for.  Entries beyond it are another pass.
+    static int pass_of(int entries) { return entries <= 4 ? 4 : entries <= 16 ? 16 : entries <= 32 || MOST == 2 ? 32 : 16 * MOST; }
+    static int pass_steps(int pass) {          // steps of its chunks (fewer in the larger cases, so each is enough for the smaller ones)
+        static_assert(Chunk<1, 4>::STEPS >= Chunk<1, 16>::STEPS && Chunk<1, 16>::STEPS >= Chunk<2, 16>::STEPS &&
+                      Chunk<2, 16>::STEPS >= Chunk<MOST, 16>::STEPS, "");
+        return pass == 4 ? Chunk<1, 4>::STEPS : pass == 16 ? Chunk<1, 16>::STEPS : pass == 32 ? Chunk<2, 16>::STEPS : Chunk<MOST, 16>::STEPS;
+    }
+    static int pass_bytes(int pass, int steps) {
+        int b = bytes<1, 4>(steps);
+        if (pass >= 16) b = std::max(b, bytes<1, 16>(steps));
+        if (pass >= 32) b = std::max(b, bytes<2, 16>(steps));
+        if (pass > 32) b = std::max(b, bytes<MOST, 16>(steps));
+        return b;
+    }
+
     struct Weights {
         Words4 w[NF][WL];
         uint32_t s[DENSE ? 1 : NF][SW];
@@ -587,8 +603,8 @@ __device__ __forceinline__ float combine_entries(int q0, int q1, const int32_t *
 template <int EL, int KIND, int G, bool HID, int NF>
 __global__ __launch_bounds__(64 * expert_waves(NF), 2) void k_experts(const ExpertLaunch a) {
     typedef Expert<EL, KIND, G, HID, NF> Ex;
-    constexpr int most = 16 * Ex::MOST;
-    __shared__ int s_count[Ex::WAVES], s_entry[most], s_row[most], s_rowptr[HID ? kJoinTokens + 1 : kNearRows], s_last;
+    const int most = a.pass_entries;
+    __shared__ int s_count[Ex::WAVES], s_entry[16 * Ex::MOST], s_row[16 * Ex::MOST], s_rowptr[HID ? kJoinTokens + 1 : kNearRows], s_last;
     __shared__ int s_col[HID ? kNearEntries : 1];
     __shared__ float s_val[HID ? kNearEntries : 1];
     extern __shared__ __align__(16) unsigned char smem[];
@@ -718,14 +734,14 @@ template <int EL> __global__ __launch_bounds__(256) void k_combine(const ExpertL
         El<EL>::put(combine_entries<false>(max(a.rowptr[t], 0), min(a.rowptr[t + 1], a.n_entries), a.colidx, a.vals, static_cast<const float *>(a.out), a.ldo, a.n_experts, c));
 }
 
+// Entries of an expert that a launch is made for: one a token, as a router leaves them.  (Rows may name an expert more than once:
+// what is more takes further passes.)
+inline int usual_entries(const ExpertLaunch &a) { return a.rowptr ? a.n_tokens : a.n_entries; }
+
 template <int EL, int KIND, int G, bool HID, int NF> int launch_experts_nf(ExpertLaunch a, int64_t units, int k_waves, hipStream_t st) {
     typedef Expert<EL, KIND, G, HID, NF> Ex;
-    const int most = a.rowptr ? a.n_tokens : a.n_entries;      // entries of an expert, one a token
-    const int steps = (a.n_cols + Ex::STEP - 1) / Ex::STEP;
-    int lds = Ex::template bytes<1, 4>(steps);
-    if (most > 4) lds = std::max(lds, Ex::template bytes<1, 16>(steps));
-    if (most > 16) lds = std::max(lds, Ex::template bytes<2, 16>(steps));
-    if (most > 32) lds = std::max(lds, Ex::template bytes<Ex::MOST, 16>(steps));
+    a.pass_entries = Ex::pass_of(usual_entries(a));
+    const int lds = Ex::pass_bytes(a.pass_entries, (a.n_cols + Ex::STEP - 1) / Ex::STEP);
     const int rows_per = Ex::WAVES / k_waves * 16 * (a.gated ? NF / 2 : NF);
     const int64_t tiles = (a.n_rows + rows_per - 1) / rows_per;
     a.k_waves = k_waves;
@@ -738,9 +754,7 @@ template <int EL, int KIND, int G, bool HID, int NF> int launch_experts_nf(Exper
 }
 // The most waves of a workgroup that may share columns: each has a step of every chunk.
 template <typename Ex> int most_k_waves(int most) {
-    const int steps = most <= 4 ? Ex::template Chunk<1, 4>::STEPS : most <= 16 ? Ex::template Chunk<1, 16>::STEPS
-                      : most <= 32 ? Ex::template Chunk<2, 16>::STEPS : Ex::template Chunk<Ex::MOST, 16>::STEPS;
-    return std::min(Ex::WAVES, steps);
+    return std::min(Ex::WAVES, Ex::pass_steps(Ex::pass_of(most)));
 }
 // How a launch is cut: k_waves and an estimate of its time, in steps of a wave that multiplies two blocks of rows.
 struct ExpertCut {
@@ -765,7 +779,7 @@ template <typename Ex, int NF> ExpertCut cut_experts(const ExpertLaunch &a, int 
     return best;
 }
 template <int EL, int KIND, int G, bool HID> int launch_experts_hid(ExpertLaunch a, hipStream_t st) {
-    const int most = a.rowptr ? a.n_tokens : a.n_entries;
+    const int most = usual_entries(a);
     const int64_t units = !a.rowptr ? 1 : a.n_entries < 1 ? 1 : a.n_entries <= a.n_experts ? a.n_entries : a.n_experts;
     if (HID && a.n_tokens > kJoinTokens) a.arrived = nullptr;
     // experts that entries name, if any is as likely as the other

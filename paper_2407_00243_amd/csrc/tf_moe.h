@@ -76,6 +76,7 @@ struct ExpertLaunch {
     int64_t ldd;
     uint32_t *arrived;            // for each block of columns: workgroups that have stored their sums (all zero between launches)
     int32_t k_waves;              // waves of a workgroup that share the columns of the same rows: 1, 2, 4 or 8
+    int32_t pass_entries;         // the most entries that a workgroup multiplies at a time (LDS and k_waves are chosen for them): 4, 16, 32 or 64
 };
 int launch_experts(const ExpertLaunch &a, void *stream);
 int launch_experts_bf16(const ExpertLaunch &a, void *stream);
