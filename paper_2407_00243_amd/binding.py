@@ -328,6 +328,7 @@ def tf_run_wavefront(plan: int, wavefront: int, B, C, D, stream=None) -> None:
 _ROUTED = {"torch.float32": TF_F32, "float32": TF_F32, "torch.bfloat16": TF_BF16,
            "torch.float16": TF_F16, "float16": TF_F16}
 _codes: dict = {}          # of element types that have been seen, by the type itself
+_csr_types: set = set()     # the types of a routing matrix's arrays that have been seen and are right, by the types themselves
 
 
 def _routed_code(dt) -> int:
@@ -354,13 +355,37 @@ def _matrix(x, what: str, cols: Optional[int] = None):
     return rows, n, ld if rows > 1 else max(ld, n)
 
 
-def _routing(A) -> tf_csr:
-    """A routing matrix as the library takes it (values are fp32)."""
+def _routing(A, device: int) -> tf_csr:
+    """A routing matrix as the library takes it: indices of 32 bits, values in fp32, arrays on `device` that hold all of them.
+    (A tf_csr is the caller's affair.)"""
     if isinstance(A, tf_csr):
         return A
-    if _routed_code(A.vals.dtype) != TF_F32:
-        raise TypeError("the values of A must be fp32")
-    return tf_csr(A.n_rows, A.n_cols, A.nnz, A.rowptr.data_ptr(), A.colidx.data_ptr(), A.vals.data_ptr(), TF_F32, 1)
+    rowptr, colidx, vals, n_rows, nnz = A.rowptr, A.colidx, A.vals, A.n_rows, A.nnz
+    types = rowptr.dtype, colidx.dtype, vals.dtype
+    if types not in _csr_types:
+        if [str(t) for t in types[:2]] != ["torch.int32"] * 2:
+            raise TypeError("rowptr and colidx of A must be int32")
+        if _routed_code(types[2]) != TF_F32:
+            raise TypeError("the values of A must be fp32")
+        _csr_types.add(types)
+    if rowptr.numel() <= n_rows or colidx.numel() < nnz or vals.numel() < nnz:
+        raise ValueError(f"the arrays of A must hold {n_rows + 1} row pointers and {nnz} columns and values")
+    if not (rowptr.is_contiguous() and colidx.is_contiguous() and vals.is_contiguous()):
+        raise ValueError("the arrays of A must be contiguous")
+    if device < 0 or rowptr.get_device() != device or colidx.get_device() != device or vals.get_device() != device:
+        _refuse_devices()
+    return tf_csr(n_rows, A.n_cols, nnz, rowptr.data_ptr(), colidx.data_ptr(), vals.data_ptr(), TF_F32, 1)
+
+
+def _refuse_devices():
+    raise ValueError("all operands must be on one device, and not on the host")
+
+
+def _device_of(W, device: int) -> int:
+    """Number of the device of a Q4Matrix, a tensor or nothing; of addresses, which are the caller's affair, `device`."""
+    if isinstance(W, Q4Matrix):
+        return device if W.device is None else W.device
+    return W.get_device() if hasattr(W, "get_device") else device
 
 
 def _contiguous(x, what: str, shape, dtype: Optional[int] = None):
@@ -382,8 +407,13 @@ class Q4Matrix:
         self.codes, self.scales = codes, scales
         need = tf_q4_sizes(n_rows, n_cols, kind, group, n_mats)
         for what, x, n in (("codes", codes, need[0]), ("scales", scales, need[1])):
-            if hasattr(x, "numel") and x.numel() * x.element_size() < n:
-                raise ValueError(f"{what} must hold {n} bytes")
+            if hasattr(x, "numel") and (x.numel() * x.element_size() < n or not x.is_contiguous()):
+                raise ValueError(f"{what} must hold {n} contiguous bytes")
+        # number of their device, -1 for the host; None where both are addresses
+        devices = {x.get_device() for x in (codes, scales) if hasattr(x, "get_device")}
+        if len(devices) > 1:
+            raise ValueError("codes and scales must be on one device")
+        self.device = devices.pop() if devices else None
         self.struct = tf_q4(self.n_mats, self.n_rows, self.n_cols, _addr(codes), _addr(scales), self.kind,
                             self.group)
         self.ref = ctypes.byref(self.struct)
@@ -405,17 +435,26 @@ def tf_q4_pack(W: Q4Matrix, codes, scales, stream=None) -> None:
             _contiguous(x, what, (W.n_mats, W.n_rows, n))
             if str(x.dtype) != t:
                 raise TypeError(f"{what} must be {t}")
+    device = _device_of(W, 0)
+    if device < 0 or _device_of(codes, device) != device or _device_of(scales, device) != device:
+        _refuse_devices()
     _check(load_library().tf_q4_pack(ctypes.byref(W.struct), _addr(codes), _addr(scales), _addr(stream)))
 
 
 def tf_q4_quantize(W: Q4Matrix, weights, stream=None) -> None:
     _contiguous(weights, "weights", (W.n_mats, W.n_rows, W.n_cols))
+    device = weights.get_device()
+    if device < 0 or _device_of(W, device) != device:
+        _refuse_devices()
     _check(load_library().tf_q4_quantize(ctypes.byref(W.struct), _addr(weights), _routed_code(weights.dtype),
                                          _addr(stream)))
 
 
 def tf_q4_unpack(W: Q4Matrix, weights, stream=None) -> None:
     _contiguous(weights, "weights", (W.n_mats, W.n_rows, W.n_cols))
+    device = weights.get_device()
+    if device < 0 or _device_of(W, device) != device:
+        _refuse_devices()
     _check(load_library().tf_q4_unpack(ctypes.byref(W.struct), _routed_code(weights.dtype), _addr(weights),
                                        _addr(stream)))
 
@@ -428,6 +467,9 @@ def tf_q4_matvec(W: Q4Matrix, X, Y, stream=None) -> None:
         raise ValueError("X and Y must have the same number of rows")
     if X.dtype != Y.dtype:
         raise TypeError("X and Y must have the same element type")
+    device = X.get_device()
+    if device < 0 or Y.get_device() != device or (W.device != device and W.device is not None):
+        _refuse_devices()
     status = load_library().tf_q4_matvec(W.ref, X.data_ptr(), ldx, Y.data_ptr(), ldy, m, _routed_code(X.dtype), stream)
     if status:
         _check(status)
@@ -441,8 +483,12 @@ def tf_moe_route(scores, A: DeviceCsr, scoring: int = TF_ROUTE_SOFTMAX_TOP, bias
         raise ValueError("A must have a row for each row of the scores")
     if bias is not None and hasattr(bias, "shape"):
         _contiguous(bias, "bias", (A.n_cols,), TF_F32)
+    device = scores.get_device()
+    a = _routing(A, device)
+    if bias is not None and _device_of(bias, device) != device:
+        _refuse_devices()
     status = load_library().tf_moe_route(scores.data_ptr(), ld, _routed_code(scores.dtype), _addr(bias), scoring, scale,
-                                         ctypes.byref(_routing(A)), stream)
+                                         ctypes.byref(a), stream)
     if status:
         _check(status)
 
@@ -461,14 +507,30 @@ def tf_moe_destroy(plan: Optional[int]) -> None:
     _check(load_library().tf_moe_destroy(plan))
 
 
+def _layer_operands(A, X, D, *weights):
+    """The routing matrix and the distances of the rows of X and D."""
+    rows, _, ldx = _matrix(X, "X")
+    rows_d, _, ldd = _matrix(D, "D")
+    if rows != A.n_rows or rows_d != rows:
+        raise ValueError("X and D must have a row for each row of A")
+    if X.dtype != D.dtype:
+        raise TypeError("X and D must have the same element type")
+    device = X.get_device()
+    a = _routing(A, device)
+    if device < 0 or D.get_device() != device or any(_device_of(w, device) != device for w in weights):
+        _refuse_devices()
+    return a, ldx, ldd
+
+
 def tf_moe_layer(plan: int, A: DeviceCsr, X, W1, W2, D, stream=None) -> None:
-    _check(load_library().tf_moe_layer(plan, ctypes.byref(_routing(A)), X.data_ptr(), _matrix(X, "X")[2], W1.data_ptr(),
-                                       W2.data_ptr(), D.data_ptr(), _matrix(D, "D")[2], stream))
+    """The caller answers for what a handle does not tell: columns, element type and weights are to be the plan's (MoePlan looks)."""
+    a, ldx, ldd = _layer_operands(A, X, D, W1, W2)
+    _check(load_library().tf_moe_layer(plan, ctypes.byref(a), X.data_ptr(), ldx, W1.data_ptr(), W2.data_ptr(), D.data_ptr(), ldd, stream))
 
 
 def tf_moe_layer_q4(plan: int, A: DeviceCsr, X, W1: Q4Matrix, W2: Q4Matrix, D, stream=None) -> None:
-    _check(load_library().tf_moe_layer_q4(plan, ctypes.byref(_routing(A)), X.data_ptr(), _matrix(X, "X")[2], W1.ref, W2.ref,
-                                          D.data_ptr(), _matrix(D, "D")[2], stream))
+    a, ldx, ldd = _layer_operands(A, X, D, W1, W2)
+    _check(load_library().tf_moe_layer_q4(plan, ctypes.byref(a), X.data_ptr(), ldx, W1.ref, W2.ref, D.data_ptr(), ldd, stream))
 
 
 class MoePlan:
@@ -490,7 +552,10 @@ class MoePlan:
             raise ValueError("X and D must have a row for each row of A")
         if _routed_code(X.dtype) != self.dtype or _routed_code(D.dtype) != self.dtype:
             raise TypeError("X and D must have the element type of the plan")
-        lib, a = load_library(), ctypes.byref(_routing(A))
+        lib, device = load_library(), X.get_device()
+        a = ctypes.byref(_routing(A, device))
+        if device < 0 or D.get_device() != device or _device_of(W1, device) != device or _device_of(W2, device) != device:
+            _refuse_devices()
         if isinstance(W1, Q4Matrix) and isinstance(W2, Q4Matrix):
             status = lib.tf_moe_layer_q4(self.handle, a, X.data_ptr(), ldx, W1.ref, W2.ref, D.data_ptr(), ldd, stream)
         elif isinstance(W1, Q4Matrix) or isinstance(W2, Q4Matrix):
