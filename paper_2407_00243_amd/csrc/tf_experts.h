@@ -702,7 +702,7 @@ __global__ __launch_bounds__(64 * expert_waves(NF), 2) void k_experts(const Expe
         else if (count <= 16) x.template run<1, 16>(a, w, k_wave, row0, count, s_entry, s_row, smem);
         else if (Ex::MOST == 2 || count <= 32) x.template run<2, 16>(a, w, k_wave, row0, count, s_entry, s_row, smem);
         else x.template run<Ex::MOST, 16>(a, w, k_wave, row0, count, s_entry, s_row, smem);
-        if (first + most >= total) break;
+        if (last_pass(first, total, most)) break;
         __syncthreads();
     }
     if constexpr (HID) {
@@ -768,7 +768,7 @@ struct ExpertCut {
 template <typename Ex, int NF> ExpertCut cut_experts(const ExpertLaunch &a, int most, double units) {
     const int steps = (a.n_cols + Ex::STEP - 1) / Ex::STEP;
     const double slots = NF == 1 ? 256.0 : 512.0, step = NF == 1 ? 0.6 : 1.0;
-    const int passes = a.rowptr ? 1 : (most + 16 * Ex::MOST - 1) / (16 * Ex::MOST);
+    const double passes = a.rowptr ? 1.0 : (double)ceil_div(most, 16 * Ex::MOST);
     ExpertCut best{0, 0.0};
     for (int k = most_k_waves<Ex>(most); k >= 1; k /= 2) {
         const int rows = Ex::WAVES / k * 16 * (a.gated ? NF / 2 : NF);

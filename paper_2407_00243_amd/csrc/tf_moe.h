@@ -6,6 +6,10 @@
 
 namespace tf {
 
+// Row counts go up to 2^31 - 1: sums of them are 64 bits wide, differences need no more than 32.
+constexpr int64_t ceil_div(int64_t n, int64_t per) { return (n + per - 1) / per; }
+constexpr bool last_pass(int32_t first, int32_t total, int32_t most) { return total - first <= most; }
+
 // ---------------------------------------------------------------------------------- 4-bit layout
 //
 // A matrix is cut into blocks of 16 rows x 128 columns, 1 KiB each, block row after block row: what one wave

@@ -101,7 +101,7 @@ template <int EL, int V> __global__ __launch_bounds__(kThreads) void k_route(con
 }
 
 template <int EL> void route_el(const RouteLaunch &a, hipStream_t st) {
-    const dim3 grid((a.n_tokens + kWaves - 1) / kWaves), block(kThreads);
+    const dim3 grid((unsigned)ceil_div(a.n_tokens, kWaves)), block(kThreads);
     if (a.n_experts <= 64) hipLaunchKernelGGL((k_route<EL, 1>), grid, block, 0, st, a);
     else if (a.n_experts <= 128) hipLaunchKernelGGL((k_route<EL, 2>), grid, block, 0, st, a);
     else if (a.n_experts <= 256) hipLaunchKernelGGL((k_route<EL, 4>), grid, block, 0, st, a);
