@@ -9,7 +9,7 @@ def run_cpp(tmp_path, body):
     """Compiles and runs `body` as main(); CHECK(x) ends it with the line number."""
     src, exe = str(tmp_path / "main.cpp"), str(tmp_path / "main")
     with open(src, "w") as f:
-        f.write('#include <cstdio>\n#include "tf_moe.h"\nusing namespace tf;\n'
+        f.write('#include <cstdio>\n#include <initializer_list>\n#include "tf_moe.h"\nusing namespace tf;\n'
                 "#define CHECK(x) do { if (!(x)) { std::printf(\"line %d: %s\\n\", __LINE__, #x); return 1; } } while (0)\n"
                 "int main() {\n" + body + "\nreturn 0;\n}\n")
     subprocess.run(["g++", "-std=c++17", "-O1", "-fsanitize=undefined", "-fno-sanitize-recover=all", "-I", CSRC, src,
