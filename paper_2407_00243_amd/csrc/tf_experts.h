@@ -728,7 +728,7 @@ __global__ __launch_bounds__(64 * expert_waves(NF), 2) void k_experts(const Expe
 }
 
 template <int EL> __global__ __launch_bounds__(256) void k_combine(const ExpertLaunch a, int col_blocks) {
-    const int t = blockIdx.x / col_blocks, c = blockIdx.x % col_blocks * 256 + threadIdx.x;
+    const int t = a.first_token + (int)(blockIdx.x / col_blocks), c = blockIdx.x % col_blocks * 256 + threadIdx.x;
     if (c >= a.n_rows) return;
     static_cast<typename El<EL>::T *>(a.D)[(int64_t)t * a.ldd + c] =
         El<EL>::put(combine_entries<false>(max(a.rowptr[t], 0), min(a.rowptr[t + 1], a.n_entries), a.colidx, a.vals, static_cast<const float *>(a.out), a.ldo, a.n_experts, c));
@@ -765,14 +765,17 @@ struct ExpertCut {
 // as its waves' steps and some four more for what comes before and after them.  A step of one block of rows takes 0.6 of one of
 // two.  More waves on the same columns make shorter workgroups, and more of them.  (64 bf16 rows times 4-bit 8192 x 8192: one block of rows
 // and four waves on the same columns 38 us, two blocks 59; fp16 row times 32768 x 8192: two blocks and two waves 29.5, four waves 34 to 44.)
-template <typename Ex, int NF> ExpertCut cut_experts(const ExpertLaunch &a, int most, double units) {
+// units: experts that have work, in the mean; launched: those that workgroups are launched for.  k_waves is 0 if no cut fits a launch.
+template <typename Ex, int NF> ExpertCut cut_experts(const ExpertLaunch &a, int most, double units, int64_t launched) {
     const int steps = (a.n_cols + Ex::STEP - 1) / Ex::STEP;
     const double slots = NF == 1 ? 256.0 : 512.0, step = NF == 1 ? 0.6 : 1.0;
     const double passes = a.rowptr ? 1.0 : (double)ceil_div(most, 16 * Ex::MOST);
     ExpertCut best{0, 0.0};
     for (int k = most_k_waves<Ex>(most); k >= 1; k /= 2) {
         const int rows = Ex::WAVES / k * 16 * (a.gated ? NF / 2 : NF);
-        const double rounds = std::ceil((a.n_rows + rows - 1) / rows * units / slots);
+        const int64_t tiles = ceil_div(a.n_rows, rows);
+        if (tiles * launched > most_workgroups(Ex::THREADS)) continue;
+        const double rounds = std::ceil(tiles * units / slots);
         const double cost = rounds * passes * (step * ((steps + k - 1) / k) + 4.0);
         if (!best.k_waves || cost < best.cost) best = ExpertCut{k, cost};
     }
@@ -785,14 +788,21 @@ template <int EL, int KIND, int G, bool HID> int launch_experts_hid(ExpertLaunch
     // experts that entries name, if any is as likely as the other
     const double named = !a.rowptr ? 1.0 : std::max(1.0, a.n_experts * -std::expm1(a.n_entries * std::log1p(-1.0 / (a.n_experts + 1.0))));
     // Two blocks of rows a wave, so that what is read of X from LDS is used twice; one where workgroups would be too few otherwise.
-    const ExpertCut two = cut_experts<Expert<EL, KIND, G, HID, 2>, 2>(a, most, named);
-    const ExpertCut one = a.gated ? ExpertCut{0, 0.0} : cut_experts<Expert<EL, KIND, G, HID, 1>, 1>(a, most, named);
-    const int e = one.k_waves && one.cost < two.cost ? launch_experts_nf<EL, KIND, G, HID, 1>(a, units, one.k_waves, st)
-                                                     : launch_experts_nf<EL, KIND, G, HID, 2>(a, units, two.k_waves, st);
+    const ExpertCut two = cut_experts<Expert<EL, KIND, G, HID, 2>, 2>(a, most, named, units);
+    const ExpertCut one = a.gated ? ExpertCut{0, 0.0} : cut_experts<Expert<EL, KIND, G, HID, 1>, 1>(a, most, named, units);
+    if (!one.k_waves && !two.k_waves) return (int)hipErrorInvalidConfiguration;
+    const int e = one.k_waves && (!two.k_waves || one.cost < two.cost) ? launch_experts_nf<EL, KIND, G, HID, 1>(a, units, one.k_waves, st)
+                                                                         : launch_experts_nf<EL, KIND, G, HID, 2>(a, units, two.k_waves, st);
     if (e || !HID || a.arrived) return e;
     const int col_blocks = (a.n_rows + 255) / 256;
-    hipLaunchKernelGGL((k_combine<EL>), dim3((unsigned)(col_blocks * (int64_t)a.n_tokens)), dim3(256), 0, st, a, col_blocks);
-    return (int)hipGetLastError();
+    const int64_t most_tokens = most_workgroups(256) / col_blocks;
+    for (int64_t first = 0; first < a.n_tokens; first += most_tokens) {
+        a.first_token = (int32_t)first;
+        hipLaunchKernelGGL((k_combine<EL>), dim3((unsigned)(col_blocks * std::min(most_tokens, a.n_tokens - first))), dim3(256), 0, st, a, col_blocks);
+        const hipError_t error = hipGetLastError();
+        if (error != hipSuccess) return (int)error;
+    }
+    return 0;
 }
 template <int EL, int KIND, int G> int launch_experts_g(const ExpertLaunch &a, hipStream_t st) {
     return a.x_hidden ? launch_experts_hid<EL, KIND, G, true>(a, st) : launch_experts_hid<EL, KIND, G, false>(a, st);

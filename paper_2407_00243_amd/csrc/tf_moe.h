@@ -8,6 +8,8 @@ namespace tf {
 
 // Row counts go up to 2^31 - 1: sums of them are 64 bits wide, differences need no more than 32.
 constexpr int64_t ceil_div(int64_t n, int64_t per) { return (n + per - 1) / per; }
+// The most workgroups of a launch, whose threads must be fewer than 2^32.
+constexpr int64_t most_workgroups(int64_t threads) { return (((int64_t)1 << 32) - 1) / threads; }
 constexpr bool last_pass(int32_t first, int32_t total, int32_t most) { return total - first <= most; }
 
 // ---------------------------------------------------------------------------------- 4-bit layout
@@ -50,6 +52,7 @@ struct RouteLaunch {
     float *vals;
     int32_t n_tokens, n_experts, k, dtype, scoring;
     float scale;
+    int32_t first;                // token that a launch begins with
 };
 int launch_route(const RouteLaunch &a, void *stream);
 
@@ -72,6 +75,7 @@ struct ExpertLaunch {
     int64_t x_part;               // bytes from the high parts of hidden rows to the low ones
     const int32_t *rowptr, *colidx;   // rowptr NULL: one matrix, entry q is row q of X
     int32_t n_tokens, n_entries, n_experts;
+    int32_t first_token;          // that a launch of the sum over entries begins with
     int32_t out_kind, activation, gated;
     void *out;
     int64_t ldo, out_part;        // elements; bytes

@@ -1,4 +1,6 @@
 // Router: the largest scores of each token and their weights.
+#include <algorithm>
+
 #include "tf_moe_device.h"
 
 namespace tf {
@@ -23,7 +25,7 @@ __device__ __forceinline__ float wave_max(float x) {
 template <int EL, int V> __global__ __launch_bounds__(kThreads) void k_route(const RouteLaunch a) {
     typedef typename El<EL>::T T;
     const int lane = threadIdx.x & 63;
-    const int t = blockIdx.x * kWaves + (threadIdx.x >> 6);
+    const int t = a.first + (int)(blockIdx.x * kWaves + (threadIdx.x >> 6));      // (below 2^31: a launch's first is a multiple of kWaves)
     if (t >= a.n_tokens) return;
     const T *row = static_cast<const T *>(a.scores) + (int64_t)t * a.ld;
     const float low = -__builtin_inff();
@@ -101,7 +103,7 @@ template <int EL, int V> __global__ __launch_bounds__(kThreads) void k_route(con
 }
 
 template <int EL> void route_el(const RouteLaunch &a, hipStream_t st) {
-    const dim3 grid((unsigned)ceil_div(a.n_tokens, kWaves)), block(kThreads);
+    const dim3 grid((unsigned)std::min(ceil_div((int64_t)a.n_tokens - a.first, kWaves), most_workgroups(kThreads))), block(kThreads);
     if (a.n_experts <= 64) hipLaunchKernelGGL((k_route<EL, 1>), grid, block, 0, st, a);
     else if (a.n_experts <= 128) hipLaunchKernelGGL((k_route<EL, 2>), grid, block, 0, st, a);
     else if (a.n_experts <= 256) hipLaunchKernelGGL((k_route<EL, 4>), grid, block, 0, st, a);
@@ -112,10 +114,16 @@ template <int EL> void route_el(const RouteLaunch &a, hipStream_t st) {
 
 int launch_route(const RouteLaunch &a, void *stream) {
     const hipStream_t st = static_cast<hipStream_t>(stream);
-    if (a.dtype == TF_BF16) route_el<TF_BF16>(a, st);
-    else if (a.dtype == TF_F16) route_el<TF_F16>(a, st);
-    else route_el<TF_F32>(a, st);
-    return (int)hipGetLastError();
+    RouteLaunch b = a;
+    for (int64_t first = 0; first < a.n_tokens; first += most_workgroups(kThreads) * kWaves) {
+        b.first = (int32_t)first;
+        if (a.dtype == TF_BF16) route_el<TF_BF16>(b, st);
+        else if (a.dtype == TF_F16) route_el<TF_F16>(b, st);
+        else route_el<TF_F32>(b, st);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return (int)e;
+    }
+    return 0;
 }
 
 }  // namespace tf

@@ -1,4 +1,6 @@
 """Routed operators where their calls end: experts named again and again, the ends of the numbers' range, long launches."""
+import math
+
 import pytest
 
 pytestmark = pytest.mark.gpu
@@ -7,7 +9,7 @@ torch = pytest.importorskip("torch")
 
 import paper_2407_00243_amd as tf  # noqa: E402
 import routed_util as ru  # noqa: E402
-from test_gpu_routed import DT, run_layer  # noqa: E402
+from test_gpu_routed import DT, csr, gen, randn, run_layer, stream  # noqa: E402
 
 
 # ------------------------------------------------------------------- rows that name an expert more than once
@@ -29,3 +31,40 @@ from test_gpu_routed import DT, run_layer  # noqa: E402
 def test_layer_with_experts_named_again(dtype, quant, H, I, gated, rows, E):
     D, ref, b = run_layer(rows, E, H, I, 72, dtype, "silu" if gated else "relu", gated, quant)
     ru.check(D, ref, b, DT[dtype])
+
+
+# ------------------------------------------------- more rows than the threads of one launch (2^32) have room for
+
+def test_route_of_more_tokens_than_a_launch_takes():
+    T = (1 << 26) + 9                   # one wave a token
+    scores = torch.zeros(T, 1, dtype=torch.bfloat16, device="cuda")
+    scores[T - 1], scores[1 << 26], scores[(1 << 26) - 5] = 3.0, 2.0, -1.0
+    A = tf.DeviceCsr(T, 1, torch.full((T + 1,), -9, dtype=torch.int32, device="cuda"),
+                     torch.full((T,), -9, dtype=torch.int32, device="cuda"), torch.full((T,), -9.0, device="cuda"))
+    tf.tf_moe_route(scores, A, tf.TF_ROUTE_SIGMOID, scale=2.0, stream=stream())
+    assert torch.equal(A.rowptr, torch.arange(T + 1, dtype=torch.int32, device="cuda")) and not A.colidx.any()
+    ref = 2 * torch.sigmoid(scores[:, 0].float())
+    assert ((A.vals - ref).abs() <= 2.0 ** -20).all() and A.vals[T - 1] > 1.9
+
+
+def test_layer_of_more_rows_than_a_launch_takes():
+    T, E, H, I, O = (1 << 24) + 70, 3, 8, 16, 8          # 256 threads a row of D
+    at = [0, 5, (1 << 24) - 1, 1 << 24, T - 1]
+    g = gen(41)
+    W1, W2 = randn(g, E, 2 * I, H).bfloat16(), randn(g, E, O, I).bfloat16()
+    X = torch.zeros(T, H, dtype=torch.bfloat16, device="cuda")
+    X[at] = randn(g, len(at), H, dtype=torch.bfloat16)
+    cols = [0, 2, 1, 1, 0]
+    A, _, _ = csr([[e] for e in cols], E)
+    rowptr = torch.zeros(T + 1, dtype=torch.int32, device="cuda")
+    rowptr[torch.tensor(at, device="cuda") + 1] = 1
+    A = tf.DeviceCsr(T, E, torch.cumsum(rowptr, 0).int(), A.colidx, A.vals)
+    D = torch.full((T, O), math.nan, dtype=torch.bfloat16, device="cuda")
+    with tf.MoePlan(E, H, I, torch.bfloat16, T, len(at), n_out=O) as plan:
+        plan.run(A, X, W1, W2, D, stream())
+        torch.cuda.synchronize()
+    ref, b = ru.layer(X[at].double(), list(range(len(at) + 1)), cols, A.vals.tolist(), lambda e: W1[e].double(),
+                      lambda e: W2[e].double(), "silu", True, torch.bfloat16)
+    ru.check(D[at], ref, b, torch.bfloat16)
+    D[at] = 0
+    assert (D == 0).all()

@@ -32,3 +32,11 @@ def test_passes_over_rows_up_to_the_last_count(tmp_path):
             }
             CHECK(passes == ceil_div(total, most) && rows == total);
         }""")
+
+
+def test_launches_stay_below_32_bits_of_threads(tmp_path):
+    run_cpp(tmp_path, """
+    for (int64_t threads : {256, 512}) {
+        CHECK(most_workgroups(threads) * threads < (int64_t)1 << 32);
+        CHECK((most_workgroups(threads) + 1) * threads >= (int64_t)1 << 32);
+    }""")
