@@ -64,12 +64,14 @@ template <int EL, int KIND> __device__ __forceinline__ Words4 q4_decode(uint32_t
     return y;
 }
 
-// Two fp32 numbers in three bf16 parts each (cut off, not rounded: the parts of a number have its sign and add up to it
-// exactly, and no part of a finite number is infinite).  An infinity is its first part alone.
+// Two fp32 numbers in three bf16 parts each: h + 2^-8 (m + l) (cut off, not rounded: the parts of a number have its sign, and no
+// part of a finite number is infinite).  They add up to it exactly from 2^-118 on; parts below 2^-133 are subnormal,
+// and without the factor that would begin at 2^-110.  An infinity is its first part alone.
+constexpr float kRestUp = 256.0f;
 __device__ __forceinline__ void cut_pair(uint32_t &h, uint32_t &m, uint32_t &l, float a, float b) {
     const uint32_t ua = __float_as_uint(a), ub = __float_as_uint(b);
     h = (ua >> 16) | (ub & 0xffff0000u);
-    float ra = a - __uint_as_float(ua & 0xffff0000u), rb = b - __uint_as_float(ub & 0xffff0000u);
+    float ra = kRestUp * (a - __uint_as_float(ua & 0xffff0000u)), rb = kRestUp * (b - __uint_as_float(ub & 0xffff0000u));
     ra = __builtin_isinf(a) ? 0.0f : ra;
     rb = __builtin_isinf(b) ? 0.0f : rb;
     const uint32_t va = __float_as_uint(ra), vb = __float_as_uint(rb);
@@ -332,7 +334,8 @@ template <int EL, int KIND, int G, bool HID, int NF> struct Expert {
                             for (int v = 0; v < 4; ++v) {
                                 float d = acc[p & 1][0][f][n][v];
                                 if constexpr (SETS > 1)
-                                    d = EL == TF_F16 ? fmaf(d, kHalfHigh, acc[p & 1][SETS - 1][f][n][v]) : d + acc[p & 1][SETS - 1][f][n][v];
+                                    d = EL == TF_F16 ? fmaf(d, kHalfHigh, acc[p & 1][SETS - 1][f][n][v])
+                                                     : fmaf(acc[p & 1][SETS - 1][f][n][v], 1.0f / kRestUp, d);
                                 c.v[0][f][n][v] = fmaf(s, d, c.v[0][f][n][v]);
                             }
                     }

@@ -9,7 +9,7 @@ torch = pytest.importorskip("torch")
 
 import paper_2407_00243_amd as tf  # noqa: E402
 import routed_util as ru  # noqa: E402
-from test_gpu_routed import DT, csr, gen, randn, run_layer, stream  # noqa: E402
+from test_gpu_routed import DT, csr, empty_q4, gen, randn, run_layer, stream  # noqa: E402
 
 
 # ------------------------------------------------------------------- rows that name an expert more than once
@@ -68,3 +68,24 @@ def test_layer_of_more_rows_than_a_launch_takes():
     ru.check(D[at], ref, b, torch.bfloat16)
     D[at] = 0
     assert (D == 0).all()
+
+
+# --------------------------------------------------------------------- the smallest and the largest numbers
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("kind,scale", [(tf.TF_Q4_INT, 1.0), (tf.TF_Q4_E2M1, 64.0)])
+@pytest.mark.parametrize("v", [1.3 * 2.0 ** -105, 1.1 * 2.0 ** -113, 1.7 * 2.0 ** -119])
+def test_group_sums_of_small_numbers(dtype, kind, scale, v):
+    n, k = 16, 256
+    codes = torch.ones(1, n, k, dtype=torch.int8, device="cuda")
+    scales = torch.full((1, n, 2), scale, dtype=torch.bfloat16, device="cuda")
+    q = empty_q4(n, k, kind, 128)
+    tf.tf_q4_pack(q, codes, scales, stream())
+    w = ru.values(codes, scales, kind, 128)[0]
+    x = torch.full((2, k), v, device="cuda").to(DT[dtype])
+    x[1, ::2] *= -0.25
+    y = torch.empty(2, n, dtype=DT[dtype], device="cuda")
+    tf.tf_q4_matvec(q, x, y, stream())
+    ref, b = ru.product(x.double(), w)
+    # additions of subnormal numbers are off by half of 2^-149 each, 2^-10 of what is summed
+    ru.check(y, ref, b + scale * 3 * k * 2.0 ** -140, DT[dtype])
