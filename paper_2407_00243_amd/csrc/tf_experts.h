@@ -31,9 +31,15 @@ __device__ __forceinline__ Float4 mfma_f32(float a, float b, Float4 c) {
     return __builtin_amdgcn_mfma_f32_16x16x4f32(a, b, c, 0, 0, 0);
 }
 
+// 4-bit weights meet bf16 and fp32 rows of X as 2^-10 of their codes' values, and results are multiplied by 2^10 at the very end:
+// a group's sum is taken before its scale, and 128 codes of 7 times the largest X would pass 2^128 where the result does not.
+// What is below 2^-126 is subnormal, so a group's sum is good to 2^-139 at the best.  (fp16 rows are far from either end.)
+constexpr float kCodeDown = 0x1p-10f, kCodeUp = 0x1p10f;
+
 // Eight weights of a word of codes, as numbers of sixteen bits (bf16 where X is fp32).  INT: sign and magnitude m
 // sit where an e4m3 number has its sign and its lowest bits; without exponent bits that is m 2^-9.
 template <int EL, int KIND> __device__ __forceinline__ Words4 q4_decode(uint32_t w) {
+    constexpr float e2m1_down = kCodeDown, int_down = 512.0f * kCodeDown;
     Words4 y;
     if constexpr (KIND == TF_Q4_E2M1) {
         if constexpr (EL == TF_F16) {
@@ -42,10 +48,10 @@ template <int EL, int KIND> __device__ __forceinline__ Words4 q4_decode(uint32_t
             y[2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, 1.0f, 2));
             y[3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, 1.0f, 3));
         } else {
-            y[0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, 1.0f, 0));
-            y[1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, 1.0f, 1));
-            y[2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, 1.0f, 2));
-            y[3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, 1.0f, 3));
+            y[0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, e2m1_down, 0));
+            y[1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, e2m1_down, 1));
+            y[2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, e2m1_down, 2));
+            y[3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, e2m1_down, 3));
         }
     } else {
         const uint32_t lo = w & 0x87878787u, hi = __builtin_amdgcn_alignbit(w, w, 4) & 0x87878787u;
@@ -55,10 +61,10 @@ template <int EL, int KIND> __device__ __forceinline__ Words4 q4_decode(uint32_t
             y[2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(hi, 512.0f, false));
             y[3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(hi, 512.0f, true));
         } else {
-            y[0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, 512.0f, false));
-            y[1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, 512.0f, true));
-            y[2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, 512.0f, false));
-            y[3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, 512.0f, true));
+            y[0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, int_down, false));
+            y[1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, int_down, true));
+            y[2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, int_down, false));
+            y[3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, int_down, true));
         }
     }
     return y;
@@ -298,7 +304,8 @@ template <int EL, int KIND, int G, bool HID, int NF> struct Expert {
         }
     }
 
-    // Dense weights: sums of high and of low parts; 4 bits: sums that the scales are in.
+    // Dense weights: sums of high and of low parts; 4 bits: sums that the scales are in (DOWN: 2^-10 of them).
+    static constexpr bool DOWN = !DENSE && EL != TF_F16;
     template <int NT> struct Sums {
         Float4 v[DENSE ? SETS : 1][NF][NT];
     };
@@ -564,6 +571,10 @@ template <int EL, int KIND, int G, bool HID, int NF> struct Expert {
                 p += NF / 2 * NT * 64;
                 up = p[0];
                 for (int w = 1; w < a.k_waves; ++w) up += p[w * (NF * NT * 64)];
+            }
+            if constexpr (DOWN) {
+                y *= kCodeUp;
+                if (a.gated) up *= kCodeUp;
             }
             const int f = in / (NT * 64), n = in / 64 % NT, il = in & 63;
             const int slot = 16 * n + 4 * (il >> 4);

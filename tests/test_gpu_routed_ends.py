@@ -1,4 +1,5 @@
 """Routed operators where their calls end: experts named again and again, the ends of the numbers' range, long launches."""
+import itertools
 import math
 
 import pytest
@@ -89,3 +90,62 @@ def test_group_sums_of_small_numbers(dtype, kind, scale, v):
     ref, b = ru.product(x.double(), w)
     # additions of subnormal numbers are off by half of 2^-149 each, 2^-10 of what is summed
     ru.check(y, ref, b + scale * 3 * k * 2.0 ** -140, DT[dtype])
+
+
+def top_q4(n, k, kind, group, scale, mats=1):
+    """The largest codes, every second output's negative, and one scale: weights in 64 bits beside them."""
+    codes = torch.full((mats, n, k), 7, dtype=torch.int8, device="cuda")
+    codes[:, 1::2] = -7 if kind == tf.TF_Q4_INT else 15
+    scales = torch.full((mats, n, -(-k // group)), scale, dtype=torch.bfloat16, device="cuda")
+    q = empty_q4(n, k, kind, group, mats)
+    tf.tf_q4_pack(q, codes, scales, stream())
+    return q, ru.values(codes, scales, kind, group)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("kind,group", itertools.product([tf.TF_Q4_INT, tf.TF_Q4_E2M1], [32, 64, 128]))
+@pytest.mark.parametrize("m", [1, 20, 40])
+def test_group_sums_may_pass_the_largest_number(dtype, kind, group, m):
+    # 300 times the largest number times 7 (6) is far beyond it; with the scale the sums are not
+    n, k = 40, 300
+    q, w = top_q4(n, k, kind, group, 2.0 ** -12)
+    x = torch.full((m, k), torch.finfo(DT[dtype]).max, dtype=DT[dtype], device="cuda")
+    x[m // 2, ::3] *= -0.5
+    y = torch.empty(m, n, dtype=DT[dtype], device="cuda")
+    tf.tf_q4_matvec(q, x, y, stream())
+    ref, b = ru.product(x.double(), w[0])
+    assert ref.abs().max() < torch.finfo(DT[dtype]).max
+    ru.check(y, ref, b, DT[dtype])
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("kind", [tf.TF_Q4_INT, tf.TF_Q4_E2M1])
+def test_one_largest_number_comes_back(dtype, kind):
+    # code 2 (value 2, and 1 of E2M1) times a scale that makes 1 of it
+    n, k = 16, 128
+    codes = torch.full((1, n, k), 2, dtype=torch.int8, device="cuda")
+    scales = torch.full((1, n, 1), 0.5 if kind == tf.TF_Q4_INT else 1.0, dtype=torch.bfloat16, device="cuda")
+    q = empty_q4(n, k, kind, 128)
+    tf.tf_q4_pack(q, codes, scales, stream())
+    x = torch.zeros(1, k, dtype=DT[dtype], device="cuda")
+    x[0, 77] = torch.finfo(DT[dtype]).max
+    y = torch.empty(1, n, dtype=DT[dtype], device="cuda")
+    tf.tf_q4_matvec(q, x, y, stream())
+    assert (y == x[0, 77]).all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("group", [32, 128])
+def test_group_sums_of_hidden_rows_may_pass_the_largest_number(dtype, group):
+    T, H, I, O = 3, 96, 200, 40
+    W1, v1 = top_q4(I, H, tf.TF_Q4_INT, group, 2.0 ** -10, mats=2)
+    W2, v2 = top_q4(O, I, tf.TF_Q4_INT, group, 2.0 ** -12, mats=2)
+    X = torch.full((T, H), 0.75 * torch.finfo(DT[dtype]).max, device="cuda").to(DT[dtype])
+    A, rowptr, cols = csr([[0], [1, 0], [1]], 2, torch.full((4,), 0.5, device="cuda"))
+    D = torch.empty(T, O, dtype=DT[dtype], device="cuda")
+    with tf.MoePlan(2, H, I, DT[dtype], T, 4, n_out=O, activation=tf.TF_ACT_RELU, gated=False) as plan:
+        plan.run(A, X, W1, W2, D, stream())
+        torch.cuda.synchronize()
+    ref, b = ru.layer(X.double(), rowptr, cols, A.vals.tolist(), lambda e: v1[e], lambda e: v2[e], "relu", False, DT[dtype])
+    assert torch.finfo(DT[dtype]).max / 64 < ref.abs().max() < torch.finfo(DT[dtype]).max
+    ru.check(D, ref, b, DT[dtype])
