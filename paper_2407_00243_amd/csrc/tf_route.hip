@@ -88,9 +88,12 @@ template <int EL, int V> __global__ __launch_bounds__(kThreads) void k_route(con
         }
         w = expf(score - top) / wave_sum(sum);
     } else {
-        w = 1.0f / (1.0f + expf(-score));
-        // (all selected ones below 2^-126: the sum must not be zero)
-        if (a.scoring == TF_ROUTE_SIGMOID_TOP) w /= fmaxf(wave_sum(mine >= 0 ? w : 0.0f), 0x1p-126f);
+        // 1 / (1 + exp(-l)) = exp(min(l, 0)) / (1 + exp(-|l|)), where nothing overflows.  Shares are taken of numerators over the largest
+        // one, so that their sum is 1/2 or more however small the sigmoids are.
+        const float below = fminf(score, 0.0f);
+        const float top = a.scoring == TF_ROUTE_SIGMOID_TOP ? wave_max(mine >= 0 ? below : low) : 0.0f;
+        w = expf(below - top) / (1.0f + expf(-fabsf(score)));
+        if (a.scoring == TF_ROUTE_SIGMOID_TOP) w /= wave_sum(mine >= 0 ? w : 0.0f);
     }
     if (lane < a.k) {
         a.colidx[(int64_t)t * a.k + lane] = mine;

@@ -10,7 +10,7 @@ torch = pytest.importorskip("torch")
 
 import paper_2407_00243_amd as tf  # noqa: E402
 import routed_util as ru  # noqa: E402
-from test_gpu_routed import DT, csr, empty_q4, gen, randn, run_layer, stream  # noqa: E402
+from test_gpu_routed import DT, csr, empty_q4, gen, randn, run_layer, run_route, stream  # noqa: E402
 
 
 # ------------------------------------------------------------------- rows that name an expert more than once
@@ -149,3 +149,28 @@ def test_group_sums_of_hidden_rows_may_pass_the_largest_number(dtype, group):
     ref, b = ru.layer(X.double(), rowptr, cols, A.vals.tolist(), lambda e: v1[e], lambda e: v2[e], "relu", False, DT[dtype])
     assert torch.finfo(DT[dtype]).max / 64 < ref.abs().max() < torch.finfo(DT[dtype]).max
     ru.check(D, ref, b, DT[dtype])
+
+
+# ---------------------------------------------------------------------------------------- router
+
+@pytest.mark.parametrize("scoring", [tf.TF_ROUTE_SIGMOID, tf.TF_ROUTE_SIGMOID_TOP])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_sigmoid_weights_of_small_scores(scoring, dtype):
+    E, k = 70, 4
+    rows = [[-90.0, -91.0], [-87.0, -87.5, -88.0], [-100.0] * 4, [-1000.0, -1001.0, -1003.0, -1000.0], [3.0, -90.0, -95.0],
+            [-88.5, -88.75, -89.0, -103.0], [60.0, 50.0, -1.0]]
+    scores = torch.full((len(rows), E), -math.inf, device="cuda")
+    for t, r in enumerate(rows):
+        scores[t, 3:3 + 7 * len(r):7] = torch.tensor(r, device="cuda")
+    scores = scores.to(DT[dtype])
+    cols, vals = run_route(scores, None, k, scoring, 1.0)
+    for t, r in enumerate(rows):
+        c = [e for e in cols[t].tolist() if e >= 0]
+        assert len(c) == len(r) and (vals[t, len(r):] == 0).all()
+        l = scores[t, c].double().cpu()
+        log = -torch.nn.functional.softplus(-l, threshold=800.0)        # of the sigmoid
+        w = torch.exp(log - log.max()) / torch.exp(log - log.max()).sum() if scoring == tf.TF_ROUTE_SIGMOID_TOP else torch.exp(log)
+        # functions good to a few units, arguments rounded once: 2^-24 of their size; below the normal numbers half a spacing and
+        # the few units again
+        bound = 2.0 ** -24 * (40 + 2 * l.abs().max().item()) * w + 2.0 ** -147
+        assert ((vals[t, :len(r)].double() - w).abs() <= bound).all(), (t, vals[t], w)
