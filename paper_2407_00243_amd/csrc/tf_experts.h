@@ -392,7 +392,9 @@ template <int EL, int KIND, int G, bool HID, int NF> struct Expert {
             if constexpr (EL == TF_F32) {
                 hi[at] = h;
             } else if constexpr (EL == TF_BF16) {
-                const uint16_t top = El<EL>::put(h);
+                // (numbers that round to infinity take the largest bf16 number as their high part)
+                const uint16_t near = El<EL>::put(h);
+                const uint16_t top = near - (__builtin_isinf(El<EL>::get(near)) && !__builtin_isinf(h));
                 const float rest = h - El<EL>::get(top);
                 hi[at] = top;
                 lo[at] = __builtin_isinf(El<EL>::get(top)) ? 0 : El<EL>::put(rest);

@@ -174,3 +174,36 @@ def test_sigmoid_weights_of_small_scores(scoring, dtype):
         # the few units again
         bound = 2.0 ** -24 * (40 + 2 * l.abs().max().item()) * w + 2.0 ** -147
         assert ((vals[t, :len(r)].double() - w).abs() <= bound).all(), (t, vals[t], w)
+
+
+# ------------------------------------------------------------------------------------- hidden rows
+
+@pytest.mark.parametrize("quant", [False, True])
+def test_hidden_rows_of_bf16_reach_the_largest_number_of_fp32(quant):
+    # between the largest bf16 number and the largest fp32 number, where rounding to bf16 would make an infinity
+    big = torch.finfo(torch.bfloat16).max
+    X = torch.zeros(2, 8, dtype=torch.bfloat16, device="cuda")
+    X[0, :2] = torch.tensor([big, 1.5 * 2.0 ** 119], device="cuda")
+    X[1, :2] = -X[0, :2]
+    w1, w2 = torch.ones(1, 8, 8, device="cuda"), torch.full((1, 8, 8), 2.0 ** -10, device="cuda")
+    W1, W2 = w1.bfloat16(), w2.bfloat16()
+    if quant:
+        (W1, w1), (W2, w2) = one_q4(8, 1.0), one_q4(8, 2.0 ** -10)
+    A, rowptr, cols = csr([[0], [0]], 1, torch.ones(2, device="cuda"))
+    D = torch.empty(2, 8, dtype=torch.bfloat16, device="cuda")
+    with tf.MoePlan(1, 8, 8, torch.bfloat16, 2, 2, activation=tf.TF_ACT_IDENTITY, gated=False) as plan:
+        plan.run(A, X, W1, W2, D, stream())
+        torch.cuda.synchronize()
+    h = X.double() @ w1[0].double().t()
+    assert (big < h.abs()).all() and (h.abs() < torch.finfo(torch.float32).max).all()
+    ref, b = ru.layer(X.double(), rowptr, cols, [1.0, 1.0], lambda e: w1[e].double(), lambda e: w2[e].double(), "identity", False,
+                      torch.bfloat16)
+    ru.check(D, ref, b, torch.bfloat16)
+
+
+def one_q4(n, scale):
+    codes = torch.ones(1, n, n, dtype=torch.int8, device="cuda")
+    scales = torch.full((1, n, 1), scale, dtype=torch.bfloat16, device="cuda")
+    q = empty_q4(n, n, tf.TF_Q4_INT, 128)
+    tf.tf_q4_pack(q, codes, scales, stream())
+    return q, ru.values(codes, scales, tf.TF_Q4_INT, 128)
