@@ -87,11 +87,15 @@ __device__ __forceinline__ void cut_pair(uint32_t &h, uint32_t &m, uint32_t &l, 
     l = (wa >> 16) | (wb & 0xffff0000u);
 }
 
+// (in forms that keep their relative precision where they come close to zero: no 1 - 1, no exp that overflows)
 __device__ __forceinline__ float activate(int act, float x) {
     switch (act) {
         case TF_ACT_RELU: return x < 0.0f ? 0.0f : x;       // (a NaN stays one)
-        case TF_ACT_SILU: return x / (1.0f + expf(-x));
-        case TF_ACT_GELU: return 0.5f * x * (1.0f + erff(x * 0.70710678118654752f));
+        case TF_ACT_SILU: {
+            const float e = expf(-fabsf(x));
+            return (x < 0.0f ? x * e : x) / (1.0f + e);
+        }
+        case TF_ACT_GELU: return 0.5f * x * erfcf(x * -0.70710678118654752f);
         default: return x;
     }
 }

@@ -10,7 +10,7 @@ torch = pytest.importorskip("torch")
 
 import paper_2407_00243_amd as tf  # noqa: E402
 import routed_util as ru  # noqa: E402
-from test_gpu_routed import DT, csr, empty_q4, gen, randn, run_layer, run_route, stream  # noqa: E402
+from test_gpu_routed import ACT, DT, csr, empty_q4, gen, randn, run_layer, run_route, stream  # noqa: E402
 
 
 # ------------------------------------------------------------------- rows that name an expert more than once
@@ -207,3 +207,27 @@ def one_q4(n, scale):
     q = empty_q4(n, n, tf.TF_Q4_INT, 128)
     tf.tf_q4_pack(q, codes, scales, stream())
     return q, ru.values(codes, scales, tf.TF_Q4_INT, 128)
+
+
+# ------------------------------------------------------------------------------------- activations
+
+@pytest.mark.parametrize("activation,lowest", [("gelu", -12.9), ("silu", -91.0)])
+def test_activations_keep_their_tails(activation, lowest):
+    # both products are with the identity matrix, and exact: D is the activation of X
+    n = 64
+    X = torch.linspace(lowest, 6.0, 4 * n, device="cuda").view(4, n)
+    one = torch.eye(n, device="cuda")[None].contiguous()
+    A, _, _ = csr([[0]] * 4, 1, torch.ones(4, device="cuda"))
+    D = torch.empty(4, n, device="cuda")
+    with tf.MoePlan(1, n, n, torch.float32, 4, 4, activation=ACT[activation], gated=False) as plan:
+        plan.run(A, X, one, one, D, stream())
+        torch.cuda.synchronize()
+    x = X.double()
+    if activation == "gelu":
+        ref = 0.5 * x * torch.special.erfc(-x * math.sqrt(0.5))
+        # the argument of erfc is rounded twice, which moves its logarithm by x^2 times that
+        rel = 16 + 2 * x * x
+    else:
+        ref = x * torch.exp(x.clamp(max=0)) / (1 + torch.exp(-x.abs()))
+        rel = 16 + 2 * x.abs()
+    assert ((D.double() - ref).abs() <= 2.0 ** -24 * rel * ref.abs() + 2.0 ** -126).all()
