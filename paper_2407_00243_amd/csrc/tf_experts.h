@@ -765,10 +765,16 @@ template <int EL, int KIND, int G, bool HID, int NF> int launch_experts_nf(Exper
     const int rows_per = Ex::WAVES / k_waves * 16 * (a.gated ? NF / 2 : NF);
     const int64_t tiles = (a.n_rows + rows_per - 1) / rows_per;
     a.k_waves = k_waves;
-    // (more than a launch may ask for by default)
-    static const int raised = (int)hipFuncSetAttribute(reinterpret_cast<const void *>(&k_experts<EL, KIND, G, HID, NF>),
-                                                       hipFuncAttributeMaxDynamicSharedMemorySize, 144 << 10);
-    if (raised) return raised;
+    // (more LDS than a launch may ask for by default; a limit of the kernel on one device)
+    static DoneOnDevices raised;
+    int device = 0;
+    hipError_t e = hipGetDevice(&device);
+    if (e == hipSuccess && !raised.has(device)) {
+        e = hipFuncSetAttribute(reinterpret_cast<const void *>(&k_experts<EL, KIND, G, HID, NF>),
+                                hipFuncAttributeMaxDynamicSharedMemorySize, 144 << 10);
+        if (e == hipSuccess) raised.add(device);
+    }
+    if (e != hipSuccess) return (int)e;
     hipLaunchKernelGGL((k_experts<EL, KIND, G, HID, NF>), dim3((unsigned)(tiles * units)), dim3(Ex::THREADS), lds, st, a);
     return (int)hipGetLastError();
 }

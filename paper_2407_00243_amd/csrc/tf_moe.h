@@ -1,5 +1,6 @@
 // Routed operators (router, experts' products, 4-bit weights): what their sources share.
 #pragma once
+#include <atomic>
 #include <cstdint>
 
 #include "../../include/tilefusion.h"
@@ -11,6 +12,17 @@ constexpr int64_t ceil_div(int64_t n, int64_t per) { return (n + per - 1) / per;
 // The most workgroups of a launch, whose threads must be fewer than 2^32.
 constexpr int64_t most_workgroups(int64_t threads) { return (((int64_t)1 << 32) - 1) / threads; }
 constexpr bool last_pass(int32_t first, int32_t total, int32_t most) { return total - first <= most; }
+
+// The devices for which something that lasts has been done; any thread may ask.  (Beyond the 64th it is done each time.)
+class DoneOnDevices {
+    std::atomic<uint64_t> done_{0};
+
+  public:
+    bool has(int device) const { return device >= 0 && device < 64 && (done_.load(std::memory_order_acquire) >> device & 1); }
+    void add(int device) {
+        if (device >= 0 && device < 64) done_.fetch_or((uint64_t)1 << device, std::memory_order_release);
+    }
+};
 
 // ---------------------------------------------------------------------------------- 4-bit layout
 //

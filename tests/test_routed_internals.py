@@ -40,3 +40,19 @@ def test_launches_stay_below_32_bits_of_threads(tmp_path):
         CHECK(most_workgroups(threads) * threads < (int64_t)1 << 32);
         CHECK((most_workgroups(threads) + 1) * threads >= (int64_t)1 << 32);
     }""")
+
+
+def test_what_is_done_once_for_each_device(tmp_path):
+    run_cpp(tmp_path, """
+    DoneOnDevices done;
+    for (int d : {0, 5, 63}) {
+        CHECK(!done.has(d));
+        CHECK(!done.has(d));            // (asking, as before a call that then fails, changes nothing)
+        done.add(d);
+        CHECK(done.has(d) && !done.has(d - 1) && !done.has(d + 1));
+    }
+    for (int d : {-1, 64, 1000}) {
+        done.add(d);
+        CHECK(!done.has(d));
+    }
+    CHECK(done.has(0) && done.has(5) && done.has(63) && !done.has(1));""")
