@@ -411,7 +411,8 @@ tf_status tf_moe_destroy(tf_moe *plan);
  * output, of 16 bytes or more (TF_EUNSUPPORTED otherwise).  A: device arrays, values TF_F32, at most max_tokens rows and max_entries entries, any number of them
  * in a row; entries whose column is not one of the experts are passed over, whatever their value; a row without
  * entries gives a row of zeros.  A's arrays are not validated (see tf_spmm_spmm).  What lies between the products is
- * held in 16 bits or more of precision (TF_F16: magnitudes up to 2^28, larger ones become infinite).
+ * off by up to 2^-16 of its size or 2^-134, whichever is more, where X is bf16; by 2^-22 of it or 2^-25 where X is fp16
+ * (magnitudes up to 2^28, larger ones become infinite); and held in 32 bits where X is fp32.
  * Two executions of one plan must not overlap (they share its workspace). */
 tf_status tf_moe_layer(const tf_moe *plan, const tf_csr *A, const void *X, int64_t ldx, const void *W1, const void *W2,
                        void *D, int64_t ldd, void *hip_stream);

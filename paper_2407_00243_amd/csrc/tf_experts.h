@@ -18,7 +18,8 @@ constexpr int kNearEntries = 256;     // entries whose sum finds columns and val
 constexpr int kJoinTokens = 16;
 
 // Hidden rows of TF_F16 are held in two parts, high * 2^12 + low: fp16 alone ends at 65504, which a gate times
-// what it gates passes easily.
+// what it gates passes easily.  Two parts in fp16, since that is what the instructions multiply beside fp16 weights: up to 2^28, off by 2^-22
+// of a number and, where the low part is subnormal, by 2^-25, which is what fp16 itself holds of numbers below 2^-14.
 constexpr float kHalfHigh = 4096.0f;
 
 __device__ __forceinline__ Float4 mfma_bf16(const Words4 &a, const Words4 &b, Float4 c) {

@@ -231,3 +231,21 @@ def test_activations_keep_their_tails(activation, lowest):
         ref = x * torch.exp(x.clamp(max=0)) / (1 + torch.exp(-x.abs()))
         rel = 16 + 2 * x.abs()
     assert ((D.double() - ref).abs() <= 2.0 ** -24 * rel * ref.abs() + 2.0 ** -126).all()
+
+
+def test_hidden_rows_of_fp16_are_off_by_what_the_call_says():
+    # the first product is with the identity matrix, the second with 1024 times it: D is 1024 times what is held of X
+    n = 64
+    X = torch.linspace(1, 2, n, device="cuda") * torch.tensor([[2.0 ** -11], [-2.0 ** -6], [2.0 ** -2], [4.0]], device="cuda")
+    X = X.half()
+    one = torch.eye(n, dtype=torch.float16, device="cuda")[None]
+    A, _, _ = csr([[0]] * 4, 1, torch.ones(4, device="cuda"))
+    D = torch.empty(4, n, dtype=torch.float16, device="cuda")
+    # h = x^2 / 2 (identity gate times a half of x), which has up to 22 bits and sizes from 2^-23 to 2^5
+    W1 = torch.cat([one, one * 0.5], 1).contiguous()
+    with tf.MoePlan(1, n, n, torch.float16, 4, 4, activation=tf.TF_ACT_IDENTITY) as plan:
+        plan.run(A, X, W1, (one * 1024).contiguous(), D, stream())
+        torch.cuda.synchronize()
+    h = X.double() ** 2 / 2
+    bound = 1024 * torch.maximum(2.0 ** -22 * h, torch.full_like(h, 2.0 ** -25))
+    ru.check(D, 1024 * h, bound, torch.float16)
