@@ -260,7 +260,7 @@ template <int EL, int KIND, int G, bool HID, int NF> struct Expert {
             // rows behind a gate's: the first of a block is row o of a block of the layout, whose next one exists where rows of it
             // are used (rows beyond the matrix: others are read)
             const int row = (a.n_rows & 15) + r;
-            const bool next = row > 15 && (NF > 2 || (a.n_rows + block_row(a, row0, 0)) >> 4 < (2 * a.n_rows - 1) >> 4);
+            const bool next = row > 15 && (a.n_rows + block_row(a, row0, 0)) >> 4 < (2 * a.n_rows - 1) >> 4;
             w_up = (next ? (uint32_t)blocks * 1024 : 0) + (16 * g + (row & 15)) * 16;
             s_up = (next ? (uint32_t)blocks * (32 * G) : 0) + (row & 15) * (2 * G);
         }

@@ -103,7 +103,7 @@ int launch_experts_bf16(const ExpertLaunch &a, void *stream);
 int launch_experts_f16(const ExpertLaunch &a, void *stream);
 int launch_experts_f32(const ExpertLaunch &a, void *stream);
 
-// Elements from one hidden row to the next: whole 4-bit blocks, zeros beyond n_hidden.
+// Elements from one hidden row to the next: rows begin on lines of memory.  (What lies between them is neither written nor read.)
 inline int64_t hidden_ld(int64_t n_hidden) { return (n_hidden + kQ4Block - 1) / kQ4Block * kQ4Block; }
 
 // ----------------------------------------------------------------------------------------- errors

@@ -288,8 +288,6 @@ tf_status tf_moe_create(const tf_moe_desc *desc, tf_moe **out) {
         p->hidden_part = d.max_entries * ld * es;
         const size_t hidden = (size_t)p->hidden_part * (d.dtype == TF_F32 ? 1 : 2);
         e = hipMalloc(&p->hidden.p, hidden);
-        // columns beyond n_hidden stay zero
-        if (e == hipSuccess) e = hipMemset(p->hidden.p, 0, hidden);
         if (e == hipSuccess) e = hipMalloc(&p->sums.p, (size_t)(d.max_entries * d.n_out) * 4);
         const size_t counts = (size_t)((d.n_out + 15) / 16) * sizeof(uint32_t);
         if (e == hipSuccess) e = hipMalloc(&p->arrived.p, counts);

@@ -10,9 +10,7 @@ namespace {
 typedef float Float4 __attribute__((ext_vector_type(4)));
 typedef uint32_t Words4 __attribute__((ext_vector_type(4)));
 typedef __bf16 Bf8 __attribute__((ext_vector_type(8)));
-typedef __bf16 Bf2 __attribute__((ext_vector_type(2)));
 typedef _Float16 Half8 __attribute__((ext_vector_type(8)));
-typedef _Float16 Half2 __attribute__((ext_vector_type(2)));
 
 // Element types by their tf_dtype.
 template <int EL> struct El;

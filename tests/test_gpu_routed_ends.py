@@ -249,3 +249,16 @@ def test_hidden_rows_of_fp16_are_off_by_what_the_call_says():
     h = X.double() ** 2 / 2
     bound = 1024 * torch.maximum(2.0 ** -22 * h, torch.full_like(h, 2.0 ** -25))
     ru.check(D, 1024 * h, bound, torch.float16)
+
+
+@pytest.mark.parametrize("dtype", DT)
+@pytest.mark.parametrize("quant,I", [(None, 71), ((tf.TF_Q4_INT, 32), 3), ((tf.TF_Q4_E2M1, 64), 133)])
+def test_what_lies_between_hidden_rows_is_not_read(dtype, quant, I):
+    # a workspace in memory that held NaN before, as far as the allocator gives it out again
+    torch.cuda.empty_cache()
+    junk = torch.full((1 << 26,), math.nan, device="cuda")
+    torch.cuda.synchronize()
+    del junk
+    torch.cuda.empty_cache()
+    D, ref, b = run_layer([[0, 2], [1], [2, 0, 1]] * 7, 3, 130, I, 50, dtype, quant=quant)
+    ru.check(D, ref, b, DT[dtype])
