@@ -10,7 +10,7 @@ torch = pytest.importorskip("torch")
 
 import paper_2407_00243_amd as tf  # noqa: E402
 import routed_util as ru  # noqa: E402
-from test_gpu_routed import ACT, DT, csr, empty_q4, gen, randn, run_layer, run_route, stream  # noqa: E402
+from test_gpu_routed import ACT, DT, csr, empty_q4, gen, randn, random_q4, run_layer, run_route, stream  # noqa: E402
 
 
 # ------------------------------------------------------------------- rows that name an expert more than once
@@ -261,4 +261,38 @@ def test_what_lies_between_hidden_rows_is_not_read(dtype, quant, I):
     del junk
     torch.cuda.empty_cache()
     D, ref, b = run_layer([[0, 2], [1], [2, 0, 1]] * 7, 3, 130, I, 50, dtype, quant=quant)
+    ru.check(D, ref, b, DT[dtype])
+
+
+# ---------------------------------------------------------------- launches that other tests' sizes do not lead to
+
+@pytest.mark.parametrize("dtype", DT)
+@pytest.mark.parametrize("kind,group", [(tf.TF_Q4_INT, 64), (tf.TF_Q4_E2M1, 32)])
+@pytest.mark.parametrize("m,n,k", [(1, 33000, 200), (7, 40000, 300), (20, 40000, 200), (90, 60000, 200)])
+def test_matvec_with_many_outputs(dtype, kind, group, m, n, k):
+    # two blocks of rows a wave without a gate
+    check_matvec(dtype, kind, group, m, n, k)
+
+
+@pytest.mark.parametrize("dtype", DT)
+@pytest.mark.parametrize("kind,group", [(tf.TF_Q4_INT, 128), (tf.TF_Q4_E2M1, 32)])
+@pytest.mark.parametrize("m,n,k", [(1, 1024, 8192), (20, 1024, 8192), (33, 1040, 8200), (64, 1000, 6001), (90, 520, 4100)])
+def test_matvec_with_few_outputs_and_many_inputs(dtype, kind, group, m, n, k):
+    check_matvec(dtype, kind, group, m, n, k)
+
+
+def check_matvec(dtype, kind, group, m, n, k):
+    g = gen(m + n + k)
+    q, w = random_q4(g, n, k, kind, group)
+    x = randn(g, m, k, dtype=DT[dtype])
+    y = torch.full((m, n), math.nan, dtype=DT[dtype], device="cuda")
+    tf.tf_q4_matvec(q, x, y, stream())
+    ref, b = ru.product(x.double(), w[0])
+    ru.check(y, ref, b, DT[dtype])
+
+
+@pytest.mark.parametrize("dtype", DT)
+@pytest.mark.parametrize("H,I,O", [(200, 33000, 64), (64, 200, 33000)])
+def test_layer_with_many_outputs_and_no_gate(dtype, H, I, O):
+    D, ref, b = run_layer([[0], [1], [0, 1]], 2, H, I, O, dtype, "relu", False)
     ru.check(D, ref, b, DT[dtype])
