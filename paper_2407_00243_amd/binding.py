@@ -381,10 +381,12 @@ def _refuse_devices():
     raise ValueError("all operands must be on one device, and not on the host")
 
 
-def _device_of(W, device: int) -> int:
-    """Number of the device of a Q4Matrix, a tensor or nothing; of addresses, which are the caller's affair, `device`."""
+def _device_of(W, device):
+    """Number of the device of a Q4Matrix or an array, -1 for the host; for addresses, which are the caller's affair, `device`."""
     if isinstance(W, Q4Matrix):
         return device if W.device is None else W.device
+    if isinstance(W, np.ndarray):
+        return -1
     return W.get_device() if hasattr(W, "get_device") else device
 
 
@@ -410,7 +412,7 @@ class Q4Matrix:
             if hasattr(x, "numel") and (x.numel() * x.element_size() < n or not x.is_contiguous()):
                 raise ValueError(f"{what} must hold {n} contiguous bytes")
         # number of their device, -1 for the host; None where both are addresses
-        devices = {x.get_device() for x in (codes, scales) if hasattr(x, "get_device")}
+        devices = {_device_of(x, None) for x in (codes, scales)} - {None}
         if len(devices) > 1:
             raise ValueError("codes and scales must be on one device")
         self.device = devices.pop() if devices else None

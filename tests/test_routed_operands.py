@@ -87,3 +87,17 @@ def test_layer_calls_by_handle_look_at_their_rows():
     for X, D, error in ((X[1:], X, ValueError), (X, X[1:], ValueError), (X, X.bfloat16(), TypeError), (X, X.t().contiguous().t(), ValueError)):
         with pytest.raises(error):
             tf.tf_moe_layer(1, A, X, W1, W2, D)
+
+
+def test_numpy_arrays_are_on_the_host():
+    np = pytest.importorskip("numpy")
+    address = 4096
+    W = tf.Q4Matrix(32, 64, tf.TF_Q4_INT, 32, address, address)          # addresses are the caller's affair
+    assert W.device is None
+    for codes, scales in ((np.zeros((1, 32, 64), np.int8), address), (address, np.zeros((1, 32, 2), np.uint16))):
+        with pytest.raises(ValueError, match="device"):
+            tf.tf_q4_pack(W, codes, scales)
+    sizes = tf.tf_q4_sizes(32, 64, tf.TF_Q4_INT, 32)
+    host = tf.Q4Matrix(32, 64, tf.TF_Q4_INT, 32, *(np.zeros(n, np.uint8) for n in sizes))
+    with pytest.raises(ValueError, match="device"):
+        tf.tf_q4_pack(host, address, address)
