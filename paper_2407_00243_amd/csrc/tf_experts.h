@@ -13,8 +13,8 @@ namespace {
 constexpr int expert_waves(int nf) { return nf == 1 ? 8 : 4; }
 constexpr int kNearRows = 256;        // row pointers that are held in LDS
 constexpr int kNearEntries = 256;     // entries whose sum finds columns and values in LDS
-// The most tokens whose entries the last workgroups add up: one token 3 us less than a launch of its own, but 32 tokens through
-// 64 experts 212 us, with that launch 161.
+// The most tokens whose entries the last workgroups add up: one bf16 token through two experts of 4096 x 8192 85.4 us, with a launch of
+// its own 86.7 (calls of small layers 0.5 us); but 32 tokens through 64 experts of 2048 x 1024 158 us, with that launch 141.
 constexpr int kJoinTokens = 16;
 
 // Hidden rows of TF_F16 are held in two parts, high * 2^12 + low: fp16 alone ends at 65504, which a gate times
@@ -152,11 +152,15 @@ template <typename T> __device__ __forceinline__ Words4 load_short(const char *p
 // where all waves read it.  X is the first of the two: a lane then holds sums of four entries and one row of weights, whose
 // group has one scale (with the weights first it took four scales a group and 128-column steps of twice the registers).
 //
-// Bound by memory where entries of an expert are few: 32 bf16 tokens through 64 experts of 2048 x 1024 (0.77 GB) 142 us, 5.4 TB/s;
-// one through two of 4096 x 8192 85 us, 4.7; an fp16 row times a 4-bit matrix of 32768 x 8192 28.5 us, 5.3; and by the instructions of
-// products and staging where they are many: 128 fp16 tokens through 16 4-bit experts of 4096 x 8192 284 us, 3.2 TB/s, vector
-// instructions a quarter of the waves' cycles, waits 40 %, at the two waves a SIMD that 256 registers leave (three or four with
-// spilled registers were slower).  X in registers instead of LDS (the first kernel): 983 us there, 247 for the 32 tokens.
+// Bound by memory where entries of an expert are few: 32 bf16 tokens through 64 experts of 2048 x 1024 (0.77 GB) 145 us, 5.3 TB/s;
+// one through two of 4096 x 8192 85 us, 4.7; an fp16 row times a 4-bit matrix of 32768 x 8192 29.6 us, 5.1; and by the instructions of
+// products and staging where they are many: 128 fp16 tokens through 16 4-bit experts of 4096 x 8192 305 us, 3.0 TB/s, vector
+// instructions 28 to 31 % of the waves' cycles, waits 36 to 39, at the two waves a SIMD that 256 registers leave (three or four with
+// spilled registers were slower).  (Medians of passes in a graph over two sets of inputs in turn.)
+//
+// X in registers, straight from memory into the operand, took 983 us there, and 247 for the 32 tokens.  It was ahead where little
+// is multiplied with an X that is staged: a bf16 row times 4-bit 4096 x 4096 6.4 us (now 6.9), 13 fp32 rows times 5003 x 2891
+// 9.5 (13.4), 64 bf16 rows times 8192 x 8192 36.7 (37.1), 11 fp16 tokens through 10 experts of 1037 x 515 20 (26).
 //
 // Dense weights are loaded by whole lines of 128 bytes: an instruction takes eight rows x 128 bytes, and two of them are
 // put in operand order (sixteen rows x 64 bytes) by exchanging halves of sixteen lanes (a read of 512 MiB by itself, rows of
@@ -417,7 +421,7 @@ template <int EL, int KIND, int G, bool HID, int NF> struct Expert {
     // all.  A piece's place among those of its operand is rotated with its column: without that the 64 pieces of a row that a wave
     // writes would all be in the same four banks (of the LDS cycles of 128 fp16 tokens through 4-bit experts 40 % are
     // still conflicts; with pieces dealt operand by operand, sixteen rows x 64 bytes a load, none are, but 64 bf16 rows times a 4-bit
-    // 8192 x 8192 matrix took 66 us instead of 59).
+    // 8192 x 8192 matrix took 66 us where this took 59, both with two blocks of rows a wave).
     template <int NT, int TOK> struct Piece {
         static constexpr int ROW = Chunk<NT, TOK>::STEPS * SUB * 4;       // pieces of a row in a chunk
         int e, c;                                                        // entry, piece of its row
@@ -728,8 +732,10 @@ __global__ __launch_bounds__(64 * expert_waves(NF), 2) void k_experts(const Expe
     }
     if constexpr (HID) {
         if (!join) return;
-        // this workgroup's sums are where all others see them, then it counts itself in; the last one for a block of columns
-        // adds up the entries of each token
+        // This workgroup's sums are where all others see them, then it counts itself in; the last one for a block of columns
+        // adds up the entries of each token.  The sums are stored and loaded by relaxed atomics of agent scope, which pass the caches that
+        // workgroups do not share, so it is enough that a thread's stores are complete (the wait for all of them) before its workgroup's
+        // count; the fences only keep the compiler from moving accesses.  A release of agent scope would write back the whole L2.
         __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup");
         __builtin_amdgcn_s_waitcnt(0);
         __syncthreads();
@@ -790,8 +796,9 @@ struct ExpertCut {
 };
 // Workgroups run in rounds of as many as the card holds (two of four waves a compute unit, or one of eight), each as long
 // as its waves' steps and some four more for what comes before and after them.  A step of one block of rows takes 0.6 of one of
-// two.  More waves on the same columns make shorter workgroups, and more of them.  (64 bf16 rows times 4-bit 8192 x 8192: one block of rows
-// and four waves on the same columns 38 us, two blocks 59; fp16 row times 32768 x 8192: two blocks and two waves 29.5, four waves 34 to 44.)
+// two.  More waves on the same columns make shorter workgroups, and more of them.  (64 bf16 rows times 4-bit 8192 x 8192: one block
+// of rows and four waves on the same columns 37 us, two blocks 58 to 109; fp16 row times 32768 x 8192: two blocks and two waves 29.7,
+// four 32.5, one 37, one block 38 to 64.)
 // units: experts that have work, in the mean; launched: those that workgroups are launched for.  k_waves is 0 if no cut fits a launch.
 template <typename Ex, int NF> ExpertCut cut_experts(const ExpertLaunch &a, int most, double units, int64_t launched) {
     const int steps = (a.n_cols + Ex::STEP - 1) / Ex::STEP;

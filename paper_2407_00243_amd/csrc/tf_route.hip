@@ -20,8 +20,8 @@ __device__ __forceinline__ float wave_max(float x) {
 }
 
 // One wave per token; lane l holds the scores of experts l, l + 64, ..., V of them.  k times the largest of those left: k exchanges
-// over the wave, all in registers, no LDS and no barrier.  Bound by launch and latency: 1 token, 64 experts, k = 6 5.6 us in a graph; 2048
-// tokens, 160 experts, k = 8 (0.8 MB) 8.8 us.
+// over the wave, all in registers, no LDS and no barrier.  Bound by launch and latency: 1 token, 64 experts, k = 6 5.5 us in a graph; 2048
+// tokens, 160 experts, k = 8 (0.8 MB) 8.9 us.
 template <int EL, int V> __global__ __launch_bounds__(kThreads) void k_route(const RouteLaunch a) {
     typedef typename El<EL>::T T;
     const int lane = threadIdx.x & 63;
