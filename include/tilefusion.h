@@ -420,6 +420,68 @@ tf_status tf_moe_layer(const tf_moe *plan, const tf_csr *A, const void *X, int64
 tf_status tf_moe_layer_q4(const tf_moe *plan, const tf_csr *A, const void *X, int64_t ldx, const tf_q4 *W1,
                           const tf_q4 *W2, void *D, int64_t ldd, void *hip_stream);
 
+/* ------------------------------------------------------------------------------------------------
+ * Losses and their gradients: what trains a routed network or a classifier (of a graph's nodes, of tokens).
+ * The conventions of the routed operators hold: fp32, bf16 and fp16, 32-bit sums rounded once, rows that may be further apart
+ * than they are wide, calls that allocate nothing and may be captured.
+ */
+
+/* Balance of a router.  With p_te the share of expert e in the scores of token t (softmax scorings: exp(l_e) over its sum over all
+ * experts; sigmoid scorings: sigma(l_e) over its sum; a score of -inf or NaN has none),
+ *     counts[e] = entries of A whose column is e          counts[n_cols] = n = rows of A that have such an entry
+ *     mass[e]   = 1/n sum over those rows of p_te         *loss = n_cols sum_e f_e mass[e],   f_e = counts[e] / sum counts
+ * which is 1 where experts are met evenly.  All are 0 where n is.  A is a matrix as tf_moe_route makes it: the same number of entries in
+ * each row (at most 64, for at most 1024 columns), columns that are not an expert's (-1) are passed over; rowptr and vals are not read.
+ * counts (n_cols + 1), mass, loss and the workspace are device arrays; the workspace has the size that tf_moe_balance_size
+ * tells (at most 4 MiB) and may be used by one call at a time.  A score of +inf makes the shares of its row, and so mass and loss, NaN. */
+tf_status tf_moe_balance_size(int64_t n_tokens, int64_t n_experts, int64_t *bytes);
+tf_status tf_moe_balance(const void *scores, int64_t ld, int32_t dtype, int32_t scoring, const tf_csr *A, int32_t *counts, float *mass,
+                         float *loss, void *workspace, void *hip_stream);
+
+/* Gradient of the scores: dscores (like scores, rows ldd apart) gets the sum of
+ *   - the gradient by way of the entries' values that tf_moe_route made with this scoring and scale: dvals (A->nnz floats) is that of
+ *     A's values, those of entries that are passed over are not looked at;
+ *   - *dloss (a device float) times the gradient of the balance loss, with the counts of tf_moe_balance (held constant; those of
+ *     several devices may have been added up).
+ * Either dvals, or counts and dloss, may be NULL.  Scores of -inf or NaN get 0, rows without an entry zeros.  An expert that a row names
+ * more than once counts as often.  dscores may be the scores' own array. */
+tf_status tf_moe_route_grad(const void *scores, int64_t ld, int32_t dtype, int32_t scoring, float scale, const tf_csr *A, const float *dvals,
+                            const int32_t *counts, const float *dloss, void *dscores, int64_t ldd, void *hip_stream);
+
+/* Softmax cross entropy of a product: the chain whose middle, the logits l = X W^T (rows x classes), is never kept.
+ * Row t of X has the class labels[t]; rows whose label is not one of the classes (-1) have no part in anything: they are not read, their loss,
+ * lse and rows of dX are 0.
+ *     lse[t] = log sum_v exp(l_tv)                                 loss[t] = lse[t] - l_t,labels[t]
+ *     g_tv   = dloss[t] (exp(l_tv - lse[t]) - [v = labels[t]])     dX = g W      dW = g^T X
+ * The logits are made for a piece of the classes at a time, by both calls; g is held for a piece, rounded to 16 bits (bf16: to bf16; fp16: to
+ * fp16 after division by the largest |dloss|, so that no size of dloss is lost; fp32: as three bf16 numbers, which hold 24 bits). */
+typedef struct tf_xent_desc {
+    int64_t n_classes;    /* rows of W, at most 2^30                                       */
+    int64_t n_in;         /* columns of X and W, at most 2^22                              */
+    int64_t max_rows;     /* largest number of rows of X, at most 2^28                     */
+    int32_t dtype;        /* of X, W, dX and dW                                            */
+    int32_t gradients;    /* 1: the workspace also holds what tf_xent_grad needs, 0: it does not */
+} tf_xent_desc;
+
+typedef struct tf_xent tf_xent; /* opaque, library-owned: the sizes above and a workspace */
+
+/* Allocates the workspace on the current device.  On failure *out is NULL. */
+tf_status tf_xent_create(const tf_xent_desc *desc, tf_xent **out);
+/* Frees it.  NULL is accepted. */
+tf_status tf_xent_destroy(tf_xent *plan);
+/* The number of the device that the plan was made on, which has to be the current one of every call. */
+tf_status tf_xent_device(const tf_xent *plan, int32_t *device);
+
+/* loss and lse (n_rows floats each) of X (n_rows x n_in, rows ldx apart) and W (n_classes x n_in, rows ldw apart).  W is read fastest where it is
+ * 16-bit, its rows begin at multiples of 16 bytes and n_in is a multiple of 8; otherwise a copy is made of it, piece by piece.
+ * Two executions of one plan must not overlap (they share its workspace). */
+tf_status tf_xent_loss(const tf_xent *plan, const void *X, int64_t ldx, const void *W, int64_t ldw, const int32_t *labels, int64_t n_rows,
+                       float *loss, float *lse, void *hip_stream);
+/* dX (n_rows x n_in, rows lddx apart) and dW (n_classes x n_in, rows lddw apart), either of which may be NULL, from the lse that
+ * tf_xent_loss made and the gradient of each row's loss.  dX and dW are overwritten; they must not overlap X, W or each other. */
+tf_status tf_xent_grad(const tf_xent *plan, const void *X, int64_t ldx, const void *W, int64_t ldw, const int32_t *labels, const float *lse,
+                       const float *dloss, int64_t n_rows, void *dX, int64_t lddx, void *dW, int64_t lddw, void *hip_stream);
+
 /* Message for the most recent failure on the calling thread ("" if none). */
 const char *tf_last_error(void);
 

@@ -99,11 +99,18 @@ class tf_moe_desc(ctypes.Structure):
                 ("reserved0", ctypes.c_int32)]
 
 
+class tf_xent_desc(ctypes.Structure):
+    _fields_ = [("n_classes", ctypes.c_int64), ("n_in", ctypes.c_int64), ("max_rows", ctypes.c_int64),
+                ("dtype", ctypes.c_int32), ("gradients", ctypes.c_int32)]
+
+
 EXPORTS = ["tf_plan_create", "tf_plan_destroy", "tf_plan_schedule", "tf_plan_workspace",
            "tf_gemm_spmm", "tf_gemm_spmm_static", "tf_spmm_spmm", "tf_unfused_gemm_spmm",
            "tf_unfused_spmm_spmm", "tf_run_wavefront", "tf_plan_prepare_unfused", "tf_plan_workspace_unfused",
            "tf_csr_validate", "tf_q4_sizes", "tf_q4_pack", "tf_q4_quantize", "tf_q4_unpack", "tf_q4_matvec",
            "tf_moe_route", "tf_moe_create", "tf_moe_destroy", "tf_moe_layer", "tf_moe_layer_q4",
+           "tf_moe_balance_size", "tf_moe_balance", "tf_moe_route_grad", "tf_xent_create", "tf_xent_destroy",
+           "tf_xent_device", "tf_xent_loss", "tf_xent_grad",
            "tf_last_error", "tf_version"]
 _INT_RETURNS = [e for e in EXPORTS if e not in ("tf_last_error", "tf_version")]
 
@@ -148,6 +155,14 @@ def load_library():
     lib.tf_moe_destroy.argtypes = [vp]
     lib.tf_moe_layer.argtypes = [vp, csr, vp, i64, vp, vp, vp, i64, vp]
     lib.tf_moe_layer_q4.argtypes = [vp, csr, vp, i64, q4, q4, vp, i64, vp]
+    lib.tf_moe_balance_size.argtypes = [i64, i64, ctypes.POINTER(i64)]
+    lib.tf_moe_balance.argtypes = [vp, i64, i32, i32, csr, vp, vp, vp, vp, vp]
+    lib.tf_moe_route_grad.argtypes = [vp, i64, i32, i32, ctypes.c_float, csr, vp, vp, vp, vp, i64, vp]
+    lib.tf_xent_create.argtypes = [ctypes.POINTER(tf_xent_desc), ctypes.POINTER(vp)]
+    lib.tf_xent_destroy.argtypes = [vp]
+    lib.tf_xent_device.argtypes = [vp, ctypes.POINTER(i32)]
+    lib.tf_xent_loss.argtypes = [vp, vp, i64, vp, i64, vp, i64, vp, vp, vp]
+    lib.tf_xent_grad.argtypes = [vp, vp, i64, vp, i64, vp, vp, vp, i64, vp, i64, vp, i64, vp]
     for name in _INT_RETURNS:
         getattr(lib, name).restype = ctypes.c_int
     lib.tf_last_error.restype = ctypes.c_char_p
@@ -572,6 +587,184 @@ class MoePlan:
     def close(self) -> None:
         if self.handle:
             tf_moe_destroy(self.handle)
+            self.handle = None
+
+    def __enter__(self):
+        return self
+
+    def __exit__(self, *exc):
+        self.close()
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+
+# -------------------------------------------------------------------------- losses and their gradients
+
+def _vector(x, what: str, n: int, dtype: str, device: int):
+    """Address of a contiguous vector of n elements on `device`."""
+    if str(x.dtype) != dtype:
+        raise TypeError(f"{what} must be {dtype}")
+    if tuple(x.shape) != (n,) or not x.is_contiguous():
+        raise ValueError(f"{what} must be contiguous and have {n} elements")
+    if x.get_device() != device:
+        _refuse_devices()
+    return x.data_ptr()
+
+
+def _router_operands(scores, A):
+    """Address, distance of the rows, device and routing matrix of a call on a router's scores."""
+    rows, _, ld = _matrix(scores, "scores", A.n_cols)
+    if rows != A.n_rows:
+        raise ValueError("A must have a row for each row of the scores")
+    device = scores.get_device()
+    if device < 0:
+        _refuse_devices()
+    return scores.data_ptr(), ld, device, ctypes.byref(_routing(A, device))
+
+
+def tf_moe_balance_size(n_tokens: int, n_experts: int) -> int:
+    """Bytes of the workspace of tf_moe_balance."""
+    out = ctypes.c_int64()
+    _check(load_library().tf_moe_balance_size(n_tokens, n_experts, ctypes.byref(out)))
+    return out.value
+
+
+def tf_moe_balance(scores, A: DeviceCsr, counts, mass, loss, workspace, scoring: int = TF_ROUTE_SOFTMAX_TOP,
+                   stream=None) -> None:
+    """Writes counts (int32, experts + 1), mass (float32, experts) and loss (float32, 1).  workspace: bytes."""
+    p, ld, device, a = _router_operands(scores, A)
+    e = A.n_cols
+    if str(workspace.dtype) != "torch.uint8" or not workspace.is_contiguous() or workspace.get_device() != device:
+        raise ValueError("the workspace must be contiguous bytes on the device of the scores")
+    if workspace.numel() < tf_moe_balance_size(A.n_rows, e):
+        raise ValueError("the workspace is too small")
+    status = load_library().tf_moe_balance(
+        p, ld, _routed_code(scores.dtype), scoring, a, _vector(counts, "counts", e + 1, "torch.int32", device),
+        _vector(mass, "mass", e, "torch.float32", device), _vector(loss, "loss", 1, "torch.float32", device),
+        workspace.data_ptr(), stream)
+    if status:
+        _check(status)
+
+
+def tf_moe_route_grad(scores, A: DeviceCsr, dscores, scoring: int = TF_ROUTE_SOFTMAX_TOP, scale: float = 1.0, dvals=None,
+                      counts=None, dloss=None, stream=None) -> None:
+    """Writes dscores: dvals (float32, one for each entry of A) and dloss (float32, 1, with the counts of
+    tf_moe_balance) are the gradients of A's values and of the balance loss."""
+    p, ld, device, a = _router_operands(scores, A)
+    rows, _, ldd = _matrix(dscores, "dscores", A.n_cols)
+    if rows != A.n_rows:
+        raise ValueError("dscores must have a row for each row of the scores")
+    if dscores.dtype != scores.dtype:
+        raise TypeError("scores and dscores must have the same element type")
+    if dscores.get_device() != device:
+        _refuse_devices()
+    status = load_library().tf_moe_route_grad(
+        p, ld, _routed_code(scores.dtype), scoring, scale, a,
+        None if dvals is None else _vector(dvals, "dvals", A.nnz, "torch.float32", device),
+        None if counts is None else _vector(counts, "counts", A.n_cols + 1, "torch.int32", device),
+        None if dloss is None else _vector(dloss, "dloss", 1, "torch.float32", device), dscores.data_ptr(), ldd, stream)
+    if status:
+        _check(status)
+
+
+def tf_xent_create(n_classes: int, n_in: int, dtype, max_rows: int, gradients: bool = True) -> int:
+    """Returns the opaque handle of a plan for the cross entropy of products of these sizes."""
+    d = tf_xent_desc(n_classes, n_in, max_rows, _routed_code(dtype), 1 if gradients else 0)
+    out = ctypes.c_void_p()
+    _check(load_library().tf_xent_create(ctypes.byref(d), ctypes.byref(out)))
+    return out.value
+
+
+def tf_xent_destroy(plan: Optional[int]) -> None:
+    _check(load_library().tf_xent_destroy(plan))
+
+
+def tf_xent_device(plan: int) -> int:
+    out = ctypes.c_int32()
+    _check(load_library().tf_xent_device(plan, ctypes.byref(out)))
+    return out.value
+
+
+def tf_xent_loss(plan: int, X, W, labels, loss, lse, stream=None) -> None:
+    """The caller answers for what a handle does not tell: columns, classes and element type are to be the plan's (XentPlan looks)."""
+    rows, n, ldx = _matrix(X, "X")
+    _, _, ldw = _matrix(W, "W", n)
+    _xent_types(X, W)
+    device = X.get_device()
+    status = load_library().tf_xent_loss(
+        plan, X.data_ptr(), ldx, W.data_ptr(), ldw, _vector(labels, "labels", rows, "torch.int32", device), rows,
+        _vector(loss, "loss", rows, "torch.float32", device), _vector(lse, "lse", rows, "torch.float32", device), stream)
+    if status:
+        _check(status)
+
+
+def tf_xent_grad(plan: int, X, W, labels, lse, dloss, dX=None, dW=None, stream=None) -> None:
+    rows, n, ldx = _matrix(X, "X")
+    classes, _, ldw = _matrix(W, "W", n)
+    _xent_types(X, W, dX, dW)
+    device = X.get_device()
+    lddx = lddw = n
+    for what, d, want in (("dX", dX, rows), ("dW", dW, classes)):
+        if d is not None:
+            have, _, step = _matrix(d, what, n)
+            if have != want:
+                raise ValueError(f"{what} must have {want} rows, not {have}")
+            lddx, lddw = (step, lddw) if what == "dX" else (lddx, step)
+    status = load_library().tf_xent_grad(
+        plan, X.data_ptr(), ldx, W.data_ptr(), ldw, _vector(labels, "labels", rows, "torch.int32", device),
+        _vector(lse, "lse", rows, "torch.float32", device), _vector(dloss, "dloss", rows, "torch.float32", device), rows,
+        _addr(dX), lddx, _addr(dW), lddw, stream)
+    if status:
+        _check(status)
+
+
+def _xent_types(X, *others):
+    """All operands (or None) have X's element type and lie on its device, which is not the host."""
+    device = X.get_device()
+    for x in others:
+        if x is not None:
+            if x.dtype != X.dtype:
+                raise TypeError("X, W and their gradients must have the same element type")
+            if x.get_device() != device:
+                _refuse_devices()
+    if device < 0:
+        _refuse_devices()
+
+
+class XentPlan:
+    """Owns a plan for the softmax cross entropy of X W^T; checks the operands that it is given."""
+
+    def __init__(self, n_classes: int, n_in: int, dtype, max_rows: int, gradients: bool = True):
+        self.handle = None
+        self.n_classes, self.n_in, self.dtype = n_classes, n_in, _routed_code(dtype)
+        self.handle = tf_xent_create(n_classes, n_in, self.dtype, max_rows, gradients)
+        self.device = tf_xent_device(self.handle)
+
+    def _look(self, X, W):
+        if tuple(W.shape) != (self.n_classes, self.n_in) or X.shape[-1] != self.n_in:
+            raise ValueError(f"W must have the shape {(self.n_classes, self.n_in)} and X {self.n_in} columns")
+        if _routed_code(X.dtype) != self.dtype:
+            raise TypeError("X must have the element type of the plan")
+        if X.get_device() != self.device:
+            _refuse_devices()
+
+    def loss(self, X, W, labels, loss, lse, stream=None) -> None:
+        """Writes loss and lse (float32, one for each row of X).  labels: int32, others than 0 .. n_classes - 1 for rows without one."""
+        self._look(X, W)
+        tf_xent_loss(self.handle, X, W, labels, loss, lse, stream)
+
+    def grad(self, X, W, labels, lse, dloss, dX=None, dW=None, stream=None) -> None:
+        """Writes dX and dW (like X and W; None: not wanted) from lse and the gradient of each row's loss (float32)."""
+        self._look(X, W)
+        tf_xent_grad(self.handle, X, W, labels, lse, dloss, dX, dW, stream)
+
+    def close(self) -> None:
+        if self.handle:
+            tf_xent_destroy(self.handle)
             self.handle = None
 
     def __enter__(self):

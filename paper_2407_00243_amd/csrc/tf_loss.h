@@ -1,0 +1,107 @@
+// Losses of a routed network or a classifier and their gradients: what their sources share.
+#pragma once
+#include "tf_moe.h"
+
+namespace tf {
+
+// ---------------------------------------------------------------------- router: balance and gradient
+
+// Workgroups of a balance's first launch, each of which leaves its sums in the workspace.
+constexpr int kBalanceGroups = 256;
+// Bytes of that workspace: for each workgroup a sum and a count for each expert, and its number of rows.
+inline int64_t balance_bytes(int64_t n_experts) { return (int64_t)kBalanceGroups * (2 * n_experts + 1) * 4; }
+
+struct RouterLaunch {
+    const void *scores;
+    int64_t ld;
+    const int32_t *colidx;
+    int32_t n_tokens, n_experts, k, dtype, scoring;
+    // balance
+    int32_t *counts;              // n_experts, and behind them the rows that have an entry
+    float *mass, *loss;
+    void *workspace;
+    // gradient
+    float scale;
+    const float *dvals, *dloss;   // NULL: no such part
+    void *dscores;
+    int64_t ldg;
+};
+int launch_balance(const RouterLaunch &a, void *stream);
+int launch_route_grad(const RouterLaunch &a, void *stream);
+
+// ------------------------------------------------------------------------- cross entropy of a product
+
+constexpr int64_t kXentMaxColumns = (int64_t)1 << 22;      // 256 rows of 16-bit numbers are below 2^32 bytes
+constexpr int64_t kXentMaxRows = (int64_t)1 << 28, kXentMaxClasses = (int64_t)1 << 30;
+constexpr int64_t round_up(int64_t n, int64_t to) { return ceil_div(n, to) * to; }
+
+// A plan's workspace.  Rows that have a label ("kept") are numbered in their order; arrays by row are by that number.
+struct XentSpace {
+    int32_t *list, *pos;          // row of X of a kept row; number of a row or -1
+    int32_t *block_rows;          // kept rows of each block of kRowBlock rows
+    float *block_top;             // largest |dloss| there
+    int32_t *n;                   // kept rows
+    float *unit;                  // what sums of gradients are multiplied by at the end
+    int32_t *label;
+    float *lse, *g, *hit;         // log of the sum, gradient over the unit, logit of the label
+    float *top, *sum;             // running maximum and sum of exponentials
+    float *part_top, *part_sum;   // the same of blocks of classes, block after block
+    void *x, *w, *G;              // operands: planes of 16-bit numbers
+    float *dx, *dw;               // sums in 32 bits, one slab for each share of a contraction
+    int64_t ld;                   // row length of x and w: n_in rounded up to 256
+    int64_t x_plane;              // elements
+    int64_t part_cap, g_cap, w_cap, dx_cap, dw_cap;     // elements that there is room for (of a plane)
+};
+constexpr int kRowBlock = 4096;
+
+struct XentLaunch {
+    XentSpace s;
+    const void *X, *W;
+    int64_t ldx, ldw, lddx, lddw;
+    const int32_t *labels;
+    int32_t n_rows, n_classes, n_in, dtype;
+    float *loss, *lse;
+    const float *lse_in, *dloss;
+    void *dX, *dW;
+};
+int launch_xent(const XentLaunch &a, void *stream);
+int launch_xent_grad(const XentLaunch &a, void *stream);
+
+// Products of the cross entropy (tf_product.h): C = M N^T summed over K, tiles of C by workgroups.
+struct Side {
+    const void *p;                // 16-bit elements
+    int64_t ld, plane;            // elements: from row to row, from part to part
+    int64_t rows, cols;           // what there is of it (cols: a multiple of 8); further elements count as zeros
+};
+enum ProductEnd { kEndSums = 0, kEndGradient = 1, kEndSlab = 2, kEndOut = 3 };
+enum ProductTile { kTile256 = 0, kTile128 = 1, kTile64 = 2, kTile16 = 3 };
+struct ProductLaunch {
+    Side M, N;
+    int32_t parts;                // of a number: 1, or 3 whose six largest products are taken
+    int32_t k_steps;              // of 64
+    const int32_t *n;             // kept rows
+    int32_t k_rows;               // 1: K goes over kept rows
+    int32_t n_rows;               // 1: N does
+    int32_t m_tiles, n_tiles, splits;
+    ProductEnd end;
+    ProductTile tile;
+    int32_t m_count, n_count;     // rows of M and N that count
+    // ends
+    int32_t first_class;
+    const int32_t *label;
+    const float *lse, *g, *unit;
+    float *hit, *part_top, *part_sum;
+    int64_t part_ld;
+    void *G;
+    int64_t g_ld, g_plane;
+    float *slab;
+    int64_t slab_ld, slab_size;
+    int32_t add;                  // to what the slab holds
+    void *out;
+    int64_t ldo;
+    int32_t out_dtype;
+};
+int launch_product_bf16(const ProductLaunch &a, void *stream);
+int launch_product_f16(const ProductLaunch &a, void *stream);
+
+}  // namespace tf

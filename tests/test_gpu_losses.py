@@ -1,0 +1,562 @@
+"""The losses and their gradients against their definitions in 64 bits (bounds derived in loss_util.py)."""
+import math
+
+import pytest
+import torch
+
+import loss_util as lu
+import paper_2407_00243_amd as tf
+
+pytestmark = pytest.mark.gpu
+
+BF, HF, F = torch.bfloat16, torch.float16, torch.float32
+
+
+def stream():
+    return torch.cuda.current_stream().cuda_stream
+
+
+def gen(seed):
+    g = torch.Generator(device="cuda")
+    g.manual_seed(seed)
+    return g
+
+
+# ------------------------------------------------------------------------------------------ router
+
+def router_case(T, E, k, dtype, seed, masked=0.0, pad=0):
+    """Scores whose rows are E + pad apart (NaN in between), and a routing matrix of the k best."""
+    g = gen(seed)
+    wide = torch.full((T, E + pad), math.nan, device="cuda", dtype=dtype)
+    scores = wide[:, :E]
+    l = 2 * torch.randn(T, E, device="cuda", generator=g)
+    if masked:
+        l[torch.rand(T, E, device="cuda", generator=g) < masked] = -math.inf
+        l[torch.rand(T, device="cuda", generator=g) < 0.1] = -math.inf
+    scores.copy_(l)
+    top = scores.float().topk(k, 1)
+    c = torch.where(top.values > -math.inf, top.indices, -1).to(torch.int32).reshape(-1)
+    return scores, c
+
+
+def matrix(T, E, k, c):
+    return tf.DeviceCsr(T, E, torch.zeros(T + 1, dtype=torch.int32, device="cuda"), c, torch.zeros(T * k, device="cuda"))
+
+
+def run_balance(scores, A, scoring, work=None):
+    E = scores.shape[1]
+    counts = torch.full((E + 1,), -7, dtype=torch.int32, device="cuda")
+    mass, loss = torch.full((E,), math.nan, device="cuda"), torch.full((1,), math.nan, device="cuda")
+    if work is None:
+        work = torch.full((tf.tf_moe_balance_size(scores.shape[0], E),), 255, dtype=torch.uint8, device="cuda")
+    tf.tf_moe_balance(scores, A, counts, mass, loss, work, scoring, stream())
+    return counts, mass, loss
+
+
+def check_balance(scores, c, k, scoring, what=""):
+    T, E = scores.shape
+    counts, mass, loss = run_balance(scores, matrix(T, E, k, c), scoring)
+    rc, rm, bm, rl, bl = lu.balance(scores, c, k, scoring)
+    assert torch.equal(counts.double(), rc), what
+    lu.check(mass, rm, bm, what=f"{what} mass")
+    lu.check(loss, rl.reshape(1), bl.reshape(1), what=f"{what} loss")
+    return counts
+
+
+def check_grad(scores, c, k, scoring, dvals, counts, dloss, scale=1.5, dscores=None, what=""):
+    T, E = scores.shape
+    before = scores.clone()
+    if dscores is None:
+        dscores = torch.full((T, E), math.nan, device="cuda", dtype=scores.dtype)
+    tf.tf_moe_route_grad(scores, matrix(T, E, k, c), dscores, scoring, scale, dvals, counts, dloss, stream())
+    ref, bound = lu.route_grad(before, c, k, scoring, scale, dvals, counts, dloss)
+    lu.check(dscores, ref, bound, scores.dtype, what)
+
+
+@pytest.mark.parametrize("dtype", [F, BF, HF])
+@pytest.mark.parametrize("T,E,k", [(1, 1, 1), (1, 16, 2), (3, 3, 3), (7, 8, 2), (64, 9, 4), (65, 33, 5), (300, 60, 6), (129, 65, 64), (1000, 129, 8),
+                                   (257, 256, 8), (33, 257, 3), (70, 513, 8), (40, 1000, 7), (2, 1024, 64)])
+def test_router(T, E, k, dtype):
+    for scoring in range(4):
+        what = f"T{T} E{E} k{k} {dtype} scoring {scoring}"
+        print(what, flush=True)
+        scores, c = router_case(T, E, k, dtype, T + E + scoring, masked=0.25 * (scoring % 2), pad=(T + scoring) % 5)
+        counts = check_balance(scores, c, k, scoring, what)
+        dvals = torch.randn(T * k, device="cuda", generator=gen(k))
+        dloss = torch.full((1,), 0.3 * T, device="cuda")
+        check_grad(scores, c, k, scoring, dvals, None, None, what=what + " values")
+        check_grad(scores, c, k, scoring, None, counts, dloss, what=what + " balance")
+        check_grad(scores, c, k, scoring, dvals, counts, dloss, what=what + " both")
+
+
+@pytest.mark.parametrize("T", [0, 31, 32, 33, 511, 512, 513, 4095, 20001])
+def test_balance_over_many_rows(T):
+    """Around the numbers of rows at which one workgroup becomes many, whole rounds become parts of one."""
+    for E, dtype in ((16, F), (64, BF), (256, HF)):
+        scores, c = router_case(T, E, 2, dtype, T + E) if T else (torch.empty(0, E, device="cuda", dtype=dtype),
+                                                                  torch.empty(0, device="cuda", dtype=torch.int32))
+        if T == 0:
+            counts, mass, loss = run_balance(scores, matrix(0, E, 2, c), lu.SOFTMAX)
+            assert not counts.any() and not mass.any() and not loss.any()
+        else:
+            check_balance(scores, c, 2, lu.SOFTMAX, f"T{T} E{E}")
+
+
+def test_even_experts_have_loss_one():
+    T, E = 64, 8
+    scores = torch.zeros(T, E, device="cuda")
+    c = torch.arange(T * 2, device="cuda", dtype=torch.int32) % E
+    _, mass, loss = run_balance(scores, matrix(T, E, 2, c), lu.SOFTMAX)
+    assert abs(loss.item() - 1) < 1e-6 and (mass - 1 / E).abs().max().item() < 1e-7
+
+
+@pytest.mark.parametrize("scoring", range(4))
+def test_rows_without_entries(scoring):
+    """All rows closed; and closed rows among others, whose gradients are zeros."""
+    T, E, k = 37, 24, 3
+    scores = torch.full((T, E), -math.inf, device="cuda")
+    c = torch.full((T * k,), -1, dtype=torch.int32, device="cuda")
+    counts, mass, loss = run_balance(scores, matrix(T, E, k, c), scoring)
+    assert not counts.any() and not mass.any() and not loss.any()
+    out = torch.full((T, E), math.nan, device="cuda")
+    one = torch.ones(1, device="cuda")
+    tf.tf_moe_route_grad(scores, matrix(T, E, k, c), out, scoring, 1.0, torch.full((T * k,), math.nan, device="cuda"), counts, one, stream())
+    assert not out.any()
+    # finite scores, but no entry: no part in the balance either
+    scores, c = router_case(T, E, k, F, 5)
+    c.view(T, k)[::2] = -1
+    counts = check_balance(scores, c, k, scoring)
+    check_grad(scores, c, k, scoring, torch.randn(T * k, device="cuda"), counts, one)
+
+
+@pytest.mark.parametrize("scoring", range(4))
+def test_entries_that_are_passed_over(scoring):
+    """Columns that are no expert's, with NaN and infinite gradients; experts named twice or three times; NaN scores."""
+    T, E, k = 50, 20, 6
+    scores, c = router_case(T, E, k, F, 11)
+    c = c.view(T, k)
+    c[:, 1] = c[:, 0]
+    c[::3, 2] = c[::3, 0]
+    c[:, 4] = torch.tensor([-1, E, 2 ** 31 - 1, -2 ** 31, E + 7], device="cuda", dtype=torch.int32).repeat(10)
+    dvals = torch.randn(T, k, device="cuda", generator=gen(3))
+    dvals[:, 4] = math.nan
+    dvals[::2, 4] = math.inf
+    free = torch.ones(T, E, device="cuda", dtype=torch.bool)
+    free.scatter_(1, torch.where((c >= 0) & (c < E), c, 0).long(), False)
+    scores[free & (torch.rand(T, E, device="cuda", generator=gen(4)) < 0.2)] = math.nan
+    c = c.reshape(-1).contiguous()
+    counts = check_balance(scores, c, k, scoring)
+    ref_vals = torch.where(torch.isfinite(dvals), dvals, 0.0).reshape(-1)
+    out = torch.empty(T, E, device="cuda")
+    tf.tf_moe_route_grad(scores, matrix(T, E, k, c), out, scoring, 2.0, dvals.reshape(-1), counts, torch.ones(1, device="cuda"), stream())
+    ref, bound = lu.route_grad(scores, c, k, scoring, 2.0, ref_vals, counts, torch.ones(1))
+    lu.check(out, ref, bound)
+
+
+@pytest.mark.parametrize("scoring", range(4))
+def test_selected_far_below_the_largest(scoring):
+    """A bias may select experts whose scores are far below the others'; and all scores may be far below zero."""
+    T, E, k = 20, 40, 4
+    for low, shift in ((-150.0, 0.0), (0.0, -120.0), (-300.0, -90.0), (0.0, 95.0)):
+        l = torch.randn(T, E, device="cuda", generator=gen(1))
+        c = torch.stack([torch.randperm(E, device="cuda", generator=gen(t))[:k] for t in range(T)]).to(torch.int32)
+        l.scatter_add_(1, c.long(), torch.full((T, k), low, device="cuda"))
+        l += shift
+        counts = check_balance(l, c.reshape(-1), k, scoring)
+        check_grad(l, c.reshape(-1), k, scoring, torch.randn(T * k, device="cuda", generator=gen(2)), counts, torch.ones(1, device="cuda"))
+
+
+def test_a_row_of_infinity_stays_a_row():
+    T, E, k = 30, 16, 2
+    scores, c = router_case(T, E, k, BF, 2)
+    scores[7, 3] = math.inf
+    counts = run_balance(scores, matrix(T, E, k, c), lu.SOFTMAX)[0]
+    out = torch.empty_like(scores)
+    tf.tf_moe_route_grad(scores, matrix(T, E, k, c), out, lu.SOFTMAX_TOP, 1.0, torch.ones(T * k, device="cuda"), counts,
+                         torch.ones(1, device="cuda"), stream())
+    rest = torch.arange(T, device="cuda") != 7
+    assert torch.isfinite(out[rest]).all()
+
+
+def test_gradient_in_place_and_strided():
+    for E, pad in ((64, 0), (60, 4), (61, 3)):
+        scores, c = router_case(99, E, 3, BF, E, pad=pad)
+        dvals = torch.randn(99 * 3, device="cuda", generator=gen(1))
+        check_grad(scores, c, 3, lu.SOFTMAX, dvals, None, None, dscores=scores, what=f"in place {E}")
+        scores, c = router_case(99, E, 3, BF, E, pad=pad)
+        wide = torch.full((99, E + 5), 3.0, device="cuda", dtype=BF)
+        check_grad(scores, c, 3, lu.SOFTMAX, dvals, None, None, dscores=wide[:, 2:2 + E], what=f"strided {E}")
+        assert (wide[:, :2] == 3).all() and (wide[:, 2 + E:] == 3).all()
+
+
+@pytest.mark.parametrize("scoring", range(4))
+def test_router_gradient_against_differences(scoring):
+    """Through the router itself: differences of its weights' and the balance's sums over two steps of one score."""
+    T, E, k, h = 3, 6, 2, 2.0 ** -7
+    scores, _ = router_case(T, E, k, F, 21)
+    w = torch.randn(T * k, device="cuda", generator=gen(5))
+    A = matrix(T, E, k, torch.empty(T * k, dtype=torch.int32, device="cuda"))
+    tf.tf_moe_route(scores, A, scoring, scale=1.5, stream=stream())
+    columns = A.colidx.clone()
+    counts, mass, loss = run_balance(scores, A, scoring)
+    grad = torch.empty_like(scores)
+    tf.tf_moe_route_grad(scores, A, grad, scoring, 1.5, w, counts, torch.ones(1, device="cuda"), stream())
+
+    def value(l):
+        """In 64 bits: the weights' sum with the columns held, and the balance loss with the counts held."""
+        l = l.double()
+        col = columns.long().reshape(T, k)
+        z = torch.sigmoid(l) if scoring >= 2 else torch.exp(l)
+        p = z / z.sum(1, keepdim=True)
+        chosen = torch.gather(z, 1, col)
+        weights = {0: torch.gather(p, 1, col), 1: chosen / chosen.sum(1, keepdim=True), 2: chosen,
+                   3: chosen / chosen.sum(1, keepdim=True)}[scoring]
+        f = counts[:E].double() / counts[:E].sum()
+        return (1.5 * weights.reshape(-1) * w.double()).sum() + E * (f * p.mean(0)).sum()
+
+    got_vals = 1.5 * 0 + A.vals.double()
+    assert torch.isfinite(got_vals).all()
+    for t in range(T):
+        for e in range(E):
+            up, down = scores.clone().double(), scores.clone().double()
+            up[t, e] += h
+            down[t, e] -= h
+            slope = ((value(up) - value(down)) / (2 * h)).item()
+            # third derivatives of shares are below 1, weights below 4: h^2 / 6 of that, and the gradient's own rounding
+            assert abs(slope - grad[t, e].item()) <= 8 * h * h / 6 + 1e-5 * (1 + abs(slope))
+
+
+# ----------------------------------------------------------------------------------- cross entropy
+
+def xent_case(T, V, d, dtype, seed, unlabelled=0.2, ldx=0, ldw=0, offset=0):
+    """X and W with rows further apart than they are wide (NaN in between) and beginning at any element."""
+    g = gen(seed)
+
+    def put(rows, ld, values):
+        flat = torch.full((rows * (d + ld) + offset,), math.nan, device="cuda", dtype=dtype)
+        m = flat[offset:].view(rows, d + ld)[:, :d]
+        m.copy_(values)
+        return m
+
+    W = put(V, ldw, 3 / math.sqrt(d) * torch.randn(V, d, device="cuda", generator=g))
+    labels = torch.randint(0, V, (T,), device="cuda", generator=g).to(torch.int32)
+    X = put(T, ldx, torch.randn(T, d, device="cuda", generator=g) + W.float()[labels.long()] * 1.3 * torch.rand(T, 1, device="cuda", generator=g))
+    labels[torch.rand(T, device="cuda", generator=g) < unlabelled] = -1
+    dloss = torch.randn(T, device="cuda", generator=g) / max(T, 1)
+    return X, W, labels, dloss
+
+
+def check_xent(X, W, labels, dloss, plan=None, grads="XW", what=""):
+    T, V = X.shape[0], W.shape[0]
+    own = plan is None
+    if own:
+        plan = tf.XentPlan(V, X.shape[1], X.dtype, max_rows=max(T, 1))
+    loss, lse = torch.full((T,), math.nan, device="cuda"), torch.full((T,), math.nan, device="cuda")
+    dX = torch.full((T, X.shape[1]), math.nan, device="cuda", dtype=X.dtype) if "X" in grads else None
+    dW = torch.full((V, X.shape[1]), math.nan, device="cuda", dtype=X.dtype) if "W" in grads else None
+    plan.loss(X, W, labels, loss, lse, stream())
+    plan.grad(X, W, labels, lse, dloss, dX, dW, stream())
+    ref = lu.xent(X, W, labels, dloss)
+    for name, got in (("loss", loss), ("lse", lse), ("dX", dX), ("dW", dW)):
+        if got is not None:
+            lu.check(got, *ref[name], got.dtype, f"{what} {name}")
+    if own:
+        torch.cuda.synchronize()
+        plan.close()
+
+
+@pytest.mark.parametrize("dtype", [BF, HF, F])
+@pytest.mark.parametrize("T,V,d", [(1, 1, 1), (1, 2, 3), (2, 300, 8), (5, 7, 16), (16, 64, 64), (17, 129, 72), (64, 257, 65), (65, 256, 128),
+                                   (130, 1000, 96), (300, 513, 257), (128, 128, 1000), (257, 2049, 200), (5, 30000, 48), (1, 9000, 520),
+                                   (700, 31, 40), (9000, 47, 24)])
+def test_xent(T, V, d, dtype):
+    what = f"T{T} V{V} d{d} {dtype}"
+    print(what, flush=True)
+    X, W, labels, dloss = xent_case(T, V, d, dtype, T + V + d)
+    if T <= 2:
+        labels[0] = V - 1
+    check_xent(X, W, labels, dloss, what=what)
+
+
+@pytest.mark.parametrize("dtype", [BF, HF, F])
+@pytest.mark.parametrize("T,V,d", [(3500, 3600, 72), (40, 3600, 3500), (3600, 70, 3500)])
+def test_xent_large_tiles(T, V, d, dtype):
+    """Enough tiles of 256 x 256 for the logits, for dW and for dX."""
+    print(f"T{T} V{V} d{d} {dtype}", flush=True)
+    check_xent(*xent_case(T, V, d, dtype, 1), what=f"T{T} V{V} d{d} {dtype}")
+
+
+@pytest.mark.parametrize("dtype,d", [(BF, 8), (F, 7)])
+def test_xent_in_pieces(dtype, d):
+    """So many rows that three pieces of the classes are taken one after the other (in fp32 the loss's too)."""
+    X, W, labels, dloss = xent_case(600000, 700, d, dtype, 3, unlabelled=0.5)
+    check_xent(X, W, labels, dloss, what=f"pieces {dtype}")
+
+
+@pytest.mark.parametrize("dtype", [BF, HF, F])
+def test_xent_strides_and_alignment(dtype):
+    """Rows further apart than they are wide, beginning at any element; NaN between them is not read."""
+    for ldx, ldw, offset, d in ((3, 0, 0, 40), (0, 8, 0, 40), (0, 16, 8, 64), (5, 7, 1, 33), (8, 8, 4, 64), (1, 1, 3, 64)):
+        print(dtype, ldx, ldw, offset, d, flush=True)
+        check_xent(*xent_case(70, 300, d, dtype, d + ldx, ldx=ldx, ldw=ldw, offset=offset), what=f"{ldx} {ldw} {offset}")
+        check_xent(*xent_case(9, 300, d, dtype, d + ldx, ldx=ldx, ldw=ldw, offset=offset), what=f"few rows {ldx} {ldw} {offset}")
+
+
+@pytest.mark.parametrize("dtype", [BF, F])
+def test_xent_outputs_strided(dtype):
+    T, V, d = 40, 150, 36
+    X, W, labels, dloss = xent_case(T, V, d, dtype, 8)
+    plan = tf.XentPlan(V, d, dtype, max_rows=64)
+    loss, lse = torch.empty(T, device="cuda"), torch.empty(T, device="cuda")
+    plan.loss(X, W, labels, loss, lse, stream())
+    wx, ww = torch.full((T, d + 7), 5.0, device="cuda", dtype=dtype), torch.full((V + 1, d + 3), 5.0, device="cuda", dtype=dtype)
+    plan.grad(X, W, labels, lse, dloss, wx[:, 3:3 + d], ww[:V, 1:1 + d], stream())
+    ref = lu.xent(X, W, labels, dloss)
+    lu.check(wx[:, 3:3 + d], *ref["dX"], dtype)
+    lu.check(ww[:V, 1:1 + d], *ref["dW"], dtype)
+    assert (wx[:, :3] == 5).all() and (wx[:, 3 + d:] == 5).all()
+    assert (ww[:, :1] == 5).all() and (ww[:, 1 + d:] == 5).all() and (ww[V] == 5).all()
+    torch.cuda.synchronize()
+
+
+@pytest.mark.parametrize("dtype", [BF, HF, F])
+def test_rows_without_a_label_are_not_read(dtype):
+    """Labels outside of the classes: -1, -100, the number of classes, the largest; NaN in those rows, their lse and gradients."""
+    T, V, d = 90, 200, 48
+    X, W, labels, dloss = xent_case(T, V, d, dtype, 4, unlabelled=0.0)
+    labels[::4] = torch.tensor([-1, -100, V, 2 ** 31 - 1, -2 ** 31], device="cuda", dtype=torch.int32).repeat(5)[:23]
+    X[::4] = math.nan
+    dloss[::4] = math.nan
+    X[1::4] = X[1::4]
+    plan = tf.XentPlan(V, d, dtype, max_rows=T)
+    loss, lse = torch.full((T,), math.nan, device="cuda"), torch.full((T,), math.nan, device="cuda")
+    plan.loss(X, W, labels, loss, lse, stream())
+    ref = lu.xent(X, W, labels, dloss)
+    lu.check(loss, *ref["loss"])
+    lse[::4] = math.nan
+    dX, dW = torch.full_like(X, math.nan), torch.full_like(W, math.nan)
+    plan.grad(X, W, labels, lse, dloss, dX, dW, stream())
+    lu.check(dX, *ref["dX"], dtype)
+    lu.check(dW, *ref["dW"], dtype)
+    # no row has a label, and no row at all
+    none = torch.full_like(labels, -1)
+    plan.loss(X, W, none, loss, lse, stream())
+    assert not loss.any() and not lse.any()
+    plan.grad(X, W, none, lse, dloss, dX, dW, stream())
+    assert not dX.any() and not dW.any()
+    dW.fill_(math.nan)
+    e = torch.empty(0, device="cuda")
+    plan.grad(X[:0], W, none[:0], e, e, X[:0], dW, stream())
+    assert not dW.any()
+    torch.cuda.synchronize()
+
+
+@pytest.mark.parametrize("dtype", [BF, HF, F])
+def test_one_gradient_alone_and_fewer_rows(dtype):
+    V, d = 400, 96
+    plan = tf.XentPlan(V, d, dtype, max_rows=500)
+    for T, grads in ((500, "X"), (1, "W"), (77, "XW"), (499, "W"), (20, "X")):
+        check_xent(*xent_case(T, V, d, dtype, T), plan=plan, grads=grads, what=f"T{T} {grads}")
+    torch.cuda.synchronize()
+
+
+@pytest.mark.parametrize("dtype", [BF, HF, F])
+def test_gradients_of_very_different_rows(dtype):
+    """dloss from 1e-20 to 1e4, some zero: each row of dX keeps its precision where the type can hold it."""
+    T, V, d = 60, 150, 64
+    X, W, labels, _ = xent_case(T, V, d, dtype, 6, unlabelled=0.0)
+    lo = -4 if dtype == HF else -20
+    dloss = 10.0 ** torch.linspace(lo, 2 if dtype == HF else 4, T, device="cuda")
+    dloss[::7] = 0.0
+    check_xent(X, W, labels, dloss)
+    check_xent(X, W, labels, torch.zeros(T, device="cuda"))
+
+
+@pytest.mark.parametrize("dtype", [BF, F])
+def test_large_and_certain_logits(dtype):
+    """Logits of thousands; rows whose loss is very small keep its relative precision."""
+    T, V, d = 33, 90, 32
+    X, W, labels, dloss = xent_case(T, V, d, dtype, 9, unlabelled=0.0)
+    check_xent(X * 300, W, labels, dloss, what="large")
+    X = (W[labels.long()].float() * torch.linspace(0.5, 8, T, device="cuda")[:, None]).to(dtype)
+    check_xent(X, W, labels, dloss, what="certain")
+
+
+def test_a_row_of_nan_stays_a_row():
+    T, V, d = 40, 100, 64
+    X, W, labels, dloss = xent_case(T, V, d, BF, 2, unlabelled=0.0)
+    ref = lu.xent(X, W, labels, dloss)
+    X[11, 5], X[12, 6] = math.nan, math.inf
+    plan = tf.XentPlan(V, d, BF, max_rows=T)
+    loss, lse, dX = torch.empty(T, device="cuda"), torch.empty(T, device="cuda"), torch.empty_like(X)
+    plan.loss(X, W, labels, loss, lse, stream())
+    plan.grad(X, W, labels, lse, dloss, dX, None, stream())
+    rest = torch.ones(T, dtype=torch.bool, device="cuda")
+    rest[11:13] = False
+    lu.check(loss[rest], ref["loss"][0][rest], ref["loss"][1][rest])
+    lu.check(dX[rest], ref["dX"][0][rest], ref["dX"][1][rest], BF)
+    assert torch.isnan(loss[11]) and not torch.isfinite(loss[12]) and torch.isnan(dX[11]).all()
+    # a gradient of NaN or infinity likewise
+    X, W, labels, dloss = xent_case(T, V, d, BF, 2, unlabelled=0.0)
+    dloss[3], dloss[4] = math.nan, math.inf
+    plan.loss(X, W, labels, loss, lse, stream())
+    plan.grad(X, W, labels, lse, dloss, dX, None, stream())
+    rest[:] = True
+    rest[3:5] = False
+    lu.check(dX[rest], ref["dX"][0][rest], ref["dX"][1][rest], BF)
+    assert torch.isnan(dX[3]).all() and not torch.isfinite(dX[4]).any()
+    torch.cuda.synchronize()
+
+
+def test_gradient_against_differences():
+    """fp32: dX and dW against differences of the loss in 64 bits."""
+    T, V, d, h = 4, 9, 5, 2.0 ** -10
+    X, W, labels, _ = xent_case(T, V, d, F, 3, unlabelled=0.0)
+    labels[1] = -1
+    dloss = torch.randn(T, device="cuda", generator=gen(3))
+    plan = tf.XentPlan(V, d, F, max_rows=T)
+    loss, lse, dX, dW = torch.empty(T, device="cuda"), torch.empty(T, device="cuda"), torch.empty_like(X), torch.empty_like(W)
+    plan.loss(X, W, labels, loss, lse, stream())
+    plan.grad(X, W, labels, lse, dloss, dX, dW, stream())
+
+    def value(x, w):
+        l = x @ w.t()
+        each = torch.logsumexp(l, 1) - l.gather(1, labels.clamp_min(0).long()[:, None]).squeeze(1)
+        return (each * dloss.double() * (labels >= 0)).sum().item()
+
+    for M, G, other in ((X, dX, 0), (W, dW, 1)):
+        for i in range(M.shape[0]):
+            for j in range(M.shape[1]):
+                up, down = M.double().clone(), M.double().clone()
+                up[i, j] += h
+                down[i, j] -= h
+                pair = [(m, W.double()) if other == 0 else (X.double(), m) for m in (up, down)]
+                slope = (value(*pair[0]) - value(*pair[1])) / (2 * h)
+                # third derivatives of a row's loss are below the cube of the largest weight (6): h^2 / 6 times that and the sum of |dloss|
+                assert abs(slope - G[i, j].item()) <= 216 * h * h / 6 * dloss.abs().sum().item() + 1e-5 * (1 + abs(slope))
+    torch.cuda.synchronize()
+
+
+# -------------------------------------------------------------------------- streams, graphs, together
+
+def test_same_results_every_time():
+    """Bit by bit, whatever ran before on the plan; split contractions among them."""
+    X, W, labels, dloss = xent_case(33, 20000, 72, BF, 1)
+    plan = tf.XentPlan(20000, 72, BF, max_rows=40)
+    scores, c = router_case(20001, 64, 4, BF, 1)
+    runs = []
+    for _ in range(3):
+        loss, lse, dX, dW = torch.empty(33, device="cuda"), torch.empty(33, device="cuda"), torch.empty_like(X), torch.empty_like(W)
+        plan.loss(X, W, labels, loss, lse, stream())
+        plan.grad(X, W, labels, lse, dloss, dX, dW, stream())
+        runs.append((loss, lse, dX, dW, *run_balance(scores, matrix(20001, 64, 4, c), lu.SIGMOID)))
+        check_xent(*xent_case(7, 20000, 72, BF, 2), plan=plan)
+    for other in runs[1:]:
+        assert all(torch.equal(a, b) for a, b in zip(runs[0], other))
+    torch.cuda.synchronize()
+
+
+def test_two_plans_on_two_streams():
+    cases = [xent_case(200, 900, 64, BF, s) for s in (1, 2)]
+    plans = [tf.XentPlan(900, 64, BF, max_rows=200) for _ in cases]
+    streams = [torch.cuda.Stream() for _ in cases]
+    outs = []
+    for _ in range(5):
+        for s in streams:
+            s.wait_stream(torch.cuda.current_stream())
+        outs = []
+        for (X, W, labels, dloss), plan, s in zip(cases, plans, streams):
+            with torch.cuda.stream(s):
+                o = torch.empty(200, device="cuda"), torch.empty(200, device="cuda"), torch.empty_like(X), torch.empty_like(W)
+                plan.loss(X, W, labels, o[0], o[1], s.cuda_stream)
+                plan.grad(X, W, labels, o[1], dloss, o[2], o[3], s.cuda_stream)
+                outs.append(o)
+        torch.cuda.synchronize()
+    for (X, W, labels, dloss), o in zip(cases, outs):
+        ref = lu.xent(X, W, labels, dloss)
+        for name, got in zip(("loss", "lse", "dX", "dW"), o):
+            lu.check(got, *ref[name], got.dtype, name)
+
+
+def test_one_training_step_in_a_graph():
+    """Router, balance, loss and all gradients in one graph, replayed with other inputs, against the same calls without it."""
+    T, E, k, V, d = 96, 16, 2, 500, 64
+    Xs = [xent_case(T, V, d, BF, s) for s in range(3)]
+    Ls = [router_case(T, E, k, BF, s)[0] for s in range(3)]
+    X, W, labels, dloss = (t.clone() for t in Xs[0])
+    scores = Ls[0].clone()
+    A = matrix(T, E, k, torch.zeros(T * k, dtype=torch.int32, device="cuda"))
+    plan = tf.XentPlan(V, d, BF, max_rows=T)
+    counts, mass, bal = torch.empty(E + 1, dtype=torch.int32, device="cuda"), torch.empty(E, device="cuda"), torch.empty(1, device="cuda")
+    work = torch.empty(tf.tf_moe_balance_size(T, E), dtype=torch.uint8, device="cuda")
+    loss, lse, dX, dW, dl = (torch.empty(T, device="cuda"), torch.empty(T, device="cuda"), torch.empty_like(X), torch.empty_like(W),
+                             torch.empty_like(scores))
+    dvals, one = torch.randn(T * k, device="cuda"), torch.ones(1, device="cuda")
+
+    def step(s):
+        tf.tf_moe_route(scores, A, lu.SOFTMAX_TOP, stream=s)
+        tf.tf_moe_balance(scores, A, counts, mass, bal, work, lu.SOFTMAX_TOP, s)
+        plan.loss(X, W, labels, loss, lse, s)
+        plan.grad(X, W, labels, lse, dloss, dX, dW, s)
+        tf.tf_moe_route_grad(scores, A, dl, lu.SOFTMAX_TOP, 1.0, dvals, counts, one, s)
+
+    outs = (counts, mass, bal, loss, lse, dX, dW, dl)
+    want = []
+    for i in range(3):
+        for to, frm in zip((X, W, labels, dloss, scores), (*Xs[i], Ls[i])):
+            to.copy_(frm)
+        step(stream())
+        want.append([o.clone() for o in outs])
+    graph = torch.cuda.CUDAGraph()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        with torch.cuda.graph(graph, stream=side):
+            step(side.cuda_stream)
+    for i in (1, 0, 2, 2, 1):
+        for to, frm in zip((X, W, labels, dloss, scores), (*Xs[i], Ls[i])):
+            to.copy_(frm)
+        for o in outs:
+            o.fill_(-3)
+        graph.replay()
+        torch.cuda.synchronize()
+        for got, ref in zip(outs, want[i]):
+            assert torch.equal(got, ref)
+
+
+def test_refusals_of_the_binding():
+    T, V, d = 8, 20, 16
+    X, W, labels, dloss = xent_case(T, V, d, BF, 1)
+    plan = tf.XentPlan(V, d, BF, max_rows=T, gradients=False)
+    loss, lse = torch.empty(T, device="cuda"), torch.empty(T, device="cuda")
+    plan.loss(X, W, labels, loss, lse, stream())
+    with pytest.raises(tf.TfError) as e:
+        plan.grad(X, W, labels, lse, dloss, torch.empty_like(X), None, stream())
+    assert e.value.status_name == "TF_EMISMATCH"
+    big = xent_case(T + 1, V, d, BF, 1)
+    with pytest.raises(tf.TfError) as e:
+        plan.loss(big[0], W, big[2], torch.empty(T + 1, device="cuda"), torch.empty(T + 1, device="cuda"), stream())
+    assert e.value.status_name == "TF_EMISMATCH"
+    for bad in (dict(X=X.float()), dict(W=W[:, :8]), dict(W=W[:-1]), dict(X=X.cpu()), dict(labels=labels.long()), dict(labels=labels[:-1]),
+                dict(loss=loss.double()), dict(lse=lse[::2]), dict(X=X.t())):
+        a = dict(X=X, W=W, labels=labels, loss=loss, lse=lse)
+        a.update(bad)
+        with pytest.raises((TypeError, ValueError)):
+            plan.loss(**a, stream=stream())
+    scores, c = router_case(6, 8, 2, F, 1)
+    A = matrix(6, 8, 2, c)
+    counts, mass, bal = torch.empty(9, dtype=torch.int32, device="cuda"), torch.empty(8, device="cuda"), torch.empty(1, device="cuda")
+    work = torch.empty(tf.tf_moe_balance_size(6, 8), dtype=torch.uint8, device="cuda")
+    for bad in (dict(counts=counts[:8]), dict(counts=counts.float()), dict(mass=mass.cpu()), dict(workspace=work[:-1]), dict(scores=scores[:5]),
+                dict(scores=scores.t())):
+        a = dict(scores=scores, A=A, counts=counts, mass=mass, loss=bal, workspace=work)
+        a.update(bad)
+        with pytest.raises((TypeError, ValueError)):
+            tf.tf_moe_balance(**a, stream=stream())
+    for bad in (dict(dscores=torch.empty(6, 8, device="cuda", dtype=BF)), dict(dscores=torch.empty(5, 8, device="cuda")),
+                dict(dvals=torch.empty(11, device="cuda")), dict(dvals=torch.empty(12, device="cuda", dtype=BF))):
+        a = dict(scores=scores, A=A, dscores=torch.empty_like(scores), dvals=torch.zeros(12, device="cuda"))
+        a.update(bad)
+        with pytest.raises((TypeError, ValueError)):
+            tf.tf_moe_route_grad(**a, stream=stream())
+    torch.cuda.synchronize()

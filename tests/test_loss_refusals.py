@@ -1,0 +1,113 @@
+"""What the losses and their gradients refuse, on the host: nothing here launches a kernel."""
+import ctypes
+
+import numpy as np
+import pytest
+import torch
+
+import paper_2407_00243_amd as tf
+from paper_2407_00243_amd import binding
+
+P = 4096          # an aligned address that nothing reads
+
+
+def csr(**over):
+    f = dict(n_rows=4, n_cols=8, nnz=8, rowptr=P, colidx=P, vals=P, dtype=tf.TF_F32, on_device=1)
+    f.update(over)
+    return binding.tf_csr(f["n_rows"], f["n_cols"], f["nnz"], f["rowptr"], f["colidx"], f["vals"], f["dtype"],
+                          f["on_device"])
+
+
+def status(code):
+    return binding._STATUS[code]
+
+
+def test_struct_layout():
+    assert ctypes.sizeof(binding.tf_xent_desc) == 3 * 8 + 2 * 4
+
+
+ROUTER = [
+    (dict(on_device=0), {}, "TF_EINVAL"), (dict(nnz=7), {}, "TF_EINVAL"), (dict(nnz=0), {}, "TF_EINVAL"),
+    (dict(n_cols=2000), dict(ld=2000), "TF_EUNSUPPORTED"), (dict(nnz=4 * 65, n_cols=100), dict(ld=100), "TF_EUNSUPPORTED"),
+    (dict(colidx=None), {}, "TF_EINVAL"), (dict(colidx=P + 2), {}, "TF_EINVAL"), (dict(n_rows=-1), {}, "TF_EINVAL"),
+    (dict(n_cols=0), {}, "TF_EINVAL"), ({}, dict(scores=None), "TF_EINVAL"), ({}, dict(scores=P + 2), "TF_EINVAL"),
+    ({}, dict(ld=7), "TF_EINVAL"), ({}, dict(dtype=tf.TF_F64), "TF_EUNSUPPORTED"), ({}, dict(scoring=4), "TF_EINVAL"),
+    ({}, dict(scoring=-1), "TF_EINVAL"),
+]
+
+
+@pytest.mark.parametrize("over,args,want", ROUTER + [
+    ({}, dict(counts=None), "TF_EINVAL"), ({}, dict(mass=None), "TF_EINVAL"), ({}, dict(loss=None), "TF_EINVAL"),
+    ({}, dict(workspace=None), "TF_EINVAL"), ({}, dict(mass=P + 1), "TF_EINVAL"), ({}, dict(workspace=P + 2), "TF_EINVAL"),
+])
+def test_balance_refuses(over, args, want):
+    a = dict(scores=P, ld=8, dtype=tf.TF_F32, scoring=0, counts=P, mass=P, loss=P, workspace=P)
+    a.update(args)
+    st = tf.load_library().tf_moe_balance(a["scores"], a["ld"], a["dtype"], a["scoring"], ctypes.byref(csr(**over)), a["counts"],
+                                          a["mass"], a["loss"], a["workspace"], None)
+    assert status(st) == want and tf.tf_last_error()
+
+
+@pytest.mark.parametrize("over,args,want", ROUTER + [
+    ({}, dict(dvals=None, counts=None, dloss=None), "TF_EINVAL"), ({}, dict(counts=None), "TF_EINVAL"),
+    ({}, dict(dloss=None), "TF_EINVAL"), ({}, dict(dscores=None), "TF_EINVAL"), ({}, dict(ldd=7), "TF_EINVAL"),
+    ({}, dict(dscores=P + 2), "TF_EINVAL"), ({}, dict(dvals=P + 2), "TF_EINVAL"), ({}, dict(dloss=P + 1), "TF_EINVAL"),
+])
+def test_route_grad_refuses(over, args, want):
+    a = dict(scores=P, ld=8, dtype=tf.TF_F32, scoring=0, dvals=P, counts=P, dloss=P, dscores=P, ldd=8)
+    a.update(args)
+    st = tf.load_library().tf_moe_route_grad(a["scores"], a["ld"], a["dtype"], a["scoring"], 1.0, ctypes.byref(csr(**over)), a["dvals"],
+                                             a["counts"], a["dloss"], a["dscores"], a["ldd"], None)
+    assert status(st) == want and tf.tf_last_error()
+
+
+def test_balance_size():
+    assert 0 < tf.tf_moe_balance_size(1, 1) <= tf.tf_moe_balance_size(1 << 20, 1024) <= 4 << 20
+    for tokens, experts, want in ((-1, 8, "TF_EINVAL"), (8, 0, "TF_EINVAL"), (8, 1025, "TF_EUNSUPPORTED")):
+        with pytest.raises(tf.TfError) as e:
+            tf.tf_moe_balance_size(tokens, experts)
+        assert e.value.status_name == want
+
+
+@pytest.mark.parametrize("over,want", [
+    (dict(n_classes=0), "TF_EINVAL"), (dict(n_in=0), "TF_EINVAL"), (dict(max_rows=0), "TF_EINVAL"),
+    (dict(n_classes=(1 << 30) + 1), "TF_EUNSUPPORTED"), (dict(n_in=(1 << 22) + 1), "TF_EUNSUPPORTED"),
+    (dict(max_rows=(1 << 28) + 1), "TF_EUNSUPPORTED"), (dict(dtype=tf.TF_F64), "TF_EUNSUPPORTED"), (dict(gradients=2), "TF_EINVAL"),
+])
+def test_xent_create_refuses(over, want):
+    f = dict(n_classes=8, n_in=8, max_rows=8, dtype=tf.TF_BF16, gradients=1)
+    f.update(over)
+    d = binding.tf_xent_desc(*f.values())
+    out = ctypes.c_void_p(7)
+    assert status(tf.load_library().tf_xent_create(ctypes.byref(d), ctypes.byref(out))) == want
+    assert out.value is None and tf.tf_last_error()
+
+
+def test_null_plans():
+    lib = tf.load_library()
+    assert status(lib.tf_xent_create(None, ctypes.byref(ctypes.c_void_p()))) == "TF_EINVAL"
+    assert status(lib.tf_xent_create(ctypes.byref(binding.tf_xent_desc(8, 8, 8, 0, 1)), None)) == "TF_EINVAL"
+    assert lib.tf_xent_destroy(None) == 0
+    assert status(lib.tf_xent_loss(None, P, 8, P, 8, P, 4, P, P, None)) == "TF_EINVAL"
+    assert status(lib.tf_xent_grad(None, P, 8, P, 8, P, P, P, 4, P, 8, P, 8, None)) == "TF_EINVAL"
+    assert status(lib.tf_xent_device(None, ctypes.byref(ctypes.c_int32()))) == "TF_EINVAL"
+
+
+def test_host_arrays_are_refused():
+    """Addresses of host memory never reach a kernel."""
+    t, e, k = 4, 8, 2
+    A = tf.DeviceCsr(t, e, torch.zeros(t + 1, dtype=torch.int32), torch.zeros(t * k, dtype=torch.int32), torch.zeros(t * k))
+    scores = torch.zeros(t, e)
+    counts, mass, loss = torch.zeros(e + 1, dtype=torch.int32), torch.zeros(e), torch.zeros(1)
+    work = torch.zeros(tf.tf_moe_balance_size(t, e), dtype=torch.uint8)
+    with pytest.raises(ValueError):
+        tf.tf_moe_balance(scores, A, counts, mass, loss, work)
+    with pytest.raises(ValueError):
+        tf.tf_moe_route_grad(scores, A, torch.zeros(t, e), dvals=torch.zeros(t * k))
+    X, W, y = torch.zeros(t, 8), torch.zeros(5, 8), torch.zeros(t, dtype=torch.int32)
+    with pytest.raises(ValueError):
+        tf.tf_xent_loss(1, X, W, y, torch.zeros(t), torch.zeros(t))
+    with pytest.raises(ValueError):
+        tf.tf_xent_grad(1, X, W, y, torch.zeros(t), torch.zeros(t), X, W)
+    with pytest.raises((TypeError, ValueError, AttributeError)):
+        tf.tf_xent_loss(1, np.zeros((4, 8), np.float32), W, y, torch.zeros(t), torch.zeros(t))
