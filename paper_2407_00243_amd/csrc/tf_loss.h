@@ -48,11 +48,13 @@ struct XentSpace {
     float *part_top, *part_sum;   // the same of blocks of classes, block after block
     void *x, *w, *G;              // operands: planes of 16-bit numbers
     float *dx, *dw;               // sums in 32 bits, one slab for each share of a contraction
-    int64_t ld;                   // row length of x and w: n_in rounded up to 256
+    int64_t ld;                   // row length of x and w: n_in rounded up to 256, and kRowPad
     int64_t x_plane;              // elements
     int64_t part_cap, g_cap, w_cap, dx_cap, dw_cap;     // elements that there is room for (of a plane)
 };
 constexpr int kRowBlock = 4096;
+// Elements between the rows of x, w and G: rows a power of two apart would all lie in one channel of an XCD's L2.
+constexpr int64_t kRowPad = 64;
 
 struct XentLaunch {
     XentSpace s;

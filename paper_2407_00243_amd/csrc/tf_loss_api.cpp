@@ -82,12 +82,12 @@ int64_t lay_out(tf_xent &p, char *base) {
     tf::XentSpace &s = p.s;
     const int64_t rows = round_up(d.max_rows, 256), classes = round_up(d.n_classes, 256), blocks = ceil_div(d.max_rows, tf::kRowBlock);
     const int64_t planes = d.dtype == TF_F32 ? 3 : 1;
-    s.ld = round_up(d.n_in, 256);
+    s.ld = round_up(d.n_in, 256) + tf::kRowPad;
     s.x_plane = rows * s.ld;
     s.part_cap = std::max(std::min(classes / 128 * std::max(2 * rows, (int64_t)4 * 256), (int64_t)1 << 25), std::max(4 * rows, (int64_t)8 * 256));
     const int64_t piece = std::max<int64_t>(256, std::min(classes, ((int64_t)1 << 28) / std::max(rows, s.ld) / 256 * 256));
     s.w_cap = piece * s.ld;
-    s.g_cap = d.gradients ? piece * rows : 0;
+    s.g_cap = d.gradients ? (piece + tf::kRowPad) * rows : 0;
     s.dx_cap = d.gradients ? std::max(rows * s.ld, std::min((int64_t)1 << 24, 512 * 64 * s.ld)) : 0;
     s.dw_cap = d.gradients ? (int64_t)1 << 24 : 0;
     Cut c{base};

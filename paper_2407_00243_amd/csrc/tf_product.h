@@ -1,6 +1,7 @@
 // Products of the cross entropy: C = M N^T, a tile of C by each workgroup, 16-bit operands, sums in 32 bits.
 #pragma once
 #include <algorithm>
+#include <type_traits>
 
 #include "tf_loss.h"
 #include "tf_moe_device.h"
@@ -12,10 +13,12 @@ template <int EL> struct Mfma;
 template <> struct Mfma<TF_BF16> {
     typedef Bf8 V;
     static __device__ __forceinline__ Float4 mul(V a, V b, Float4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
+    static __device__ __forceinline__ void add(Float4 &c, V a, V b) { asm volatile("v_mfma_f32_16x16x32_bf16 %0, %1, %2, %0" : "+a"(c) : "v"(a), "v"(b)); }
 };
 template <> struct Mfma<TF_F16> {
     typedef Half8 V;
     static __device__ __forceinline__ Float4 mul(V a, V b, Float4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
+    static __device__ __forceinline__ void add(Float4 &c, V a, V b) { asm volatile("v_mfma_f32_16x16x32_f16 %0, %1, %2, %0" : "+a"(c) : "v"(a), "v"(b)); }
 };
 
 typedef __attribute__((address_space(3))) void *LdsPtr;
@@ -25,6 +28,13 @@ typedef __attribute__((address_space(3))) Short4 *LdsShort4;
 
 constexpr int kStep = 64;      // of K
 
+// Sixteen bytes a lane from a buffer to LDS, lane by lane from `to` + AT on (bytes).  In assembly, because the compiler would have every read of
+// LDS that transposes wait for all loads before it.  It writes no vector register; what it writes in LDS is waited for in arrive().  (Nothing
+// else here uses m0, which cannot be named as clobbered.)
+template <int AT> __device__ __forceinline__ void load_to_lds(const Words4 &from, uint32_t offset, uint32_t to) {
+    asm volatile("s_add_u32 m0, %2, %3\n\ts_nop 0\n\tbuffer_load_dwordx4 %0, %1, 0 offen lds" ::"v"(offset), "s"(from), "s"(to), "i"(AT) : "scc");
+}
+
 // A step of an operand in LDS: W rows (of M or N) x 64 columns (K) if it lies in memory that way, else 64 rows (K) x W columns
 // (TR).  It comes sixteen bytes a lane straight from memory, 1 KiB an instruction, and LDS gets them in the order of the lanes; so
 // that sixteen lanes that read an operand of an instruction meet different banks, the pieces of a row are permuted on the way
@@ -32,46 +42,57 @@ constexpr int kStep = 64;      // of K
 template <int W, bool TR, int WAVES> struct Loader {
     static constexpr int INSTR = W / 8, PER = (INSTR + WAVES - 1) / WAVES, CPR = TR ? W / 8 : 8;
     static_assert(!TR || W >= 64, "rows of a transposed operand");
-    uint32_t off[PER];
-    int chunk;                     // of the first one
-    const char *base;
-    int64_t left;                  // rows (TR) or columns of K from the base on
-    int64_t ld2;                   // bytes
+    uint32_t off[PER];             // of each instruction's sixteen bytes, from the step's first ones on
+    uint64_t base, at;             // of the tile in a part's first step; of the step that comes next
+    uint32_t row, stride;          // bytes from row to row, from step to step
+    uint32_t records, tail;        // bytes of a whole step, of a row of it (TR)
+    int32_t left, left0;           // of K: from the next step on, in all
 
     static __device__ __forceinline__ int row_of(int j, int lane) { return j * (64 / CPR) + lane / CPR; }
     static __device__ __forceinline__ int chunk_of(int j, int lane) {
         const int r = row_of(j, lane), s = lane % CPR;
         return TR ? s ^ ((((r & 3) | ((r >> 3) & 1) << 2) << 1) & (CPR - 1)) : s ^ (r & 7);
     }
-    int64_t outer, inner;          // of the tile, what there is
-
-    // first: the tile's first row of M or N.
-    __device__ __forceinline__ void begin(const Side &s, int64_t first, int wave, int lane) {
-        ld2 = s.ld * 2;
-        outer = TR ? s.cols - first : s.rows - first;
+    // first: the tile's first row of M or N; k: the first column (row with TR) of K.
+    __device__ __forceinline__ void begin(const Side &s, int64_t first, int64_t k, int part, int wave, int lane) {
+        row = (uint32_t)(s.ld * 2);
+        const int64_t there = (TR ? s.cols : s.rows) - first;      // of M or N
+        const uint32_t some = (uint32_t)(there < 0 ? 0 : there < W ? there : W);
+        tail = some * 2;
+        base = (uint64_t)s.p + (uint64_t)((TR ? k * s.ld + first : first * s.ld + k) * 2);
+        stride = TR ? kStep * row : kStep * 2;
+        records = TR ? (kStep - 1) * row + tail : some ? (some - 1) * row + kStep * 2 : 0;
+        left0 = (int32_t)((TR ? s.rows : s.cols) - k);
+        go_to(s, part);
 #pragma unroll
         for (int c = 0; c < PER; ++c) {
             const int j = wave + WAVES * c;
-            const uint32_t o = (uint32_t)(row_of(j, lane) * (uint32_t)ld2 + chunk_of(j, lane) * 16);
-            off[c] = (TR ? chunk_of(j, lane) * 8 < outer : row_of(j, lane) < outer) ? o : ~0u;
+            const uint32_t o = (uint32_t)row_of(j, lane) * row + chunk_of(j, lane) * 16;
+            off[c] = (uint32_t)(TR ? chunk_of(j, lane) * 8 : row_of(j, lane)) < some ? o : ~0u;
         }
     }
-    // Loads the step that begins at column (row with TR) k of a part into `lds`.
-    __device__ __forceinline__ void load(const Side &s, int64_t first, int64_t k, int part, char *lds, int wave, int lane) const {
-        const char *p = static_cast<const char *>(s.p) + (part * s.plane + (TR ? k * s.ld + first : first * s.ld + k)) * 2;
-        // bytes up to the end of the last row
-        int64_t n = TR ? ((s.rows - k - 1) * ld2 + outer * 2) : ((outer - 1) * ld2 + (s.cols - k) * 2);
-        if ((TR ? s.rows - k : outer) <= 0) n = 0;
-        const auto r = __builtin_amdgcn_make_buffer_rsrc(const_cast<char *>(p), 0, (int)(uint32_t)(n < 0xffffffe0ll ? n : 0xffffffe0ll), 0x00020000);
+    __device__ __forceinline__ void go_to(const Side &s, int part) {
+        at = base + (uint64_t)(part * s.plane * 2);
+        left = left0;
+    }
+    // Where the next step lies, what lies behind its end counting as zeros; goes on to the one after it.
+    __device__ __forceinline__ Words4 next(int lane) {
+        const uint32_t n = !TR || left >= kStep ? records : left <= 0 ? 0u : (uint32_t)(left - 1) * row + tail;
+        const Words4 w{(uint32_t)at, (uint32_t)(at >> 32), n, 0x00020000u};
+        if (!TR && left < kStep) {
+            // The last step, which ends inside of a piece of 64 columns.  (A lane's columns are the same ones in every instruction; numbers in parts have
+            // whole pieces, so that this is the end of all steps.)
+            if (chunk_of(0, lane) * 8 >= left)
 #pragma unroll
-        for (int c = 0; c < PER; ++c) {
-            const int j = wave + WAVES * c;
-            if (INSTR % WAVES == 0 || j < INSTR) {
-                uint32_t o = off[c];
-                if (!TR && k + kStep > s.cols && k + chunk_of(j, lane) * 8 >= s.cols) o = ~0u;
-                __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (LdsPtr)(lds + j * 1024), 16, (int)o, 0, 0, 0);
-            }
+                for (int c = 0; c < PER; ++c) off[c] = ~0u;
         }
+        at += stride;
+        left -= kStep;
+        return w;
+    }
+    // Instruction C of those that load a step into LDS from lds + AT on; lds: of this wave's first instruction.
+    template <int C, int AT> __device__ __forceinline__ void load(const Words4 &from, uint32_t lds, int wave) const {
+        if (INSTR % WAVES == 0 || wave + WAVES * C < INSTR) load_to_lds<AT + WAVES * C * 1024>(from, off[C], lds);
     }
 };
 
@@ -91,27 +112,20 @@ template <int W, bool TR, int T> struct Reader {
             for (int kk = 0; kk < 2; ++kk) at[kk] = (first + lane % 16) * 128 + (((kk * 4 + lane / 16) ^ (lane & 7)) * 16);
         }
     }
-    template <int EL> __device__ __forceinline__ void read(typename Mfma<EL>::V (&v)[T], const char *lds, int kk) const {
-#pragma unroll
-        for (int i = 0; i < T; ++i) {
-            if constexpr (TR) {
-                const Short4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsShort4)(lds + at[i] + kk * 32 * W * 2));
-                const Short4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsShort4)(lds + at[i] + kk * 32 * W * 2 + 4 * W * 2));
-                v[i] = __builtin_bit_cast(typename Mfma<EL>::V, (Short8){lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]});
-            } else {
-                v[i] = *reinterpret_cast<const typename Mfma<EL>::V *>(lds + at[kk] + i * 2048);
-            }
+    // Operand i of half kk of a step that lies at lds.
+    template <int EL> __device__ __forceinline__ typename Mfma<EL>::V read(const char *lds, int kk, int i) const {
+        if constexpr (TR) {
+            const Short4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsShort4)(lds + at[i] + kk * 32 * W * 2));
+            const Short4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsShort4)(lds + at[i] + kk * 32 * W * 2 + 4 * W * 2));
+            return __builtin_bit_cast(typename Mfma<EL>::V, (Short8){lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]});
+        } else {
+            return *reinterpret_cast<const typename Mfma<EL>::V *>(lds + at[kk] + i * 2048);
         }
     }
 };
 
-// Waits for this wave's loads, then for all waves.  (Neither builtin orders memory accesses for the compiler.)
-__device__ __forceinline__ void arrive() {
-    asm volatile("" ::: "memory");
-    __builtin_amdgcn_s_waitcnt(0x0f70);      // vmcnt(0)
-    __builtin_amdgcn_s_barrier();
-    asm volatile("" ::: "memory");
-}
+// Waits for this wave's loads and reads, then for all waves.
+__device__ __forceinline__ void arrive() { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
 
 // The parts of M and N whose products are summed, small products first.
 __device__ __forceinline__ int part_m(int pair) { return (0x001102 >> (4 * pair)) & 15; }
@@ -125,13 +139,23 @@ template <int EL> __device__ __forceinline__ void split3(float x, uint16_t (&p)[
     }
 }
 
+// f(0), f(1), ... f(N - 1), the number known when the code is made.
+template <int N, int I = 0, typename F> __device__ __forceinline__ void each(F &&f) {
+    if constexpr (I < N) {
+        f(std::integral_constant<int, I>{});
+        each<N, I + 1>(f);
+    }
+}
+
 template <int EL, int WM, int WN, int TM, int TN, bool MTR, bool NTR, int END>
-__global__ __launch_bounds__(WM * WN * 64, 2) void k_product(const ProductLaunch a) {
-    constexpr int WAVES = WM * WN, BM = WM * TM * 16, BN = WN * TN * 16, STAGE = (BM + BN) * 128;
+__global__ __launch_bounds__(WM * WN * 64, TM * TN > 32 ? 1 : 2) void k_product(const ProductLaunch a) {
+    constexpr int WAVES = WM * WN, BM = WM * TM * 16, BN = WN * TN * 16;
+    constexpr bool BIG = TM * TN > 32;      // sums fill the accumulation registers: left alone, the compiler moves them about in every step
     extern __shared__ __attribute__((aligned(1024))) char lds[];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wm = wave / WN, wn = wave % WN;
     const int kept = a.n ? *a.n : 0;
-    // tiles: a contiguous share for each XCD, whose L2 then meets few rows of M
+    // Tiles: a contiguous share for each XCD, in bands of eight rows of tiles, so that the 32 workgroups that an XCD runs at a time are eight by four
+    // tiles and its L2 is asked for twelve pieces of operands a step, not 33.
     const int tiles = a.m_tiles * a.n_tiles, all = tiles * a.splits;
     int b = blockIdx.x;
     {
@@ -139,7 +163,8 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void k_product(const ProductLaunch
         b = xcd * each + min(xcd, more) + at;
     }
     const int split = b / tiles, tile = b % tiles;
-    const int mt = tile / a.n_tiles, nt = tile % a.n_tiles;
+    const int band = tile / (8 * a.n_tiles), high = min(8, a.m_tiles - 8 * band), in_band = tile - band * 8 * a.n_tiles;
+    const int mt = 8 * band + in_band % high, nt = in_band / high;
     const int64_t m0 = (int64_t)mt * BM, n0 = (int64_t)nt * BN;
     if (a.n_rows && n0 >= kept) return;
     Side M = a.M, N = a.N;
@@ -153,48 +178,111 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void k_product(const ProductLaunch
         s0 = (int)((int64_t)steps * split / a.splits);
         s1 = (int)((int64_t)steps * (split + 1) / a.splits);
     }
-    Loader<BM, MTR, WAVES> lm;
-    Loader<BN, NTR, WAVES> ln;
-    lm.begin(M, m0, wave, lane);
-    ln.begin(N, n0, wave, lane);
+    const int pairs = a.parts == 3 ? 6 : 1, total = pairs * (s1 - s0);
+    int pair = a.parts == 3 ? 0 : 5, in_pair = s1 - s0, to_load = total;
+    typedef Loader<BM, MTR, WAVES> LM;
+    typedef Loader<BN, NTR, WAVES> LN;
+    LM lm;
+    LN ln;
+    lm.begin(M, m0, (int64_t)s0 * kStep, part_m(pair), wave, lane);
+    ln.begin(N, n0, (int64_t)s0 * kStep, part_n(pair), wave, lane);
     Reader<BM, MTR, TM> rm;
     Reader<BN, NTR, TN> rn;
     rm.begin(wm * TM * 16, lane);
     rn.begin(wn * TN * 16, lane);
     Float4 acc[TM][TN] = {};
-    const int pairs = a.parts == 3 ? 6 : 1, total = pairs * (s1 - s0);
-    int pair = a.parts == 3 ? 0 : 5, step = s0;
-    char *cur = lds, *other = lds + STAGE;
-    auto load = [&](char *to) {
-        lm.load(M, m0, (int64_t)step * kStep, part_m(pair), to, wave, lane);
-        ln.load(N, n0, (int64_t)step * kStep, part_n(pair), to + BM * 128, wave, lane);
-        if (++step == s1) {
-            step = s0;
+    Words4 from_m, from_n;
+    auto next = [&]() {           // sets up the loads of the next step
+        from_m = lm.next(lane);
+        from_n = ln.next(lane);
+        if (--to_load < 0) from_m[2] = from_n[2] = 0;
+        if (--in_pair == 0 && to_load > 0) {
+            in_pair = s1 - s0;
             ++pair;
+            lm.go_to(M, part_m(pair));
+            ln.go_to(N, part_n(pair));
         }
     };
-    if (total > 0) load(cur);
-    for (int i = 0; i < total; ++i) {
+    constexpr int LOADS = LM::PER + LN::PER, READS = TM + TN, PRODUCTS = TM * TN;
+    // LDS: M of two steps, then N of two steps.  The place of a step is known when the code is made: then all addresses are registers that stay and a
+    // constant.
+    constexpr int AT_N = 2 * BM * 128;
+    const uint32_t lds0 = (uint32_t)(uintptr_t)(LdsPtr)lds + wave * 1024;
+    auto load = [&](auto c, auto to) {
+        constexpr int C = decltype(c)::value, TO = decltype(to)::value;
+        if constexpr (C < LM::PER) lm.template load<C, TO * BM * 128>(from_m, lds0, wave);
+        else if constexpr (C < LOADS) ln.template load<C - LM::PER, AT_N + TO * BN * 128>(from_n, lds0, wave);
+    };
+    typename Mfma<EL>::V vm[2][TM], vn[2][TN];
+    auto read = [&](int r, int half, int from) {
+        if (r < TM) vm[half][r] = rm.template read<EL>(lds + from * BM * 128, half, r);
+        else if (r < READS) vn[half][r - TM] = rn.template read<EL>(lds + AT_N + from * BN * 128, half, r - TM);
+    };
+    // Multiplies one half of a step.  Meanwhile the other half's operands come from LDS (`reads`: of the step at place `from`), the loads of a step go
+    // out (`loads`: to place `to`), or are set up.  An instruction of the matrix cores takes the time of four others: these are spread, a few
+    // behind each product.
+    auto multiply = [&](auto half, auto reads, auto from, auto loads, auto to, auto sets_up) {
+        constexpr int HALF = decltype(half)::value, SLOTS = PRODUCTS > 1 ? PRODUCTS / 2 : 1;
+        each<PRODUCTS>([&](auto slot) {
+            constexpr int P = decltype(slot)::value;
+            if constexpr (decltype(loads)::value && P < SLOTS)
+                each<LOADS * (P + 1) / SLOTS - LOADS * P / SLOTS>([&](auto c) { load(std::integral_constant<int, LOADS * P / SLOTS + decltype(c)::value>{}, to); });
+            if constexpr (decltype(reads)::value && P < SLOTS) {
+                // (half a turn later than the loads)
+                constexpr int lo = P ? (READS * (2 * P + 1) / 2) / SLOTS : 0, hi = P + 1 < SLOTS ? (READS * (2 * P + 3) / 2) / SLOTS : READS;
+                each<hi - lo>([&](auto r) { read(lo + decltype(r)::value, 1 - HALF, decltype(from)::value); });
+            }
+            if constexpr (decltype(sets_up)::value && P == SLOTS) next();
+            constexpr int x = P / TN, y = P % TN;
+            if constexpr (BIG) Mfma<EL>::add(acc[x][y], vm[HALF][x], vn[HALF][y]);
+            else acc[x][y] = Mfma<EL>::mul(vm[HALF][x], vn[HALF][y], acc[x][y]);
+            __builtin_amdgcn_sched_barrier(0);
+        });
+    };
+    constexpr std::integral_constant<int, 0> zero{};
+    constexpr std::integral_constant<int, 1> one{};
+    constexpr std::true_type yes{};
+    constexpr std::false_type no{};
+    // The barrier lies between a step's halves: behind it the next step is in LDS, and nobody reads this one any more.
+    auto step = [&](auto place, auto other) {
+        multiply(zero, yes, place, no, zero, yes);
         arrive();
-        if (i + 1 < total) load(other);
+        multiply(one, yes, other, yes, place, no);
+    };
+    next();
+    each<LOADS>([&](auto c) { load(c, zero); });
+    arrive();
+    next();
+    each<LOADS>([&](auto c) { load(c, one); });
 #pragma unroll
-        for (int kk = 0; kk < 2; ++kk) {
-            typename Mfma<EL>::V vm[TM], vn[TN];
-            rm.template read<EL>(vm, cur, kk);
-            rn.template read<EL>(vn, cur + BM * 128, kk);
-#pragma unroll
-            for (int x = 0; x < TM; ++x)
-#pragma unroll
-                for (int y = 0; y < TN; ++y) acc[x][y] = Mfma<EL>::mul(vm[x], vn[y], acc[x][y]);
-        }
-        char *t = cur;
-        cur = other;
-        other = t;
+    for (int r = 0; r < READS; ++r) read(r, 0, 0);
+    // Two steps a round, as addresses are made for; steps behind the last one are zeros, which come from no memory.
+    for (int i = 0; i < total; i += 2) {
+        step(zero, one);
+        step(one, zero);
     }
+    arrive();        // (loads that nobody reads: LDS is given away when the workgroup ends)
+    if constexpr (BIG) {
+        // (the compiler does not know what the last instructions write, nor when)
+        asm volatile("s_nop 15\n\ts_nop 15" ::: "memory");
+        __builtin_amdgcn_sched_barrier(0);
+    }
+    auto value = [&](int x, int y, int v) {
+        if constexpr (BIG) {
+            float f;
+            asm volatile("v_accvgpr_read_b32 %0, %1" : "=v"(f) : "a"(acc[x][y][v]));
+            return f;
+        } else {
+            return acc[x][y][v];
+        }
+    };
     // Lane 16 g + r holds, of acc[x][y], rows 16 x + 4 g .. + 3 of M (from `mw` on) and row 16 y + r of N.
     const int g = lane / 16;
     const int64_t mw = m0 + wm * TM * 16, nw = n0 + wn * TN * 16 + lane % 16;
     if constexpr (END == kEndSums || END == kEndGradient) {
+        // Exponentials are powers of two of l log2(e) - c: one multiplication and addition and one instruction of a quarter of the others' rate for each
+        // logit, 256 of them a lane.  What c = fl(top log2(e)) is off by scales all terms alike, by less than 2^-24 |top|.
+        constexpr float LOG2E = 1.44269504088896340736f;
         const bool whole = mw + TM * 16 <= a.m_count;
 #pragma unroll
         for (int y = 0; y < TN; ++y) {
@@ -202,23 +290,39 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void k_product(const ProductLaunch
             const bool is = row < kept;
             const int label = is ? a.label[row] - a.first_class : -1;
             const int64_t at = (int64_t)label - mw - 4 * g;      // 16 x + v where the label's logit is in this lane
+            const bool any = __ballot(at >= 0 && at < 16 * TM && (at & 15) < 4) != 0;      // (in this wave: seldom)
             if constexpr (END == kEndSums) {
-                float top = -__builtin_inff(), sum = 0.0f;
+                float top = -__builtin_inff(), sum = 0.0f, l[TM][4];
 #pragma unroll
                 for (int x = 0; x < TM; ++x)
 #pragma unroll
-                    for (int v = 0; v < 4; ++v) {
-                        if (!whole && mw + 16 * x + 4 * g + v >= a.m_count) acc[x][y][v] = -__builtin_inff();
-                        top = fmaxf(top, acc[x][y][v]);
-                        if (at == 16 * x + v) a.hit[row] = acc[x][y][v];
-                    }
+                    for (int v = 0; v < 4; ++v) l[x][v] = value(x, y, v);
+                if (!whole)
+#pragma unroll
+                    for (int x = 0; x < TM; ++x)
+#pragma unroll
+                        for (int v = 0; v < 4; ++v)
+                            if (mw + 16 * x + 4 * g + v >= a.m_count) l[x][v] = -__builtin_inff();
+#pragma unroll
+                for (int x = 0; x < TM; ++x)
+#pragma unroll
+                    for (int v = 0; v < 4; ++v) top = fmaxf(top, l[x][v]);
                 top = fmaxf(top, __shfl_xor(top, 16, 64));
                 top = fmaxf(top, __shfl_xor(top, 32, 64));
-                const float from = top == -__builtin_inff() ? 0.0f : top;
+                if (any)        // the label's own is added to the sum at the end
+#pragma unroll
+                    for (int x = 0; x < TM; ++x)
+#pragma unroll
+                        for (int v = 0; v < 4; ++v)
+                            if (at == 16 * x + v) {
+                                a.hit[row] = l[x][v];
+                                l[x][v] = -__builtin_inff();
+                            }
+                const float from = top == -__builtin_inff() ? 0.0f : top * LOG2E;
 #pragma unroll
                 for (int x = 0; x < TM; ++x)
 #pragma unroll
-                    for (int v = 0; v < 4; ++v) sum += at == 16 * x + v ? 0.0f : expf(acc[x][y][v] - from);      // (the label's is added at the end)
+                    for (int v = 0; v < 4; ++v) sum += __builtin_amdgcn_exp2f(fmaf(l[x][v], LOG2E, -from));
                 sum += __shfl_xor(sum, 16, 64);
                 sum += __shfl_xor(sum, 32, 64);
                 if (is && g == 0) {
@@ -227,22 +331,31 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void k_product(const ProductLaunch
                     a.part_sum[to] = sum;
                 }
             } else if (is) {
-                const float lse = a.lse[row], scale = a.g[row];
+                const float from = a.lse[row] * LOG2E, scale = a.g[row];
                 uint16_t *out = static_cast<uint16_t *>(a.G) + row * a.g_ld + mw + 4 * g;
+                typedef uint16_t U4 __attribute__((ext_vector_type(4)));
 #pragma unroll
                 for (int x = 0; x < TM; ++x) {
-                    uint16_t p[4][3];
+                    float d[4];
 #pragma unroll
-                    for (int v = 0; v < 4; ++v) {
-                        float d = (expf(acc[x][y][v] - lse) - (at == 16 * x + v ? 1.0f : 0.0f)) * scale;
-                        if (!whole && mw + 16 * x + 4 * g + v >= a.m_count) d = 0.0f;
-                        split3<EL>(d, p[v]);
-                    }
-                    typedef uint16_t U4 __attribute__((ext_vector_type(4)));
-                    *reinterpret_cast<U4 *>(out + 16 * x) = U4{p[0][0], p[1][0], p[2][0], p[3][0]};
-                    if (a.parts == 3) {
-                        *reinterpret_cast<U4 *>(out + a.g_plane + 16 * x) = U4{p[0][1], p[1][1], p[2][1], p[3][1]};
-                        *reinterpret_cast<U4 *>(out + 2 * a.g_plane + 16 * x) = U4{p[0][2], p[1][2], p[2][2], p[3][2]};
+                    for (int v = 0; v < 4; ++v) d[v] = __builtin_amdgcn_exp2f(fmaf(value(x, y, v), LOG2E, -from));
+                    if (any)
+#pragma unroll
+                        for (int v = 0; v < 4; ++v) d[v] -= at == 16 * x + v ? 1.0f : 0.0f;
+#pragma unroll
+                    for (int v = 0; v < 4; ++v) d[v] *= scale;
+                    if (!whole)
+#pragma unroll
+                        for (int v = 0; v < 4; ++v)
+                            if (mw + 16 * x + 4 * g + v >= a.m_count) d[v] = 0.0f;
+                    if (EL == TF_BF16 && a.parts == 3) {
+                        uint16_t p[4][3];
+#pragma unroll
+                        for (int v = 0; v < 4; ++v) split3<EL>(d[v], p[v]);
+#pragma unroll
+                        for (int i = 0; i < 3; ++i) *reinterpret_cast<U4 *>(out + i * a.g_plane + 16 * x) = U4{p[0][i], p[1][i], p[2][i], p[3][i]};
+                    } else {
+                        *reinterpret_cast<U4 *>(out + 16 * x) = U4{El<EL>::put(d[0]), El<EL>::put(d[1]), El<EL>::put(d[2]), El<EL>::put(d[3])};
                     }
                 }
             }
@@ -257,7 +370,8 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void k_product(const ProductLaunch
 #pragma unroll
                 for (int x = 0; x < TM; ++x) {
                     Float4 *to = reinterpret_cast<Float4 *>(out + 16 * x);
-                    *to = a.add ? *to + acc[x][y] : acc[x][y];
+                    const Float4 d = {value(x, y, 0), value(x, y, 1), value(x, y, 2), value(x, y, 3)};
+                    *to = a.add ? *to + d : d;
                 }
             }
         }
@@ -270,20 +384,22 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void k_product(const ProductLaunch
 #pragma unroll
             for (int x = 0; x < TM; ++x) {
                 const int64_t m = mw + 16 * x + 4 * g;
+                Float4 f;
+#pragma unroll
+                for (int v = 0; v < 4; ++v) f[v] = value(x, y, v) * unit;
                 if (a.out_dtype == TF_F32) {
                     float *to = static_cast<float *>(a.out) + row * a.ldo + m;
                     typedef float F4 __attribute__((ext_vector_type(4), aligned(4)));
-                    const Float4 d = acc[x][y] * unit;
-                    if (m + 4 <= a.m_count) *reinterpret_cast<F4 *>(to) = d;
+                                        if (m + 4 <= a.m_count) *reinterpret_cast<F4 *>(to) = f;
                     else
                         for (int v = 0; v < 4; ++v)
-                            if (m + v < a.m_count) to[v] = d[v];
+                            if (m + v < a.m_count) to[v] = f[v];
                 } else {
                     uint16_t *to = static_cast<uint16_t *>(a.out) + row * a.ldo + m;
                     typedef uint16_t U4 __attribute__((ext_vector_type(4), aligned(2)));
                     U4 d;
 #pragma unroll
-                    for (int v = 0; v < 4; ++v) d[v] = El<EL>::put(acc[x][y][v] * unit);
+                    for (int v = 0; v < 4; ++v) d[v] = El<EL>::put(f[v]);
                     if (m + 4 <= a.m_count) *reinterpret_cast<U4 *>(to) = d;
                     else
                         for (int v = 0; v < 4; ++v)
@@ -316,7 +432,7 @@ template <int EL, int WM, int WN, int TM, int TN, bool MTR, bool NTR, int END> i
 }
 
 template <int EL, bool MTR, bool NTR, int END> int product_tile(const ProductLaunch &a, hipStream_t st) {
-    if (a.tile == kTile256) return product_with<EL, 2, 4, 8, 4, MTR, NTR, END>(a, st);
+    if (a.tile == kTile256) return product_with<EL, 2, 2, 8, 8, MTR, NTR, END>(a, st);
     if constexpr (!NTR) {
         if (a.tile == kTile64) return product_with<EL, 4, 1, 2, 4, MTR, NTR, END>(a, st);
         if (a.tile == kTile16) return product_with<EL, 4, 1, 2, 1, MTR, NTR, END>(a, st);

@@ -375,8 +375,9 @@ int launch_xent_grad(const XentLaunch &a, void *stream) {
     int e = begin(a, st);
     if (e) return e;
     const int64_t rows = round_up(std::max(a.n_rows, 1), 256);
-    int64_t piece = std::min(round_up(a.n_classes, 256), a.s.g_cap / rows / 256 * 256);
+    int64_t piece = std::min(round_up(a.n_classes, 256), (a.s.g_cap / rows - kRowPad) / 256 * 256);
     if (!in_place(a)) piece = std::min(piece, a.s.w_cap / a.s.ld);
+    const int64_t g_ld = piece + kRowPad;
     const int parts = a.dtype == TF_F32 ? 3 : 1;
     const int64_t dx_size = rows * a.s.ld;
     // (the same shares for every piece: the slabs are added to)
@@ -392,14 +393,14 @@ int launch_xent_grad(const XentLaunch &a, void *stream) {
             p.lse = a.s.lse;
             p.g = a.s.g;
             p.G = a.s.G;
-            p.g_ld = piece;
+            p.g_ld = g_ld;
             p.g_plane = a.s.g_cap;
             e = launch_product(p, a.dtype, stream);
             if (e) return e;
             if (a.dX) {
                 ProductLaunch q{};
                 q.M = W;
-                q.N = Side{a.s.G, piece, a.s.g_cap, rows, round_up(count, 64)};
+                q.N = Side{a.s.G, g_ld, a.s.g_cap, rows, round_up(count, 64)};
                 q.parts = parts;
                 q.k_steps = (int32_t)ceil_div(count, 64);
                 q.n = a.s.n;
@@ -420,7 +421,7 @@ int launch_xent_grad(const XentLaunch &a, void *stream) {
         if (a.dW) {
             ProductLaunch q{};
             q.M = Side{a.s.x, a.s.ld, a.s.x_plane, 0, a.s.ld};
-            q.N = Side{a.s.G, piece, a.s.g_cap, 0, piece};
+            q.N = Side{a.s.G, g_ld, a.s.g_cap, 0, piece};
             q.parts = parts;
             q.n = a.s.n;
             q.k_rows = 1;
