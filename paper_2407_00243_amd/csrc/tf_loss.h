@@ -38,7 +38,7 @@ constexpr int64_t round_up(int64_t n, int64_t to) { return ceil_div(n, to) * to;
 // A plan's workspace.  Rows that have a label ("kept") are numbered in their order; arrays by row are by that number.
 struct XentSpace {
     int32_t *list, *pos;          // row of X of a kept row; number of a row or -1
-    int32_t *block_rows;          // kept rows of each block of kRowBlock rows
+    int32_t *block_rows;          // kept rows of each block of rows
     float *block_top;             // largest |dloss| there
     int32_t *n;                   // kept rows
     float *unit;                  // what sums of gradients are multiplied by at the end
@@ -52,7 +52,7 @@ struct XentSpace {
     int64_t x_plane;              // elements
     int64_t part_cap, g_cap, w_cap, dx_cap, dw_cap;     // elements that there is room for (of a plane)
 };
-constexpr int kRowBlock = 4096;
+constexpr int64_t kMostBlocks = 4096;      // of rows
 // Elements between the rows of x, w and G: rows a power of two apart would all lie in one channel of an XCD's L2.
 constexpr int64_t kRowPad = 64;
 
@@ -65,6 +65,7 @@ struct XentLaunch {
     float *loss, *lse;
     const float *lse_in, *dloss;
     void *dX, *dW;
+    int32_t direct_dx;            // dX is written by its product; rows without a label get their zeros first
 };
 int launch_xent(const XentLaunch &a, void *stream);
 int launch_xent_grad(const XentLaunch &a, void *stream);
@@ -101,6 +102,7 @@ struct ProductLaunch {
     int32_t add;                  // to what the slab holds
     void *out;
     int64_t ldo;
+    const int32_t *out_row;       // NULL: as they are
     int32_t out_dtype;
 };
 int launch_product_bf16(const ProductLaunch &a, void *stream);

@@ -80,11 +80,11 @@ struct Cut {
 int64_t lay_out(tf_xent &p, char *base) {
     const tf_xent_desc &d = p.d;
     tf::XentSpace &s = p.s;
-    const int64_t rows = round_up(d.max_rows, 256), classes = round_up(d.n_classes, 256), blocks = ceil_div(d.max_rows, tf::kRowBlock);
+    const int64_t rows = round_up(d.max_rows, 256), classes = round_up(d.n_classes, 256);
     const int64_t planes = d.dtype == TF_F32 ? 3 : 1;
     s.ld = round_up(d.n_in, 256) + tf::kRowPad;
     s.x_plane = rows * s.ld;
-    s.part_cap = std::max(std::min(classes / 128 * std::max(2 * rows, (int64_t)4 * 256), (int64_t)1 << 25), std::max(4 * rows, (int64_t)8 * 256));
+    s.part_cap = std::max(std::min(classes / 64 * std::max(rows, (int64_t)4 * 256), (int64_t)1 << 25), std::max(8 * rows, (int64_t)16 * 256));
     const int64_t piece = std::max<int64_t>(256, std::min(classes, ((int64_t)1 << 28) / std::max(rows, s.ld) / 256 * 256));
     s.w_cap = piece * s.ld;
     s.g_cap = d.gradients ? (piece + tf::kRowPad) * rows : 0;
@@ -93,8 +93,8 @@ int64_t lay_out(tf_xent &p, char *base) {
     Cut c{base};
     c.take(s.list, d.max_rows);
     c.take(s.pos, d.max_rows);
-    c.take(s.block_rows, blocks);
-    c.take(s.block_top, blocks);
+    c.take(s.block_rows, tf::kMostBlocks);
+    c.take(s.block_top, tf::kMostBlocks);
     c.take(s.n, 1);
     c.take(s.unit, 1);
     c.take(s.label, d.max_rows);

@@ -40,7 +40,7 @@ template <int AT> __device__ __forceinline__ void load_to_lds(const Words4 &from
 // that sixteen lanes that read an operand of an instruction meet different banks, the pieces of a row are permuted on the way
 // by which lane asks for which: piece p of row r is at p ^ (r & 7); with TR 32-byte units u of row k at u ^ (k & 3 | k / 8 % 2 * 4).
 template <int W, bool TR, int WAVES> struct Loader {
-    static constexpr int INSTR = W / 8, PER = (INSTR + WAVES - 1) / WAVES, CPR = TR ? W / 8 : 8;
+    static constexpr int INSTR = W / 8, PER = (INSTR + WAVES - 1) / WAVES, PER_LEAST = INSTR / WAVES, CPR = TR ? W / 8 : 8;
     static_assert(!TR || W >= 64, "rows of a transposed operand");
     uint32_t off[PER];             // of each instruction's sixteen bytes, from the step's first ones on
     uint64_t base, at;             // of the tile in a part's first step; of the step that comes next
@@ -124,8 +124,8 @@ template <int W, bool TR, int T> struct Reader {
     }
 };
 
-// Waits for this wave's loads and reads, then for all waves.
-__device__ __forceinline__ void arrive() { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
+// Waits for this wave's reads and for its loads but the last LATER ones, then for all waves.
+template <int LATER> __device__ __forceinline__ void arrive() { asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"i"(LATER) : "memory"); }
 
 // The parts of M and N whose products are summed, small products first.
 __device__ __forceinline__ int part_m(int pair) { return (0x001102 >> (4 * pair)) & 15; }
@@ -147,7 +147,7 @@ template <int N, int I = 0, typename F> __device__ __forceinline__ void each(F &
     }
 }
 
-template <int EL, int WM, int WN, int TM, int TN, bool MTR, bool NTR, int END>
+template <int EL, int WM, int WN, int TM, int TN, int PLACES, bool MTR, bool NTR, int END>
 __global__ __launch_bounds__(WM * WN * 64, TM * TN > 32 ? 1 : 2) void k_product(const ProductLaunch a) {
     constexpr int WAVES = WM * WN, BM = WM * TM * 16, BN = WN * TN * 16;
     constexpr bool BIG = TM * TN > 32;      // sums fill the accumulation registers: left alone, the compiler moves them about in every step
@@ -204,9 +204,9 @@ __global__ __launch_bounds__(WM * WN * 64, TM * TN > 32 ? 1 : 2) void k_product(
         }
     };
     constexpr int LOADS = LM::PER + LN::PER, READS = TM + TN, PRODUCTS = TM * TN;
-    // LDS: M of two steps, then N of two steps.  The place of a step is known when the code is made: then all addresses are registers that stay and a
-    // constant.
-    constexpr int AT_N = 2 * BM * 128;
+    // LDS has places for PLACES steps, first M's, then N's.  A step's place is known when the code is made: then all addresses are registers that stay and
+    // a constant.  A wave waits until all but the loads of the steps behind the next one have arrived.
+    constexpr int AT_N = PLACES * BM * 128, LEAST = LM::PER_LEAST + LN::PER_LEAST;
     const uint32_t lds0 = (uint32_t)(uintptr_t)(LdsPtr)lds + wave * 1024;
     auto load = [&](auto c, auto to) {
         constexpr int C = decltype(c)::value, TO = decltype(to)::value;
@@ -232,7 +232,7 @@ __global__ __launch_bounds__(WM * WN * 64, TM * TN > 32 ? 1 : 2) void k_product(
                 constexpr int lo = P ? (READS * (2 * P + 1) / 2) / SLOTS : 0, hi = P + 1 < SLOTS ? (READS * (2 * P + 3) / 2) / SLOTS : READS;
                 each<hi - lo>([&](auto r) { read(lo + decltype(r)::value, 1 - HALF, decltype(from)::value); });
             }
-            if constexpr (decltype(sets_up)::value && P == SLOTS) next();
+            if constexpr (decltype(sets_up)::value && P == (SLOTS < PRODUCTS ? SLOTS : PRODUCTS - 1)) next();
             constexpr int x = P / TN, y = P % TN;
             if constexpr (BIG) Mfma<EL>::add(acc[x][y], vm[HALF][x], vn[HALF][y]);
             else acc[x][y] = Mfma<EL>::mul(vm[HALF][x], vn[HALF][y], acc[x][y]);
@@ -246,22 +246,20 @@ __global__ __launch_bounds__(WM * WN * 64, TM * TN > 32 ? 1 : 2) void k_product(
     // The barrier lies between a step's halves: behind it the next step is in LDS, and nobody reads this one any more.
     auto step = [&](auto place, auto other) {
         multiply(zero, yes, place, no, zero, yes);
-        arrive();
+        arrive<(PLACES - 2) * LEAST>();
         multiply(one, yes, other, yes, place, no);
     };
-    next();
-    each<LOADS>([&](auto c) { load(c, zero); });
-    arrive();
-    next();
-    each<LOADS>([&](auto c) { load(c, one); });
+    each<PLACES>([&](auto place) {
+        next();
+        each<LOADS>([&](auto c) { load(c, place); });
+    });
+    arrive<(PLACES - 1) * LEAST>();
 #pragma unroll
     for (int r = 0; r < READS; ++r) read(r, 0, 0);
-    // Two steps a round, as addresses are made for; steps behind the last one are zeros, which come from no memory.
-    for (int i = 0; i < total; i += 2) {
-        step(zero, one);
-        step(one, zero);
-    }
-    arrive();        // (loads that nobody reads: LDS is given away when the workgroup ends)
+    // A round of steps, as addresses are made for; steps behind the last one are zeros, which come from no memory.
+    for (int i = 0; i < total; i += PLACES)
+        each<PLACES>([&](auto place) { step(place, std::integral_constant<int, (decltype(place)::value + 1) % PLACES>{}); });
+    arrive<0>();        // (loads that nobody reads: LDS is given away when the workgroup ends)
     if constexpr (BIG) {
         // (the compiler does not know what the last instructions write, nor when)
         asm volatile("s_nop 15\n\ts_nop 15" ::: "memory");
@@ -377,10 +375,12 @@ __global__ __launch_bounds__(WM * WN * 64, TM * TN > 32 ? 1 : 2) void k_product(
         }
     } else {
         const float unit = *a.unit;
+        const int64_t rows = a.n_rows ? kept : a.n_count;
 #pragma unroll
         for (int y = 0; y < TN; ++y) {
-            const int64_t row = nw + 16 * y;
-            if (row >= a.n_count) continue;
+            int64_t row = nw + 16 * y;
+            if (row >= rows) continue;
+            if (a.out_row) row = a.out_row[row];
 #pragma unroll
             for (int x = 0; x < TM; ++x) {
                 const int64_t m = mw + 16 * x + 4 * g;
@@ -410,14 +410,14 @@ __global__ __launch_bounds__(WM * WN * 64, TM * TN > 32 ? 1 : 2) void k_product(
     }
 }
 
-template <int EL, int WM, int WN, int TM, int TN, bool MTR, bool NTR, int END> int product_with(ProductLaunch a, hipStream_t st) {
-    constexpr int BM = WM * TM * 16, BN = WN * TN * 16, LDS = 2 * (BM + BN) * 128;
+template <int EL, int WM, int WN, int TM, int TN, int PLACES, bool MTR, bool NTR, int END> int product_with(ProductLaunch a, hipStream_t st) {
+    constexpr int BM = WM * TM * 16, BN = WN * TN * 16, LDS = PLACES * (BM + BN) * 128;
     static DoneOnDevices done;
     int device = 0;
     hipError_t e = hipGetDevice(&device);
     if (e != hipSuccess) return (int)e;
     if (!done.has(device)) {
-        e = hipFuncSetAttribute(reinterpret_cast<const void *>(k_product<EL, WM, WN, TM, TN, MTR, NTR, END>),
+        e = hipFuncSetAttribute(reinterpret_cast<const void *>(k_product<EL, WM, WN, TM, TN, PLACES, MTR, NTR, END>),
                                 hipFuncAttributeMaxDynamicSharedMemorySize, LDS);
         if (e != hipSuccess) return (int)e;
         done.add(device);
@@ -427,17 +427,17 @@ template <int EL, int WM, int WN, int TM, int TN, bool MTR, bool NTR, int END> i
     const int64_t groups = (int64_t)a.m_tiles * a.n_tiles * a.splits;
     if (groups == 0) return 0;
     if (groups > most_workgroups(WM * WN * 64)) return (int)hipErrorInvalidConfiguration;
-    hipLaunchKernelGGL((k_product<EL, WM, WN, TM, TN, MTR, NTR, END>), dim3((unsigned)groups), dim3(WM * WN * 64), LDS, st, a);
+    hipLaunchKernelGGL((k_product<EL, WM, WN, TM, TN, PLACES, MTR, NTR, END>), dim3((unsigned)groups), dim3(WM * WN * 64), LDS, st, a);
     return (int)hipGetLastError();
 }
 
 template <int EL, bool MTR, bool NTR, int END> int product_tile(const ProductLaunch &a, hipStream_t st) {
-    if (a.tile == kTile256) return product_with<EL, 2, 2, 8, 8, MTR, NTR, END>(a, st);
+    if (a.tile == kTile256) return product_with<EL, 2, 2, 8, 8, 2, MTR, NTR, END>(a, st);
     if constexpr (!NTR) {
-        if (a.tile == kTile64) return product_with<EL, 4, 1, 2, 4, MTR, NTR, END>(a, st);
-        if (a.tile == kTile16) return product_with<EL, 4, 1, 2, 1, MTR, NTR, END>(a, st);
+        if (a.tile == kTile64) return product_with<EL, 4, 1, 2, 4, 3, MTR, NTR, END>(a, st);
+        if (a.tile == kTile16) return product_with<EL, 4, 1, 1, 1, 4, MTR, NTR, END>(a, st);
     }
-    return product_with<EL, 2, 2, 4, 4, MTR, NTR, END>(a, st);
+    return product_with<EL, 2, 2, 4, 4, 2, MTR, NTR, END>(a, st);
 }
 
 // The four products: logits (their sums, or the gradient), dX (W by columns), dW (both operands by columns).
@@ -447,6 +447,7 @@ template <int EL> int product(const ProductLaunch &a, void *stream) {
     if (a.end == kEndGradient) return product_tile<EL, false, false, kEndGradient>(a, st);
     if (a.end == kEndSlab && !a.k_rows) return product_tile<EL, true, false, kEndSlab>(a, st);
     if (a.end == kEndSlab) return product_tile<EL, true, true, kEndSlab>(a, st);
+    if (!a.k_rows) return product_tile<EL, true, false, kEndOut>(a, st);
     return product_tile<EL, true, true, kEndOut>(a, st);
 }
 

@@ -9,73 +9,6 @@ namespace {
 
 constexpr float kLow = -__builtin_inff();
 
-// ------------------------------------------------------------------------------ rows with a label
-
-// Numbers the rows that have a label in their order.  A block of 4096 rows a workgroup: with `sums` 1 it only counts, with 0 it takes the
-// counts of the blocks before it and writes.
-__global__ __launch_bounds__(1024) void k_rows(const XentLaunch a, const int only_count) {
-    __shared__ int of_wave[16], before[16];
-    __shared__ float top_of_wave[16];
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    const int64_t r0 = (int64_t)blockIdx.x * kRowBlock + tid * 4;
-    int mine = 0;
-    float top = 0.0f;
-    bool keep[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        keep[i] = false;
-        if (r0 + i < a.n_rows) {
-            const int y = a.labels[r0 + i];
-            keep[i] = y >= 0 && y < a.n_classes;
-            if (keep[i] && a.dloss) {
-                const float g = fabsf(a.dloss[r0 + i]);
-                if (g < __builtin_inff()) top = fmaxf(top, g);
-            }
-        }
-        mine += keep[i];
-    }
-    int upto = mine;
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) {
-        const int x = __shfl_up(upto, d, 64);
-        if (lane >= d) upto += x;
-    }
-#pragma unroll
-    for (int d = 32; d; d >>= 1) top = fmaxf(top, __shfl_xor(top, d, 64));
-    int earlier = 0;
-    if (!only_count)
-        for (int b = tid; b < (int)blockIdx.x; b += 1024) earlier += a.s.block_rows[b];
-#pragma unroll
-    for (int d = 32; d; d >>= 1) earlier += __shfl_xor(earlier, d, 64);
-    if (lane == 63) of_wave[wave] = upto;
-    if (lane == 0) {
-        top_of_wave[wave] = top;
-        before[wave] = earlier;
-    }
-    __syncthreads();
-    int at = upto - mine, all = 0;
-    top = 0.0f;
-    for (int w = 0; w < 16; ++w) {
-        if (w < wave) at += of_wave[w];
-        all += of_wave[w];
-        top = fmaxf(top, top_of_wave[w]);
-        if (!only_count) at += before[w];
-    }
-    if (tid == 0 && (only_count || gridDim.x == 1)) {
-        a.s.block_rows[blockIdx.x] = all;
-        a.s.block_top[blockIdx.x] = top;
-    }
-    if (only_count) return;
-    if (tid == 1023 && blockIdx.x == gridDim.x - 1) *a.s.n = at + mine;
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-        if (r0 + i < a.n_rows) {
-            a.s.pos[r0 + i] = keep[i] ? at : -1;
-            if (keep[i]) a.s.list[at++] = (int)(r0 + i);
-            else if (a.loss) a.loss[r0 + i] = a.lse[r0 + i] = 0.0f;
-        }
-}
-
 // -------------------------------------------------------------------------------------- operands
 
 // Eight columns of a row, from column k on, in 32 bits; zeros behind the last one.
@@ -146,96 +79,207 @@ template <int EL> __device__ __forceinline__ void put8(const float (&x)[8], uint
     for (int p = 0; p < (EL == TF_F32 ? 3 : 1); ++p) *reinterpret_cast<Words4 *>(to + p * plane) = w[p];
 }
 
-// x: the rows that count, one after the other; columns up to a multiple of 64 are zeros behind the last one.
-template <int EL> __global__ __launch_bounds__(256) void k_pack_rows(const XentLaunch a) {
-    const int n = *a.s.n;
-    const int64_t k = ((int64_t)blockIdx.y * 256 + threadIdx.x) * 8;
+// How many threads take a row of `columns`, eight columns each: a power of two, 256 at most.
+__device__ __forceinline__ int threads_of_row(int64_t columns) {
+    const int n = (int)min(ceil_div(columns, 8), (int64_t)256);
+    return n <= 1 ? 1 : 1 << (32 - __builtin_clz((unsigned)n - 1));
+}
+
+__device__ __forceinline__ int wave_sum(int x) {
+#pragma unroll
+    for (int d = 32; d; d >>= 1) x += __shfl_xor(x, d, 64);
+    return x;
+}
+__device__ __forceinline__ float wave_max(float x) {
+#pragma unroll
+    for (int d = 32; d; d >>= 1) x = fmaxf(x, __shfl_xor(x, d, 64));
+    return x;
+}
+
+// What a row adds to a count of the rows that have a label; the largest finite |dloss| of those goes to `top`.
+__device__ __forceinline__ bool counts(const XentLaunch &a, int64_t row, float &top) {
+    const int y = a.labels[row];
+    const bool keep = y >= 0 && y < a.n_classes;
+    if (keep && a.dloss) {
+        const float g = fabsf(a.dloss[row]);
+        if (g < __builtin_inff()) top = fmaxf(top, g);
+    }
+    return keep;
+}
+
+// Count and largest gradient of a block of rows a workgroup.
+__global__ __launch_bounds__(256) void k_count_rows(const XentLaunch a, const int block) {
+    __shared__ int n_of[4];
+    __shared__ float top_of[4];
+    const int tid = threadIdx.x;
+    const int64_t first = (int64_t)blockIdx.x * block, end = min(first + block, (int64_t)a.n_rows);
+    int n = 0;
     float top = 0.0f;
-    if (a.dloss && blockIdx.y == 0)
-        for (int b = 0; b < (int)ceil_div(a.n_rows, kRowBlock); ++b) top = fmaxf(top, a.s.block_top[b]);
+    for (int64_t r = first + tid; r < end; r += 256) n += counts(a, r, top);
+    n = wave_sum(n);
+    top = wave_max(top);
+    if ((tid & 63) == 0) {
+        n_of[tid >> 6] = n;
+        top_of[tid >> 6] = top;
+    }
+    __syncthreads();
+    if (tid == 0) {
+        a.s.block_rows[blockIdx.x] = n_of[0] + n_of[1] + n_of[2] + n_of[3];
+        a.s.block_top[blockIdx.x] = fmaxf(fmaxf(top_of[0], top_of[1]), fmaxf(top_of[2], top_of[3]));
+    }
+}
+
+// Numbers the rows that have a label in their order and copies them, one after the other, to x, where columns up to a multiple of 64 are zeros behind
+// the last one; rows without a label get their zeros.  A block of rows a workgroup, which sums up the counts of the blocks before
+// it; where there are few rows (`counted` 0) it counts them itself, which saves a launch.
+template <int EL> __global__ __launch_bounds__(256) void k_pack_rows(const XentLaunch a, const int block, const int counted) {
+    __shared__ int n_of[4], rows[256], ats[256];
+    __shared__ float top_of[4];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int64_t first = (int64_t)blockIdx.x * block, end = min(first + block, (int64_t)a.n_rows);
+    int n = 0;
+    float top = 0.0f;
+    if (counted) {
+        for (int b = tid; b < (int)gridDim.x; b += 256) {
+            if (b < (int)blockIdx.x) n += a.s.block_rows[b];
+            top = fmaxf(top, a.s.block_top[b]);
+        }
+    } else {
+        for (int64_t r = tid; r < (a.dloss ? (int64_t)a.n_rows : first); r += 256) {
+            const bool keep = counts(a, r, top);
+            n += keep && r < first;
+        }
+    }
+    n = wave_sum(n);
+    top = wave_max(top);
+    if (lane == 0) {
+        n_of[wave] = n;
+        top_of[wave] = top;
+    }
+    __syncthreads();
+    n = n_of[0] + n_of[1] + n_of[2] + n_of[3];
+    top = fmaxf(fmaxf(top_of[0], top_of[1]), fmaxf(top_of[2], top_of[3]));
+    // gradients are divided by the largest one, so that no size of dloss is lost in 16 bits
     const float scale = a.dtype == TF_F16 ? 32768.0f : 1.0f;
     if (top == 0.0f) top = 1.0f;
-    if (a.dloss && blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0) *a.s.unit = top / scale;
-    for (int64_t i = blockIdx.x; i < n; i += gridDim.x) {
-        const int64_t row = a.s.list[i];
-        if (blockIdx.y == 0 && threadIdx.x == 0) {
-            a.s.label[i] = a.labels[row];
-            if (a.dloss) {
-                a.s.lse[i] = a.lse_in[row];
-                a.s.g[i] = a.dloss[row] / top * scale;
-            }
+    if (a.dloss && blockIdx.x == 0 && tid == 0) *a.s.unit = top / scale;
+    const int64_t columns = round_up(a.n_in, 64);
+    const int per_row = threads_of_row(columns), at_once = 256 / per_row;
+    for (int64_t r0 = first; r0 < end; r0 += 256) {
+        const int64_t r = r0 + tid;
+        float unused = 0.0f;
+        const bool keep = r < end && counts(a, r, unused);
+        const uint64_t kept = __ballot(keep);
+        __syncthreads();        // (the last round's lists have been read)
+        if (lane == 0) n_of[wave] = __popcll(kept);
+        __syncthreads();
+        int at = __popcll(kept & (((uint64_t)1 << lane) - 1)), here = 0;
+        for (int w = 0; w < 4; ++w) {
+            if (w < wave) at += n_of[w];
+            here += n_of[w];
         }
-        if (k >= round_up(a.n_in, 64)) continue;
-        float x[8];
-        read8<EL>(x, static_cast<const typename El<EL>::T *>(a.X) + row * a.ldx, k, a.n_in);
-        put8<EL>(x, static_cast<uint16_t *>(a.s.x) + i * a.s.ld + k, a.s.x_plane);
+        if (r < end) {
+            a.s.pos[r] = keep ? n + at : -1;
+            if (keep) {
+                rows[at] = (int)r;
+                a.s.list[n + at] = (int)r;
+                a.s.label[n + at] = a.labels[r];
+                if (a.dloss) {
+                    a.s.lse[n + at] = a.lse_in[r];
+                    a.s.g[n + at] = a.dloss[r] / top * scale;
+                }
+            } else if (a.loss) {
+                a.loss[r] = a.lse[r] = 0.0f;
+            }
+            ats[tid] = keep;
+        }
+        __syncthreads();
+        for (int i = tid / per_row; i < here; i += at_once)
+            for (int64_t k = tid % per_row * 8; k < columns; k += per_row * 8) {
+                float x[8];
+                read8<EL>(x, static_cast<const typename El<EL>::T *>(a.X) + rows[i] * a.ldx, k, a.n_in);
+                put8<EL>(x, static_cast<uint16_t *>(a.s.x) + (n + i) * a.s.ld + k, a.s.x_plane);
+            }
+        if (a.dX && a.direct_dx)
+            for (int i = tid / per_row; i < (int)min(end - r0, (int64_t)256); i += at_once)
+                if (!ats[i])
+                    for (int64_t k = tid % per_row * 8; k < a.n_in; k += per_row * 8) {
+                        const float x[8] = {};
+                        write8<EL>(x, static_cast<typename El<EL>::T *>(a.dX) + (r0 + i) * a.lddx, k, a.n_in);
+                    }
+        n += here;
     }
+    if (blockIdx.x == gridDim.x - 1 && tid == 0) *a.s.n = n;
 }
 // w: rows first .. first + count of W likewise.
 template <int EL> __global__ __launch_bounds__(256) void k_pack_classes(const XentLaunch a, const int64_t first, const int64_t count, const int64_t plane) {
-    const int64_t k = ((int64_t)blockIdx.y * 256 + threadIdx.x) * 8;
-    if (k >= round_up(a.n_in, 64)) return;
-    for (int64_t i = blockIdx.x; i < count; i += gridDim.x) {
-        float x[8];
-        read8<EL>(x, static_cast<const typename El<EL>::T *>(a.W) + (first + i) * a.ldw, k, a.n_in);
-        put8<EL>(x, static_cast<uint16_t *>(a.s.w) + i * a.s.ld + k, plane);
-    }
+    const int64_t columns = round_up(a.n_in, 64);
+    const int per_row = threads_of_row(columns), at_once = 256 / per_row;
+    for (int64_t i = (int64_t)blockIdx.x * at_once + threadIdx.x / per_row; i < count; i += (int64_t)gridDim.x * at_once)
+        for (int64_t k = threadIdx.x % per_row * 8; k < columns; k += per_row * 8) {
+            float x[8];
+            read8<EL>(x, static_cast<const typename El<EL>::T *>(a.W) + (first + i) * a.ldw, k, a.n_in);
+            put8<EL>(x, static_cast<uint16_t *>(a.s.w) + i * a.s.ld + k, plane);
+        }
 }
 
 // ------------------------------------------------------------------------------------------- ends
 
-// Adds the sums of `blocks` blocks of classes to those of the classes before them (unless `first`): 64 rows a workgroup, whose 16 waves take
-// every sixteenth block each.  The last call writes the results.
-__global__ __launch_bounds__(1024) void k_merge(const XentLaunch a, const int64_t blocks, const int64_t ld, const int first, const int last) {
-    __shared__ float tops[16][64], sums[16][64];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int64_t row = (int64_t)blockIdx.x * 64 + lane;
-    const int n = *a.s.n;
-    if ((int64_t)blockIdx.x * 64 >= n) return;
-    float top = kLow, sum = 0.0f;
-    if (row < n)
-#pragma unroll 4
-        for (int64_t b = wave; b < blocks; b += 16) {
-            const float t = a.s.part_top[b * ld + row], s = a.s.part_sum[b * ld + row], m = fmaxf(top, t);
-            sum = (top == kLow ? sum : sum * expf(top - m)) + (t == kLow ? s : s * expf(t - m));
-            top = m;
-        }
-    tops[wave][lane] = top;
-    sums[wave][lane] = sum;
-    __syncthreads();
-    if (wave || row >= n) return;
-    if (!first) {
-        top = a.s.top[row];
-        sum = a.s.sum[row];
-    }
-    for (int w = first ? 1 : 0; w < 16; ++w) {
-        const float t = tops[w][lane], s = sums[w][lane], m = fmaxf(top, t);
+// Adds the sums of `blocks` blocks of classes to those of the classes before them (unless `first`).  ROWS rows a workgroup: 64 / ROWS lanes of each of
+// its 16 waves take a row, and all of them every block once.  The last call writes the results.
+struct Sum {
+    float top, sum;
+    __device__ __forceinline__ void add(float t, float s) {
+        const float m = fmaxf(top, t);
         sum = (top == kLow ? sum : sum * expf(top - m)) + (t == kLow ? s : s * expf(t - m));
         top = m;
     }
+};
+template <int ROWS> __global__ __launch_bounds__(1024) void k_merge(const XentLaunch a, const int64_t blocks, const int64_t ld, const int first, const int last) {
+    __shared__ float tops[16][ROWS], sums[16][ROWS];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int64_t row = (int64_t)blockIdx.x * ROWS + lane % ROWS;
+    const int n = *a.s.n;
+    if ((int64_t)blockIdx.x * ROWS >= n) return;
+    Sum x{kLow, 0.0f};
+    if (row < n)
+#pragma unroll 4
+        for (int64_t b = wave * (64 / ROWS) + lane / ROWS; b < blocks; b += 16 * (64 / ROWS)) x.add(a.s.part_top[b * ld + row], a.s.part_sum[b * ld + row]);
+#pragma unroll
+    for (int d = ROWS; d < 64; d <<= 1) x.add(__shfl_xor(x.top, d, 64), __shfl_xor(x.sum, d, 64));
+    if (lane < ROWS) {
+        tops[wave][lane] = x.top;
+        sums[wave][lane] = x.sum;
+    }
+    __syncthreads();
+    if (wave || row >= n || lane >= ROWS) return;
+    x = first ? Sum{kLow, 0.0f} : Sum{a.s.top[row], a.s.sum[row]};
+    for (int w = 0; w < 16; ++w) x.add(tops[w][lane], sums[w][lane]);
     if (!last) {
-        a.s.top[row] = top;
-        a.s.sum[row] = sum;
+        a.s.top[row] = x.top;
+        a.s.sum[row] = x.sum;
         return;
     }
     // `sum` is that of the other classes: a small loss keeps its precision as log(1 + sum / exp(label's logit))
-    const float hit = a.s.hit[row], lse = top + logf(sum + expf(hit - top));
+    const float hit = a.s.hit[row], lse = x.top + logf(x.sum + expf(hit - x.top));
     const int64_t to = a.s.list[row];
     a.lse[to] = lse;
-    a.loss[to] = top - hit < 40.0f ? log1pf(sum * expf(top - hit)) : lse - hit;
+    a.loss[to] = x.top - hit < 40.0f ? log1pf(x.sum * expf(x.top - hit)) : lse - hit;
 }
 
-// dX: the shares' sums of each row that counts, zeros in the others.
-template <int EL> __global__ __launch_bounds__(256) void k_finish_rows(const XentLaunch a, const int splits, const int64_t size) {
-    const int64_t k = ((int64_t)blockIdx.y * 256 + threadIdx.x) * 8;
-    if (k >= a.n_in) return;
-    const float unit = *a.s.unit;
-    for (int64_t t = blockIdx.x; t < a.n_rows; t += gridDim.x) {
-        const int64_t i = a.s.pos[t];
+// Rows `row` of an output from the sums of `splits` slabs, `none` for zeros.  A row's columns lie in `per_row` threads; the others of a workgroup take
+// other rows, or, where there are many slabs, other slabs (`by_slab`), added up in their order.
+template <int EL> __device__ __forceinline__ void finish_row(const float *slab, int64_t size, int splits, void *out, int64_t n_in, bool none, float unit,
+                                                             int per_row, bool by_slab, bool is) {
+    __shared__ float part[256][9];
+    const int tid = threadIdx.x, slices = by_slab ? 256 / per_row : 1, slice = by_slab ? tid / per_row : 0;
+    for (int64_t k0 = 0; k0 < n_in; k0 += per_row * 8) {
+        const int64_t k = k0 + tid % per_row * 8;
         float x[8] = {};
-        if (i >= 0) {
-            for (int z = 0; z < splits; ++z) {
-                const Float4 *p = reinterpret_cast<const Float4 *>(a.s.dx + z * size + i * a.s.ld + k);
+        if (is && !none && k < n_in)
+#pragma unroll 4
+            for (int z = slice; z < splits; z += slices) {
+                const Float4 *p = reinterpret_cast<const Float4 *>(slab + z * size + k);
                 const Float4 lo = p[0], hi = p[1];
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
@@ -243,39 +287,57 @@ template <int EL> __global__ __launch_bounds__(256) void k_finish_rows(const Xen
                     x[4 + j] += hi[j];
                 }
             }
+        if (by_slab) {
+            __syncthreads();
+#pragma unroll
+            for (int j = 0; j < 8; ++j) part[tid][j] = x[j];
+            __syncthreads();
+            if (slice == 0)
+                for (int s = 1; s < slices; ++s)
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) x[j] += part[s * per_row + tid][j];
+        }
+        if (is && slice == 0 && k < n_in) {
 #pragma unroll
             for (int j = 0; j < 8; ++j) x[j] *= unit;
+            write8<EL>(x, out, k, n_in);
         }
-        write8<EL>(x, static_cast<typename El<EL>::T *>(a.dX) + t * a.lddx, k, a.n_in);
+    }
+}
+constexpr int kManySlabs = 8;
+
+// dX: the shares' sums of each row that counts, zeros in the others.
+template <int EL> __global__ __launch_bounds__(256) void k_finish_rows(const XentLaunch a, const int splits, const int64_t size) {
+    const float unit = *a.s.unit;
+    const int per_row = threads_of_row(a.n_in);
+    const bool by_slab = splits >= kManySlabs;
+    const int at_once = by_slab ? 1 : 256 / per_row;
+    for (int64_t t0 = (int64_t)blockIdx.x * at_once; t0 < a.n_rows; t0 += (int64_t)gridDim.x * at_once) {
+        const int64_t t = t0 + (by_slab ? 0 : threadIdx.x / per_row);
+        const bool is = t < a.n_rows;
+        const int64_t i = is ? a.s.pos[t] : -1;
+        finish_row<EL>(a.s.dx + i * a.s.ld, size, splits, static_cast<typename El<EL>::T *>(a.dX) + t * a.lddx, a.n_in, i < 0, unit, per_row, by_slab, is);
     }
 }
 // Rows first .. first + count of dW.
 template <int EL> __global__ __launch_bounds__(256) void k_finish_classes(const XentLaunch a, const int64_t first, const int64_t count, const int splits, const int64_t size) {
-    const int64_t k = ((int64_t)blockIdx.y * 256 + threadIdx.x) * 8;
-    if (k >= a.n_in) return;
     const float unit = *a.s.unit;
-    for (int64_t i = blockIdx.x; i < count; i += gridDim.x) {
-        float x[8] = {};
-        for (int z = 0; z < splits; ++z) {
-            const Float4 *p = reinterpret_cast<const Float4 *>(a.s.dw + z * size + i * a.s.ld + k);
-            const Float4 lo = p[0], hi = p[1];
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                x[j] += lo[j];
-                x[4 + j] += hi[j];
-            }
-        }
-#pragma unroll
-        for (int j = 0; j < 8; ++j) x[j] *= unit;
-        write8<EL>(x, static_cast<typename El<EL>::T *>(a.dW) + (first + i) * a.lddw, k, a.n_in);
+    const int per_row = threads_of_row(a.n_in);
+    const bool by_slab = splits >= kManySlabs;
+    const int at_once = by_slab ? 1 : 256 / per_row;
+    for (int64_t i0 = (int64_t)blockIdx.x * at_once; i0 < count; i0 += (int64_t)gridDim.x * at_once) {
+        const int64_t i = i0 + (by_slab ? 0 : threadIdx.x / per_row);
+        finish_row<EL>(a.s.dw + i * a.s.ld, size, splits, static_cast<typename El<EL>::T *>(a.dW) + (first + i) * a.lddw, a.n_in, false, unit, per_row, by_slab,
+                       i < count);
     }
 }
 
 // --------------------------------------------------------------------------------------- launches
 
-// Rows of a launch (each workgroup goes on by this many) x blocks of 2048 columns.
+// Workgroups for `rows` rows of `columns`, 2048 columns at a time.
 dim3 row_grid(int64_t rows, int64_t columns) {
-    return dim3((unsigned)std::min<int64_t>(rows, 8192), (unsigned)ceil_div(columns, 2048));
+    const int64_t per_row = std::min<int64_t>(256, ceil_div(columns, 8));
+    return dim3((unsigned)std::max<int64_t>(1, std::min<int64_t>(ceil_div(rows * per_row, 256), 8192)));
 }
 #define TF_BY_TYPE(dtype, kernel, grid, ...)                                                                           \
     do {                                                                                                               \
@@ -294,12 +356,14 @@ bool in_place(const XentLaunch &a) {
            a.ldw <= kXentMaxColumns;
 }
 
+// Numbers and copies the rows that count.  (Also without rows: it sets the unit.)  Blocks of 32 rows, larger ones where there would be more than
+// kMostBlocks; up to 8192 rows every block counts the rows before it.
 int begin(const XentLaunch &a, hipStream_t st) {
-    const unsigned blocks = (unsigned)std::max<int64_t>(1, ceil_div(a.n_rows, kRowBlock));
-    if (blocks > 1) hipLaunchKernelGGL(k_rows, dim3(blocks), dim3(1024), 0, st, a, 1);
-    hipLaunchKernelGGL(k_rows, dim3(blocks), dim3(1024), 0, st, a, 0);
-    // (also without rows: it sets the unit)
-    TF_BY_TYPE(a.dtype, k_pack_rows, row_grid(std::max(a.n_rows, 1), round_up(a.n_in, 64)), a);
+    const int64_t block = std::max<int64_t>(32, round_up(ceil_div(a.n_rows, kMostBlocks), 32));
+    const dim3 grid((unsigned)std::max<int64_t>(1, ceil_div(a.n_rows, block)));
+    const int counted = a.n_rows > 8192;
+    if (counted) hipLaunchKernelGGL(k_count_rows, grid, dim3(256), 0, st, a, (int)block);
+    TF_BY_TYPE(a.dtype, k_pack_rows, grid, a, (int)block, counted);
     return (int)hipGetLastError();
 }
 
@@ -327,17 +391,20 @@ ProductLaunch logits(const XentLaunch &a, const Side &W, int64_t first, int64_t 
     return p;
 }
 
-// A tile of 256 x 256 where there are enough of them for the compute units, else smaller ones; few rows: all of them in one.
+// A tile of 256 x 256 where there are enough of them for the compute units, else smaller ones.  Few rows: all of them in one (the launch is bound by
+// reading the other operand), few classes or columns: all of them in one.
 ProductTile tile_for(int64_t m, int64_t n, bool rows) {
     if (rows && n <= 16) return kTile16;
-    if (rows && n <= 64) return kTile64;
+    if (rows && (n <= 64 || m <= 128)) return kTile64;
     return ceil_div(m, 256) * ceil_div(n, 256) >= 192 ? kTile256 : kTile128;
 }
-int64_t side_of(ProductTile t) { return t == kTile256 ? 256 : 128; }
+int64_t m_side(ProductTile t) { return t == kTile256 ? 256 : t == kTile16 ? 64 : 128; }
+int64_t n_side(ProductTile t) { return t == kTile256 ? 256 : t == kTile16 ? 16 : t == kTile64 ? 64 : 128; }
+// Sums that a tile of logits leaves of each row: one for each wave's rows of M.
+int64_t sums_of(ProductTile t) { return t == kTile256 || t == kTile128 ? 2 : 4; }
 // Shares of a contraction of `steps`, so that the launch has enough workgroups; each has four steps at least.
 int64_t shares(ProductTile t, int64_t m, int64_t n, int64_t steps, int64_t most) {
-    const int64_t across = t == kTile16 ? 16 : t == kTile64 ? 64 : side_of(t);
-    const int64_t groups = ceil_div(m, side_of(t)) * ceil_div(n, across), want = t == kTile256 ? 256 : 512;
+    const int64_t groups = ceil_div(m, m_side(t)) * ceil_div(n, n_side(t)), want = t == kTile256 ? 256 : t == kTile16 ? 1024 : 512;
     return std::max<int64_t>(1, std::min({want / groups, steps / 4, most}));
 }
 
@@ -348,8 +415,8 @@ int launch_xent(const XentLaunch &a, void *stream) {
     int e = begin(a, st);
     if (e || a.n_rows == 0) return e;
     const int64_t ld = round_up(a.n_rows, 256);
-    const int64_t per_tile = a.n_rows <= 64 ? 4 : 2;          // blocks of classes in a tile
-    int64_t piece = a.s.part_cap / (ld * per_tile) * 128 / 256 * 256;
+    // (tiles of few rows leave a sum for every 16 classes, those of few classes for every 32, others for 64 or 128)
+    int64_t piece = a.s.part_cap / ld * (a.n_rows <= 16 ? 16 : a.n_rows <= 64 || a.n_classes <= 128 ? 32 : 64) / 256 * 256;
     if (!in_place(a)) piece = std::min(piece, a.s.w_cap / a.s.ld);
     for (int64_t first = 0; first < a.n_classes; first += piece) {
         const int64_t count = std::min<int64_t>(piece, a.n_classes - first);
@@ -362,18 +429,20 @@ int launch_xent(const XentLaunch &a, void *stream) {
         p.part_ld = ld;
         e = launch_product(p, a.dtype, stream);
         if (e) return e;
-        const int64_t blocks = ceil_div(count, side_of(p.tile)) * per_tile;
-        hipLaunchKernelGGL(k_merge, dim3((unsigned)ceil_div(a.n_rows, 64)), dim3(1024), 0, st, a, blocks, ld, first == 0, first + count == a.n_classes);
+        const int64_t blocks = ceil_div(count, m_side(p.tile)) * sums_of(p.tile);
+        const int is_first = first == 0, is_last = first + count == a.n_classes;
+        if (a.n_rows <= 256) hipLaunchKernelGGL(k_merge<1>, dim3((unsigned)a.n_rows), dim3(1024), 0, st, a, blocks, ld, is_first, is_last);
+        else if (a.n_rows <= 4096) hipLaunchKernelGGL(k_merge<8>, dim3((unsigned)ceil_div(a.n_rows, 8)), dim3(1024), 0, st, a, blocks, ld, is_first, is_last);
+        else hipLaunchKernelGGL(k_merge<64>, dim3((unsigned)ceil_div(a.n_rows, 64)), dim3(1024), 0, st, a, blocks, ld, is_first, is_last);
         e = (int)hipGetLastError();
         if (e) return e;
     }
     return 0;
 }
 
-int launch_xent_grad(const XentLaunch &a, void *stream) {
+int launch_xent_grad(const XentLaunch &call, void *stream) {
     const hipStream_t st = static_cast<hipStream_t>(stream);
-    int e = begin(a, st);
-    if (e) return e;
+    XentLaunch a = call;
     const int64_t rows = round_up(std::max(a.n_rows, 1), 256);
     int64_t piece = std::min(round_up(a.n_classes, 256), (a.s.g_cap / rows - kRowPad) / 256 * 256);
     if (!in_place(a)) piece = std::min(piece, a.s.w_cap / a.s.ld);
@@ -383,6 +452,9 @@ int launch_xent_grad(const XentLaunch &a, void *stream) {
     // (the same shares for every piece: the slabs are added to)
     const ProductTile dx_tile = tile_for(a.n_in, a.n_rows, true);
     const int64_t dx_shares = a.dX && a.n_rows ? shares(dx_tile, a.n_in, a.n_rows, ceil_div(std::min<int64_t>(piece, a.n_classes), 64), a.s.dx_cap / dx_size) : 1;
+    a.direct_dx = piece >= a.n_classes && dx_shares == 1;
+    int e = begin(a, st);
+    if (e) return e;
     for (int64_t first = 0; first < a.n_classes; first += piece) {
         const int64_t count = std::min<int64_t>(piece, a.n_classes - first);
         if (a.n_rows) {
@@ -407,7 +479,12 @@ int launch_xent_grad(const XentLaunch &a, void *stream) {
                 q.n_rows = 1;
                 q.m_count = a.n_in;
                 q.n_count = a.n_rows;
-                q.end = kEndSlab;
+                q.end = a.direct_dx ? kEndOut : kEndSlab;
+                q.unit = a.s.unit;
+                q.out = a.dX;
+                q.ldo = a.lddx;
+                q.out_row = a.s.list;
+                q.out_dtype = a.dtype;
                 q.tile = dx_tile;
                 q.splits = (int32_t)dx_shares;
                 q.slab = a.s.dx;
@@ -443,7 +520,7 @@ int launch_xent_grad(const XentLaunch &a, void *stream) {
             if (q.splits > 1) TF_BY_TYPE(a.dtype, k_finish_classes, row_grid(count, a.n_in), a, first, count, q.splits, size);
         }
     }
-    if (a.dX && a.n_rows) TF_BY_TYPE(a.dtype, k_finish_rows, row_grid(a.n_rows, a.n_in), a, (int)dx_shares, dx_size);
+    if (a.dX && a.n_rows && !a.direct_dx) TF_BY_TYPE(a.dtype, k_finish_rows, row_grid(a.n_rows, a.n_in), a, (int)dx_shares, dx_size);
     return (int)hipGetLastError();
 }
 
