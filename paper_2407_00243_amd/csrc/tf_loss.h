@@ -33,6 +33,7 @@ int launch_route_grad(const RouterLaunch &a, void *stream);
 
 constexpr int64_t kXentMaxColumns = (int64_t)1 << 22;      // 256 rows of 16-bit numbers are below 2^32 bytes
 constexpr int64_t kXentMaxRows = (int64_t)1 << 28, kXentMaxClasses = (int64_t)1 << 30;
+typedef float Float2 __attribute__((ext_vector_type(2)));
 constexpr int64_t round_up(int64_t n, int64_t to) { return ceil_div(n, to) * to; }
 
 // A plan's workspace.  Rows that have a label ("kept") are numbered in their order; arrays by row are by that number.
@@ -45,14 +46,14 @@ struct XentSpace {
     int32_t *label;
     float *lse, *g, *hit;         // log of the sum, gradient over the unit, logit of the label
     float *top, *sum;             // running maximum and sum of exponentials
-    float *part_top, *part_sum;   // the same of blocks of classes, block after block
+    Float2 *part;                 // both for blocks of classes, block after block
     void *x, *w, *G;              // operands: planes of 16-bit numbers
     float *dx, *dw;               // sums in 32 bits, one slab for each share of a contraction
     int64_t ld;                   // row length of x and w: n_in rounded up to 256, and kRowPad
     int64_t x_plane;              // elements
     int64_t part_cap, g_cap, w_cap, dx_cap, dw_cap;     // elements that there is room for (of a plane)
 };
-constexpr int64_t kMostBlocks = 4096;      // of rows
+constexpr int64_t kMostBlocks = 1024;      // of rows
 // Elements between the rows of x, w and G: rows a power of two apart would all lie in one channel of an XCD's L2.
 constexpr int64_t kRowPad = 64;
 
@@ -76,6 +77,8 @@ struct Side {
     int64_t ld, plane;            // elements: from row to row, from part to part
     int64_t rows, cols;           // what there is of it (cols: a multiple of 8); further elements count as zeros
 };
+// Shares of a contraction: each has four steps of 64 at least.
+constexpr int shares_of(int most, int steps) { return most < steps / 4 ? most : steps / 4 < 1 ? 1 : steps / 4; }
 enum ProductEnd { kEndSums = 0, kEndGradient = 1, kEndSlab = 2, kEndOut = 3 };
 enum ProductTile { kTile256 = 0, kTile128 = 1, kTile64 = 2, kTile16 = 3 };
 struct ProductLaunch {
@@ -85,7 +88,7 @@ struct ProductLaunch {
     const int32_t *n;             // kept rows
     int32_t k_rows;               // 1: K goes over kept rows
     int32_t n_rows;               // 1: N does
-    int32_t m_tiles, n_tiles, splits;
+    int32_t m_tiles, n_tiles, splits;      // splits: shares of K at most
     ProductEnd end;
     ProductTile tile;
     int32_t m_count, n_count;     // rows of M and N that count
@@ -93,7 +96,8 @@ struct ProductLaunch {
     int32_t first_class;
     const int32_t *label;
     const float *lse, *g, *unit;
-    float *hit, *part_top, *part_sum;
+    float *hit;
+    Float2 *part;                 // largest logit and sum of exponentials over it
     int64_t part_ld;
     void *G;
     int64_t g_ld, g_plane;

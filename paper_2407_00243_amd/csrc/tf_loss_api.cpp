@@ -84,12 +84,12 @@ int64_t lay_out(tf_xent &p, char *base) {
     const int64_t planes = d.dtype == TF_F32 ? 3 : 1;
     s.ld = round_up(d.n_in, 256) + tf::kRowPad;
     s.x_plane = rows * s.ld;
-    s.part_cap = std::max(std::min(classes / 64 * std::max(rows, (int64_t)4 * 256), (int64_t)1 << 25), std::max(8 * rows, (int64_t)16 * 256));
+    s.part_cap = std::max(std::min(classes / 64 * rows, (int64_t)1 << 25), 4 * rows);
     const int64_t piece = std::max<int64_t>(256, std::min(classes, ((int64_t)1 << 28) / std::max(rows, s.ld) / 256 * 256));
     s.w_cap = piece * s.ld;
     s.g_cap = d.gradients ? (piece + tf::kRowPad) * rows : 0;
-    s.dx_cap = d.gradients ? std::max(rows * s.ld, std::min((int64_t)1 << 24, 512 * 64 * s.ld)) : 0;
-    s.dw_cap = d.gradients ? (int64_t)1 << 24 : 0;
+    s.dx_cap = d.gradients ? std::max({rows * s.ld, std::min((int64_t)1 << 26, 4 * rows * s.ld), std::min((int64_t)1 << 24, 512 * 64 * s.ld)}) : 0;
+    s.dw_cap = d.gradients ? (int64_t)1 << 25 : 0;
     Cut c{base};
     c.take(s.list, d.max_rows);
     c.take(s.pos, d.max_rows);
@@ -103,8 +103,7 @@ int64_t lay_out(tf_xent &p, char *base) {
     c.take(s.hit, d.max_rows);
     c.take(s.top, d.max_rows);
     c.take(s.sum, d.max_rows);
-    c.take(s.part_top, s.part_cap);
-    c.take(s.part_sum, s.part_cap);
+    c.take(s.part, s.part_cap);
     uint16_t *x, *w, *G;
     c.take(x, planes * s.x_plane);
     c.take(w, planes * s.w_cap);

@@ -131,6 +131,13 @@ template <int LATER> __device__ __forceinline__ void arrive() { asm volatile("s_
 __device__ __forceinline__ int part_m(int pair) { return (0x001102 >> (4 * pair)) & 15; }
 __device__ __forceinline__ int part_n(int pair) { return (0x010120 >> (4 * pair)) & 15; }
 
+// Sums of exponentials over their largest argument: x holds that and the sum.
+__device__ __forceinline__ Float2 add_sums(Float2 x, Float2 y) {
+    constexpr float LOW = -__builtin_inff();
+    const float m = fmaxf(x[0], y[0]);
+    return Float2{m, (x[0] == LOW ? x[1] : x[1] * expf(x[0] - m)) + (y[0] == LOW ? y[1] : y[1] * expf(y[0] - m))};
+}
+
 template <int EL> __device__ __forceinline__ void split3(float x, uint16_t (&p)[3]) {
 #pragma unroll
     for (int i = 0; i < 3; ++i) {
@@ -156,28 +163,23 @@ __global__ __launch_bounds__(WM * WN * 64, TM * TN > 32 ? 1 : 2) void k_product(
     const int kept = a.n ? *a.n : 0;
     // Tiles: a contiguous share for each XCD, in bands of eight rows of tiles, so that the 32 workgroups that an XCD runs at a time are eight by four
     // tiles and its L2 is asked for twelve pieces of operands a step, not 33.
-    const int tiles = a.m_tiles * a.n_tiles, all = tiles * a.splits;
+    // (Only as many as there are kept rows for; a share of K that would have under four steps is not made.)
+    int steps = a.k_rows ? (kept + kStep - 1) / kStep : a.k_steps;
+    const int n_tiles = a.n_rows ? (kept + BN - 1) / BN : a.n_tiles, splits = shares_of(a.splits, steps);
+    const int tiles = a.m_tiles * n_tiles, all = tiles * splits;
     int b = blockIdx.x;
+    if (b >= all) return;
     {
         const int xcd = b & 7, at = b >> 3, each = all >> 3, more = all & 7;
         b = xcd * each + min(xcd, more) + at;
     }
     const int split = b / tiles, tile = b % tiles;
-    const int band = tile / (8 * a.n_tiles), high = min(8, a.m_tiles - 8 * band), in_band = tile - band * 8 * a.n_tiles;
+    const int band = tile / (8 * n_tiles), high = min(8, a.m_tiles - 8 * band), in_band = tile - band * 8 * n_tiles;
     const int mt = 8 * band + in_band % high, nt = in_band / high;
     const int64_t m0 = (int64_t)mt * BM, n0 = (int64_t)nt * BN;
-    if (a.n_rows && n0 >= kept) return;
     Side M = a.M, N = a.N;
-    int steps = a.k_steps;
-    if (a.k_rows) {
-        steps = (kept + kStep - 1) / kStep;
-        M.rows = N.rows = kept;
-    }
-    int s0 = 0, s1 = steps;
-    if (a.splits > 1) {
-        s0 = (int)((int64_t)steps * split / a.splits);
-        s1 = (int)((int64_t)steps * (split + 1) / a.splits);
-    }
+    if (a.k_rows) M.rows = N.rows = kept;
+    const int s0 = (int)((int64_t)steps * split / splits), s1 = (int)((int64_t)steps * (split + 1) / splits);
     const int pairs = a.parts == 3 ? 6 : 1, total = pairs * (s1 - s0);
     int pair = a.parts == 3 ? 0 : 5, in_pair = s1 - s0, to_load = total;
     typedef Loader<BM, MTR, WAVES> LM;
@@ -323,10 +325,20 @@ __global__ __launch_bounds__(WM * WN * 64, TM * TN > 32 ? 1 : 2) void k_product(
                     for (int v = 0; v < 4; ++v) sum += __builtin_amdgcn_exp2f(fmaf(l[x][v], LOG2E, -from));
                 sum += __shfl_xor(sum, 16, 64);
                 sum += __shfl_xor(sum, 32, 64);
-                if (is && g == 0) {
-                    const int64_t to = ((int64_t)mt * WM + wm) * a.part_ld + row;
-                    a.part_top[to] = top;
-                    a.part_sum[to] = sum;
+                if constexpr (WN > 1) {
+                    if (is && g == 0) a.part[((int64_t)mt * WM + wm) * a.part_ld + row] = Float2{top, sum};
+                } else {        // few rows: the waves' sums are put together first
+                    Float2 *all = reinterpret_cast<Float2 *>(lds);
+                    if (g == 0) all[(wm * TN + y) * 16 + lane] = Float2{top, sum};
+                    if (y == TN - 1) {
+                        __syncthreads();
+                        for (int i = threadIdx.x; i < 16 * TN; i += 64 * WM) {
+                            const int64_t to = n0 + i;
+                            Float2 x = all[i];
+                            for (int w = 1; w < WM; ++w) x = add_sums(x, all[w * TN * 16 + i]);
+                            if (to < kept) a.part[(int64_t)mt * a.part_ld + to] = x;
+                        }
+                    }
                 }
             } else if (is) {
                 const float from = a.lse[row] * LOG2E, scale = a.g[row];

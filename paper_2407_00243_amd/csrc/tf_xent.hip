@@ -227,44 +227,38 @@ template <int EL> __global__ __launch_bounds__(256) void k_pack_classes(const Xe
 
 // Adds the sums of `blocks` blocks of classes to those of the classes before them (unless `first`).  ROWS rows a workgroup: 64 / ROWS lanes of each of
 // its 16 waves take a row, and all of them every block once.  The last call writes the results.
-struct Sum {
-    float top, sum;
-    __device__ __forceinline__ void add(float t, float s) {
-        const float m = fmaxf(top, t);
-        sum = (top == kLow ? sum : sum * expf(top - m)) + (t == kLow ? s : s * expf(t - m));
-        top = m;
-    }
-};
+__device__ __forceinline__ void add_sums(Float2 &x, Float2 y) {
+    const float m = fmaxf(x[0], y[0]);
+    x = Float2{m, (x[0] == kLow ? x[1] : x[1] * expf(x[0] - m)) + (y[0] == kLow ? y[1] : y[1] * expf(y[0] - m))};
+}
 template <int ROWS> __global__ __launch_bounds__(1024) void k_merge(const XentLaunch a, const int64_t blocks, const int64_t ld, const int first, const int last) {
-    __shared__ float tops[16][ROWS], sums[16][ROWS];
+    __shared__ Float2 of_wave[16][ROWS];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int64_t row = (int64_t)blockIdx.x * ROWS + lane % ROWS;
     const int n = *a.s.n;
     if ((int64_t)blockIdx.x * ROWS >= n) return;
-    Sum x{kLow, 0.0f};
+    Float2 x{kLow, 0.0f};
     if (row < n)
 #pragma unroll 4
-        for (int64_t b = wave * (64 / ROWS) + lane / ROWS; b < blocks; b += 16 * (64 / ROWS)) x.add(a.s.part_top[b * ld + row], a.s.part_sum[b * ld + row]);
+        for (int64_t b = wave * (64 / ROWS) + lane / ROWS; b < blocks; b += 16 * (64 / ROWS)) add_sums(x, a.s.part[b * ld + row]);
 #pragma unroll
-    for (int d = ROWS; d < 64; d <<= 1) x.add(__shfl_xor(x.top, d, 64), __shfl_xor(x.sum, d, 64));
-    if (lane < ROWS) {
-        tops[wave][lane] = x.top;
-        sums[wave][lane] = x.sum;
-    }
+    for (int d = ROWS; d < 64; d <<= 1) add_sums(x, Float2{__shfl_xor(x[0], d, 64), __shfl_xor(x[1], d, 64)});
+    if (lane < ROWS) of_wave[wave][lane] = x;
     __syncthreads();
     if (wave || row >= n || lane >= ROWS) return;
-    x = first ? Sum{kLow, 0.0f} : Sum{a.s.top[row], a.s.sum[row]};
-    for (int w = 0; w < 16; ++w) x.add(tops[w][lane], sums[w][lane]);
+    x = first ? Float2{kLow, 0.0f} : Float2{a.s.top[row], a.s.sum[row]};
+    for (int w = 0; w < 16; ++w) add_sums(x, of_wave[w][lane]);
+    const float top = x[0], sum = x[1];
     if (!last) {
-        a.s.top[row] = x.top;
-        a.s.sum[row] = x.sum;
+        a.s.top[row] = top;
+        a.s.sum[row] = sum;
         return;
     }
     // `sum` is that of the other classes: a small loss keeps its precision as log(1 + sum / exp(label's logit))
-    const float hit = a.s.hit[row], lse = x.top + logf(x.sum + expf(hit - x.top));
+    const float hit = a.s.hit[row], lse = top + logf(sum + expf(hit - top));
     const int64_t to = a.s.list[row];
     a.lse[to] = lse;
-    a.loss[to] = x.top - hit < 40.0f ? log1pf(x.sum * expf(x.top - hit)) : lse - hit;
+    a.loss[to] = top - hit < 40.0f ? log1pf(sum * expf(top - hit)) : lse - hit;
 }
 
 // Rows `row` of an output from the sums of `splits` slabs, `none` for zeros.  A row's columns lie in `per_row` threads; the others of a workgroup take
@@ -277,15 +271,23 @@ template <int EL> __device__ __forceinline__ void finish_row(const float *slab, 
         const int64_t k = k0 + tid % per_row * 8;
         float x[8] = {};
         if (is && !none && k < n_in)
-#pragma unroll 4
-            for (int z = slice; z < splits; z += slices) {
-                const Float4 *p = reinterpret_cast<const Float4 *>(slab + z * size + k);
-                const Float4 lo = p[0], hi = p[1];
+            for (int z0 = slice; z0 < splits; z0 += 4 * slices) {
+                Float4 lo[4], hi[4];
 #pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    x[j] += lo[j];
-                    x[4 + j] += hi[j];
+                for (int i = 0; i < 4; ++i) {
+                    const int z = min(z0 + i * slices, splits - 1);
+                    const Float4 *p = reinterpret_cast<const Float4 *>(slab + z * size + k);
+                    lo[i] = p[0];
+                    hi[i] = p[1];
                 }
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    if (z0 + i * slices < splits)
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) {
+                            x[j] += lo[i][j];
+                            x[4 + j] += hi[i][j];
+                        }
             }
         if (by_slab) {
             __syncthreads();
@@ -307,7 +309,7 @@ template <int EL> __device__ __forceinline__ void finish_row(const float *slab, 
 constexpr int kManySlabs = 8;
 
 // dX: the shares' sums of each row that counts, zeros in the others.
-template <int EL> __global__ __launch_bounds__(256) void k_finish_rows(const XentLaunch a, const int splits, const int64_t size) {
+template <int EL> __global__ __launch_bounds__(256) void k_finish_rows(const XentLaunch a, const int splits, const int64_t size) {      // (the same for every piece)
     const float unit = *a.s.unit;
     const int per_row = threads_of_row(a.n_in);
     const bool by_slab = splits >= kManySlabs;
@@ -320,7 +322,8 @@ template <int EL> __global__ __launch_bounds__(256) void k_finish_rows(const Xen
     }
 }
 // Rows first .. first + count of dW.
-template <int EL> __global__ __launch_bounds__(256) void k_finish_classes(const XentLaunch a, const int64_t first, const int64_t count, const int splits, const int64_t size) {
+template <int EL> __global__ __launch_bounds__(256) void k_finish_classes(const XentLaunch a, const int64_t first, const int64_t count, const int most, const int64_t size) {
+    const int splits = shares_of(most, (int)ceil_div(*a.s.n, 64));
     const float unit = *a.s.unit;
     const int per_row = threads_of_row(a.n_in);
     const bool by_slab = splits >= kManySlabs;
@@ -339,6 +342,10 @@ dim3 row_grid(int64_t rows, int64_t columns) {
     const int64_t per_row = std::min<int64_t>(256, ceil_div(columns, 8));
     return dim3((unsigned)std::max<int64_t>(1, std::min<int64_t>(ceil_div(rows * per_row, 256), 8192)));
 }
+// The same for rows that are summed from slabs.
+dim3 slab_grid(int64_t rows, int64_t columns, int64_t splits) {
+    return splits >= kManySlabs ? dim3((unsigned)std::min<int64_t>(rows, 8192)) : row_grid(rows, columns);
+}
 #define TF_BY_TYPE(dtype, kernel, grid, ...)                                                                           \
     do {                                                                                                               \
         if (dtype == TF_BF16) hipLaunchKernelGGL((kernel<TF_BF16>), grid, dim3(256), 0, st, __VA_ARGS__);              \
@@ -356,12 +363,11 @@ bool in_place(const XentLaunch &a) {
            a.ldw <= kXentMaxColumns;
 }
 
-// Numbers and copies the rows that count.  (Also without rows: it sets the unit.)  Blocks of 32 rows, larger ones where there would be more than
-// kMostBlocks; up to 8192 rows every block counts the rows before it.
+// Numbers and copies the rows that count.  (Also without rows: it sets the unit.)  Up to 8192 rows every block counts the rows before it.
 int begin(const XentLaunch &a, hipStream_t st) {
-    const int64_t block = std::max<int64_t>(32, round_up(ceil_div(a.n_rows, kMostBlocks), 32));
-    const dim3 grid((unsigned)std::max<int64_t>(1, ceil_div(a.n_rows, block)));
     const int counted = a.n_rows > 8192;
+    const int64_t block = std::max<int64_t>(1, ceil_div(a.n_rows, kMostBlocks));
+    const dim3 grid((unsigned)std::max<int64_t>(1, ceil_div(a.n_rows, block)));
     if (counted) hipLaunchKernelGGL(k_count_rows, grid, dim3(256), 0, st, a, (int)block);
     TF_BY_TYPE(a.dtype, k_pack_rows, grid, a, (int)block, counted);
     return (int)hipGetLastError();
@@ -391,21 +397,39 @@ ProductLaunch logits(const XentLaunch &a, const Side &W, int64_t first, int64_t 
     return p;
 }
 
-// A tile of 256 x 256 where there are enough of them for the compute units, else smaller ones.  Few rows: all of them in one (the launch is bound by
-// reading the other operand), few classes or columns: all of them in one.
-ProductTile tile_for(int64_t m, int64_t n, bool rows) {
-    if (rows && n <= 16) return kTile16;
-    if (rows && (n <= 64 || m <= 128)) return kTile64;
-    return ceil_div(m, 256) * ceil_div(n, 256) >= 192 ? kTile256 : kTile128;
-}
 int64_t m_side(ProductTile t) { return t == kTile256 ? 256 : t == kTile16 ? 64 : 128; }
 int64_t n_side(ProductTile t) { return t == kTile256 ? 256 : t == kTile16 ? 16 : t == kTile64 ? 64 : 128; }
-// Sums that a tile of logits leaves of each row: one for each wave's rows of M.
-int64_t sums_of(ProductTile t) { return t == kTile256 || t == kTile128 ? 2 : 4; }
-// Shares of a contraction of `steps`, so that the launch has enough workgroups; each has four steps at least.
-int64_t shares(ProductTile t, int64_t m, int64_t n, int64_t steps, int64_t most) {
-    const int64_t groups = ceil_div(m, m_side(t)) * ceil_div(n, n_side(t)), want = t == kTile256 ? 256 : t == kTile16 ? 1024 : 512;
-    return std::max<int64_t>(1, std::min({want / groups, steps / 4, most}));
+// Sums that a tile of logits leaves of each row.
+int64_t sums_of(ProductTile t) { return t == kTile256 || t == kTile128 ? 2 : 1; }
+// How a product of m x n, `steps` steps of 64 long (each made of `pairs` pairs of parts), is launched: its tile, and the shares of its contraction (`most` of them at most; 0: it cannot be cut).
+// Few rows: all of them in a tile (the launch is bound by reading the other operand), few classes or columns: all of them in one.  Otherwise
+// tiles of 256 x 256, one workgroup a compute unit, or of 128 x 128, two of them, whichever is expected to take less time: tenths of a microsecond,
+// fitted to ten sizes from 2048 x 2048 x 2048 to 8192 x 32768 x 4096, bf16 (which they meet within a fifth).  One as large as
+// 8192 x 32768 x 4096 takes 1.61 ms with large tiles and 1.77 with small ones, 1024 x 40960 x 1024 105 us and 91.
+struct Cut {
+    ProductTile tile;
+    int64_t shares;
+};
+Cut cut_product(int64_t m, int64_t n, int64_t steps, int pairs, bool rows, int64_t most) {
+    most = std::max<int64_t>(1, std::min(most, steps / 4));       // (a share has four steps at least)
+    n = std::max<int64_t>(n, 1);
+    if (rows && (n <= 64 || m <= 128)) {
+        const ProductTile t = n <= 16 ? kTile16 : kTile64;
+        const int64_t groups = ceil_div(m, m_side(t)) * ceil_div(n, n_side(t)), want = t == kTile16 ? 1024 : 512;
+        return Cut{t, std::max<int64_t>(1, std::min(want / groups, most))};
+    }
+    Cut best{kTile128, 1};
+    double least = 0;
+    for (const ProductTile t : {kTile256, kTile128})
+        for (int64_t s = 1; s <= std::min<int64_t>(most, 512); s = s < 8 ? s + 1 : s * 5 / 4) {
+            const double rounds = (double)ceil_div(ceil_div(m, m_side(t)) * ceil_div(n, n_side(t)) * s, 256), each = (double)steps * pairs / s;
+            const double time = (t == kTile256 ? rounds * (14 * each + 130) : std::max(4 * rounds, 6.0) * each + 18 * rounds + 80) + (s > 1 ? (double)s * m * n / 50000 : 0.0);
+            if (least == 0 || time < least) {
+                best = Cut{t, s};
+                least = time;
+            }
+        }
+    return best;
 }
 
 }  // namespace
@@ -414,18 +438,16 @@ int launch_xent(const XentLaunch &a, void *stream) {
     const hipStream_t st = static_cast<hipStream_t>(stream);
     int e = begin(a, st);
     if (e || a.n_rows == 0) return e;
-    const int64_t ld = round_up(a.n_rows, 256);
-    // (tiles of few rows leave a sum for every 16 classes, those of few classes for every 32, others for 64 or 128)
-    int64_t piece = a.s.part_cap / ld * (a.n_rows <= 16 ? 16 : a.n_rows <= 64 || a.n_classes <= 128 ? 32 : 64) / 256 * 256;
+    const int64_t ld = round_up(a.n_rows, 16);
+    int64_t piece = a.s.part_cap / ld * 64 / 256 * 256;       // (a sum of every 64 classes at the most)
     if (!in_place(a)) piece = std::min(piece, a.s.w_cap / a.s.ld);
     for (int64_t first = 0; first < a.n_classes; first += piece) {
         const int64_t count = std::min<int64_t>(piece, a.n_classes - first);
         ProductLaunch p = logits(a, classes(a, first, count, st), first, count);
-        p.tile = tile_for(count, a.n_rows, true);
+        p.tile = cut_product(count, a.n_rows, p.k_steps, p.parts == 3 ? 6 : 1, true, 0).tile;
         p.end = kEndSums;
         p.hit = a.s.hit;
-        p.part_top = a.s.part_top;
-        p.part_sum = a.s.part_sum;
+        p.part = a.s.part;
         p.part_ld = ld;
         e = launch_product(p, a.dtype, stream);
         if (e) return e;
@@ -447,12 +469,11 @@ int launch_xent_grad(const XentLaunch &call, void *stream) {
     int64_t piece = std::min(round_up(a.n_classes, 256), (a.s.g_cap / rows - kRowPad) / 256 * 256);
     if (!in_place(a)) piece = std::min(piece, a.s.w_cap / a.s.ld);
     const int64_t g_ld = piece + kRowPad;
-    const int parts = a.dtype == TF_F32 ? 3 : 1;
+    const int parts = a.dtype == TF_F32 ? 3 : 1, pairs = parts == 3 ? 6 : 1;
     const int64_t dx_size = rows * a.s.ld;
     // (the same shares for every piece: the slabs are added to)
-    const ProductTile dx_tile = tile_for(a.n_in, a.n_rows, true);
-    const int64_t dx_shares = a.dX && a.n_rows ? shares(dx_tile, a.n_in, a.n_rows, ceil_div(std::min<int64_t>(piece, a.n_classes), 64), a.s.dx_cap / dx_size) : 1;
-    a.direct_dx = piece >= a.n_classes && dx_shares == 1;
+    const Cut dx = cut_product(a.n_in, a.n_rows, ceil_div(std::min<int64_t>(piece, a.n_classes), 64), pairs, true, a.s.dx_cap / dx_size);
+    a.direct_dx = piece >= a.n_classes && dx.shares == 1;
     int e = begin(a, st);
     if (e) return e;
     for (int64_t first = 0; first < a.n_classes; first += piece) {
@@ -460,7 +481,7 @@ int launch_xent_grad(const XentLaunch &call, void *stream) {
         if (a.n_rows) {
             const Side W = classes(a, first, count, st);
             ProductLaunch p = logits(a, W, first, count);
-            p.tile = tile_for(count, a.n_rows, true);
+            p.tile = cut_product(count, a.n_rows, p.k_steps, p.parts == 3 ? 6 : 1, true, 0).tile;
             p.end = kEndGradient;
             p.lse = a.s.lse;
             p.g = a.s.g;
@@ -485,8 +506,8 @@ int launch_xent_grad(const XentLaunch &call, void *stream) {
                 q.ldo = a.lddx;
                 q.out_row = a.s.list;
                 q.out_dtype = a.dtype;
-                q.tile = dx_tile;
-                q.splits = (int32_t)dx_shares;
+                q.tile = dx.tile;
+                q.splits = (int32_t)dx.shares;
                 q.slab = a.s.dx;
                 q.slab_ld = a.s.ld;
                 q.slab_size = dx_size;
@@ -504,9 +525,10 @@ int launch_xent_grad(const XentLaunch &call, void *stream) {
             q.k_rows = 1;
             q.m_count = a.n_in;
             q.n_count = (int32_t)count;
-            q.tile = tile_for(a.n_in, count, false);
             const int64_t size = round_up(count, 256) * a.s.ld;
-            q.splits = (int32_t)shares(q.tile, a.n_in, count, ceil_div(a.n_rows, 64), a.s.dw_cap / size);
+            const Cut dw = cut_product(a.n_in, count, ceil_div(a.n_rows, 64), pairs, false, a.s.dw_cap / size);
+            q.tile = dw.tile;
+            q.splits = (int32_t)dw.shares;
             q.unit = a.s.unit;
             q.out = static_cast<char *>(a.dW) + first * a.lddw * (a.dtype == TF_F32 ? 4 : 2);
             q.ldo = a.lddw;
@@ -517,10 +539,10 @@ int launch_xent_grad(const XentLaunch &call, void *stream) {
             q.end = q.splits > 1 ? kEndSlab : kEndOut;
             e = launch_product(q, a.dtype, stream);
             if (e) return e;
-            if (q.splits > 1) TF_BY_TYPE(a.dtype, k_finish_classes, row_grid(count, a.n_in), a, first, count, q.splits, size);
+            if (q.splits > 1) TF_BY_TYPE(a.dtype, k_finish_classes, slab_grid(count, a.n_in, q.splits), a, first, count, q.splits, size);
         }
     }
-    if (a.dX && a.n_rows && !a.direct_dx) TF_BY_TYPE(a.dtype, k_finish_rows, row_grid(a.n_rows, a.n_in), a, (int)dx_shares, dx_size);
+    if (a.dX && a.n_rows && !a.direct_dx) TF_BY_TYPE(a.dtype, k_finish_rows, slab_grid(a.n_rows, a.n_in, dx.shares), a, (int)dx.shares, dx_size);
     return (int)hipGetLastError();
 }
 
