@@ -8,10 +8,59 @@ namespace tf {
 namespace {
 
 constexpr float kLow = -__builtin_inff();
+typedef int Int4 __attribute__((ext_vector_type(4)));
+
+// Sums and maxima over 2, 4, 8 or 16 neighbouring lanes take one instruction for each doubling (the neighbours' values come with it: lane ^ 1,
+// lane ^ 2, then mirror images of eight and sixteen lanes); 32 and 64 lanes exchange rows of sixteen and halves.
+template <int CONTROL> __device__ __forceinline__ float from_lane(float x) {
+    return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), CONTROL, 0xf, 0xf, true));
+}
+struct Plus {
+    static __device__ __forceinline__ float of(float x, float y) { return x + y; }
+};
+struct Larger {
+    static __device__ __forceinline__ float of(float x, float y) { return fmaxf(x, y); }
+};
+template <int L, typename F> __device__ __forceinline__ float over_lanes(float x) {
+    if constexpr (L >= 2) x = F::of(x, from_lane<0xb1>(x));
+    if constexpr (L >= 4) x = F::of(x, from_lane<0x4e>(x));
+    if constexpr (L >= 8) x = F::of(x, from_lane<0x141>(x));
+    if constexpr (L >= 16) x = F::of(x, from_lane<0x140>(x));
+    if constexpr (L >= 32) {
+        const uint32_t u = __float_as_uint(x);
+        const auto y = __builtin_amdgcn_permlane16_swap(u, u, false, false);
+        x = F::of(__uint_as_float(y[0]), __uint_as_float(y[1]));
+    }
+    if constexpr (L >= 64) {
+        const uint32_t u = __float_as_uint(x);
+        const auto y = __builtin_amdgcn_permlane32_swap(u, u, false, false);
+        x = F::of(__uint_as_float(y[0]), __uint_as_float(y[1]));
+    }
+    return x;
+}
+
+// The sum over the lanes that are a multiple of L apart: rotations of sixteen lanes, then rows and halves as above.
+template <int L> __device__ __forceinline__ float over_groups(float x) {
+    if constexpr (L <= 8) x += from_lane<0x128>(x);
+    if constexpr (L <= 4) x += from_lane<0x124>(x);
+    if constexpr (L <= 2) x += from_lane<0x122>(x);
+    if constexpr (L <= 1) x += from_lane<0x121>(x);
+    if constexpr (L <= 16) {
+        const uint32_t u = __float_as_uint(x);
+        const auto y = __builtin_amdgcn_permlane16_swap(u, u, false, false);
+        x = __uint_as_float(y[0]) + __uint_as_float(y[1]);
+    }
+    if constexpr (L <= 32) {
+        const uint32_t u = __float_as_uint(x);
+        const auto y = __builtin_amdgcn_permlane32_swap(u, u, false, false);
+        x = __uint_as_float(y[0]) + __uint_as_float(y[1]);
+    }
+    return x;
+}
 
 // A row of scores lies in L lanes; lane i of them holds NV chunks of sixteen bytes, chunk i + L c: VEC consecutive experts each.
 template <int EL, int L, int NV> struct Row {
-    static constexpr int VEC = EL == TF_F32 ? 4 : 8, N = VEC * NV, ROWS = 64 / L;
+    static constexpr int VEC = EL == TF_F32 ? 4 : 8, N = VEC * NV, LANES = L, ROWS = 64 / L;
     typedef typename El<EL>::T T;
 
     static __device__ __forceinline__ int expert(int lane, int i) { return ((lane & (L - 1)) + L * (i / VEC)) * VEC + i % VEC; }
@@ -44,36 +93,30 @@ template <int EL, int L, int NV> struct Row {
         for (int i = 0; i < N; ++i) {
             float x;
             if constexpr (EL == TF_F32) x = __uint_as_float(r.c[i / VEC][i % VEC]);
+            else if constexpr (EL == TF_BF16) x = i & 1 ? bf16_high(r.c[i / VEC][i % VEC / 2]) : bf16_low(r.c[i / VEC][i % VEC / 2]);
             else x = El<EL>::get((uint16_t)(r.c[i / VEC][i % VEC / 2] >> (16 * (i & 1))));
-            l[i] = expert(lane, i) < n_experts && !__builtin_isnan(x) ? x : kLow;
+            l[i] = __builtin_isnan(x) ? kLow : x;
+        }
+        if (n_experts < L * N)
+#pragma unroll
+            for (int i = 0; i < N; ++i)
+                if (expert(lane, i) >= n_experts) l[i] = kLow;
+    }
+    static __device__ __forceinline__ void store_chunk(T *row, const float (&d)[VEC], int c, int lane, int n_experts) {
+        const int e = expert(lane, c * VEC);
+        AnyWords4 w{0, 0, 0, 0};
+#pragma unroll
+        for (int j = 0; j < VEC; ++j) put(w, j, El<EL>::put(d[j]));
+        if (e + VEC <= n_experts) {
+            *reinterpret_cast<AnyWords4 *>(row + e) = w;
+        } else if (e < n_experts) {
+#pragma unroll
+            for (int j = 0; j < VEC; ++j)
+                if (e + j < n_experts) row[e + j] = El<EL>::put(d[j]);
         }
     }
-    static __device__ __forceinline__ void store(T *row, const float (&d)[N], int lane, int n_experts) {
-#pragma unroll
-        for (int c = 0; c < NV; ++c) {
-            const int e = expert(lane, c * VEC);
-            AnyWords4 w{0, 0, 0, 0};
-#pragma unroll
-            for (int j = 0; j < VEC; ++j) put(w, j, El<EL>::put(d[c * VEC + j]));
-            if (e + VEC <= n_experts) {
-                *reinterpret_cast<AnyWords4 *>(row + e) = w;
-            } else if (e < n_experts) {
-#pragma unroll
-                for (int j = 0; j < VEC; ++j)
-                    if (e + j < n_experts) row[e + j] = El<EL>::put(d[c * VEC + j]);
-            }
-        }
-    }
-    static __device__ __forceinline__ float sum(float x) {
-#pragma unroll
-        for (int d = L / 2; d; d >>= 1) x += __shfl_xor(x, d, 64);
-        return x;
-    }
-    static __device__ __forceinline__ float max(float x) {
-#pragma unroll
-        for (int d = L / 2; d; d >>= 1) x = fmaxf(x, __shfl_xor(x, d, 64));
-        return x;
-    }
+    static __device__ __forceinline__ float sum(float x) { return over_lanes<L, Plus>(x); }
+    static __device__ __forceinline__ float max(float x) { return over_lanes<L, Larger>(x); }
     // Whether it is true in any of the row's lanes.
     static __device__ __forceinline__ bool any(bool x) {
         const uint64_t b = __ballot(x) >> (threadIdx.x & 63 & ~(L - 1));
@@ -81,340 +124,505 @@ template <int EL, int L, int NV> struct Row {
     }
 };
 
-// What sigmoids need of a score: sigma = 1 / (1 + exp(-l)) and 1 - sigma, neither of which overflows or cancels.  (The reciprocal is
+// Exponentials are powers of two: exp(x) = 2^(x log2(e)), one instruction after a multiplication that is off by 2^-24 of x.
+constexpr float kLog2E = 1.44269504088896340736f;
+__device__ __forceinline__ float exp_of(float x) { return __builtin_amdgcn_exp2f(x * kLog2E); }
+
+// What sigmoids need of a score: sigma = 1 / (1 + exp(-l)) and sigma (1 - sigma), neither of which overflows or cancels.  (The reciprocal is
 // good to a unit of 2^-23.)
-__device__ __forceinline__ void sigmoid(float l, float &s, float &rest) {
-    const float t = expf(-fabsf(l)), r = __builtin_amdgcn_rcpf(1.0f + t);
-    s = l >= 0.0f ? r : t * r;
-    rest = l >= 0.0f ? t * r : r;
+__device__ __forceinline__ void sigmoid(float l, float &s, float &slope) {
+    const float t = exp_of(-fabsf(l)), r = __builtin_amdgcn_rcpf(1.0f + t), tr = t * r;
+    s = l >= 0.0f ? r : tr;
+    slope = r * tr;
 }
 
-// Numerators n_e of the shares n_e / sum n: exp(l_e - top) or sigma(l_e), the latter over exp(top) where all of them are small.  `top` is
-// the largest score that counts (min(l, 0) for sigmoids), which is what keeps a sum from being 0; `rest` = 1 - sigma.
-template <int N> __device__ __forceinline__ void numerators(float (&n)[N], const float (&l)[N], const float (&s)[N], bool sigmoids, float top) {
-    if (sigmoids) {
-        const bool small = top < -40.0f;
+// Shares are n_e / sum n with numerators n_e = exp(l_e - top), top the row's largest score, or sigma(l_e).  Where the latter are all so small that their
+// sum says little (scores below -40), and where a bias has selected experts whose numerators are that small, they are taken again over the
+// exponential of the largest score that counts: exp(min(l, 0) - top) / (1 + exp(-|l|)), and `slope`, sigma (1 - sigma), likewise.
+constexpr float kSmall = 1e-17f;
+template <bool SIGMOIDS> __device__ __forceinline__ float bounded(float l) { return SIGMOIDS ? fminf(l, 0.0f) : l; }
+template <bool SIGMOIDS> __device__ __forceinline__ void numerator_over(float l, float top, float &n, float &slope) {
+    const float r = SIGMOIDS ? __builtin_amdgcn_rcpf(1.0f + exp_of(-fabsf(l))) : 1.0f;
+    n = l > kLow ? exp_of(bounded<SIGMOIDS>(l) - top) * r : 0.0f;
+    slope = SIGMOIDS ? n * exp_of(fminf(-l, 0.0f)) * r : n;
+}
+// Numerators of all of a row's scores, their slopes, their sum, and whether they are over an exponential.  (The scores are taken from their chunks again where they are needed again:
+// registers are what limits the number of waves.)
+template <typename R, bool SIGMOIDS>
+__device__ __forceinline__ float numerators(float (&n)[R::N], float (&slope)[R::N], const typename R::Raw &raw, int lane, int n_experts, bool &scaled) {
+    float total = 0.0f, l[R::N];
+    scaled = false;
+    R::unpack(l, raw, lane, n_experts);
+    if constexpr (SIGMOIDS) {
 #pragma unroll
-        for (int i = 0; i < N; ++i) n[i] = s[i];
-        if (__ballot(small)) {
+        for (int i = 0; i < R::N; ++i) {
+            sigmoid(l[i], n[i], slope[i]);
+            total += n[i];
+        }
+        total = R::sum(total);
+        scaled = total < kSmall;
+        if (__ballot(scaled)) {
+            float top = kLow;
+            R::unpack(l, raw, lane, n_experts);
 #pragma unroll
-            for (int i = 0; i < N; ++i)
-                if (small) n[i] = l[i] > kLow ? expf(fminf(l[i], 0.0f) - top) * __builtin_amdgcn_rcpf(1.0f + expf(-fabsf(l[i]))) : 0.0f;
+            for (int i = 0; i < R::N; ++i) top = fmaxf(top, fminf(l[i], 0.0f));
+            top = R::max(top);
+            float again = 0.0f;
+#pragma unroll
+            for (int i = 0; i < R::N; ++i) {
+                float x, y;
+                numerator_over<true>(l[i], top, x, y);
+                again += x;
+                n[i] = scaled ? x : n[i];
+                slope[i] = scaled ? y : slope[i];
+            }
+            again = R::sum(again);
+            total = scaled ? again : total;
         }
     } else {
+        float top = kLow;
 #pragma unroll
-        for (int i = 0; i < N; ++i) n[i] = l[i] > kLow ? expf(l[i] - top) : 0.0f;
+        for (int i = 0; i < R::N; ++i) top = fmaxf(top, l[i]);
+        top = R::max(top);
+        const float from = top > kLow ? top : 0.0f;
+#pragma unroll
+        for (int i = 0; i < R::N; ++i) {
+            n[i] = slope[i] = exp_of(l[i] - from);
+            total += n[i];
+        }
+        total = R::sum(total);
     }
+    return total;
 }
 
 __device__ __forceinline__ float over(float x, float total) { return total == 0.0f ? 0.0f : x / total; }
 
 // ---------------------------------------------------------------------------------------- balance
 
-// loss = E sum_e f_e mass_e from the sums of `groups` workgroups, added up in their order: 1024 threads, each an expert and every
-// (1024 / experts)-th workgroup.
-struct Finish {
-    float mass[1024];
-    int count[1024];
-    float part[16];
-    int named[16], rows[16];
-};
-__device__ void finish(const RouterLaunch &a, int groups, Finish &sh) {
-    const int E = a.n_experts, tid = threadIdx.x, threads = blockDim.x;
-    const float *mass = static_cast<const float *>(a.workspace);
-    const int *count = reinterpret_cast<const int *>(mass + (int64_t)kBalanceGroups * E);
-    const int *rows = count + (int64_t)kBalanceGroups * E;
-    const int slices = threads / E;
-    float m = 0.0f;
-    int c = 0, r = 0;
-    if (tid < slices * E) {
-        const int e = tid % E;
-#pragma unroll 8
-        for (int g = tid / E; g < groups; g += slices) {
-            m += mass[g * E + e];
-            c += count[g * E + e];
-        }
-    }
-    for (int g = tid; g < groups; g += threads) r += rows[g];
-    sh.mass[tid] = m;
-    sh.count[tid] = c;
-    __syncthreads();
-    m = 0.0f, c = 0;
-    if (tid < E)
-        for (int s = 0; s < slices; ++s) {
-            m += sh.mass[s * E + tid];
-            c += sh.count[s * E + tid];
-        }
-    float x = m * (float)c;
-    int named = c;
+// The end of it: thread e has the sum of expert e's shares and its count, `rows` are the rows of this thread's.  loss = E sum_e f_e mass_e.
+__device__ __forceinline__ int wave_total(int x) {
 #pragma unroll
-    for (int d = 32; d; d >>= 1) {
-        x += __shfl_xor(x, d, 64);
-        named += __shfl_xor(named, d, 64);
-        r += __shfl_xor(r, d, 64);
-    }
+    for (int d = 32; d; d >>= 1) x += __shfl_xor(x, d, 64);
+    return x;
+}
+__device__ void write_balance(const RouterLaunch &a, float m, int c, int rows) {
+    __shared__ float part[16];
+    __shared__ int named_of[16], rows_of[16];
+    const int E = a.n_experts, tid = threadIdx.x;
+    const float x = over_lanes<64, Plus>(m * (float)c);
+    const int named = wave_total(c), r = wave_total(rows);
     if ((tid & 63) == 0) {
-        sh.part[tid >> 6] = x;
-        sh.named[tid >> 6] = named;
-        sh.rows[tid >> 6] = r;
+        part[tid >> 6] = x;
+        named_of[tid >> 6] = named;
+        rows_of[tid >> 6] = r;
     }
     __syncthreads();
-    x = 0.0f, named = 0, r = 0;
-    for (int w = 0; w < threads / 64; ++w) {
-        x += sh.part[w];
-        named += sh.named[w];
-        r += sh.rows[w];
+    float sum = 0.0f;
+    int n = 0, all = 0;
+    for (int w = 0; w < (int)blockDim.x / 64; ++w) {
+        sum += part[w];
+        all += named_of[w];
+        n += rows_of[w];
     }
     if (tid < E) {
         a.counts[tid] = c;
-        a.mass[tid] = r ? m / (float)r : 0.0f;
+        a.mass[tid] = n ? m / (float)n : 0.0f;
     }
     if (tid == 0) {
-        a.counts[E] = r;
-        a.loss[0] = r ? (float)E * x / ((float)named * (float)r) : 0.0f;
+        a.counts[E] = n;
+        a.loss[0] = n ? (float)E * sum / ((float)all * (float)n) : 0.0f;
     }
 }
 
+// Adds up the sums of `groups` workgroups in a fixed order: 1024 threads, each four experts and every (1024 / (experts / 4))-th workgroup.
 __global__ __launch_bounds__(1024) void k_balance_finish(const RouterLaunch a, const int groups) {
-    __shared__ Finish sh;
-    finish(a, groups, sh);
+    __shared__ Float4 masses[1024];
+    __shared__ Int4 counts[1024];
+    const int tid = threadIdx.x, fours = balance_row(a.n_experts) / 4, slices = 1024 / fours;
+    const Float4 *mass = static_cast<const Float4 *>(a.workspace);
+    const Int4 *count = reinterpret_cast<const Int4 *>(mass + (int64_t)kBalanceGroups * fours);
+    const int *rows = reinterpret_cast<const int *>(count + (int64_t)kBalanceGroups * fours);
+    Float4 m = {0, 0, 0, 0};
+    Int4 c = {0, 0, 0, 0};
+    if (tid < slices * fours) {
+        const int e = tid % fours;
+#pragma unroll 8
+        for (int g = tid / fours; g < groups; g += slices) {
+            m += mass[g * fours + e];
+            c += count[g * fours + e];
+        }
+    }
+    const int r = tid < groups ? rows[tid] : 0;
+    masses[tid] = m;
+    counts[tid] = c;
+    __syncthreads();
+    float me = 0.0f;
+    int ce = 0;
+    if (tid < a.n_experts)
+        for (int s = 0; s < slices; ++s) {
+            me += masses[s * fours + tid / 4][tid % 4];
+            ce += counts[s * fours + tid / 4][tid % 4];
+        }
+    write_balance(a, me, ce, r);
 }
 
+// What a row needs from memory: its scores, and of its entries first, first + L, ... (kEntries of them at a time) the columns and, with GRADIENTS, the
+// gradients of their values.
+constexpr int kEntries = 4;
+template <typename R, bool GRADIENTS> struct Input {
+    typename R::Raw raw;
+    int c[kEntries];
+    float x[kEntries];
+    __device__ __forceinline__ void entries(const RouterLaunch &a, int64_t t, int first, int at) {
+#pragma unroll
+        for (int j = 0; j < kEntries; ++j) {
+            c[j] = -1;
+            if (first + j * R::LANES >= a.k) break;        // (the same for all lanes)
+            const int i = first + j * R::LANES + at;
+            if (t < a.n_tokens && i < a.k) {
+                c[j] = a.colidx[t * a.k + i];
+                if (GRADIENTS && a.dvals) x[j] = a.dvals[t * a.k + i];
+            }
+        }
+    }
+    __device__ __forceinline__ void load(const RouterLaunch &a, int64_t t, int lane) {
+        if (t < a.n_tokens) R::load(raw, static_cast<const typename R::T *>(a.scores) + t * a.ld, lane, a.n_experts);
+        entries(a, t, 0, lane & (R::LANES - 1));
+    }
+    __device__ __forceinline__ bool is(const RouterLaunch &a, int j) const { return c[j] >= 0 && c[j] < a.n_experts; }
+};
+
 // Every wave takes ROWS tokens at a time and adds up their shares in registers; entries are counted in LDS (whole numbers: their order
-// does not matter).
-template <int EL, int L, int NV> __global__ __launch_bounds__(1024) void k_balance(const RouterLaunch a) {
+// does not matter).  LDS holds the counts, and at the end a line of sums for each wave.
+template <int EL, int L, int NV, bool SIGMOIDS> __global__ __launch_bounds__(1024) void k_balance(const RouterLaunch a) {
     typedef Row<EL, L, NV> R;
-    __shared__ union {
-        struct {
-            float mass[1024];
-            int count[1024];
-            int rows;
-        } own;
-        Finish fin;
-    } sh;
-    const int E = a.n_experts, lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
+    extern __shared__ __attribute__((aligned(16))) int shared[];
+    const int E = a.n_experts, line = balance_row(E), lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
+    int *counted = shared, *rows_of = shared + line;
+    float *masses = reinterpret_cast<float *>(shared + line + 16);
     const int sub = lane / L, at = lane & (L - 1);
-    const bool sigmoids = a.scoring == TF_ROUTE_SIGMOID || a.scoring == TF_ROUTE_SIGMOID_TOP;
-    for (int e = threadIdx.x; e < 1024; e += blockDim.x) sh.own.count[e] = 0;
+    for (int e = threadIdx.x; e < line; e += blockDim.x) counted[e] = 0;
     __syncthreads();
     float mass[R::N] = {};
     int rows = 0;
     const int64_t step = (int64_t)gridDim.x * waves * R::ROWS;
-    typename R::Raw raw{}, next{};
     int64_t t = ((int64_t)blockIdx.x * waves + wave) * R::ROWS + sub;
-    const typename R::T *scores = static_cast<const typename R::T *>(a.scores);
-    if (t < a.n_tokens) R::load(next, scores + t * a.ld, lane, E);
-    for (int64_t base = t - sub; base < a.n_tokens; base += step, t += step) {
-        raw = next;
-        if (t + step < a.n_tokens) R::load(next, scores + (t + step) * a.ld, lane, E);
+    Input<R, false> in[2];
+    in[0].load(a, t, lane);
+    in[1].load(a, t + step, lane);
+    auto row = [&](Input<R, false> &in) {
+        const typename R::Raw raw = in.raw;
         bool named = false;
-        if (t < a.n_tokens)
-            for (int i = at; i < a.k; i += L) {
-                const int c = a.colidx[t * a.k + i];
-                if (c >= 0 && c < E) {
+        for (int first = 0;;) {
+#pragma unroll
+            for (int j = 0; j < kEntries; ++j) {
+                if (first + j * L >= a.k) break;
+                if (in.is(a, j)) {
                     named = true;
-                    atomicAdd(&sh.own.count[c], 1);
+                    atomicAdd(counted + in.c[j], 1);
                 }
             }
+            first += kEntries * L;
+            if (first >= a.k) break;
+            in.entries(a, t, first, at);
+        }
+        in.load(a, t + 2 * step, lane);
         named = R::any(named);
         rows += named;
-        float l[R::N], s[R::N], n[R::N], rest, top = kLow, total = 0.0f;
-        R::unpack(l, raw, lane, E);
-#pragma unroll
-        for (int i = 0; i < R::N; ++i) {
-            if (sigmoids) sigmoid(l[i], s[i], rest);
-            top = fmaxf(top, sigmoids ? fminf(l[i], 0.0f) : l[i]);
-        }
-        numerators(n, l, s, sigmoids, R::max(top));
-#pragma unroll
-        for (int i = 0; i < R::N; ++i) total += n[i];
-        total = R::sum(total);
+        float n[R::N], slope[R::N];
+        bool scaled;
+        const float total = numerators<R, SIGMOIDS>(n, slope, raw, lane, E, scaled);
         const float each = named ? over(1.0f, total) : 0.0f;
         if (named)
 #pragma unroll
             for (int i = 0; i < R::N; ++i) mass[i] += n[i] * each;
+    };
+    for (int64_t base = t - sub; base < a.n_tokens; base += 2 * step) {
+        row(in[0]);
+        t += step;
+        if (base + step < a.n_tokens) row(in[1]);
+        t += step;
     }
     // rows of a wave, then waves in their order
 #pragma unroll
-    for (int d = L; d < 64; d <<= 1) {
+    for (int i = 0; i < R::N; ++i) mass[i] = over_groups<L>(mass[i]);
+    rows = wave_total(at == 0 ? rows : 0);
+    if (sub == 0) {
 #pragma unroll
-        for (int i = 0; i < R::N; ++i) mass[i] += __shfl_xor(mass[i], d, 64);
-        rows += __shfl_xor(rows, d, 64);
-    }
-    for (int w = 0; w < waves; ++w) {
-        if (w == wave && sub == 0) {
-#pragma unroll
-            for (int i = 0; i < R::N; ++i) {
-                const int e = R::expert(lane, i);
-                if (e < E) sh.own.mass[e] = w ? sh.own.mass[e] + mass[i] : mass[i];
-            }
-            if (at == 0) sh.own.rows = w ? sh.own.rows + rows : rows;
+        for (int i = 0; i < R::N; ++i) {
+            const int e = R::expert(lane, i);
+            if (e < E) masses[wave * line + e] = mass[i];
         }
-        __syncthreads();
+        if (lane == 0) rows_of[wave] = rows;
     }
+    __syncthreads();
+    const int e = threadIdx.x;
+    float m = 0.0f;
+    if (e < E)
+        for (int w = 0; w < waves; ++w) m += masses[w * line + e];
+    const int c = e < E ? counted[e] : 0, r = e < waves ? rows_of[e] : 0;
+    if (gridDim.x == 1) return write_balance(a, m, c, r);
     float *out = static_cast<float *>(a.workspace);
-    int *count = reinterpret_cast<int *>(out + (int64_t)kBalanceGroups * E);
-    for (int e = threadIdx.x; e < E; e += blockDim.x) {
-        out[blockIdx.x * E + e] = sh.own.mass[e];
-        count[blockIdx.x * E + e] = sh.own.count[e];
+    int *count = reinterpret_cast<int *>(out + (int64_t)kBalanceGroups * line);
+    if (e < line) {
+        out[blockIdx.x * line + e] = m;
+        count[blockIdx.x * line + e] = c;
     }
-    if (threadIdx.x == 0) count[(int64_t)kBalanceGroups * E + blockIdx.x] = sh.own.rows;
-    if (gridDim.x == 1) {        // few tokens: one launch
-        __syncthreads();
-        finish(a, 1, sh.fin);
+    if (wave == 0) {
+        const int all = wave_total(r);
+        if (lane == 0) count[(int64_t)kBalanceGroups * line + blockIdx.x] = all;
     }
 }
 
 // --------------------------------------------------------------------------------------- gradient
 
-template <int EL, int L, int NV> __global__ __launch_bounds__(256) void k_route_grad(const RouterLaunch a) {
+// With q the shares (over all experts, or over the named ones) and n' the slopes of their numerators, every kind of gradient is
+//     d_e = n'_e (A (f_e - sum_j p_j f_j) + B (g_e - m_e sum_j q_j g_j)),
+// g_e the sum of the gradients of a row's entries that name e, m_e their number; A, B over the sums of the numerators.
+// The entries of a row meet its scores in LDS: each puts its gradient and a one where its expert's are, and the lanes that hold the scores find
+// them there, or zeros.  (They read them, and f, twice: registers hold two numbers a score and what comes from memory next.)  Where a row names an
+// expert more than once one lane adds its entries up instead.  A wave has no barrier: its instructions of LDS are done in their order.
+__device__ __forceinline__ void in_order() { asm volatile("" ::: "memory"); }
+
+template <int EL, int L, int NV, bool SIGMOIDS> __global__ __launch_bounds__(256, NV * (EL == TF_F32 ? 4 : 8) > 8 ? 2 : 4) void k_route_grad(const RouterLaunch a) {
     typedef Row<EL, L, NV> R;
+    constexpr int VEC = R::VEC;
+    __shared__ __attribute__((aligned(16))) Float2 places[4][64 * R::N];
+    __shared__ __attribute__((aligned(16))) float named_share[L * R::N];
     const int E = a.n_experts, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int sub = lane / L, at = lane & (L - 1);
-    const bool sigmoids = a.scoring == TF_ROUTE_SIGMOID || a.scoring == TF_ROUTE_SIGMOID_TOP;
-    const bool over_all = a.dloss || a.scoring == TF_ROUTE_SOFTMAX;
-    // shares of the entries that name an expert, and what a share's gradient is multiplied by
-    float f[R::N], factor = 0.0f;
-    if (a.dloss) {
-        float named = 0.0f;
+    const bool top_only = a.scoring == TF_ROUTE_SOFTMAX_TOP || a.scoring == TF_ROUTE_SIGMOID_TOP, sigmoid_only = a.scoring == TF_ROUTE_SIGMOID;
+    Float2 *own = places[wave] + sub * L * R::N;       // of this lane's row
+#pragma unroll
+    for (int i = 0; i < R::N; ++i) places[wave][i * 64 + lane] = Float2{0.0f, 0.0f};
+    // f: shares of the entries that name an expert; and what a share's gradient is multiplied by
+    float factor = 0.0f;
+    {
+        float f[R::N], named = 0.0f;
 #pragma unroll
         for (int i = 0; i < R::N; ++i) {
             const int e = R::expert(lane, i);
-            f[i] = e < E ? (float)a.counts[e] : 0.0f;
+            f[i] = a.dloss && e < E ? (float)a.counts[e] : 0.0f;
             named += f[i];
         }
-        named = R::sum(named);
+        named = over(1.0f, R::sum(named));
+        if (threadIdx.x < L)
 #pragma unroll
-        for (int i = 0; i < R::N; ++i) f[i] = over(f[i], named);
-        factor = over(a.dloss[0] * (float)E, (float)a.counts[E]);
+            for (int i = 0; i < R::N; ++i) named_share[R::expert(lane, i)] = f[i] * named;
+        if (a.dloss) factor = over(a.dloss[0] * (float)E, (float)a.counts[E]);
     }
+    __syncthreads();
     const int64_t step = (int64_t)gridDim.x * 4 * R::ROWS;
     int64_t t = ((int64_t)blockIdx.x * 4 + wave) * R::ROWS + sub;
-    const typename R::T *scores = static_cast<const typename R::T *>(a.scores);
-    typename R::T *out = static_cast<typename R::T *>(a.dscores);
-    typename R::Raw raw{}, next{};
-    if (t < a.n_tokens) R::load(next, scores + t * a.ld, lane, E);
-    for (int64_t base = t - sub; base < a.n_tokens; base += step, t += step) {
-        raw = next;
-        if (t + step < a.n_tokens) R::load(next, scores + (t + step) * a.ld, lane, E);
-        float l[R::N], s[R::N], rest[R::N], n[R::N], d[R::N], g[R::N], m[R::N];
-        R::unpack(l, raw, lane, E);
-        float top = kLow, top_of_named = kLow;
-        // entries: how often each expert is named, and the sum of its entries' gradients
+    // four consecutive experts' f, g and m
+    auto f_of = [&](int i) { return *reinterpret_cast<const Float4 *>(named_share + R::expert(lane, i)); };
+    auto gm_of = [&](int i, Float4 &g, Float4 &m) {
+        const Float4 *w = reinterpret_cast<const Float4 *>(own + R::expert(lane, i));
+        const Float4 x = w[0], y = w[1];
+        g = Float4{x[0], x[2], y[0], y[2]};
+        m = Float4{x[1], x[3], y[1], y[3]};
+    };
+    Input<R, true> in[2];
+    in[0].load(a, t, lane);
+    in[1].load(a, t + step, lane);
+    auto row = [&](Input<R, true> &in) {
+        const typename R::Raw raw = in.raw;
+        bool named = false, twice = false;
+        for (int first = 0;;) {
 #pragma unroll
-        for (int i = 0; i < R::N; ++i) g[i] = m[i] = 0.0f;
-        bool named = false;
-        for (int first = 0; first < a.k; first += L) {
-            int c = -1;
-            float x = 0.0f;
-            if (t < a.n_tokens && first + at < a.k) {
-                c = a.colidx[t * a.k + first + at];
-                if (c >= E) c = -1;
-                if (a.dvals) x = a.dvals[t * a.k + first + at] * a.scale;
+            for (int j = 0; j < kEntries; ++j) {
+                if (first + j * L >= a.k) break;
+                const bool is = in.is(a, j);
+                named |= is;
+                // whoever finds another one's number where it has left its own shares an expert with it
+                if (a.dvals && is) {
+                    Float2 *place = own + in.c[j];
+                    const float number = (float)(first + j * L + at + 1);
+                    twice |= (*place)[1] != 0.0f;
+                    (*place)[1] = number;
+                    in_order();
+                    twice |= (*place)[1] != number;
+                    in_order();
+                    *place = Float2{in.x[j] * a.scale, 1.0f};
+                }
             }
-            named |= c >= 0;
-            const int here = min(L, a.k - first);
-            for (int i = 0; i < here; ++i) {
-                const int ci = __shfl(c, i, L);
-                const float xi = __shfl(x, i, L);
-#pragma unroll
-                for (int j = 0; j < R::N; ++j)
-                    if (R::expert(lane, j) == ci) {
-                        g[j] += xi;
-                        m[j] += 1.0f;
-                    }
-            }
+            if (first + kEntries * L >= a.k) break;
+            first += kEntries * L;
+            in.entries(a, t, first, at);
         }
         named = R::any(named);
-#pragma unroll
-        for (int i = 0; i < R::N; ++i) {
-            rest[i] = 1.0f;
-            if (sigmoids) sigmoid(l[i], s[i], rest[i]);
-            const float x = sigmoids ? fminf(l[i], 0.0f) : l[i];
-            top = fmaxf(top, x);
-            if (m[i] > 0.0f) top_of_named = fmaxf(top_of_named, x);
-            d[i] = 0.0f;
+        // clears the places again, or (`sums`) adds the entries up one after the other
+        auto each_entry = [&](bool sums) {
+            for (int i = sums ? at ? a.k : 0 : at; i < a.k; i += sums ? 1 : L) {
+                const int c = t < a.n_tokens ? a.colidx[t * a.k + i] : -1;
+                if (c >= 0 && c < E) own[c] = sums ? own[c] + Float2{a.dvals[t * a.k + i] * a.scale, 1.0f} : Float2{0.0f, 0.0f};
+            }
+        };
+        in_order();
+        if (__ballot(twice) && R::any(twice)) {
+            each_entry(false);
+            in_order();
+            each_entry(true);
         }
-        top = R::max(top);
-        numerators(n, l, s, sigmoids, top);
-        if (over_all) {
-            float total = 0.0f, fs = 0.0f, gs = 0.0f;
+        in_order();
+        float n[R::N], slope[R::N];
+        bool scaled;
+        const float total = numerators<R, SIGMOIDS>(n, slope, raw, lane, E, scaled);
+        const float over_all = named ? over(1.0f, total) : 0.0f;
+        float fs = 0.0f, gs = 0.0f, some = 0.0f;
+        if (a.dloss) {
+#pragma unroll
+            for (int i = 0; i < R::N; i += 4) {
+                const Float4 f = f_of(i);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) fs += n[i + j] * f[j];
+            }
+            fs = R::sum(fs) * over_all;
+        }
+        if (a.dvals) {
+#pragma unroll
+            for (int i = 0; i < R::N; i += 4) {
+                Float4 g, m;
+                gm_of(i, g, m);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    gs += n[i + j] * g[j];
+                    some += n[i + j] * m[j];
+                }
+            }
+            gs = R::sum(gs);
+            some = R::sum(some);
+        }
+        // (`again`: numerators that say little; with plain sigmoids, slopes that are over an exponential)
+        const bool again = a.dvals && named && (top_only ? some < kSmall : sigmoid_only && scaled);
+        const float A = factor * over_all, B = !a.dvals ? 0.0f : sigmoid_only ? 1.0f : top_only ? over(1.0f, some) : over_all;
+        gs *= sigmoid_only ? 0.0f : B;
+        // what is taken off: A sum p f, B sum q g for the experts that are named or, with shares over all experts, for all of them
+        const float Afs = A * fs, Bgs = B * gs, off = Afs + (top_only ? 0.0f : Bgs), off_named = top_only ? Bgs : 0.0f;
+        in_order();
+        const bool store = t < a.n_tokens;
+        typename R::T *out = static_cast<typename R::T *>(a.dscores) + t * a.ldg;
+        const bool any_again = __ballot(again) != 0;
+        float top = 0.0f, gs2 = 0.0f, over2 = 1.0f;
+        if (any_again) {
+            // The second term once more, over the exponential of the largest score that is named, or of nothing.
+            float l[R::N], sum2 = 0.0f;
+            R::unpack(l, raw, lane, E);
+            if (top_only) {
+                top = kLow;
+#pragma unroll
+                for (int i = 0; i < R::N; ++i)
+                    if (own[R::expert(lane, i)][1] > 0.0f) top = fmaxf(top, bounded<SIGMOIDS>(l[i]));
+                top = R::max(top);
+            }
 #pragma unroll
             for (int i = 0; i < R::N; ++i) {
-                total += n[i];
-                if (a.dloss) fs += n[i] * f[i];
-                gs += n[i] * g[i];
-            }
-            total = R::sum(total);
-            const float each = over(1.0f, total);
-            if (a.dloss && named) {
-                fs = R::sum(fs) * each;
-#pragma unroll
-                for (int i = 0; i < R::N; ++i) d[i] += factor * (n[i] * each) * rest[i] * (f[i] - fs);
-            }
-            if (a.dvals && named && a.scoring == TF_ROUTE_SOFTMAX) {
-                gs = R::sum(gs) * each;
-#pragma unroll
-                for (int i = 0; i < R::N; ++i) d[i] += n[i] * each * (g[i] - gs);
-            }
-        }
-        if (a.dvals && named && a.scoring == TF_ROUTE_SIGMOID) {
-#pragma unroll
-            for (int i = 0; i < R::N; ++i)
-                if (m[i] > 0.0f) d[i] += s[i] * rest[i] * g[i];
-        }
-        if (a.dvals && (a.scoring == TF_ROUTE_SOFTMAX_TOP || a.scoring == TF_ROUTE_SIGMOID_TOP)) {
-            // a bias may have selected experts far below the largest score: their shares are taken of the largest selected one
-            top_of_named = R::max(top_of_named);
-            if (__ballot(top_of_named < top - 40.0f)) numerators(n, l, s, sigmoids, top_of_named);
-            float total = 0.0f, gs = 0.0f;
-#pragma unroll
-            for (int i = 0; i < R::N; ++i)
-                if (m[i] > 0.0f) {
-                    total += m[i] * n[i];
-                    gs += n[i] * g[i];
+                const Float2 w = own[R::expert(lane, i)];
+                float x, y;
+                numerator_over<SIGMOIDS>(l[i], top, x, y);
+                if (w[1] > 0.0f) {
+                    sum2 += w[1] * x;
+                    gs2 += w[0] * x;
                 }
-            total = R::sum(total);
-            gs = over(R::sum(gs), total);
-#pragma unroll
-            for (int i = 0; i < R::N; ++i)
-                if (m[i] > 0.0f) d[i] += over(n[i], total) * rest[i] * (g[i] - m[i] * gs);
+            }
+            sum2 = R::sum(sum2);
+            gs2 = R::sum(gs2);
+            if (top_only) over2 = over(1.0f, sum2);
+            gs2 = top_only ? gs2 * over2 : 0.0f;
         }
-        if (t < a.n_tokens) R::store(out + t * a.ldg, d, lane, E);
+#pragma unroll
+        for (int c = 0; c < NV; ++c) {
+            float d[VEC];
+#pragma unroll
+            for (int i = c * VEC; i < (c + 1) * VEC; i += 4) {
+                const Float4 f = f_of(i);
+                Float4 g, m;
+                gm_of(i, g, m);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) d[i - c * VEC + j] = slope[i + j] * (A * f[j] + (B * g[j] - (off_named * m[j] + off)));
+            }
+            if (any_again) {
+                float l[R::N];
+                R::unpack(l, raw, lane, E);
+#pragma unroll
+                for (int i = c * VEC; i < (c + 1) * VEC; ++i) {
+                    const Float2 w = own[R::expert(lane, i)];
+                    float x, y;
+                    numerator_over<SIGMOIDS>(l[i], top, x, y);
+                    const float z = slope[i] * (A * named_share[R::expert(lane, i)] - Afs) + (w[1] > 0.0f ? y * over2 * (w[0] - w[1] * gs2) : 0.0f);
+                    if (again) d[i - c * VEC] = z;
+                }
+            }
+            if (store) R::store_chunk(out, d, c, lane, E);
+        }
+        in_order();
+        if (a.dvals) each_entry(false);
+        in_order();
+        in.load(a, t + 2 * step, lane);
+    };
+    for (int64_t base = t - sub; base < a.n_tokens; base += 2 * step) {
+        row(in[0]);
+        t += step;
+        if (base + step < a.n_tokens) row(in[1]);
+        t += step;
     }
 }
 
-template <int EL, int L, int NV> void balance_with(const RouterLaunch &a, hipStream_t st) {
-    // a workgroup for every 16 waves with two rounds of tokens
-    const int64_t groups = std::max<int64_t>(1, std::min<int64_t>(kBalanceGroups, ceil_div(a.n_tokens, 2 * 16 * (64 / L))));
-    hipLaunchKernelGGL((k_balance<EL, L, NV>), dim3((unsigned)groups), dim3(1024), 0, st, a);
-    if (groups > 1) hipLaunchKernelGGL(k_balance_finish, dim3(1), dim3(1024), 0, st, a, (int)groups);
-}
-template <int EL, int L, int NV> void grad_with(const RouterLaunch &a, hipStream_t st) {
-    const int64_t groups = std::min<int64_t>(2048, ceil_div(a.n_tokens, 4 * (64 / L)));
-    hipLaunchKernelGGL((k_route_grad<EL, L, NV>), dim3((unsigned)groups), dim3(256), 0, st, a);
-}
-template <int EL, bool GRAD> void router_el(const RouterLaunch &a, hipStream_t st) {
-    const int chunks = (int)ceil_div(a.n_experts, EL == TF_F32 ? 4 : 8);
-#define TF_ROW(L, NV) return GRAD ? grad_with<EL, L, NV>(a, st) : balance_with<EL, L, NV>(a, st)
-    if (chunks <= 8) TF_ROW(8, 1);
-    if (chunks <= 16) TF_ROW(16, 1);
-    if (chunks <= 32) TF_ROW(32, 1);
-    if (chunks <= 64) TF_ROW(64, 1);
-    if constexpr (EL == TF_F32) {
-        if (chunks <= 128) TF_ROW(64, 2);
-        TF_ROW(64, 4);
-    } else {
-        TF_ROW(64, 2);
+// One workgroup, and one launch, for scores of up to 256 KB; otherwise at least two rounds of tokens for each wave.  Workgroups have sixteen waves, or
+// four where there is little to do (a thread for each expert at the least).
+template <int EL, int L, int NV, bool SIGMOIDS> int balance_of(const RouterLaunch &a, hipStream_t st) {
+    const int waves = a.n_experts <= 256 && a.n_tokens <= 8 * (64 / L) ? 4 : 16;
+    const bool few = (int64_t)a.n_tokens * a.n_experts <= (EL == TF_F32 ? 65536 : 131072);
+    const int64_t groups = few ? 1 : std::min<int64_t>(kBalanceGroups, ceil_div(a.n_tokens, 2 * waves * (64 / L)));
+    const int line = balance_row(a.n_experts), lds = (line * (waves + 1) + 16) * 4;
+    if (lds > 65536) {
+        static DoneOnDevices done;
+        int device = 0;
+        hipError_t e = hipGetDevice(&device);
+        if (e != hipSuccess) return (int)e;
+        if (!done.has(device)) {
+            e = hipFuncSetAttribute(reinterpret_cast<const void *>(k_balance<EL, L, NV, SIGMOIDS>), hipFuncAttributeMaxDynamicSharedMemorySize, 17 * 4096 + 64);
+            if (e != hipSuccess) return (int)e;
+            done.add(device);
+        }
     }
+    hipLaunchKernelGGL((k_balance<EL, L, NV, SIGMOIDS>), dim3((unsigned)groups), dim3(64 * waves), lds, st, a);
+    if (groups > 1) hipLaunchKernelGGL(k_balance_finish, dim3(1), dim3(1024), 0, st, a, (int)groups);
+    return (int)hipGetLastError();
+}
+template <int EL, int L, int NV> int balance_with(const RouterLaunch &a, hipStream_t st) {
+    return a.scoring >= TF_ROUTE_SIGMOID ? balance_of<EL, L, NV, true>(a, st) : balance_of<EL, L, NV, false>(a, st);
+}
+template <int EL, int L, int NV> int grad_with(const RouterLaunch &a, hipStream_t st) {
+    const dim3 grid((unsigned)std::min<int64_t>(2048, ceil_div(a.n_tokens, 4 * (64 / L)))), block(256);
+    if (a.scoring >= TF_ROUTE_SIGMOID) hipLaunchKernelGGL((k_route_grad<EL, L, NV, true>), grid, block, 0, st, a);
+    else hipLaunchKernelGGL((k_route_grad<EL, L, NV, false>), grid, block, 0, st, a);
+    return (int)hipGetLastError();
+}
+// Sixteen experts a lane (eight for the gradient, which holds more of each, while there are lanes for that), in as few lanes as they need: what goes on
+// between lanes is then shared by as many rows as there can be.
+template <int EL, bool GRAD> int router_el(const RouterLaunch &a, hipStream_t st) {
+    constexpr int NV = (EL == TF_F32 ? 4 : 2) / (GRAD ? 2 : 1);
+    const int lanes = (int)ceil_div(a.n_experts, GRAD ? 8 : 16);
+#define TF_ROW(L, NV)                                            \
+    {                                                            \
+        if constexpr (GRAD) return grad_with<EL, L, NV>(a, st);  \
+        else return balance_with<EL, L, NV>(a, st);              \
+    }
+    if (lanes <= 1) TF_ROW(1, NV)
+    if (lanes <= 2) TF_ROW(2, NV)
+    if (lanes <= 4) TF_ROW(4, NV)
+    if (lanes <= 8) TF_ROW(8, NV)
+    if (lanes <= 16) TF_ROW(16, NV)
+    if (lanes <= 32) TF_ROW(32, NV)
+    if (lanes <= 64) TF_ROW(64, NV)
+    if constexpr (GRAD) return grad_with<EL, 64, 2 * NV>(a, st);
+    else return (int)hipErrorInvalidValue;       // (not reached: 1024 experts at most)
 #undef TF_ROW
 }
 template <bool GRAD> int router(const RouterLaunch &a, void *stream) {
     const hipStream_t st = static_cast<hipStream_t>(stream);
-    if (a.dtype == TF_BF16) router_el<TF_BF16, GRAD>(a, st);
-    else if (a.dtype == TF_F16) router_el<TF_F16, GRAD>(a, st);
-    else router_el<TF_F32, GRAD>(a, st);
-    return (int)hipGetLastError();
+    return a.dtype == TF_BF16 ? router_el<TF_BF16, GRAD>(a, st) : a.dtype == TF_F16 ? router_el<TF_F16, GRAD>(a, st) : router_el<TF_F32, GRAD>(a, st);
 }
 
 }  // namespace

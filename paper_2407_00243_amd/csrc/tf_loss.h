@@ -8,8 +8,9 @@ namespace tf {
 
 // Workgroups of a balance's first launch, each of which leaves its sums in the workspace.
 constexpr int kBalanceGroups = 256;
-// Bytes of that workspace: for each workgroup a sum and a count for each expert, and its number of rows.
-inline int64_t balance_bytes(int64_t n_experts) { return (int64_t)kBalanceGroups * (2 * n_experts + 1) * 4; }
+// Bytes of that workspace: for each workgroup a sum and a count for each expert (rounded up to whole fours), and its number of rows.
+constexpr int balance_row(int n_experts) { return (n_experts + 3) / 4 * 4; }
+inline int64_t balance_bytes(int n_experts) { return (int64_t)kBalanceGroups * (2 * balance_row(n_experts) + 1) * 4; }
 
 struct RouterLaunch {
     const void *scores;

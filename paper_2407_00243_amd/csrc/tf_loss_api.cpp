@@ -153,7 +153,7 @@ tf_status tf_moe_balance_size(int64_t n_tokens, int64_t n_experts, int64_t *byte
     if (!bytes) return report(TF_EINVAL, "null argument");
     if (n_tokens < 0 || n_experts < 1) return report(TF_EINVAL, "sizes must be positive");
     if (n_experts > tf::kRouteMaxExperts) return report(TF_EUNSUPPORTED, "at most 1024 experts and 64 entries in a row");
-    *bytes = tf::balance_bytes(n_experts);
+    *bytes = tf::balance_bytes((int)n_experts);
     return TF_OK;
 }
 
@@ -163,8 +163,9 @@ tf_status tf_moe_balance(const void *scores, int64_t ld, int32_t dtype, int32_t 
     const tf_status st = check_router(scores, ld, dtype, scoring, A, &k);
     if (st != TF_OK) return st;
     if (!counts || !mass || !loss || !workspace) return report(TF_EINVAL, "null argument");
-    if (!aligned(counts, 4) || !aligned(mass, 4) || !aligned(loss, 4) || !aligned(workspace, 4))
+    if (!aligned(counts, 4) || !aligned(mass, 4) || !aligned(loss, 4))
         return report(TF_EINVAL, "arrays must be aligned to their elements");
+    if (!aligned(workspace, 16)) return report(TF_EINVAL, "the workspace must be 16-byte aligned");
     tf::RouterLaunch a = router_args(scores, ld, dtype, scoring, A, k);
     a.counts = counts;
     a.mass = mass;
