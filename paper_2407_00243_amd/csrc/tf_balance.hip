@@ -238,7 +238,7 @@ __device__ void write_balance(const RouterLaunch &a, float m, int c, int rows) {
 __global__ __launch_bounds__(1024) void k_balance_finish(const RouterLaunch a, const int groups) {
     __shared__ Float4 masses[1024];
     __shared__ Int4 counts[1024];
-    const int tid = threadIdx.x, fours = balance_row(a.n_experts) / 4, slices = 1024 / fours;
+    const int tid = threadIdx.x, fours = balance_row(a.n_experts) / 4, slices = min(1024 / fours, 16);
     const Float4 *mass = static_cast<const Float4 *>(a.workspace);
     const Int4 *count = reinterpret_cast<const Int4 *>(mass + (int64_t)kBalanceGroups * fours);
     const int *rows = reinterpret_cast<const int *>(count + (int64_t)kBalanceGroups * fours);
@@ -568,12 +568,13 @@ template <int EL, int L, int NV, bool SIGMOIDS> __global__ __launch_bounds__(256
     }
 }
 
-// One workgroup, and one launch, for scores of up to 256 KB; otherwise at least two rounds of tokens for each wave.  Workgroups have sixteen waves, or
-// four where there is little to do (a thread for each expert at the least).
+// Few scores: one workgroup, and one launch.  Otherwise workgroups of four waves, one or two steps of tokens each, or of sixteen.  (A thread for each
+// expert at the least.)
 template <int EL, int L, int NV, bool SIGMOIDS> int balance_of(const RouterLaunch &a, hipStream_t st) {
-    const int waves = a.n_experts <= 256 && a.n_tokens <= 8 * (64 / L) ? 4 : 16;
-    const bool few = (int64_t)a.n_tokens * a.n_experts <= (EL == TF_F32 ? 65536 : 131072);
-    const int64_t groups = few ? 1 : std::min<int64_t>(kBalanceGroups, ceil_div(a.n_tokens, 2 * waves * (64 / L)));
+    const int64_t sets = ceil_div(a.n_tokens, 64 / L);
+    const bool few = (int64_t)a.n_tokens * a.n_experts <= 16384;
+    const int waves = a.n_experts <= 256 && (few ? sets <= 8 : sets <= 8 * kBalanceGroups) ? 4 : 16;
+    const int64_t groups = few ? 1 : std::min<int64_t>(kBalanceGroups, ceil_div(sets, waves));
     const int line = balance_row(a.n_experts), lds = (line * (waves + 1) + 16) * 4;
     if (lds > 65536) {
         static DoneOnDevices done;

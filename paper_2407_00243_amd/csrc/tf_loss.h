@@ -84,6 +84,7 @@ enum ProductEnd { kEndSums = 0, kEndGradient = 1, kEndSlab = 2, kEndOut = 3 };
 enum ProductTile { kTile256 = 0, kTile128 = 1, kTile64 = 2, kTile16 = 3 };
 struct ProductLaunch {
     Side M, N;
+    int32_t any;                  // 1: rows of M begin at any element (and its columns are any number)
     int32_t parts;                // of a number: 1, or 3 whose six largest products are taken
     int32_t k_steps;              // of 64
     const int32_t *n;             // kept rows

@@ -91,8 +91,57 @@ template <int W, bool TR, int WAVES> struct Loader {
         return w;
     }
     // Instruction C of those that load a step into LDS from lds + AT on; lds: of this wave's first instruction.
-    template <int C, int AT> __device__ __forceinline__ void load(const Words4 &from, uint32_t lds, int wave) const {
+    template <int C, int AT> __device__ __forceinline__ void load(const Words4 &from, uint32_t lds, bool, int wave, int) const {
         if (INSTR % WAVES == 0 || wave + WAVES * C < INSTR) load_to_lds<AT + WAVES * C * 1024>(from, off[C], lds);
+    }
+    __device__ __forceinline__ void put(char *, int, int) const {}
+};
+
+// The same for rows that begin at any element: through registers.  A step is fetched where the other loader's loads go out, and put into LDS before the
+// barrier that they are waited for at.
+template <int W, bool TR, int WAVES> struct AnyLoader {
+    typedef Loader<W, TR, WAVES> Way;
+    static constexpr int INSTR = Way::INSTR, PER = Way::PER, PER_LEAST = 0;      // (no load of it is waited for by counting)
+    const char *at;                // the next step's first row and column
+    int64_t row, stride;           // bytes from row to row, from step to step
+    int32_t some, left;            // of M or N in the tile; of K from the next step on
+    Words4 r[PER];
+
+    __device__ __forceinline__ void begin(const Side &s, int64_t first, int64_t k, int, int, int) {
+        row = s.ld * 2;
+        const int64_t there = (TR ? s.cols : s.rows) - first;
+        some = (int32_t)(there < 0 ? 0 : there < W ? there : W);
+        left = (int32_t)((TR ? s.rows : s.cols) - k);
+        at = static_cast<const char *>(s.p) + (TR ? k * s.ld + first : first * s.ld + k) * 2;
+        stride = TR ? kStep * row : kStep * 2;
+    }
+    __device__ __forceinline__ void go_to(const Side &, int) {}
+    __device__ __forceinline__ Words4 next(int) { return Words4{0, 0, 1, 0}; }
+    // (is: there is such a step)
+    template <int C, int AT> __device__ __forceinline__ void load(const Words4 &, uint32_t, bool is, int wave, int lane) {
+        const int j = wave + WAVES * C;
+        if (INSTR % WAVES != 0 && j >= INSTR) return;
+        const int o = Way::row_of(j, lane), c = Way::chunk_of(j, lane) * 8, n = (TR ? some : left) - c;
+        const char *p = at + o * row + c * 2;
+        Words4 w{0, 0, 0, 0};
+        if (is && o < (TR ? left : some)) {
+            if (n >= 8) {
+                w = *reinterpret_cast<const AnyWords4 *>(p);
+            } else if (n > 0) {
+                for (int i = 0; i < n; ++i) {
+                    const uint32_t x = reinterpret_cast<const uint16_t *>(p)[i];
+                    w[i / 2] |= x << (16 * (i & 1));
+                }
+            }
+        }
+        r[C] = w;
+    }
+    __device__ __forceinline__ void put(char *lds, int wave, int lane) {
+#pragma unroll
+        for (int c = 0; c < PER; ++c)
+            if (INSTR % WAVES == 0 || wave + WAVES * c < INSTR) *reinterpret_cast<Words4 *>(lds + (wave + WAVES * c) * 1024 + lane * 16) = r[c];
+        at += stride;
+        left -= kStep;
     }
 };
 
@@ -154,7 +203,7 @@ template <int N, int I = 0, typename F> __device__ __forceinline__ void each(F &
     }
 }
 
-template <int EL, int WM, int WN, int TM, int TN, int PLACES, bool MTR, bool NTR, int END>
+template <int EL, int WM, int WN, int TM, int TN, int PLACES, bool ANY, bool MTR, bool NTR, int END>
 __global__ __launch_bounds__(WM * WN * 64, TM * TN > 32 ? 1 : 2) void k_product(const ProductLaunch a) {
     constexpr int WAVES = WM * WN, BM = WM * TM * 16, BN = WN * TN * 16;
     constexpr bool BIG = TM * TN > 32;      // sums fill the accumulation registers: left alone, the compiler moves them about in every step
@@ -182,7 +231,7 @@ __global__ __launch_bounds__(WM * WN * 64, TM * TN > 32 ? 1 : 2) void k_product(
     const int s0 = (int)((int64_t)steps * split / splits), s1 = (int)((int64_t)steps * (split + 1) / splits);
     const int pairs = a.parts == 3 ? 6 : 1, total = pairs * (s1 - s0);
     int pair = a.parts == 3 ? 0 : 5, in_pair = s1 - s0, to_load = total;
-    typedef Loader<BM, MTR, WAVES> LM;
+    typedef std::conditional_t<ANY, AnyLoader<BM, MTR, WAVES>, Loader<BM, MTR, WAVES>> LM;
     typedef Loader<BN, NTR, WAVES> LN;
     LM lm;
     LN ln;
@@ -212,9 +261,10 @@ __global__ __launch_bounds__(WM * WN * 64, TM * TN > 32 ? 1 : 2) void k_product(
     const uint32_t lds0 = (uint32_t)(uintptr_t)(LdsPtr)lds + wave * 1024;
     auto load = [&](auto c, auto to) {
         constexpr int C = decltype(c)::value, TO = decltype(to)::value;
-        if constexpr (C < LM::PER) lm.template load<C, TO * BM * 128>(from_m, lds0, wave);
-        else if constexpr (C < LOADS) ln.template load<C - LM::PER, AT_N + TO * BN * 128>(from_n, lds0, wave);
+        if constexpr (C < LM::PER) lm.template load<C, TO * BM * 128>(from_m, lds0, to_load >= 0, wave, lane);
+        else if constexpr (C < LOADS) ln.template load<C - LM::PER, AT_N + TO * BN * 128>(from_n, lds0, true, wave, lane);
     };
+    auto put = [&](auto to) { lm.put(lds + decltype(to)::value * BM * 128, wave, lane); };
     typename Mfma<EL>::V vm[2][TM], vn[2][TN];
     auto read = [&](int r, int half, int from) {
         if (r < TM) vm[half][r] = rm.template read<EL>(lds + from * BM * 128, half, r);
@@ -248,12 +298,15 @@ __global__ __launch_bounds__(WM * WN * 64, TM * TN > 32 ? 1 : 2) void k_product(
     // The barrier lies between a step's halves: behind it the next step is in LDS, and nobody reads this one any more.
     auto step = [&](auto place, auto other) {
         multiply(zero, yes, place, no, zero, yes);
+        // (what is fetched is the step that the place before this one is for)
+        put(std::integral_constant<int, (decltype(place)::value + PLACES - 1) % PLACES>{});
         arrive<(PLACES - 2) * LEAST>();
         multiply(one, yes, other, yes, place, no);
     };
     each<PLACES>([&](auto place) {
         next();
         each<LOADS>([&](auto c) { load(c, place); });
+        if constexpr (decltype(place)::value + 1 < PLACES) put(place);
     });
     arrive<(PLACES - 1) * LEAST>();
 #pragma unroll
@@ -422,14 +475,14 @@ __global__ __launch_bounds__(WM * WN * 64, TM * TN > 32 ? 1 : 2) void k_product(
     }
 }
 
-template <int EL, int WM, int WN, int TM, int TN, int PLACES, bool MTR, bool NTR, int END> int product_with(ProductLaunch a, hipStream_t st) {
+template <int EL, int WM, int WN, int TM, int TN, int PLACES, bool ANY, bool MTR, bool NTR, int END> int product_with(ProductLaunch a, hipStream_t st) {
     constexpr int BM = WM * TM * 16, BN = WN * TN * 16, LDS = PLACES * (BM + BN) * 128;
     static DoneOnDevices done;
     int device = 0;
     hipError_t e = hipGetDevice(&device);
     if (e != hipSuccess) return (int)e;
     if (!done.has(device)) {
-        e = hipFuncSetAttribute(reinterpret_cast<const void *>(k_product<EL, WM, WN, TM, TN, PLACES, MTR, NTR, END>),
+        e = hipFuncSetAttribute(reinterpret_cast<const void *>(k_product<EL, WM, WN, TM, TN, PLACES, ANY, MTR, NTR, END>),
                                 hipFuncAttributeMaxDynamicSharedMemorySize, LDS);
         if (e != hipSuccess) return (int)e;
         done.add(device);
@@ -439,28 +492,29 @@ template <int EL, int WM, int WN, int TM, int TN, int PLACES, bool MTR, bool NTR
     const int64_t groups = (int64_t)a.m_tiles * a.n_tiles * a.splits;
     if (groups == 0) return 0;
     if (groups > most_workgroups(WM * WN * 64)) return (int)hipErrorInvalidConfiguration;
-    hipLaunchKernelGGL((k_product<EL, WM, WN, TM, TN, PLACES, MTR, NTR, END>), dim3((unsigned)groups), dim3(WM * WN * 64), LDS, st, a);
+    hipLaunchKernelGGL((k_product<EL, WM, WN, TM, TN, PLACES, ANY, MTR, NTR, END>), dim3((unsigned)groups), dim3(WM * WN * 64), LDS, st, a);
     return (int)hipGetLastError();
 }
 
-template <int EL, bool MTR, bool NTR, int END> int product_tile(const ProductLaunch &a, hipStream_t st) {
-    if (a.tile == kTile256) return product_with<EL, 2, 2, 8, 8, 2, MTR, NTR, END>(a, st);
+template <int EL, bool ANY, bool MTR, bool NTR, int END> int product_tile(const ProductLaunch &a, hipStream_t st) {
+    if (a.tile == kTile256) return product_with<EL, 2, 2, 8, 8, 2, ANY, MTR, NTR, END>(a, st);
     if constexpr (!NTR) {
-        if (a.tile == kTile64) return product_with<EL, 4, 1, 2, 4, 3, MTR, NTR, END>(a, st);
-        if (a.tile == kTile16) return product_with<EL, 4, 1, 1, 1, 4, MTR, NTR, END>(a, st);
+        if (a.tile == kTile64) return product_with<EL, 4, 1, 2, 4, 3, ANY, MTR, NTR, END>(a, st);
+        if (a.tile == kTile16) return product_with<EL, 4, 1, 1, 1, 4, ANY, MTR, NTR, END>(a, st);
     }
-    return product_with<EL, 2, 2, 4, 4, 2, MTR, NTR, END>(a, st);
+    return product_with<EL, 2, 2, 4, 4, 2, ANY, MTR, NTR, END>(a, st);
+}
+template <int EL, bool MTR, int END> int product_any(const ProductLaunch &a, hipStream_t st) {
+    return a.any ? product_tile<EL, true, MTR, false, END>(a, st) : product_tile<EL, false, MTR, false, END>(a, st);
 }
 
 // The four products: logits (their sums, or the gradient), dX (W by columns), dW (both operands by columns).
 template <int EL> int product(const ProductLaunch &a, void *stream) {
     const hipStream_t st = static_cast<hipStream_t>(stream);
-    if (a.end == kEndSums) return product_tile<EL, false, false, kEndSums>(a, st);
-    if (a.end == kEndGradient) return product_tile<EL, false, false, kEndGradient>(a, st);
-    if (a.end == kEndSlab && !a.k_rows) return product_tile<EL, true, false, kEndSlab>(a, st);
-    if (a.end == kEndSlab) return product_tile<EL, true, true, kEndSlab>(a, st);
-    if (!a.k_rows) return product_tile<EL, true, false, kEndOut>(a, st);
-    return product_tile<EL, true, true, kEndOut>(a, st);
+    if (a.end == kEndSums) return product_any<EL, false, kEndSums>(a, st);
+    if (a.end == kEndGradient) return product_any<EL, false, kEndGradient>(a, st);
+    if (!a.k_rows) return a.end == kEndSlab ? product_any<EL, true, kEndSlab>(a, st) : product_any<EL, true, kEndOut>(a, st);
+    return a.end == kEndSlab ? product_tile<EL, false, true, true, kEndSlab>(a, st) : product_tile<EL, false, true, true, kEndOut>(a, st);
 }
 
 }  // namespace
