@@ -105,6 +105,7 @@ template <int W, bool TR, int WAVES> struct AnyLoader {
     const char *at;                // the next step's first row and column
     int64_t row, stride;           // bytes from row to row, from step to step
     int32_t some, left;            // of M or N in the tile; of K from the next step on
+    bool wide;                     // rows have eight columns or more
     Words4 r[PER];
 
     __device__ __forceinline__ void begin(const Side &s, int64_t first, int64_t k, int, int, int) {
@@ -112,6 +113,7 @@ template <int W, bool TR, int WAVES> struct AnyLoader {
         const int64_t there = (TR ? s.cols : s.rows) - first;
         some = (int32_t)(there < 0 ? 0 : there < W ? there : W);
         left = (int32_t)((TR ? s.rows : s.cols) - k);
+        wide = s.cols >= 8;
         at = static_cast<const char *>(s.p) + (TR ? k * s.ld + first : first * s.ld + k) * 2;
         stride = TR ? kStep * row : kStep * 2;
     }
@@ -127,6 +129,13 @@ template <int W, bool TR, int WAVES> struct AnyLoader {
         if (is && o < (TR ? left : some)) {
             if (n >= 8) {
                 w = *reinterpret_cast<const AnyWords4 *>(p);
+            } else if (n > 0 && wide) {
+                // the row's last eight, of which the first ones go
+                const AnyWords4 x = *reinterpret_cast<const AnyWords4 *>(p - (8 - n) * 2);
+                const uint64_t lo = x[0] | (uint64_t)x[1] << 32, hi = x[2] | (uint64_t)x[3] << 32;
+                const int off = 16 * (8 - n);        // 16 .. 112 bits
+                const uint64_t l = off < 64 ? lo >> off | hi << (64 - off) : hi >> (off - 64), h = off < 64 ? hi >> off : 0;
+                w = Words4{(uint32_t)l, (uint32_t)(l >> 32), (uint32_t)h, (uint32_t)(h >> 32)};
             } else if (n > 0) {
                 for (int i = 0; i < n; ++i) {
                     const uint32_t x = reinterpret_cast<const uint16_t *>(p)[i];
@@ -497,12 +506,13 @@ template <int EL, int WM, int WN, int TM, int TN, int PLACES, bool ANY, bool MTR
 }
 
 template <int EL, bool ANY, bool MTR, bool NTR, int END> int product_tile(const ProductLaunch &a, hipStream_t st) {
-    if (a.tile == kTile256) return product_with<EL, 2, 2, 8, 8, 2, ANY, MTR, NTR, END>(a, st);
     if constexpr (!NTR) {
         if (a.tile == kTile64) return product_with<EL, 4, 1, 2, 4, 3, ANY, MTR, NTR, END>(a, st);
         if (a.tile == kTile16) return product_with<EL, 4, 1, 1, 1, 4, ANY, MTR, NTR, END>(a, st);
     }
-    return product_with<EL, 2, 2, 4, 4, 2, ANY, MTR, NTR, END>(a, st);
+    if constexpr (ANY && END != kEndSums) return (int)hipErrorInvalidValue;       // (gradients of few rows only)
+    else if (a.tile == kTile256) return product_with<EL, 2, 2, 8, 8, 2, ANY, MTR, NTR, END>(a, st);
+    else return product_with<EL, 2, 2, 4, 4, 2, ANY, MTR, NTR, END>(a, st);
 }
 template <int EL, bool MTR, int END> int product_any(const ProductLaunch &a, hipStream_t st) {
     return a.any ? product_tile<EL, true, MTR, false, END>(a, st) : product_tile<EL, false, MTR, false, END>(a, st);
