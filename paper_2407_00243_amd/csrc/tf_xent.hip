@@ -129,18 +129,34 @@ __global__ __launch_bounds__(256) void k_count_rows(const XentLaunch a, const in
     }
 }
 
+// w: rows first .. first + count of W, columns as above; `group` of `groups` workgroups.
+template <int EL> __device__ __forceinline__ void pack_classes(const XentLaunch &a, int64_t first, int64_t count, int64_t group, int64_t groups) {
+    const int64_t columns = round_up(a.n_in, 64);
+    const int per_row = threads_of_row(columns), at_once = 256 / per_row;
+    for (int64_t i = group * at_once + threadIdx.x / per_row; i < count; i += groups * at_once)
+        for (int64_t k = threadIdx.x % per_row * 8; k < columns; k += per_row * 8) {
+            float x[8];
+            read8<EL>(x, static_cast<const typename El<EL>::T *>(a.W) + (first + i) * a.ldw, k, a.n_in);
+            put8<EL>(x, static_cast<uint16_t *>(a.s.w) + i * a.s.ld + k, a.s.w_cap);
+        }
+}
+template <int EL> __global__ __launch_bounds__(256) void k_pack_classes(const XentLaunch a, const int64_t first, const int64_t count) {
+    pack_classes<EL>(a, first, count, blockIdx.x, gridDim.x);
+}
+
 // Numbers the rows that have a label in their order and copies them, one after the other, to x, where columns up to a multiple of 64 are zeros behind
 // the last one; rows without a label get their zeros.  A block of rows a workgroup, which sums up the counts of the blocks before
-// it; where there are few rows (`counted` 0) it counts them itself, which saves a launch.
-template <int EL> __global__ __launch_bounds__(256) void k_pack_rows(const XentLaunch a, const int block, const int counted) {
+// it; where there are few rows (`counted` 0) it counts them itself, which saves a launch.  Workgroups behind the `blocks` first ones pack W's first rows.
+template <int EL> __global__ __launch_bounds__(256) void k_pack_rows(const XentLaunch a, const int block, const int blocks, const int counted, const int64_t classes) {
     __shared__ int n_of[4], rows[256], ats[256];
     __shared__ float top_of[4];
+    if ((int)blockIdx.x >= blocks) return pack_classes<EL>(a, 0, classes, blockIdx.x - blocks, gridDim.x - blocks);
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int64_t first = (int64_t)blockIdx.x * block, end = min(first + block, (int64_t)a.n_rows);
     int n = 0;
     float top = 0.0f;
     if (counted) {
-        for (int b = tid; b < (int)gridDim.x; b += 256) {
+        for (int b = tid; b < blocks; b += 256) {
             if (b < (int)blockIdx.x) n += a.s.block_rows[b];
             top = fmaxf(top, a.s.block_top[b]);
         }
@@ -209,20 +225,8 @@ template <int EL> __global__ __launch_bounds__(256) void k_pack_rows(const XentL
                     }
         n += here;
     }
-    if (blockIdx.x == gridDim.x - 1 && tid == 0) *a.s.n = n;
+    if ((int)blockIdx.x == blocks - 1 && tid == 0) *a.s.n = n;
 }
-// w: rows first .. first + count of W likewise.
-template <int EL> __global__ __launch_bounds__(256) void k_pack_classes(const XentLaunch a, const int64_t first, const int64_t count, const int64_t plane) {
-    const int64_t columns = round_up(a.n_in, 64);
-    const int per_row = threads_of_row(columns), at_once = 256 / per_row;
-    for (int64_t i = (int64_t)blockIdx.x * at_once + threadIdx.x / per_row; i < count; i += (int64_t)gridDim.x * at_once)
-        for (int64_t k = threadIdx.x % per_row * 8; k < columns; k += per_row * 8) {
-            float x[8];
-            read8<EL>(x, static_cast<const typename El<EL>::T *>(a.W) + (first + i) * a.ldw, k, a.n_in);
-            put8<EL>(x, static_cast<uint16_t *>(a.s.w) + i * a.s.ld + k, plane);
-        }
-}
-
 // ------------------------------------------------------------------------------------------- ends
 
 // Adds the sums of `blocks` blocks of classes to those of the classes before them (unless `first`).  ROWS rows a workgroup: 64 / ROWS lanes of each of
@@ -367,22 +371,22 @@ bool whole_pieces(const XentLaunch &a) {
 bool through_registers(const XentLaunch &a) { return a.dtype != TF_F32 && !whole_pieces(a) && a.n_rows <= (a.loss ? 1023 : 64); }
 bool in_place(const XentLaunch &a) { return whole_pieces(a) || through_registers(a); }
 
-// Numbers and copies the rows that count.  (Also without rows: it sets the unit.)  Up to 8192 rows every block counts the rows before it.
-int begin(const XentLaunch &a, hipStream_t st) {
+// Numbers and copies the rows that count.  (Also without rows: it sets the unit.)  Up to 8192 rows every block counts the rows before it.  Packs the
+// first `classes` of W as well, where it has to be.
+int begin(const XentLaunch &a, int64_t classes, hipStream_t st) {
     const int counted = a.n_rows > 8192;
-    const int64_t block = std::max<int64_t>(1, ceil_div(a.n_rows, kMostBlocks));
-    const dim3 grid((unsigned)std::max<int64_t>(1, ceil_div(a.n_rows, block)));
-    if (counted) hipLaunchKernelGGL(k_count_rows, grid, dim3(256), 0, st, a, (int)block);
-    TF_BY_TYPE(a.dtype, k_pack_rows, grid, a, (int)block, counted);
+    const int64_t block = std::max<int64_t>(1, ceil_div(a.n_rows, kMostBlocks)), blocks = std::max<int64_t>(1, ceil_div(a.n_rows, block));
+    if (counted) hipLaunchKernelGGL(k_count_rows, dim3((unsigned)blocks), dim3(256), 0, st, a, (int)block);
+    const int64_t others = a.n_rows && !in_place(a) ? row_grid(classes, round_up(a.n_in, 64)).x : 0;
+    TF_BY_TYPE(a.dtype, k_pack_rows, dim3((unsigned)(blocks + others)), a, (int)block, (int)blocks, counted, classes);
     return (int)hipGetLastError();
 }
 
-// W's rows as an operand, packed first where they cannot be read in place.
+// W's rows as an operand, packed where they cannot be read in place (the first ones have been).
 Side classes(const XentLaunch &a, int64_t first, int64_t count, hipStream_t st) {
     if (in_place(a)) return Side{static_cast<const uint16_t *>(a.W) + first * a.ldw, a.ldw, 0, count, a.n_in};
-    const int64_t plane = a.s.w_cap;
-    TF_BY_TYPE(a.dtype, k_pack_classes, row_grid(count, round_up(a.n_in, 64)), a, first, count, plane);
-    return Side{a.s.w, a.s.ld, plane, count, round_up(a.n_in, 64)};
+    if (first) TF_BY_TYPE(a.dtype, k_pack_classes, row_grid(count, round_up(a.n_in, 64)), a, first, count);
+    return Side{a.s.w, a.s.ld, a.s.w_cap, count, round_up(a.n_in, 64)};
 }
 
 ProductLaunch logits(const XentLaunch &a, const Side &W, int64_t first, int64_t count) {
@@ -428,7 +432,7 @@ Cut cut_product(int64_t m, int64_t n, int64_t steps, int pairs, bool rows, int64
     for (const ProductTile t : {kTile256, kTile128})
         for (int64_t s = 1; s <= std::min<int64_t>(most, 512); s = s < 8 ? s + 1 : s * 5 / 4) {
             const double rounds = (double)ceil_div(ceil_div(m, m_side(t)) * ceil_div(n, n_side(t)) * s, 256), each = (double)steps * pairs / s;
-            const double time = (t == kTile256 ? rounds * (14 * each + 130) : std::max(4 * rounds, 6.0) * each + 18 * rounds + 80) + (s > 1 ? (double)s * m * n / 50000 : 0.0);
+            const double time = (t == kTile256 ? rounds * (14 * each + 130) : std::max(4 * rounds, 6.0) * each + 18 * rounds + 80) + (s > 1 ? 40 + (double)s * m * n / 50000 : 0.0);
             if (least == 0 || time < least) {
                 best = Cut{t, s};
                 least = time;
@@ -441,11 +445,11 @@ Cut cut_product(int64_t m, int64_t n, int64_t steps, int pairs, bool rows, int64
 
 int launch_xent(const XentLaunch &a, void *stream) {
     const hipStream_t st = static_cast<hipStream_t>(stream);
-    int e = begin(a, st);
-    if (e || a.n_rows == 0) return e;
     const int64_t ld = round_up(a.n_rows, 16);
     int64_t piece = a.s.part_cap / ld * 64 / 256 * 256;       // (a sum of every 64 classes at the most)
     if (!in_place(a)) piece = std::min(piece, a.s.w_cap / a.s.ld);
+    int e = begin(a, std::min<int64_t>(piece, a.n_classes), st);
+    if (e) return e;
     for (int64_t first = 0; first < a.n_classes; first += piece) {
         const int64_t count = std::min<int64_t>(piece, a.n_classes - first);
         ProductLaunch p = logits(a, classes(a, first, count, st), first, count);
@@ -479,7 +483,7 @@ int launch_xent_grad(const XentLaunch &call, void *stream) {
     // (the same shares for every piece: the slabs are added to)
     const Cut dx = cut_product(a.n_in, a.n_rows, ceil_div(std::min<int64_t>(piece, a.n_classes), 64), pairs, true, a.s.dx_cap / dx_size);
     a.direct_dx = piece >= a.n_classes && dx.shares == 1;
-    int e = begin(a, st);
+    int e = begin(a, std::min<int64_t>(piece, a.n_classes), st);
     if (e) return e;
     for (int64_t first = 0; first < a.n_classes; first += piece) {
         const int64_t count = std::min<int64_t>(piece, a.n_classes - first);
