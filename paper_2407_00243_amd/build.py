@@ -12,7 +12,8 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libtilefusion.so")
 SOURCES = ["tf_kernels.hip", "tf_gemm.hip", "tf_chain.hip", "tf_gather.hip", "tf_inspector.cpp", "tf_api.cpp",
            "tf_experts_bf16.hip", "tf_experts_f16.hip", "tf_experts_f32.hip", "tf_q4.hip", "tf_route.hip", "tf_moe_api.cpp",
-           "tf_balance.hip", "tf_product_bf16.hip", "tf_product_f16.hip", "tf_xent.hip", "tf_loss_api.cpp"]
+           "tf_balance.hip", "tf_product_bf16.hip", "tf_product_f16.hip", "tf_product_f32.hip",
+           "tf_xent.hip", "tf_loss_api.cpp"]
 HEADERS = ["tf_internal.h", "tf_device.h", "tf_moe.h", "tf_moe_device.h", "tf_experts.h",
            "tf_loss.h", "tf_product.h", os.path.join("..", "..", "include", "tilefusion.h")]
 

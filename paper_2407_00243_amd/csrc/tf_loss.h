@@ -67,6 +67,7 @@ struct XentLaunch {
     float *loss, *lse;
     const float *lse_in, *dloss;
     void *dX, *dW;
+    int32_t native;               // fp32 operands are multiplied as they are, not in parts
     int32_t direct_dx;            // dX is written by its product; rows without a label get their zeros first
 };
 int launch_xent(const XentLaunch &a, void *stream);
@@ -74,9 +75,9 @@ int launch_xent_grad(const XentLaunch &a, void *stream);
 
 // Products of the cross entropy (tf_product.h): C = M N^T summed over K, tiles of C by workgroups.
 struct Side {
-    const void *p;                // 16-bit elements
+    const void *p;
     int64_t ld, plane;            // elements: from row to row, from part to part
-    int64_t rows, cols;           // what there is of it (cols: a multiple of 8); further elements count as zeros
+    int64_t rows, cols;           // what there is of it (cols: whole pieces of 16 bytes, unless `any`); further elements count as zeros
 };
 // Shares of a contraction: each has four steps of 64 at least.
 constexpr int shares_of(int most, int steps) { return most < steps / 4 ? most : steps / 4 < 1 ? 1 : steps / 4; }
@@ -86,7 +87,7 @@ struct ProductLaunch {
     Side M, N;
     int32_t any;                  // 1: rows of M begin at any element (and its columns are any number)
     int32_t parts;                // of a number: 1, or 3 whose six largest products are taken
-    int32_t k_steps;              // of 64
+    int32_t k_steps;              // of 64 columns (fp32: 32)
     const int32_t *n;             // kept rows
     int32_t k_rows;               // 1: K goes over kept rows
     int32_t n_rows;               // 1: N does
@@ -113,5 +114,6 @@ struct ProductLaunch {
 };
 int launch_product_bf16(const ProductLaunch &a, void *stream);
 int launch_product_f16(const ProductLaunch &a, void *stream);
+int launch_product_f32(const ProductLaunch &a, void *stream);
 
 }  // namespace tf

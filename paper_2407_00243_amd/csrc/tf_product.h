@@ -9,7 +9,17 @@
 namespace tf {
 namespace {
 
+// Matrix instructions by the type of the elements: D (16 x 16) += M (16 x K) N^T, K 32 or (fp32) four times 4.  A lane holds eight (four) columns of K.
 template <int EL> struct Mfma;
+template <> struct Mfma<TF_F32> {
+    typedef Float4 V;
+    static __device__ __forceinline__ Float4 mul(V a, V b, Float4 c) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) c = __builtin_amdgcn_mfma_f32_16x16x4f32(a[i], b[i], c, 0, 0, 0);
+        return c;
+    }
+    static __device__ __forceinline__ void add(Float4 &c, V a, V b) { c = mul(a, b, c); }
+};
 template <> struct Mfma<TF_BF16> {
     typedef Bf8 V;
     static __device__ __forceinline__ Float4 mul(V a, V b, Float4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
@@ -26,7 +36,10 @@ typedef short Short4 __attribute__((ext_vector_type(4)));
 typedef short Short8 __attribute__((ext_vector_type(8)));
 typedef __attribute__((address_space(3))) Short4 *LdsShort4;
 
-constexpr int kStep = 64;      // of K
+// A step of K: 128 bytes of a row, whose pieces of sixteen bytes are the units of all that follows.
+template <int EL> struct Size {
+    static constexpr int BYTES = EL == TF_F32 ? 4 : 2, PIECE = 16 / BYTES, STEP = 128 / BYTES;
+};
 
 // Sixteen bytes a lane from a buffer to LDS, lane by lane from `to` + AT on (bytes).  In assembly, because the compiler would have every read of
 // LDS that transposes wait for all loads before it.  It writes no vector register; what it writes in LDS is waited for in arrive().  (Nothing
@@ -35,12 +48,15 @@ template <int AT> __device__ __forceinline__ void load_to_lds(const Words4 &from
     asm volatile("s_add_u32 m0, %2, %3\n\ts_nop 0\n\tbuffer_load_dwordx4 %0, %1, 0 offen lds" ::"v"(offset), "s"(from), "s"(to), "i"(AT) : "scc");
 }
 
-// A step of an operand in LDS: W rows (of M or N) x 64 columns (K) if it lies in memory that way, else 64 rows (K) x W columns
+// A step of an operand in LDS: W rows (of M or N) x 64 columns (K; 32 of fp32) if it lies in memory that way, else 64 rows (K) x W columns
 // (TR).  It comes sixteen bytes a lane straight from memory, 1 KiB an instruction, and LDS gets them in the order of the lanes; so
 // that sixteen lanes that read an operand of an instruction meet different banks, the pieces of a row are permuted on the way
-// by which lane asks for which: piece p of row r is at p ^ (r & 7); with TR 32-byte units u of row k at u ^ (k & 3 | k / 8 % 2 * 4).
-template <int W, bool TR, int WAVES> struct Loader {
-    static constexpr int INSTR = W / 8, PER = (INSTR + WAVES - 1) / WAVES, PER_LEAST = INSTR / WAVES, CPR = TR ? W / 8 : 8;
+// by which lane asks for which: piece p of row r is at p ^ (r & 7); with TR piece p of row k at p ^ swap(k): a unit of
+// sixteen columns stays one.
+template <int EL> __device__ __forceinline__ int swap(int k) { return EL == TF_F32 ? ((k >> 2) & 3) << 2 : ((k & 3) | ((k >> 3) & 1) << 2) << 1; }
+template <int EL, int W, bool TR, int WAVES> struct Loader {
+    static constexpr int BYTES = Size<EL>::BYTES, PIECE = Size<EL>::PIECE, STEP = Size<EL>::STEP;
+    static constexpr int INSTR = W / 8, PER = (INSTR + WAVES - 1) / WAVES, PER_LEAST = INSTR / WAVES, CPR = TR ? W / PIECE : 8;
     static_assert(!TR || W >= 64, "rows of a transposed operand");
     uint32_t off[PER];             // of each instruction's sixteen bytes, from the step's first ones on
     uint64_t base, at;             // of the tile in a part's first step; of the step that comes next
@@ -51,43 +67,43 @@ template <int W, bool TR, int WAVES> struct Loader {
     static __device__ __forceinline__ int row_of(int j, int lane) { return j * (64 / CPR) + lane / CPR; }
     static __device__ __forceinline__ int chunk_of(int j, int lane) {
         const int r = row_of(j, lane), s = lane % CPR;
-        return TR ? s ^ ((((r & 3) | ((r >> 3) & 1) << 2) << 1) & (CPR - 1)) : s ^ (r & 7);
+        return TR ? s ^ (swap<EL>(r) & (CPR - 1)) : s ^ (r & 7);
     }
     // first: the tile's first row of M or N; k: the first column (row with TR) of K.
     __device__ __forceinline__ void begin(const Side &s, int64_t first, int64_t k, int part, int wave, int lane) {
-        row = (uint32_t)(s.ld * 2);
+        row = (uint32_t)(s.ld * BYTES);
         const int64_t there = (TR ? s.cols : s.rows) - first;      // of M or N
         const uint32_t some = (uint32_t)(there < 0 ? 0 : there < W ? there : W);
-        tail = some * 2;
-        base = (uint64_t)s.p + (uint64_t)((TR ? k * s.ld + first : first * s.ld + k) * 2);
-        stride = TR ? kStep * row : kStep * 2;
-        records = TR ? (kStep - 1) * row + tail : some ? (some - 1) * row + kStep * 2 : 0;
+        tail = some * BYTES;
+        base = (uint64_t)s.p + (uint64_t)((TR ? k * s.ld + first : first * s.ld + k) * BYTES);
+        stride = TR ? STEP * row : 128;
+        records = TR ? (STEP - 1) * row + tail : some ? (some - 1) * row + 128 : 0;
         left0 = (int32_t)((TR ? s.rows : s.cols) - k);
         go_to(s, part);
 #pragma unroll
         for (int c = 0; c < PER; ++c) {
             const int j = wave + WAVES * c;
             const uint32_t o = (uint32_t)row_of(j, lane) * row + chunk_of(j, lane) * 16;
-            off[c] = (uint32_t)(TR ? chunk_of(j, lane) * 8 : row_of(j, lane)) < some ? o : ~0u;
+            off[c] = (uint32_t)(TR ? chunk_of(j, lane) * PIECE : row_of(j, lane)) < some ? o : ~0u;
         }
     }
     __device__ __forceinline__ void go_to(const Side &s, int part) {
-        at = base + (uint64_t)(part * s.plane * 2);
+        at = base + (uint64_t)(part * s.plane * BYTES);
         left = left0;
     }
     // Where the next step lies, what lies behind its end counting as zeros; goes on to the one after it.
     __device__ __forceinline__ Words4 next(int lane) {
-        const uint32_t n = !TR || left >= kStep ? records : left <= 0 ? 0u : (uint32_t)(left - 1) * row + tail;
+        const uint32_t n = !TR || left >= STEP ? records : left <= 0 ? 0u : (uint32_t)(left - 1) * row + tail;
         const Words4 w{(uint32_t)at, (uint32_t)(at >> 32), n, 0x00020000u};
-        if (!TR && left < kStep) {
-            // The last step, which ends inside of a piece of 64 columns.  (A lane's columns are the same ones in every instruction; numbers in parts have
-            // whole pieces, so that this is the end of all steps.)
-            if (chunk_of(0, lane) * 8 >= left)
+        if (!TR && left < STEP) {
+            // The last step, which ends inside of its columns.  (A lane's columns are the same ones in every instruction; numbers in parts have
+            // whole steps, so that this is the end of all steps.)
+            if (chunk_of(0, lane) * PIECE >= left)
 #pragma unroll
                 for (int c = 0; c < PER; ++c) off[c] = ~0u;
         }
         at += stride;
-        left -= kStep;
+        left -= STEP;
         return w;
     }
     // Instruction C of those that load a step into LDS from lds + AT on; lds: of this wave's first instruction.
@@ -99,23 +115,24 @@ template <int W, bool TR, int WAVES> struct Loader {
 
 // The same for rows that begin at any element: through registers.  A step is fetched where the other loader's loads go out, and put into LDS before the
 // barrier that they are waited for at.
-template <int W, bool TR, int WAVES> struct AnyLoader {
-    typedef Loader<W, TR, WAVES> Way;
+template <int EL, int W, bool TR, int WAVES> struct AnyLoader {
+    typedef Loader<EL, W, TR, WAVES> Way;
+    static constexpr int BYTES = Way::BYTES, PIECE = Way::PIECE, STEP = Way::STEP;
     static constexpr int INSTR = Way::INSTR, PER = Way::PER, PER_LEAST = 0;      // (no load of it is waited for by counting)
     const char *at;                // the next step's first row and column
     int64_t row, stride;           // bytes from row to row, from step to step
     int32_t some, left;            // of M or N in the tile; of K from the next step on
-    bool wide;                     // rows have eight columns or more
+    bool wide;                     // rows have a piece or more
     Words4 r[PER];
 
     __device__ __forceinline__ void begin(const Side &s, int64_t first, int64_t k, int, int, int) {
-        row = s.ld * 2;
+        row = s.ld * BYTES;
         const int64_t there = (TR ? s.cols : s.rows) - first;
         some = (int32_t)(there < 0 ? 0 : there < W ? there : W);
         left = (int32_t)((TR ? s.rows : s.cols) - k);
-        wide = s.cols >= 8;
-        at = static_cast<const char *>(s.p) + (TR ? k * s.ld + first : first * s.ld + k) * 2;
-        stride = TR ? kStep * row : kStep * 2;
+        wide = s.cols >= PIECE;
+        at = static_cast<const char *>(s.p) + (TR ? k * s.ld + first : first * s.ld + k) * BYTES;
+        stride = TR ? STEP * row : 128;
     }
     __device__ __forceinline__ void go_to(const Side &, int) {}
     __device__ __forceinline__ Words4 next(int) { return Words4{0, 0, 1, 0}; }
@@ -123,23 +140,27 @@ template <int W, bool TR, int WAVES> struct AnyLoader {
     template <int C, int AT> __device__ __forceinline__ void load(const Words4 &, uint32_t, bool is, int wave, int lane) {
         const int j = wave + WAVES * C;
         if (INSTR % WAVES != 0 && j >= INSTR) return;
-        const int o = Way::row_of(j, lane), c = Way::chunk_of(j, lane) * 8, n = (TR ? some : left) - c;
-        const char *p = at + o * row + c * 2;
+        const int o = Way::row_of(j, lane), c = Way::chunk_of(j, lane) * PIECE, n = (TR ? some : left) - c;
+        const char *p = at + o * row + c * BYTES;
         Words4 w{0, 0, 0, 0};
         if (is && o < (TR ? left : some)) {
-            if (n >= 8) {
+            if (n >= PIECE) {
                 w = *reinterpret_cast<const AnyWords4 *>(p);
             } else if (n > 0 && wide) {
-                // the row's last eight, of which the first ones go
-                const AnyWords4 x = *reinterpret_cast<const AnyWords4 *>(p - (8 - n) * 2);
+                // the row's last piece, whose first elements go
+                const AnyWords4 x = *reinterpret_cast<const AnyWords4 *>(p - (PIECE - n) * BYTES);
                 const uint64_t lo = x[0] | (uint64_t)x[1] << 32, hi = x[2] | (uint64_t)x[3] << 32;
-                const int off = 16 * (8 - n);        // 16 .. 112 bits
+                const int off = 8 * BYTES * (PIECE - n);        // 16 .. 112 bits
                 const uint64_t l = off < 64 ? lo >> off | hi << (64 - off) : hi >> (off - 64), h = off < 64 ? hi >> off : 0;
                 w = Words4{(uint32_t)l, (uint32_t)(l >> 32), (uint32_t)h, (uint32_t)(h >> 32)};
             } else if (n > 0) {
                 for (int i = 0; i < n; ++i) {
-                    const uint32_t x = reinterpret_cast<const uint16_t *>(p)[i];
-                    w[i / 2] |= x << (16 * (i & 1));
+                    if constexpr (BYTES == 4) {
+                        w[i] = reinterpret_cast<const uint32_t *>(p)[i];
+                    } else {
+                        const uint32_t x = reinterpret_cast<const uint16_t *>(p)[i];
+                        w[i / 2] |= x << (16 * (i & 1));
+                    }
                 }
             }
         }
@@ -150,34 +171,41 @@ template <int W, bool TR, int WAVES> struct AnyLoader {
         for (int c = 0; c < PER; ++c)
             if (INSTR % WAVES == 0 || wave + WAVES * c < INSTR) *reinterpret_cast<Words4 *>(lds + (wave + WAVES * c) * 1024 + lane * 16) = r[c];
         at += stride;
-        left -= kStep;
+        left -= STEP;
     }
 };
 
-// T operands of 16 rows x 32 of K, from row `first` of the step on.
-template <int W, bool TR, int T> struct Reader {
+// T operands of 16 rows x half a step, from row `first` of the step on: lane l has row l % 16 and a piece of K, number l / 16 of the half's four.
+template <int EL, int W, bool TR, int T> struct Reader {
+    static constexpr int BYTES = Size<EL>::BYTES, PIECE = Size<EL>::PIECE, HALF = Size<EL>::STEP / 2;
+    typedef typename Mfma<EL>::V V;
     uint32_t at[TR ? T : 2];
     __device__ __forceinline__ void begin(int first, int lane) {
-        if constexpr (TR) {
-            const int k = 8 * (lane / 16) + lane % 16 / 4, swap = (k & 3) | ((k >> 3) & 1) << 2;
+        if constexpr (TR && BYTES == 4) {
+            const int k = 4 * (lane / 16), m = lane % 16;
 #pragma unroll
-            for (int i = 0; i < T; ++i) {
-                const int unit = (first / 16 + i) ^ (swap & (W / 16 - 1));
-                at[i] = k * (W * 2) + unit * 32 + (lane % 4) * 8;
-            }
+            for (int i = 0; i < T; ++i) at[i] = k * (W * 4) + (((first + 16 * i + m) / 4) ^ (swap<EL>(k) & (W / 4 - 1))) * 16 + m % 4 * 4;
+        } else if constexpr (TR) {
+            const int k = 8 * (lane / 16) + lane % 16 / 4;
+#pragma unroll
+            for (int i = 0; i < T; ++i) at[i] = k * (W * 2) + (((first + 16 * i) / 8 + lane % 4 / 2) ^ (swap<EL>(k) & (W / 8 - 1))) * 16 + lane % 2 * 8;
         } else {
 #pragma unroll
             for (int kk = 0; kk < 2; ++kk) at[kk] = (first + lane % 16) * 128 + (((kk * 4 + lane / 16) ^ (lane & 7)) * 16);
         }
     }
     // Operand i of half kk of a step that lies at lds.
-    template <int EL> __device__ __forceinline__ typename Mfma<EL>::V read(const char *lds, int kk, int i) const {
-        if constexpr (TR) {
-            const Short4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsShort4)(lds + at[i] + kk * 32 * W * 2));
-            const Short4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsShort4)(lds + at[i] + kk * 32 * W * 2 + 4 * W * 2));
-            return __builtin_bit_cast(typename Mfma<EL>::V, (Short8){lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]});
+    __device__ __forceinline__ V read(const char *lds, int kk, int i) const {
+        if constexpr (TR && BYTES == 4) {
+            const char *p = lds + at[i] + kk * HALF * W * 4;
+            return V{*reinterpret_cast<const float *>(p), *reinterpret_cast<const float *>(p + W * 4), *reinterpret_cast<const float *>(p + W * 8),
+                     *reinterpret_cast<const float *>(p + W * 12)};
+        } else if constexpr (TR) {
+            const Short4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsShort4)(lds + at[i] + kk * HALF * W * 2));
+            const Short4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsShort4)(lds + at[i] + kk * HALF * W * 2 + 4 * W * 2));
+            return __builtin_bit_cast(V, (Short8){lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]});
         } else {
-            return *reinterpret_cast<const typename Mfma<EL>::V *>(lds + at[kk] + i * 2048);
+            return *reinterpret_cast<const V *>(lds + at[kk] + i * 2048);
         }
     }
 };
@@ -215,6 +243,7 @@ template <int N, int I = 0, typename F> __device__ __forceinline__ void each(F &
 template <int EL, int WM, int WN, int TM, int TN, int PLACES, bool ANY, bool MTR, bool NTR, int END>
 __global__ __launch_bounds__(WM * WN * 64, TM * TN > 32 ? 1 : 2) void k_product(const ProductLaunch a) {
     constexpr int WAVES = WM * WN, BM = WM * TM * 16, BN = WN * TN * 16;
+    constexpr int STEP = Size<EL>::STEP;
     constexpr bool BIG = TM * TN > 32;      // sums fill the accumulation registers: left alone, the compiler moves them about in every step
     extern __shared__ __attribute__((aligned(1024))) char lds[];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wm = wave / WN, wn = wave % WN;
@@ -222,7 +251,7 @@ __global__ __launch_bounds__(WM * WN * 64, TM * TN > 32 ? 1 : 2) void k_product(
     // Tiles: a contiguous share for each XCD, in bands of eight rows of tiles, so that the 32 workgroups that an XCD runs at a time are eight by four
     // tiles and its L2 is asked for twelve pieces of operands a step, not 33.
     // (Only as many as there are kept rows for; a share of K that would have under four steps is not made.)
-    int steps = a.k_rows ? (kept + kStep - 1) / kStep : a.k_steps;
+    int steps = a.k_rows ? (kept + STEP - 1) / STEP : a.k_steps;
     const int n_tiles = a.n_rows ? (kept + BN - 1) / BN : a.n_tiles, splits = shares_of(a.splits, steps);
     const int tiles = a.m_tiles * n_tiles, all = tiles * splits;
     int b = blockIdx.x;
@@ -240,14 +269,14 @@ __global__ __launch_bounds__(WM * WN * 64, TM * TN > 32 ? 1 : 2) void k_product(
     const int s0 = (int)((int64_t)steps * split / splits), s1 = (int)((int64_t)steps * (split + 1) / splits);
     const int pairs = a.parts == 3 ? 6 : 1, total = pairs * (s1 - s0);
     int pair = a.parts == 3 ? 0 : 5, in_pair = s1 - s0, to_load = total;
-    typedef std::conditional_t<ANY, AnyLoader<BM, MTR, WAVES>, Loader<BM, MTR, WAVES>> LM;
-    typedef Loader<BN, NTR, WAVES> LN;
+    typedef std::conditional_t<ANY, AnyLoader<EL, BM, MTR, WAVES>, Loader<EL, BM, MTR, WAVES>> LM;
+    typedef Loader<EL, BN, NTR, WAVES> LN;
     LM lm;
     LN ln;
-    lm.begin(M, m0, (int64_t)s0 * kStep, part_m(pair), wave, lane);
-    ln.begin(N, n0, (int64_t)s0 * kStep, part_n(pair), wave, lane);
-    Reader<BM, MTR, TM> rm;
-    Reader<BN, NTR, TN> rn;
+    lm.begin(M, m0, (int64_t)s0 * STEP, part_m(pair), wave, lane);
+    ln.begin(N, n0, (int64_t)s0 * STEP, part_n(pair), wave, lane);
+    Reader<EL, BM, MTR, TM> rm;
+    Reader<EL, BN, NTR, TN> rn;
     rm.begin(wm * TM * 16, lane);
     rn.begin(wn * TN * 16, lane);
     Float4 acc[TM][TN] = {};
@@ -276,8 +305,8 @@ __global__ __launch_bounds__(WM * WN * 64, TM * TN > 32 ? 1 : 2) void k_product(
     auto put = [&](auto to) { lm.put(lds + decltype(to)::value * BM * 128, wave, lane); };
     typename Mfma<EL>::V vm[2][TM], vn[2][TN];
     auto read = [&](int r, int half, int from) {
-        if (r < TM) vm[half][r] = rm.template read<EL>(lds + from * BM * 128, half, r);
-        else if (r < READS) vn[half][r - TM] = rn.template read<EL>(lds + AT_N + from * BN * 128, half, r - TM);
+        if (r < TM) vm[half][r] = rm.read(lds + from * BM * 128, half, r);
+        else if (r < READS) vn[half][r - TM] = rn.read(lds + AT_N + from * BN * 128, half, r - TM);
     };
     // Multiplies one half of a step.  Meanwhile the other half's operands come from LDS (`reads`: of the step at place `from`), the loads of a step go
     // out (`loads`: to place `to`), or are set up.  An instruction of the matrix cores takes the time of four others: these are spread, a few
@@ -404,7 +433,8 @@ __global__ __launch_bounds__(WM * WN * 64, TM * TN > 32 ? 1 : 2) void k_product(
                 }
             } else if (is) {
                 const float from = a.lse[row] * LOG2E, scale = a.g[row];
-                uint16_t *out = static_cast<uint16_t *>(a.G) + row * a.g_ld + mw + 4 * g;
+                typedef typename El<EL>::T T;
+                T *out = static_cast<T *>(a.G) + row * a.g_ld + mw + 4 * g;
                 typedef uint16_t U4 __attribute__((ext_vector_type(4)));
 #pragma unroll
                 for (int x = 0; x < TM; ++x) {
@@ -420,7 +450,9 @@ __global__ __launch_bounds__(WM * WN * 64, TM * TN > 32 ? 1 : 2) void k_product(
 #pragma unroll
                         for (int v = 0; v < 4; ++v)
                             if (mw + 16 * x + 4 * g + v >= a.m_count) d[v] = 0.0f;
-                    if (EL == TF_BF16 && a.parts == 3) {
+                    if constexpr (EL == TF_F32) {
+                        *reinterpret_cast<Float4 *>(out + 16 * x) = Float4{d[0], d[1], d[2], d[3]};
+                    } else if (EL == TF_BF16 && a.parts == 3) {
                         uint16_t p[4][3];
 #pragma unroll
                         for (int v = 0; v < 4; ++v) split3<EL>(d[v], p[v]);
@@ -473,7 +505,7 @@ __global__ __launch_bounds__(WM * WN * 64, TM * TN > 32 ? 1 : 2) void k_product(
                     typedef uint16_t U4 __attribute__((ext_vector_type(4), aligned(2)));
                     U4 d;
 #pragma unroll
-                    for (int v = 0; v < 4; ++v) d[v] = El<EL>::put(f[v]);
+                    for (int v = 0; v < 4; ++v) d[v] = El<EL == TF_F32 ? TF_BF16 : EL>::put(f[v]);
                     if (m + 4 <= a.m_count) *reinterpret_cast<U4 *>(to) = d;
                     else
                         for (int v = 0; v < 4; ++v)
@@ -511,8 +543,9 @@ template <int EL, bool ANY, bool MTR, bool NTR, int END> int product_tile(const 
         if (a.tile == kTile16) return product_with<EL, 4, 1, 1, 1, 4, ANY, MTR, NTR, END>(a, st);
     }
     if constexpr (ANY && END != kEndSums) return (int)hipErrorInvalidValue;       // (gradients of few rows only)
-    else if (a.tile == kTile256) return product_with<EL, 2, 2, 8, 8, 2, ANY, MTR, NTR, END>(a, st);
-    else return product_with<EL, 2, 2, 4, 4, 2, ANY, MTR, NTR, END>(a, st);
+    if constexpr (EL != TF_F32 && !(ANY && END != kEndSums))
+        if (a.tile == kTile256) return product_with<EL, 2, 2, 8, 8, 2, ANY, MTR, NTR, END>(a, st);
+    if constexpr (!(ANY && END != kEndSums)) return product_with<EL, 2, 2, 4, 4, 2, ANY, MTR, NTR, END>(a, st);
 }
 template <int EL, bool MTR, int END> int product_any(const ProductLaunch &a, hipStream_t st) {
     return a.any ? product_tile<EL, true, MTR, false, END>(a, st) : product_tile<EL, false, MTR, false, END>(a, st);

@@ -58,7 +58,8 @@ template <int EL> __device__ __forceinline__ void write8(const float (&x)[8], vo
 }
 
 // Eight columns as an operand of the products: 16-bit numbers as they are, fp32 ones as three bf16 numbers that add up to them.
-template <int EL> __device__ __forceinline__ void put8(const float (&x)[8], uint16_t *to, int64_t plane) {
+template <int EL> __device__ __forceinline__ void put8(const float (&x)[8], void *to_row, int64_t k, int64_t plane) {
+    uint16_t *to = static_cast<uint16_t *>(to_row) + k;
     Words4 w[3];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
@@ -137,7 +138,7 @@ template <int EL> __device__ __forceinline__ void pack_classes(const XentLaunch 
         for (int64_t k = threadIdx.x % per_row * 8; k < columns; k += per_row * 8) {
             float x[8];
             read8<EL>(x, static_cast<const typename El<EL>::T *>(a.W) + (first + i) * a.ldw, k, a.n_in);
-            put8<EL>(x, static_cast<uint16_t *>(a.s.w) + i * a.s.ld + k, a.s.w_cap);
+            put8<EL>(x, static_cast<uint16_t *>(a.s.w) + i * a.s.ld, k, a.s.w_cap);
         }
 }
 template <int EL> __global__ __launch_bounds__(256) void k_pack_classes(const XentLaunch a, const int64_t first, const int64_t count) {
@@ -214,7 +215,8 @@ template <int EL> __global__ __launch_bounds__(256) void k_pack_rows(const XentL
             for (int64_t k = tid % per_row * 8; k < columns; k += per_row * 8) {
                 float x[8];
                 read8<EL>(x, static_cast<const typename El<EL>::T *>(a.X) + rows[i] * a.ldx, k, a.n_in);
-                put8<EL>(x, static_cast<uint16_t *>(a.s.x) + (n + i) * a.s.ld + k, a.s.x_plane);
+                if (EL == TF_F32 && a.native) write8<TF_F32>(x, static_cast<float *>(a.s.x) + (n + i) * a.s.ld, k, columns);
+                else put8<EL>(x, static_cast<uint16_t *>(a.s.x) + (n + i) * a.s.ld, k, a.s.x_plane);
             }
         if (a.dX && a.direct_dx)
             for (int i = tid / per_row; i < (int)min(end - r0, (int64_t)256); i += at_once)
@@ -311,6 +313,8 @@ template <int EL> __device__ __forceinline__ void finish_row(const float *slab, 
     }
 }
 constexpr int kManySlabs = 8;
+// Columns of a step of the products.
+__host__ __device__ constexpr int step_of(const XentLaunch &a) { return a.native ? 32 : 64; }
 
 // dX: the shares' sums of each row that counts, zeros in the others.
 template <int EL> __global__ __launch_bounds__(256) void k_finish_rows(const XentLaunch a, const int splits, const int64_t size) {      // (the same for every piece)
@@ -327,7 +331,7 @@ template <int EL> __global__ __launch_bounds__(256) void k_finish_rows(const Xen
 }
 // Rows first .. first + count of dW.
 template <int EL> __global__ __launch_bounds__(256) void k_finish_classes(const XentLaunch a, const int64_t first, const int64_t count, const int most, const int64_t size) {
-    const int splits = shares_of(most, (int)ceil_div(*a.s.n, 64));
+    const int splits = shares_of(most, (int)ceil_div(*a.s.n, step_of(a)));
     const float unit = *a.s.unit;
     const int per_row = threads_of_row(a.n_in);
     const bool by_slab = splits >= kManySlabs;
@@ -357,19 +361,25 @@ dim3 slab_grid(int64_t rows, int64_t columns, int64_t splits) {
         else hipLaunchKernelGGL((kernel<TF_F32>), grid, dim3(256), 0, st, __VA_ARGS__);                                \
     } while (0)
 
-int launch_product(const ProductLaunch &p, int dtype, void *stream) {
-    return dtype == TF_F16 ? launch_product_f16(p, stream) : launch_product_bf16(p, stream);
+int launch_product(const ProductLaunch &p, const XentLaunch &a, void *stream) {
+    return a.dtype == TF_F16 ? launch_product_f16(p, stream) : a.native ? launch_product_f32(p, stream) : launch_product_bf16(p, stream);
 }
 
-// Whether W's rows are whole 16-byte pieces of 16-bit numbers, as the products load them.
+// Few fp32 rows are multiplied by the fp32 instructions, W where it lies: as parts its numbers would be written and read again several times.
+constexpr int kNativeRows = 64;
+bool is_native(const XentLaunch &a) { return a.dtype == TF_F32 && a.n_rows <= kNativeRows; }
+
+// Whether W's rows are whole 16-byte pieces, as the products load them.
 bool whole_pieces(const XentLaunch &a) {
-    return a.dtype != TF_F32 && a.n_in % 8 == 0 && (a.ldw % 8 == 0 || a.n_classes == 1) && reinterpret_cast<uintptr_t>(a.W) % 16 == 0 && a.ldw <= kXentMaxColumns;
+    const int64_t piece = a.dtype == TF_F32 ? 4 : 8;
+    return a.n_in % piece == 0 && (a.ldw % piece == 0 || a.n_classes == 1) && reinterpret_cast<uintptr_t>(a.W) % 16 == 0 && a.ldw <= kXentMaxColumns;
 }
-// Otherwise 16-bit numbers go through registers while there are few rows, and are copied first where the products take long enough to pay for that.
+// Otherwise they go through registers while there are few rows, and are copied first where the products take long enough to pay for that.
 // 1023 -> 40000 classes, bf16, through registers / copied, us: loss of 64 rows 37 / 60, 300 64 / 78, 1024 135 / 133; gradients of 64 126 / 140, 300 226 / 201.
-// fp32 is always packed, as three parts.
-bool through_registers(const XentLaunch &a) { return a.dtype != TF_F32 && !whole_pieces(a) && a.n_rows <= (a.loss ? 1023 : 64); }
-bool in_place(const XentLaunch &a) { return whole_pieces(a) || through_registers(a); }
+// fp32 numbers that are multiplied in parts are always packed.
+bool through_registers(const XentLaunch &a) { return !whole_pieces(a) && (a.dtype == TF_F32 ? a.native : a.n_rows <= (a.loss ? 1023 : 64)); }
+bool in_place(const XentLaunch &a) { return a.dtype == TF_F32 ? a.native : whole_pieces(a) || through_registers(a); }
+int parts_of(const XentLaunch &a) { return a.dtype == TF_F32 && !a.native ? 3 : 1; }
 
 // Numbers and copies the rows that count.  (Also without rows: it sets the unit.)  Up to 8192 rows every block counts the rows before it.  Packs the
 // first `classes` of W as well, where it has to be.
@@ -384,7 +394,7 @@ int begin(const XentLaunch &a, int64_t classes, hipStream_t st) {
 
 // W's rows as an operand, packed where they cannot be read in place (the first ones have been).
 Side classes(const XentLaunch &a, int64_t first, int64_t count, hipStream_t st) {
-    if (in_place(a)) return Side{static_cast<const uint16_t *>(a.W) + first * a.ldw, a.ldw, 0, count, a.n_in};
+    if (in_place(a)) return Side{static_cast<const char *>(a.W) + first * a.ldw * (a.dtype == TF_F32 ? 4 : 2), a.ldw, 0, count, a.n_in};
     if (first) TF_BY_TYPE(a.dtype, k_pack_classes, row_grid(count, round_up(a.n_in, 64)), a, first, count);
     return Side{a.s.w, a.s.ld, a.s.w_cap, count, round_up(a.n_in, 64)};
 }
@@ -394,8 +404,8 @@ ProductLaunch logits(const XentLaunch &a, const Side &W, int64_t first, int64_t 
     p.M = W;
     p.N = Side{a.s.x, a.s.ld, a.s.x_plane, round_up(a.n_rows, 256), round_up(a.n_in, 64)};
     p.any = through_registers(a);
-    p.parts = a.dtype == TF_F32 ? 3 : 1;
-    p.k_steps = (int32_t)ceil_div(a.n_in, 64);
+    p.parts = parts_of(a);
+    p.k_steps = (int32_t)ceil_div(a.n_in, step_of(a));
     p.n = a.s.n;
     p.n_rows = 1;
     p.splits = 1;
@@ -443,8 +453,10 @@ Cut cut_product(int64_t m, int64_t n, int64_t steps, int pairs, bool rows, int64
 
 }  // namespace
 
-int launch_xent(const XentLaunch &a, void *stream) {
+int launch_xent(const XentLaunch &call, void *stream) {
     const hipStream_t st = static_cast<hipStream_t>(stream);
+    XentLaunch a = call;
+    a.native = is_native(a);
     const int64_t ld = round_up(a.n_rows, 16);
     int64_t piece = a.s.part_cap / ld * 64 / 256 * 256;       // (a sum of every 64 classes at the most)
     if (!in_place(a)) piece = std::min(piece, a.s.w_cap / a.s.ld);
@@ -458,7 +470,7 @@ int launch_xent(const XentLaunch &a, void *stream) {
         p.hit = a.s.hit;
         p.part = a.s.part;
         p.part_ld = ld;
-        e = launch_product(p, a.dtype, stream);
+        e = launch_product(p, a, stream);
         if (e) return e;
         const int64_t blocks = ceil_div(count, m_side(p.tile)) * sums_of(p.tile);
         const int is_first = first == 0, is_last = first + count == a.n_classes;
@@ -474,14 +486,15 @@ int launch_xent(const XentLaunch &a, void *stream) {
 int launch_xent_grad(const XentLaunch &call, void *stream) {
     const hipStream_t st = static_cast<hipStream_t>(stream);
     XentLaunch a = call;
+    a.native = is_native(a);
     const int64_t rows = round_up(std::max(a.n_rows, 1), 256);
     int64_t piece = std::min(round_up(a.n_classes, 256), (a.s.g_cap / rows - kRowPad) / 256 * 256);
     if (!in_place(a)) piece = std::min(piece, a.s.w_cap / a.s.ld);
     const int64_t g_ld = piece + kRowPad;
-    const int parts = a.dtype == TF_F32 ? 3 : 1, pairs = parts == 3 ? 6 : 1;
+    const int parts = parts_of(a), pairs = parts == 3 ? 6 : 1, step = step_of(a);
     const int64_t dx_size = rows * a.s.ld;
     // (the same shares for every piece: the slabs are added to)
-    const Cut dx = cut_product(a.n_in, a.n_rows, ceil_div(std::min<int64_t>(piece, a.n_classes), 64), pairs, true, a.s.dx_cap / dx_size);
+    const Cut dx = cut_product(a.n_in, a.n_rows, ceil_div(std::min<int64_t>(piece, a.n_classes), step), pairs, true, a.s.dx_cap / dx_size);
     a.direct_dx = piece >= a.n_classes && dx.shares == 1;
     int e = begin(a, std::min<int64_t>(piece, a.n_classes), st);
     if (e) return e;
@@ -497,7 +510,7 @@ int launch_xent_grad(const XentLaunch &call, void *stream) {
             p.G = a.s.G;
             p.g_ld = g_ld;
             p.g_plane = a.s.g_cap;
-            e = launch_product(p, a.dtype, stream);
+            e = launch_product(p, a, stream);
             if (e) return e;
             if (a.dX) {
                 ProductLaunch q{};
@@ -505,7 +518,7 @@ int launch_xent_grad(const XentLaunch &call, void *stream) {
                 q.any = through_registers(a);
                 q.N = Side{a.s.G, g_ld, a.s.g_cap, rows, round_up(count, 64)};
                 q.parts = parts;
-                q.k_steps = (int32_t)ceil_div(count, 64);
+                q.k_steps = (int32_t)ceil_div(count, step);
                 q.n = a.s.n;
                 q.n_rows = 1;
                 q.m_count = a.n_in;
@@ -522,7 +535,7 @@ int launch_xent_grad(const XentLaunch &call, void *stream) {
                 q.slab_ld = a.s.ld;
                 q.slab_size = dx_size;
                 q.add = first != 0;
-                e = launch_product(q, a.dtype, stream);
+                e = launch_product(q, a, stream);
                 if (e) return e;
             }
         }
@@ -536,7 +549,7 @@ int launch_xent_grad(const XentLaunch &call, void *stream) {
             q.m_count = a.n_in;
             q.n_count = (int32_t)count;
             const int64_t size = round_up(count, 256) * a.s.ld;
-            const Cut dw = cut_product(a.n_in, count, ceil_div(a.n_rows, 64), pairs, false, a.s.dw_cap / size);
+            const Cut dw = cut_product(a.n_in, count, ceil_div(a.n_rows, step), pairs, false, a.s.dw_cap / size);
             q.tile = dw.tile;
             q.splits = (int32_t)dw.shares;
             q.unit = a.s.unit;
@@ -547,7 +560,7 @@ int launch_xent_grad(const XentLaunch &call, void *stream) {
             q.slab_ld = a.s.ld;
             q.slab_size = size;
             q.end = q.splits > 1 ? kEndSlab : kEndOut;
-            e = launch_product(q, a.dtype, stream);
+            e = launch_product(q, a, stream);
             if (e) return e;
             if (q.splits > 1) TF_BY_TYPE(a.dtype, k_finish_classes, slab_grid(count, a.n_in, q.splits), a, first, count, q.splits, size);
         }
