@@ -542,10 +542,13 @@ template <int EL, bool ANY, bool MTR, bool NTR, int END> int product_tile(const 
         if (a.tile == kTile64) return product_with<EL, 4, 1, 2, 4, 3, ANY, MTR, NTR, END>(a, st);
         if (a.tile == kTile16) return product_with<EL, 4, 1, 1, 1, 4, ANY, MTR, NTR, END>(a, st);
     }
-    if constexpr (ANY && END != kEndSums) return (int)hipErrorInvalidValue;       // (gradients of few rows only)
-    if constexpr (EL != TF_F32 && !(ANY && END != kEndSums))
-        if (a.tile == kTile256) return product_with<EL, 2, 2, 8, 8, 2, ANY, MTR, NTR, END>(a, st);
-    if constexpr (!(ANY && END != kEndSums)) return product_with<EL, 2, 2, 4, 4, 2, ANY, MTR, NTR, END>(a, st);
+    if constexpr (ANY && END != kEndSums && EL != TF_F32) {
+        return (int)hipErrorInvalidValue;       // (gradients of few rows only)
+    } else {
+        if constexpr (EL != TF_F32)
+            if (a.tile == kTile256) return product_with<EL, 2, 2, 8, 8, 2, ANY, MTR, NTR, END>(a, st);
+        return product_with<EL, 2, 2, 4, 4, 2, ANY, MTR, NTR, END>(a, st);
+    }
 }
 template <int EL, bool MTR, int END> int product_any(const ProductLaunch &a, hipStream_t st) {
     return a.any ? product_tile<EL, true, MTR, false, END>(a, st) : product_tile<EL, false, MTR, false, END>(a, st);

@@ -366,8 +366,9 @@ int launch_product(const ProductLaunch &p, const XentLaunch &a, void *stream) {
 }
 
 // Few fp32 rows are multiplied by the fp32 instructions, W where it lies: as parts its numbers would be written and read again several times.
-constexpr int kNativeRows = 64;
-bool is_native(const XentLaunch &a) { return a.dtype == TF_F32 && a.n_rows <= kNativeRows; }
+// 4096 -> 100000 classes, fp32 instructions / parts, us: loss of 1 row 320 / 1666, 128 948 / 1976, 600 3706 / 4077, 1024 5766 / 5153; gradients
+// of 128 2757 / 3801, 300 6560 / 6357.
+bool is_native(const XentLaunch &a) { return a.dtype == TF_F32 && a.n_rows <= (a.loss ? 448 : 192); }
 
 // Whether W's rows are whole 16-byte pieces, as the products load them.
 bool whole_pieces(const XentLaunch &a) {
@@ -429,10 +430,11 @@ struct Cut {
     ProductTile tile;
     int64_t shares;
 };
-Cut cut_product(int64_t m, int64_t n, int64_t steps, int pairs, bool rows, int64_t most) {
+Cut cut_product(int64_t m, int64_t n, int64_t steps, int pairs, bool native, bool rows, int64_t most) {
     most = std::max<int64_t>(1, std::min(most, steps / 4));       // (a share has four steps at least)
     n = std::max<int64_t>(n, 1);
-    if (rows && (n <= 64 || m <= 128)) {
+    // (fp32 instructions are what such a launch is bound by: no more rows of padding than there have to be)
+    if (rows && (n <= 64 || m <= 128 || (native && round_up(n, 64) < round_up(n, 128)))) {
         const ProductTile t = n <= 16 ? kTile16 : kTile64;
         const int64_t groups = ceil_div(m, m_side(t)) * ceil_div(n, n_side(t)), want = t == kTile16 ? 1024 : 512;
         return Cut{t, std::max<int64_t>(1, std::min(want / groups, most))};
@@ -465,7 +467,7 @@ int launch_xent(const XentLaunch &call, void *stream) {
     for (int64_t first = 0; first < a.n_classes; first += piece) {
         const int64_t count = std::min<int64_t>(piece, a.n_classes - first);
         ProductLaunch p = logits(a, classes(a, first, count, st), first, count);
-        p.tile = cut_product(count, a.n_rows, p.k_steps, p.parts == 3 ? 6 : 1, true, 0).tile;
+        p.tile = cut_product(count, a.n_rows, p.k_steps, p.parts == 3 ? 6 : 1, a.native, true, 0).tile;
         p.end = kEndSums;
         p.hit = a.s.hit;
         p.part = a.s.part;
@@ -494,7 +496,7 @@ int launch_xent_grad(const XentLaunch &call, void *stream) {
     const int parts = parts_of(a), pairs = parts == 3 ? 6 : 1, step = step_of(a);
     const int64_t dx_size = rows * a.s.ld;
     // (the same shares for every piece: the slabs are added to)
-    const Cut dx = cut_product(a.n_in, a.n_rows, ceil_div(std::min<int64_t>(piece, a.n_classes), step), pairs, true, a.s.dx_cap / dx_size);
+    const Cut dx = cut_product(a.n_in, a.n_rows, ceil_div(std::min<int64_t>(piece, a.n_classes), step), pairs, a.native, true, a.s.dx_cap / dx_size);
     a.direct_dx = piece >= a.n_classes && dx.shares == 1;
     int e = begin(a, std::min<int64_t>(piece, a.n_classes), st);
     if (e) return e;
@@ -503,7 +505,7 @@ int launch_xent_grad(const XentLaunch &call, void *stream) {
         if (a.n_rows) {
             const Side W = classes(a, first, count, st);
             ProductLaunch p = logits(a, W, first, count);
-            p.tile = cut_product(count, a.n_rows, p.k_steps, p.parts == 3 ? 6 : 1, true, 0).tile;
+            p.tile = cut_product(count, a.n_rows, p.k_steps, p.parts == 3 ? 6 : 1, a.native, true, 0).tile;
             p.end = kEndGradient;
             p.lse = a.s.lse;
             p.g = a.s.g;
@@ -549,7 +551,7 @@ int launch_xent_grad(const XentLaunch &call, void *stream) {
             q.m_count = a.n_in;
             q.n_count = (int32_t)count;
             const int64_t size = round_up(count, 256) * a.s.ld;
-            const Cut dw = cut_product(a.n_in, count, ceil_div(a.n_rows, step), pairs, false, a.s.dw_cap / size);
+            const Cut dw = cut_product(a.n_in, count, ceil_div(a.n_rows, step), pairs, a.native, false, a.s.dw_cap / size);
             q.tile = dw.tile;
             q.splits = (int32_t)dw.shares;
             q.unit = a.s.unit;
