@@ -441,7 +441,8 @@ Cut cut_product(int64_t m, int64_t n, int64_t steps, int pairs, bool native, boo
     }
     Cut best{kTile128, 1};
     double least = 0;
-    for (const ProductTile t : {kTile256, kTile128})
+    for (const ProductTile t : {kTile128, kTile256}) {
+        if (native && t == kTile256) continue;
         for (int64_t s = 1; s <= std::min<int64_t>(most, 512); s = s < 8 ? s + 1 : s * 5 / 4) {
             const double rounds = (double)ceil_div(ceil_div(m, m_side(t)) * ceil_div(n, n_side(t)) * s, 256), each = (double)steps * pairs / s;
             const double time = (t == kTile256 ? rounds * (14 * each + 130) : std::max(4 * rounds, 6.0) * each + 18 * rounds + 80) + (s > 1 ? 40 + (double)s * m * n / 50000 : 0.0);
@@ -450,6 +451,7 @@ Cut cut_product(int64_t m, int64_t n, int64_t steps, int pairs, bool native, boo
                 least = time;
             }
         }
+    }
     return best;
 }
 

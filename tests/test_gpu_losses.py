@@ -279,7 +279,7 @@ def test_xent(T, V, d, dtype):
 
 
 @pytest.mark.parametrize("dtype", [BF, HF, F])
-@pytest.mark.parametrize("T,V,d", [(3500, 3600, 72), (40, 3600, 3500), (3600, 70, 3500), (1500, 5000, 523), (1600, 2100, 523), (1024, 20000, 515)])
+@pytest.mark.parametrize("T,V,d", [(3500, 3600, 72), (40, 3600, 3500), (3600, 70, 3500), (1500, 5000, 523), (1600, 2100, 523), (1024, 20000, 515), (440, 40000, 1030)])
 def test_xent_large_tiles(T, V, d, dtype):
     """Enough tiles of 256 x 256 for the logits, for dW and for dX."""
     print(f"T{T} V{V} d{d} {dtype}", flush=True)
