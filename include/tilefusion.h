@@ -444,7 +444,7 @@ tf_status tf_moe_balance(const void *scores, int64_t ld, int32_t dtype, int32_t 
  *   - *dloss (a device float) times the gradient of the balance loss, with the counts of tf_moe_balance (held constant; those of
  *     several devices may have been added up).
  * Either dvals, or counts and dloss, may be NULL.  Scores of -inf or NaN get 0, rows without an entry zeros.  An expert that a row names
- * more than once counts as often.  dscores may be the scores' own array. */
+ * more than once counts as often.  dscores may be the scores' own array (with ldd = ld). */
 tf_status tf_moe_route_grad(const void *scores, int64_t ld, int32_t dtype, int32_t scoring, float scale, const tf_csr *A, const float *dvals,
                             const int32_t *counts, const float *dloss, void *dscores, int64_t ldd, void *hip_stream);
 
@@ -454,7 +454,8 @@ tf_status tf_moe_route_grad(const void *scores, int64_t ld, int32_t dtype, int32
  *     lse[t] = log sum_v exp(l_tv)                                 loss[t] = lse[t] - l_t,labels[t]
  *     g_tv   = dloss[t] (exp(l_tv - lse[t]) - [v = labels[t]])     dX = g W      dW = g^T X
  * The logits are made for a piece of the classes at a time, by both calls; g is held for a piece, rounded to 16 bits (bf16: to bf16; fp16: to
- * fp16 after division by the largest |dloss|, so that no size of dloss is lost; fp32: as three bf16 numbers, which hold 24 bits). */
+ * fp16 after division by the largest |dloss|, so that no size of dloss is lost; fp32: in 32 bits for few rows, else as three bf16 numbers, which
+ * hold 24 bits). */
 typedef struct tf_xent_desc {
     int64_t n_classes;    /* rows of W, at most 2^30                                       */
     int64_t n_in;         /* columns of X and W, at most 2^22                              */
@@ -472,8 +473,9 @@ tf_status tf_xent_destroy(tf_xent *plan);
 /* The number of the device that the plan was made on, which has to be the current one of every call. */
 tf_status tf_xent_device(const tf_xent *plan, int32_t *device);
 
-/* loss and lse (n_rows floats each) of X (n_rows x n_in, rows ldx apart) and W (n_classes x n_in, rows ldw apart).  W is read fastest where it is
- * 16-bit, its rows begin at multiples of 16 bytes and n_in is a multiple of 8; otherwise a copy is made of it, piece by piece.
+/* loss and lse (n_rows floats each) of X (n_rows x n_in, rows ldx apart) and W (n_classes x n_in, rows ldw apart).  W is read fastest where its
+ * rows begin at multiples of 16 bytes and are whole ones of them; with other rows, calls of many rows make a copy of it, piece by piece, and
+ * so do calls of many fp32 rows.
  * Two executions of one plan must not overlap (they share its workspace). */
 tf_status tf_xent_loss(const tf_xent *plan, const void *X, int64_t ldx, const void *W, int64_t ldw, const int32_t *labels, int64_t n_rows,
                        float *loss, float *lse, void *hip_stream);

@@ -48,7 +48,8 @@ struct XentSpace {
     float *lse, *g, *hit;         // log of the sum, gradient over the unit, logit of the label
     float *top, *sum;             // running maximum and sum of exponentials
     Float2 *part;                 // both for blocks of classes, block after block
-    void *x, *w, *G;              // operands: planes of 16-bit numbers
+    void *x, *w, *G;              // operands: rows that count, a copy of W where there has to be one, gradient of the logits; planes of 16-bit
+                                  // numbers, or (native) fp32
     float *dx, *dw;               // sums in 32 bits, one slab for each share of a contraction
     int64_t ld;                   // row length of x and w: n_in rounded up to 256, and kRowPad
     int64_t x_plane;              // elements

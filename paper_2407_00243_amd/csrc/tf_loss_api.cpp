@@ -75,8 +75,9 @@ struct Cut {
     }
 };
 
-// Sizes of the workspace: G (the gradient of the logits) is held for as many classes at a time as 2^28 numbers allow, partial sums
-// for 2^25 blocks of classes, slabs of split contractions up to 2^24 numbers, or what one share needs.
+// Sizes of the workspace: G (the gradient of the logits) and a copy of W are held for as many classes at a time as 2^28 numbers allow (256 at
+// least), partial sums for as many as leave 2^25 of them, slabs of the shares of dX up to 2^26 numbers, or what one share needs, of dW 2^25.  fp32 numbers
+// take three planes of 16 bits, in which they also lie as they are.
 int64_t lay_out(tf_xent &p, char *base) {
     const tf_xent_desc &d = p.d;
     tf::XentSpace &s = p.s;
@@ -183,6 +184,7 @@ tf_status tf_moe_route_grad(const void *scores, int64_t ld, int32_t dtype, int32
     if (!dscores || !counts != !dloss) return report(TF_EINVAL, "null argument");
     if (!dvals && !dloss) return report(TF_EINVAL, "no gradient is given");
     if (ldd < A->n_cols) return report(TF_EINVAL, "rows of the gradient are closer together than they are wide");
+    if (dscores == scores && ldd != ld) return report(TF_EINVAL, "a gradient in the scores' place has their rows");
     if (!aligned(dscores, bytes_of(dtype)) || !aligned(dvals, 4) || !aligned(counts, 4) || !aligned(dloss, 4))
         return report(TF_EINVAL, "arrays must be aligned to their elements");
     tf::RouterLaunch a = router_args(scores, ld, dtype, scoring, A, k);

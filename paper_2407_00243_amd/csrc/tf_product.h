@@ -18,7 +18,6 @@ template <> struct Mfma<TF_F32> {
         for (int i = 0; i < 4; ++i) c = __builtin_amdgcn_mfma_f32_16x16x4f32(a[i], b[i], c, 0, 0, 0);
         return c;
     }
-    static __device__ __forceinline__ void add(Float4 &c, V a, V b) { c = mul(a, b, c); }
 };
 template <> struct Mfma<TF_BF16> {
     typedef Bf8 V;
@@ -247,7 +246,7 @@ __global__ __launch_bounds__(WM * WN * 64, TM * TN > 32 ? 1 : 2) void k_product(
     constexpr bool BIG = TM * TN > 32;      // sums fill the accumulation registers: left alone, the compiler moves them about in every step
     extern __shared__ __attribute__((aligned(1024))) char lds[];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wm = wave / WN, wn = wave % WN;
-    const int kept = a.n ? *a.n : 0;
+    const int kept = *a.n;
     // Tiles: a contiguous share for each XCD, in bands of eight rows of tiles, so that the 32 workgroups that an XCD runs at a time are eight by four
     // tiles and its L2 is asked for twelve pieces of operands a step, not 33.
     // (Only as many as there are kept rows for; a share of K that would have under four steps is not made.)
@@ -493,10 +492,10 @@ __global__ __launch_bounds__(WM * WN * 64, TM * TN > 32 ? 1 : 2) void k_product(
                 Float4 f;
 #pragma unroll
                 for (int v = 0; v < 4; ++v) f[v] = value(x, y, v) * unit;
-                if (a.out_dtype == TF_F32) {
+                if (EL == TF_F32 || a.out_dtype == TF_F32) {
                     float *to = static_cast<float *>(a.out) + row * a.ldo + m;
                     typedef float F4 __attribute__((ext_vector_type(4), aligned(4)));
-                                        if (m + 4 <= a.m_count) *reinterpret_cast<F4 *>(to) = f;
+                    if (m + 4 <= a.m_count) *reinterpret_cast<F4 *>(to) = f;
                     else
                         for (int v = 0; v < 4; ++v)
                             if (m + v < a.m_count) to[v] = f[v];

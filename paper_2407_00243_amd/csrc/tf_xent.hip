@@ -455,6 +455,9 @@ Cut cut_product(int64_t m, int64_t n, int64_t steps, int pairs, bool native, boo
     return best;
 }
 
+// 256 rows of G stay below 2^32 bytes, as the products' loads count them.  (A plan for very many rows has room for more columns of few.)
+constexpr int64_t kMostColumnsOfG = (int64_t)1 << 22;
+
 }  // namespace
 
 int launch_xent(const XentLaunch &call, void *stream) {
@@ -492,7 +495,7 @@ int launch_xent_grad(const XentLaunch &call, void *stream) {
     XentLaunch a = call;
     a.native = is_native(a);
     const int64_t rows = round_up(std::max(a.n_rows, 1), 256);
-    int64_t piece = std::min(round_up(a.n_classes, 256), (a.s.g_cap / rows - kRowPad) / 256 * 256);
+    int64_t piece = std::min({round_up(a.n_classes, 256), (a.s.g_cap / rows - kRowPad) / 256 * 256, kMostColumnsOfG});
     if (!in_place(a)) piece = std::min(piece, a.s.w_cap / a.s.ld);
     const int64_t g_ld = piece + kRowPad;
     const int parts = parts_of(a), pairs = parts == 3 ? 6 : 1, step = step_of(a);

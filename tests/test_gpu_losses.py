@@ -286,6 +286,21 @@ def test_xent_large_tiles(T, V, d, dtype):
     check_xent(*xent_case(T, V, d, dtype, 1), what=f"T{T} V{V} d{d} {dtype}")
 
 
+@pytest.mark.parametrize("T,d,dtype", [(64, 33, BF), (65, 33, HF), (1023, 65, HF), (1024, 65, BF), (192, 33, F), (193, 33, F), (448, 70, F), (449, 70, F),
+                                       (193, 64, F), (449, 36, F), (257, 64, BF), (256, 64, HF)])
+def test_xent_around_borders(T, d, dtype):
+    """Numbers of rows at which another kernel is taken."""
+    print(f"T{T} d{d} {dtype}", flush=True)
+    check_xent(*xent_case(T, 1100, d, dtype, T + d, unlabelled=0.0), what=f"T{T} d{d} {dtype}")
+
+
+def test_xent_few_rows_of_a_plan_for_many():
+    """Such a plan has room for more columns of few rows' gradients than are taken at a time."""
+    V, d = (1 << 22) + 1000, 8
+    plan = tf.XentPlan(V, d, BF, max_rows=3500000)
+    check_xent(*xent_case(70, V, d, BF, 5), plan=plan, what="plan for many")
+
+
 @pytest.mark.parametrize("dtype,d", [(BF, 8), (F, 7)])
 def test_xent_in_pieces(dtype, d):
     """So many rows that three pieces of the classes are taken one after the other (in fp32 the loss's too)."""

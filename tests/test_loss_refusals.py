@@ -39,6 +39,7 @@ ROUTER = [
 @pytest.mark.parametrize("over,args,want", ROUTER + [
     ({}, dict(counts=None), "TF_EINVAL"), ({}, dict(mass=None), "TF_EINVAL"), ({}, dict(loss=None), "TF_EINVAL"),
     ({}, dict(workspace=None), "TF_EINVAL"), ({}, dict(mass=P + 1), "TF_EINVAL"), ({}, dict(workspace=P + 2), "TF_EINVAL"),
+    ({}, dict(workspace=P + 8), "TF_EINVAL"), (dict(n_rows=1 << 26, nnz=1 << 32), {}, "TF_EUNSUPPORTED"),
 ])
 def test_balance_refuses(over, args, want):
     a = dict(scores=P, ld=8, dtype=tf.TF_F32, scoring=0, counts=P, mass=P, loss=P, workspace=P)
@@ -52,6 +53,7 @@ def test_balance_refuses(over, args, want):
     ({}, dict(dvals=None, counts=None, dloss=None), "TF_EINVAL"), ({}, dict(counts=None), "TF_EINVAL"),
     ({}, dict(dloss=None), "TF_EINVAL"), ({}, dict(dscores=None), "TF_EINVAL"), ({}, dict(ldd=7), "TF_EINVAL"),
     ({}, dict(dscores=P + 2), "TF_EINVAL"), ({}, dict(dvals=P + 2), "TF_EINVAL"), ({}, dict(dloss=P + 1), "TF_EINVAL"),
+    ({}, dict(dscores=P, ldd=9), "TF_EINVAL"),
 ])
 def test_route_grad_refuses(over, args, want):
     a = dict(scores=P, ld=8, dtype=tf.TF_F32, scoring=0, dvals=P, counts=P, dloss=P, dscores=P, ldd=8)
