@@ -15,7 +15,7 @@ SOURCES = ["tf_kernels.hip", "tf_gemm.hip", "tf_chain.hip", "tf_gather.hip", "tf
            "tf_balance.hip", "tf_product_bf16.hip", "tf_product_f16.hip", "tf_product_f32.hip",
            "tf_xent.hip", "tf_loss_api.cpp"]
 HEADERS = ["tf_internal.h", "tf_device.h", "tf_moe.h", "tf_moe_device.h", "tf_experts.h",
-           "tf_loss.h", "tf_product.h", os.path.join("..", "..", "include", "tilefusion.h")]
+           "tf_loss.h", "tf_loss_device.h", "tf_product.h", os.path.join("..", "..", "include", "tilefusion.h")]
 
 # packed-fp32 instructions are switched off for all device code
 HIPCC_FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",

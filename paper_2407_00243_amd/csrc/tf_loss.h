@@ -43,6 +43,7 @@ struct XentSpace {
     int32_t *block_rows;          // kept rows of each block of rows
     float *block_top;             // largest |dloss| there
     int32_t *n;                   // kept rows
+    unsigned *arrived;            // for blocks of rows: workgroups that have left their sums
     float *unit;                  // what sums of gradients are multiplied by at the end
     int32_t *label;
     float *lse, *g, *hit;         // log of the sum, gradient over the unit, logit of the label
@@ -56,6 +57,7 @@ struct XentSpace {
     int64_t part_cap, g_cap, w_cap, dx_cap, dw_cap;     // elements that there is room for (of a plane)
 };
 constexpr int64_t kMostBlocks = 1024;      // of rows
+constexpr int kMostJoins = 1024;           // blocks of rows whose sums the last workgroup adds up
 // Elements between the rows of x, w and G: rows a power of two apart would all lie in one channel of an XCD's L2.
 constexpr int64_t kRowPad = 64;
 
@@ -103,6 +105,9 @@ struct ProductLaunch {
     float *hit;
     Float2 *part;                 // largest logit and sum of exponentials over it
     int64_t part_ld;
+    int32_t join;                 // 1: the last workgroup of a block of rows adds up its sums and writes
+    unsigned *arrived;
+    float *loss, *lse_out;        // (at out_row)
     void *G;
     int64_t g_ld, g_plane;
     float *slab;

@@ -3,7 +3,7 @@
 #include <algorithm>
 #include <type_traits>
 
-#include "tf_loss.h"
+#include "tf_loss_device.h"
 #include "tf_moe_device.h"
 
 namespace tf {
@@ -216,19 +216,58 @@ template <int LATER> __device__ __forceinline__ void arrive() { asm volatile("s_
 __device__ __forceinline__ int part_m(int pair) { return (0x001102 >> (4 * pair)) & 15; }
 __device__ __forceinline__ int part_n(int pair) { return (0x010120 >> (4 * pair)) & 15; }
 
-// Sums of exponentials over their largest argument: x holds that and the sum.
-__device__ __forceinline__ Float2 add_sums(Float2 x, Float2 y) {
-    constexpr float LOW = -__builtin_inff();
-    const float m = fmaxf(x[0], y[0]);
-    return Float2{m, (x[0] == LOW ? x[1] : x[1] * expf(x[0] - m)) + (y[0] == LOW ? y[1] : y[1] * expf(y[0] - m))};
-}
-
 template <int EL> __device__ __forceinline__ void split3(float x, uint16_t (&p)[3]) {
 #pragma unroll
     for (int i = 0; i < 3; ++i) {
         p[i] = El<EL>::put(x);
         x -= El<EL>::get(p[i]);
     }
+}
+
+// Numbers that another workgroup of the launch may read: past the caches that it does not share.
+__device__ __forceinline__ void store_past(float *to, float x) { __hip_atomic_store(to, x, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
+__device__ __forceinline__ void store_past(Float2 *to, Float2 x) {
+    __hip_atomic_store(reinterpret_cast<uint64_t *>(to), __builtin_bit_cast(uint64_t, x), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+__device__ __forceinline__ Float2 load_past(const Float2 *from) {
+    return __builtin_bit_cast(Float2, __hip_atomic_load(reinterpret_cast<const uint64_t *>(from), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT));
+}
+
+// The last workgroup of the `blocks` sums of rows first .. first + n adds them up in an order of its own and writes the losses: where there are few sums
+// that is sooner done than another launch.  A thread's stores are complete (the wait for all of them) before its workgroup's count; stores and loads pass
+// the caches that workgroups do not share, and the fences only keep the compiler from moving them.
+template <int THREADS> __device__ __forceinline__ void join_sums(const ProductLaunch &a, char *lds, int tile, int64_t first, int n, int blocks) {
+    int *flag = reinterpret_cast<int *>(lds + THREADS * sizeof(Float2));
+    Float2 *sums = reinterpret_cast<Float2 *>(lds);
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup");
+    __builtin_amdgcn_s_waitcnt(0);
+    __syncthreads();
+    if (a.m_tiles > 1) {
+        if (threadIdx.x == 0) *flag = atomicInc(a.arrived + tile, (unsigned)a.m_tiles - 1) == (unsigned)a.m_tiles - 1;
+        __syncthreads();
+        if (!*flag) return;
+    }
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup");
+    const int rows = n <= 1 ? 1 : 1 << (32 - __builtin_clz((unsigned)n - 1)), r = threadIdx.x & (rows - 1), slices = THREADS / rows;
+    Float2 x{-__builtin_inff(), 0.0f};
+    if (r < n) {
+        const Float2 *p = a.part + first + r;
+        for (int b0 = threadIdx.x / rows; b0 < blocks; b0 += 8 * slices) {
+            Float2 y[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) y[i] = load_past(p + (int64_t)min(b0 + i * slices, blocks - 1) * a.part_ld);
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                if (b0 + i * slices < blocks) x = add_sums(x, y[i]);
+        }
+    }
+    for (int d = rows; d < 64; d <<= 1) x = add_sums(x, Float2{__shfl_xor(x[0], d, 64), __shfl_xor(x[1], d, 64)});
+    sums[threadIdx.x] = x;
+    __syncthreads();
+    if ((int)threadIdx.x >= n) return;
+    for (int s = max(rows, 64); s < THREADS; s += max(rows, 64)) x = add_sums(x, sums[s + threadIdx.x]);
+    const int64_t to = a.out_row[first + threadIdx.x];
+    write_loss(x, __hip_atomic_load(a.hit + first + threadIdx.x, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT), a.loss + to, a.lse_out + to);
 }
 
 // f(0), f(1), ... f(N - 1), the number known when the code is made.
@@ -405,7 +444,7 @@ __global__ __launch_bounds__(WM * WN * 64, TM * TN > 32 ? 1 : 2) void k_product(
 #pragma unroll
                         for (int v = 0; v < 4; ++v)
                             if (at == 16 * x + v) {
-                                a.hit[row] = l[x][v];
+                                store_past(a.hit + row, l[x][v]);
                                 l[x][v] = -__builtin_inff();
                             }
                 const float from = top == -__builtin_inff() ? 0.0f : top * LOG2E;
@@ -416,7 +455,7 @@ __global__ __launch_bounds__(WM * WN * 64, TM * TN > 32 ? 1 : 2) void k_product(
                 sum += __shfl_xor(sum, 16, 64);
                 sum += __shfl_xor(sum, 32, 64);
                 if constexpr (WN > 1) {
-                    if (is && g == 0) a.part[((int64_t)mt * WM + wm) * a.part_ld + row] = Float2{top, sum};
+                    if (is && g == 0) store_past(a.part + ((int64_t)mt * WM + wm) * a.part_ld + row, Float2{top, sum});
                 } else {        // few rows: the waves' sums are put together first
                     Float2 *all = reinterpret_cast<Float2 *>(lds);
                     if (g == 0) all[(wm * TN + y) * 16 + lane] = Float2{top, sum};
@@ -426,7 +465,7 @@ __global__ __launch_bounds__(WM * WN * 64, TM * TN > 32 ? 1 : 2) void k_product(
                             const int64_t to = n0 + i;
                             Float2 x = all[i];
                             for (int w = 1; w < WM; ++w) x = add_sums(x, all[w * TN * 16 + i]);
-                            if (to < kept) a.part[(int64_t)mt * a.part_ld + to] = x;
+                            if (to < kept) store_past(a.part + (int64_t)mt * a.part_ld + to, x);
                         }
                     }
                 }
@@ -463,6 +502,8 @@ __global__ __launch_bounds__(WM * WN * 64, TM * TN > 32 ? 1 : 2) void k_product(
                 }
             }
         }
+        if constexpr (END == kEndSums)
+            if (a.join) join_sums<WM * WN * 64>(a, lds, nt, n0, (int)min((int64_t)BN, kept - n0), a.m_tiles * (WN > 1 ? WM : 1));
     } else if constexpr (END == kEndSlab) {
         const int64_t rows = a.n_rows ? kept : a.n_count;
 #pragma unroll

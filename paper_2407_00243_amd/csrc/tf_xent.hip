@@ -1,7 +1,7 @@
 // Cross entropy of a product: the rows that count, operands, merging of sums, and the launches of a call.
 #include <algorithm>
 
-#include "tf_loss.h"
+#include "tf_loss_device.h"
 #include "tf_moe_device.h"
 
 namespace tf {
@@ -228,15 +228,13 @@ template <int EL> __global__ __launch_bounds__(256) void k_pack_rows(const XentL
         n += here;
     }
     if ((int)blockIdx.x == blocks - 1 && tid == 0) *a.s.n = n;
+    if (blockIdx.x == 0)
+        for (int i = tid; i < kMostJoins; i += 256) a.s.arrived[i] = 0;
 }
 // ------------------------------------------------------------------------------------------- ends
 
 // Adds the sums of `blocks` blocks of classes to those of the classes before them (unless `first`).  ROWS rows a workgroup: 64 / ROWS lanes of each of
 // its 16 waves take a row, and all of them every block once.  The last call writes the results.
-__device__ __forceinline__ void add_sums(Float2 &x, Float2 y) {
-    const float m = fmaxf(x[0], y[0]);
-    x = Float2{m, (x[0] == kLow ? x[1] : x[1] * expf(x[0] - m)) + (y[0] == kLow ? y[1] : y[1] * expf(y[0] - m))};
-}
 template <int ROWS> __global__ __launch_bounds__(1024) void k_merge(const XentLaunch a, const int64_t blocks, const int64_t ld, const int first, const int last) {
     __shared__ Float2 of_wave[16][ROWS];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
@@ -246,25 +244,24 @@ template <int ROWS> __global__ __launch_bounds__(1024) void k_merge(const XentLa
     Float2 x{kLow, 0.0f};
     if (row < n)
 #pragma unroll 4
-        for (int64_t b = wave * (64 / ROWS) + lane / ROWS; b < blocks; b += 16 * (64 / ROWS)) add_sums(x, a.s.part[b * ld + row]);
+        for (int64_t b = wave * (64 / ROWS) + lane / ROWS; b < blocks; b += 16 * (64 / ROWS)) x = add_sums(x, a.s.part[b * ld + row]);
 #pragma unroll
-    for (int d = ROWS; d < 64; d <<= 1) add_sums(x, Float2{__shfl_xor(x[0], d, 64), __shfl_xor(x[1], d, 64)});
+    for (int d = ROWS; d < 64; d <<= 1) x = add_sums(x, Float2{__shfl_xor(x[0], d, 64), __shfl_xor(x[1], d, 64)});
     if (lane < ROWS) of_wave[wave][lane] = x;
     __syncthreads();
-    if (wave || row >= n || lane >= ROWS) return;
-    x = first ? Float2{kLow, 0.0f} : Float2{a.s.top[row], a.s.sum[row]};
-    for (int w = 0; w < 16; ++w) add_sums(x, of_wave[w][lane]);
-    const float top = x[0], sum = x[1];
+    if (wave) return;
+    x = !first && row < n && lane < ROWS ? Float2{a.s.top[row], a.s.sum[row]} : Float2{kLow, 0.0f};
+    for (int w = lane / ROWS; w < 16; w += 64 / ROWS) x = add_sums(x, of_wave[w][lane % ROWS]);
+#pragma unroll
+    for (int d = ROWS; d < 64; d <<= 1) x = add_sums(x, Float2{__shfl_xor(x[0], d, 64), __shfl_xor(x[1], d, 64)});
+    if (row >= n || lane >= ROWS) return;
     if (!last) {
-        a.s.top[row] = top;
-        a.s.sum[row] = sum;
+        a.s.top[row] = x[0];
+        a.s.sum[row] = x[1];
         return;
     }
-    // `sum` is that of the other classes: a small loss keeps its precision as log(1 + sum / exp(label's logit))
-    const float hit = a.s.hit[row], lse = top + logf(sum + expf(hit - top));
     const int64_t to = a.s.list[row];
-    a.lse[to] = lse;
-    a.loss[to] = top - hit < 40.0f ? log1pf(sum * expf(top - hit)) : lse - hit;
+    write_loss(x, a.s.hit[row], a.loss + to, a.lse + to);
 }
 
 // Rows `row` of an output from the sums of `splits` slabs, `none` for zeros.  A row's columns lie in `per_row` threads; the others of a workgroup take
@@ -458,6 +455,10 @@ Cut cut_product(int64_t m, int64_t n, int64_t steps, int pairs, bool native, boo
 // 256 rows of G stay below 2^32 bytes, as the products' loads count them.  (A plan for very many rows has room for more columns of few.)
 constexpr int64_t kMostColumnsOfG = (int64_t)1 << 22;
 
+// Whether the last workgroup of a block of rows adds up its `sums` sums: the workgroups count themselves in one after the other, 20 ns each.
+// (65536 classes of one row, 1024 workgroups: 125 us, by another launch 99 + 7.)
+bool joins(int64_t m_tiles, int64_t n_tiles, int64_t sums) { return m_tiles == 1 || (m_tiles <= 1024 && n_tiles <= kMostJoins && sums <= 8192); }
+
 }  // namespace
 
 int launch_xent(const XentLaunch &call, void *stream) {
@@ -477,9 +478,15 @@ int launch_xent(const XentLaunch &call, void *stream) {
         p.hit = a.s.hit;
         p.part = a.s.part;
         p.part_ld = ld;
+        const int64_t blocks = ceil_div(count, m_side(p.tile)) * sums_of(p.tile);
+        p.join = count == a.n_classes && joins(ceil_div(count, m_side(p.tile)), ceil_div(a.n_rows, n_side(p.tile)), blocks * std::min<int64_t>(a.n_rows, n_side(p.tile)));
+        p.arrived = a.s.arrived;
+        p.out_row = a.s.list;
+        p.loss = a.loss;
+        p.lse_out = a.lse;
         e = launch_product(p, a, stream);
         if (e) return e;
-        const int64_t blocks = ceil_div(count, m_side(p.tile)) * sums_of(p.tile);
+        if (p.join) return 0;
         const int is_first = first == 0, is_last = first + count == a.n_classes;
         if (a.n_rows <= 256) hipLaunchKernelGGL(k_merge<1>, dim3((unsigned)a.n_rows), dim3(1024), 0, st, a, blocks, ld, is_first, is_last);
         else if (a.n_rows <= 4096) hipLaunchKernelGGL(k_merge<8>, dim3((unsigned)ceil_div(a.n_rows, 8)), dim3(1024), 0, st, a, blocks, ld, is_first, is_last);
