@@ -58,6 +58,7 @@ struct XentSpace {
 };
 constexpr int64_t kMostBlocks = 1024;      // of rows
 constexpr int kMostJoins = 1024;           // blocks of rows whose sums the last workgroup adds up
+constexpr int kJoinApart = 32;             // their counters: a line of memory each, else all workgroups would count in one
 // Elements between the rows of x, w and G: rows a power of two apart would all lie in one channel of an XCD's L2.
 constexpr int64_t kRowPad = 64;
 

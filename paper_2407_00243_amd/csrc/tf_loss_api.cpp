@@ -97,7 +97,7 @@ int64_t lay_out(tf_xent &p, char *base) {
     c.take(s.block_rows, tf::kMostBlocks);
     c.take(s.block_top, tf::kMostBlocks);
     c.take(s.n, 1);
-    c.take(s.arrived, tf::kMostJoins);
+    c.take(s.arrived, tf::kMostJoins * tf::kJoinApart);
     c.take(s.unit, 1);
     c.take(s.label, d.max_rows);
     c.take(s.lse, d.max_rows);

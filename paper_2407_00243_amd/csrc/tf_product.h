@@ -243,7 +243,7 @@ template <int THREADS> __device__ __forceinline__ void join_sums(const ProductLa
     __builtin_amdgcn_s_waitcnt(0);
     __syncthreads();
     if (a.m_tiles > 1) {
-        if (threadIdx.x == 0) *flag = atomicInc(a.arrived + tile, (unsigned)a.m_tiles - 1) == (unsigned)a.m_tiles - 1;
+        if (threadIdx.x == 0) *flag = atomicInc(a.arrived + tile * kJoinApart, (unsigned)a.m_tiles - 1) == (unsigned)a.m_tiles - 1;
         __syncthreads();
         if (!*flag) return;
     }

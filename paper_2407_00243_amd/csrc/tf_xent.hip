@@ -229,7 +229,7 @@ template <int EL> __global__ __launch_bounds__(256) void k_pack_rows(const XentL
     }
     if ((int)blockIdx.x == blocks - 1 && tid == 0) *a.s.n = n;
     if (blockIdx.x == 0)
-        for (int i = tid; i < kMostJoins; i += 256) a.s.arrived[i] = 0;
+        for (int i = tid; i < kMostJoins; i += 256) a.s.arrived[i * kJoinApart] = 0;
 }
 // ------------------------------------------------------------------------------------------- ends
 
@@ -418,31 +418,37 @@ int64_t m_side(ProductTile t) { return t == kTile256 ? 256 : t == kTile16 ? 64 :
 int64_t n_side(ProductTile t) { return t == kTile256 ? 256 : t == kTile16 ? 16 : t == kTile64 ? 64 : 128; }
 // Sums that a tile of logits leaves of each row.
 int64_t sums_of(ProductTile t) { return t == kTile256 || t == kTile128 ? 2 : 1; }
-// How a product of m x n, `steps` steps of 64 long (each made of `pairs` pairs of parts), is launched: its tile, and the shares of its contraction (`most` of them at most; 0: it cannot be cut).
-// Few rows: all of them in a tile (the launch is bound by reading the other operand), few classes or columns: all of them in one.  Otherwise
-// tiles of 256 x 256, one workgroup a compute unit, or of 128 x 128, two of them, whichever is expected to take less time: tenths of a microsecond,
-// fitted to ten sizes from 2048 x 2048 x 2048 to 8192 x 32768 x 4096, bf16 (which they meet within a fifth).  One as large as
-// 8192 x 32768 x 4096 takes 1.61 ms with large tiles and 1.77 with small ones, 1024 x 40960 x 1024 105 us and 91.
+// How a product of m x n, `steps` steps long (each made of `pairs` pairs of parts), is launched: its tile, and the shares of its contraction (`most`
+// of them at most; 0: it cannot be cut).  16 rows or fewer are one tile: the launch is bound by reading the other operand.  Otherwise whichever tile is expected
+// to take the least time: tenths of a microsecond a step and a tile, fitted to sizes from 100 x 300 x 4096 to 8192 x 32768 x 4096 in bf16 (which
+// they meet within a fifth; `any` is the loader through registers, fp32 is bound by its instructions).  Measured, us, tiles of 64 x 16, 128 x 64, 128 x 128,
+// 256 x 256: logits of 100 x 300 x 4096 13, 23, 39; 300 x 2000 x 4096 23, 24, 43; 2000 x 1000 x 2000 38, 19, 28; 500 x 10000 x 2048 74, 38, 32;
+// 1024 x 40960 x 1024 91 and 105 with the last two, 8192 x 32768 x 4096 1770 and 1610.
 struct Cut {
     ProductTile tile;
     int64_t shares;
 };
-Cut cut_product(int64_t m, int64_t n, int64_t steps, int pairs, bool native, bool rows, int64_t most) {
+double tenths(ProductTile t, int64_t tiles, double steps, bool native, bool any) {
+    const double rounds = (double)ceil_div(tiles, 256);
+    switch (t) {
+        case kTile16: return (native ? 1.6 : any ? 1.8 : 1.2) * rounds * steps + 2 * rounds + 47;
+        case kTile64: return (native ? 8.5 : 2.8) * rounds * steps + 14 * rounds + 70;
+        case kTile128: return (native ? 17 * rounds : std::max(4 * rounds, 6.0)) * steps + 18 * rounds + 80;
+        default: return 14 * rounds * steps + 130 * rounds;
+    }
+}
+Cut cut_product(int64_t m, int64_t n, int64_t steps, int pairs, bool native, bool any, bool rows, int64_t most) {
     most = std::max<int64_t>(1, std::min(most, steps / 4));       // (a share has four steps at least)
     n = std::max<int64_t>(n, 1);
-    // (fp32 instructions are what such a launch is bound by: no more rows of padding than there have to be)
-    if (rows && (n <= 64 || m <= 128 || (native && round_up(n, 64) < round_up(n, 128)))) {
-        const ProductTile t = n <= 16 ? kTile16 : kTile64;
-        const int64_t groups = ceil_div(m, m_side(t)) * ceil_div(n, n_side(t)), want = t == kTile16 ? 1024 : 512;
-        return Cut{t, std::max<int64_t>(1, std::min(want / groups, most))};
-    }
-    Cut best{kTile128, 1};
+    if (rows && n <= 16) return Cut{kTile16, std::max<int64_t>(1, std::min(1024 / ceil_div(m, m_side(kTile16)), most))};
+    const bool few = rows && (n <= 64 || m <= 128);
+    Cut best{few ? kTile64 : kTile128, 1};
     double least = 0;
-    for (const ProductTile t : {kTile128, kTile256}) {
-        if (native && t == kTile256) continue;
+    for (const ProductTile t : {kTile64, kTile16, kTile128, kTile256}) {
+        const bool small = t == kTile64 || t == kTile16;
+        if (small ? !rows : few || (native && t == kTile256)) continue;
         for (int64_t s = 1; s <= std::min<int64_t>(most, 512); s = s < 8 ? s + 1 : s * 5 / 4) {
-            const double rounds = (double)ceil_div(ceil_div(m, m_side(t)) * ceil_div(n, n_side(t)) * s, 256), each = (double)steps * pairs / s;
-            const double time = (t == kTile256 ? rounds * (14 * each + 130) : std::max(4 * rounds, 6.0) * each + 18 * rounds + 80) + (s > 1 ? 40 + (double)s * m * n / 50000 : 0.0);
+            const double time = tenths(t, ceil_div(m, m_side(t)) * ceil_div(n, n_side(t)) * s, (double)steps * pairs / s, native, any) + (s > 1 ? 40 + (double)s * m * n / 50000 : 0.0);
             if (least == 0 || time < least) {
                 best = Cut{t, s};
                 least = time;
@@ -473,13 +479,13 @@ int launch_xent(const XentLaunch &call, void *stream) {
     for (int64_t first = 0; first < a.n_classes; first += piece) {
         const int64_t count = std::min<int64_t>(piece, a.n_classes - first);
         ProductLaunch p = logits(a, classes(a, first, count, st), first, count);
-        p.tile = cut_product(count, a.n_rows, p.k_steps, p.parts == 3 ? 6 : 1, a.native, true, 0).tile;
+        p.tile = cut_product(count, a.n_rows, p.k_steps, p.parts == 3 ? 6 : 1, a.native, p.any, true, 0).tile;
         p.end = kEndSums;
         p.hit = a.s.hit;
         p.part = a.s.part;
         p.part_ld = ld;
         const int64_t blocks = ceil_div(count, m_side(p.tile)) * sums_of(p.tile);
-        p.join = count == a.n_classes && joins(ceil_div(count, m_side(p.tile)), ceil_div(a.n_rows, n_side(p.tile)), blocks * std::min<int64_t>(a.n_rows, n_side(p.tile)));
+        p.join = count == a.n_classes && joins(ceil_div(count, m_side(p.tile)), ceil_div(a.n_rows, n_side(p.tile)), blocks * std::min<int64_t>(std::max(a.n_rows, 1), n_side(p.tile)));
         p.arrived = a.s.arrived;
         p.out_row = a.s.list;
         p.loss = a.loss;
@@ -508,7 +514,7 @@ int launch_xent_grad(const XentLaunch &call, void *stream) {
     const int parts = parts_of(a), pairs = parts == 3 ? 6 : 1, step = step_of(a);
     const int64_t dx_size = rows * a.s.ld;
     // (the same shares for every piece: the slabs are added to)
-    const Cut dx = cut_product(a.n_in, a.n_rows, ceil_div(std::min<int64_t>(piece, a.n_classes), step), pairs, a.native, true, a.s.dx_cap / dx_size);
+    const Cut dx = cut_product(a.n_in, a.n_rows, ceil_div(std::min<int64_t>(piece, a.n_classes), step), pairs, a.native, through_registers(a), true, a.s.dx_cap / dx_size);
     a.direct_dx = piece >= a.n_classes && dx.shares == 1;
     int e = begin(a, std::min<int64_t>(piece, a.n_classes), st);
     if (e) return e;
@@ -517,7 +523,7 @@ int launch_xent_grad(const XentLaunch &call, void *stream) {
         if (a.n_rows) {
             const Side W = classes(a, first, count, st);
             ProductLaunch p = logits(a, W, first, count);
-            p.tile = cut_product(count, a.n_rows, p.k_steps, p.parts == 3 ? 6 : 1, a.native, true, 0).tile;
+            p.tile = cut_product(count, a.n_rows, p.k_steps, p.parts == 3 ? 6 : 1, a.native, p.any, true, 0).tile;
             p.end = kEndGradient;
             p.lse = a.s.lse;
             p.g = a.s.g;
@@ -563,7 +569,7 @@ int launch_xent_grad(const XentLaunch &call, void *stream) {
             q.m_count = a.n_in;
             q.n_count = (int32_t)count;
             const int64_t size = round_up(count, 256) * a.s.ld;
-            const Cut dw = cut_product(a.n_in, count, ceil_div(a.n_rows, step), pairs, a.native, false, a.s.dw_cap / size);
+            const Cut dw = cut_product(a.n_in, count, ceil_div(a.n_rows, step), pairs, a.native, false, false, a.s.dw_cap / size);
             q.tile = dw.tile;
             q.splits = (int32_t)dw.shares;
             q.unit = a.s.unit;
