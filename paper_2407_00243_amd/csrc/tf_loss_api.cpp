@@ -86,9 +86,9 @@ int64_t lay_out(tf_xent &p, char *base) {
     s.ld = round_up(d.n_in, 256) + tf::kRowPad;
     s.x_plane = rows * s.ld;
     s.part_cap = std::max(std::min(classes / 64 * rows, (int64_t)1 << 25), 4 * rows);
-    const int64_t piece = std::max<int64_t>(256, std::min(classes, ((int64_t)1 << 28) / std::max(rows, s.ld) / 256 * 256));
-    s.w_cap = piece * s.ld;
-    s.g_cap = d.gradients ? (piece + tf::kRowPad) * rows : 0;
+    const auto piece = [&](int64_t row) { return std::max<int64_t>(256, std::min(classes, ((int64_t)1 << 28) / row / 256 * 256)); };
+    s.w_cap = piece(s.ld) * s.ld;
+    s.g_cap = d.gradients ? (piece(rows) + tf::kRowPad) * rows : 0;
     s.dx_cap = d.gradients ? std::max({rows * s.ld, std::min((int64_t)1 << 26, 4 * rows * s.ld), std::min((int64_t)1 << 24, 512 * 64 * s.ld)}) : 0;
     s.dw_cap = d.gradients ? (int64_t)1 << 25 : 0;
     Cut c{base};

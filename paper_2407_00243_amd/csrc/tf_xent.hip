@@ -1,5 +1,6 @@
 // Cross entropy of a product: the rows that count, operands, merging of sums, and the launches of a call.
 #include <algorithm>
+#include <type_traits>
 
 #include "tf_loss_device.h"
 #include "tf_moe_device.h"
@@ -340,6 +341,83 @@ template <int EL> __global__ __launch_bounds__(256) void k_finish_classes(const 
     }
 }
 
+// dW of few rows, 32 KH at most: dW = G^T X has as little as one step of K then, and is bound by writing it.  A wave holds its 64 columns of X as
+// operands and goes over classes, 64 at a time, the next ones' G on its way.  Which rows of an operand are which columns and classes is free: with
+// those below a lane reads four classes of G at once and writes eight columns of dW.
+template <int EL, int KH> __global__ __launch_bounds__(256, KH > 1 ? 3 : 4) void k_few_rows(const XentLaunch a, const int64_t first, const int64_t count, const int64_t g_ld,
+                                                                                            const int64_t each) {
+    typedef typename El<EL>::T T;
+    typedef std::conditional_t<EL == TF_BF16, Bf8, Half8> V;
+    typedef uint16_t U4 __attribute__((ext_vector_type(4)));
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r = lane % 16, g = lane / 16, kept = *a.s.n;
+    const int64_t c0 = (int64_t)blockIdx.x * 256 + wave * 64, v_end = min(count, ((int64_t)blockIdx.y + 1) * each);
+    if (c0 >= a.n_in) return;
+    const float unit = *a.s.unit;
+    V x[4][KH];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int64_t c = c0 + 32 * (i / 2) + 8 * (r / 4) + 4 * (i % 2) + r % 4;
+#pragma unroll
+        for (int h = 0; h < KH; ++h) {
+            Words4 w;
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                const int64_t t = 32 * h + 8 * g + k;
+                const uint32_t e = t < kept && c < a.n_in ? (uint32_t)static_cast<const uint16_t *>(a.s.x)[t * a.s.ld + c] : 0u;
+                w[k / 2] = k & 1 ? w[k / 2] | e << 16 : e;
+            }
+            x[i][h] = __builtin_bit_cast(V, w);
+        }
+    }
+    U4 next[KH][8];
+    auto load = [&](int64_t v) {
+#pragma unroll
+        for (int h = 0; h < KH; ++h)
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                const int64_t t = 32 * h + 8 * g + k;
+                next[h][k] = U4{0, 0, 0, 0};
+                if (t < kept) next[h][k] = *reinterpret_cast<const U4 *>(static_cast<const uint16_t *>(a.s.G) + t * g_ld + v + 4 * r);
+            }
+    };
+    int64_t v0 = blockIdx.y * each;
+    if (v0 < v_end) load(v0);
+    for (; v0 < v_end; v0 += 64) {
+        V y[4][KH];
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+#pragma unroll
+            for (int h = 0; h < KH; ++h) {
+                Words4 w;
+#pragma unroll
+                for (int k = 0; k < 4; ++k) w[k] = next[h][2 * k][j] | (uint32_t)next[h][2 * k + 1][j] << 16;
+                y[j][h] = __builtin_bit_cast(V, w);
+            }
+        if (v0 + 64 < v_end) load(v0 + 64);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const int64_t v = v0 + 4 * r + j;
+            T *row = static_cast<T *>(a.dW) + (first + v) * a.lddw + c0;
+#pragma unroll
+            for (int p = 0; p < 2; ++p) {
+                float d[8];
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    Float4 sum = {};
+#pragma unroll
+                    for (int h = 0; h < KH; ++h) {
+                        if constexpr (EL == TF_BF16) sum = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x[2 * p + i][h], y[j][h], sum, 0, 0, 0);
+                        else sum = __builtin_amdgcn_mfma_f32_16x16x32_f16(x[2 * p + i][h], y[j][h], sum, 0, 0, 0);
+                    }
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) d[4 * i + k] = sum[k] * unit;
+                }
+                if (v < v_end) write8<EL>(d, row, 32 * p + 8 * g, a.n_in - c0);
+            }
+        }
+    }
+}
+
 // --------------------------------------------------------------------------------------- launches
 
 // Workgroups for `rows` rows of `columns`, 2048 columns at a time.
@@ -421,23 +499,23 @@ int64_t sums_of(ProductTile t) { return t == kTile256 || t == kTile128 ? 2 : 1; 
 // How a product of m x n, `steps` steps long (each made of `pairs` pairs of parts), is launched: its tile, and the shares of its contraction (`most`
 // of them at most; 0: it cannot be cut).  16 rows or fewer are one tile: the launch is bound by reading the other operand.  Otherwise whichever tile is expected
 // to take the least time: tenths of a microsecond a step and a tile, fitted to sizes from 100 x 300 x 4096 to 8192 x 32768 x 4096 in bf16 (which
-// they meet within a fifth; `any` is the loader through registers, fp32 is bound by its instructions).  Measured, us, tiles of 64 x 16, 128 x 64, 128 x 128,
+// they meet within a fifth; `slow`: operands through registers or transposed; fp32 is bound by its instructions).  Measured, us, tiles of 64 x 16, 128 x 64, 128 x 128,
 // 256 x 256: logits of 100 x 300 x 4096 13, 23, 39; 300 x 2000 x 4096 23, 24, 43; 2000 x 1000 x 2000 38, 19, 28; 500 x 10000 x 2048 74, 38, 32;
 // 1024 x 40960 x 1024 91 and 105 with the last two, 8192 x 32768 x 4096 1770 and 1610.
 struct Cut {
     ProductTile tile;
     int64_t shares;
 };
-double tenths(ProductTile t, int64_t tiles, double steps, bool native, bool any) {
+double tenths(ProductTile t, int64_t tiles, double steps, bool native, bool slow) {
     const double rounds = (double)ceil_div(tiles, 256);
     switch (t) {
-        case kTile16: return (native ? 1.6 : any ? 1.8 : 1.2) * rounds * steps + 2 * rounds + 47;
-        case kTile64: return (native ? 8.5 : 2.8) * rounds * steps + 14 * rounds + 70;
+        case kTile16: return (native ? 1.6 : slow ? 1.8 : 1.2) * rounds * steps + 2 * rounds + 47;
+        case kTile64: return (native ? 8.5 : 2.8) * rounds * steps + 22 * rounds + 50;
         case kTile128: return (native ? 17 * rounds : std::max(4 * rounds, 6.0)) * steps + 18 * rounds + 80;
         default: return 14 * rounds * steps + 130 * rounds;
     }
 }
-Cut cut_product(int64_t m, int64_t n, int64_t steps, int pairs, bool native, bool any, bool rows, int64_t most) {
+Cut cut_product(int64_t m, int64_t n, int64_t steps, int pairs, bool native, bool slow, bool rows, int64_t most) {
     most = std::max<int64_t>(1, std::min(most, steps / 4));       // (a share has four steps at least)
     n = std::max<int64_t>(n, 1);
     if (rows && n <= 16) return Cut{kTile16, std::max<int64_t>(1, std::min(1024 / ceil_div(m, m_side(kTile16)), most))};
@@ -448,7 +526,7 @@ Cut cut_product(int64_t m, int64_t n, int64_t steps, int pairs, bool native, boo
         const bool small = t == kTile64 || t == kTile16;
         if (small ? !rows : few || (native && t == kTile256)) continue;
         for (int64_t s = 1; s <= std::min<int64_t>(most, 512); s = s < 8 ? s + 1 : s * 5 / 4) {
-            const double time = tenths(t, ceil_div(m, m_side(t)) * ceil_div(n, n_side(t)) * s, (double)steps * pairs / s, native, any) + (s > 1 ? 40 + (double)s * m * n / 50000 : 0.0);
+            const double time = tenths(t, ceil_div(m, m_side(t)) * ceil_div(n, n_side(t)) * s, (double)steps * pairs / s, native, slow) + (s > 1 ? 40 + (double)s * m * n / 50000 : 0.0);
             if (least == 0 || time < least) {
                 best = Cut{t, s};
                 least = time;
@@ -456,6 +534,18 @@ Cut cut_product(int64_t m, int64_t n, int64_t steps, int pairs, bool native, boo
         }
     }
     return best;
+}
+
+// Up to 32 rows, and up to 64 where that fills the card.  Columns -> classes, us, and as a product of tiles of 128 x 128: 4096 -> 65536 1 row 93 / 210,
+// 16 rows 122 / 216; 4096 -> 20000 32 rows 35 / 70, 64 rows 50 / 70; 777 -> 50000 20 rows 35 / 42; 512 -> 1000 64 rows 10.4 / 5.7.
+bool few_rows(const XentLaunch &a, int64_t count) {
+    return a.dtype != TF_F32 && (a.n_rows <= 32 || (a.n_rows <= 64 && count * a.n_in >= (int64_t)1 << 23));
+}
+template <int EL> void launch_few_rows(const XentLaunch &a, int64_t first, int64_t count, int64_t g_ld, hipStream_t st) {
+    const int64_t columns = ceil_div(a.n_in, 256), each = round_up(std::max<int64_t>(64, count * columns / 2048), 64);
+    const dim3 grid((unsigned)columns, (unsigned)ceil_div(count, each));
+    if (a.n_rows <= 32) hipLaunchKernelGGL((k_few_rows<EL, 1>), grid, dim3(256), 0, st, a, first, count, g_ld, each);
+    else hipLaunchKernelGGL((k_few_rows<EL, 2>), grid, dim3(256), 0, st, a, first, count, g_ld, each);
 }
 
 // 256 rows of G stay below 2^32 bytes, as the products' loads count them.  (A plan for very many rows has room for more columns of few.)
@@ -514,7 +604,7 @@ int launch_xent_grad(const XentLaunch &call, void *stream) {
     const int parts = parts_of(a), pairs = parts == 3 ? 6 : 1, step = step_of(a);
     const int64_t dx_size = rows * a.s.ld;
     // (the same shares for every piece: the slabs are added to)
-    const Cut dx = cut_product(a.n_in, a.n_rows, ceil_div(std::min<int64_t>(piece, a.n_classes), step), pairs, a.native, through_registers(a), true, a.s.dx_cap / dx_size);
+    const Cut dx = cut_product(a.n_in, a.n_rows, ceil_div(std::min<int64_t>(piece, a.n_classes), step), pairs, a.native, true, true, a.s.dx_cap / dx_size);
     a.direct_dx = piece >= a.n_classes && dx.shares == 1;
     int e = begin(a, std::min<int64_t>(piece, a.n_classes), st);
     if (e) return e;
@@ -559,7 +649,12 @@ int launch_xent_grad(const XentLaunch &call, void *stream) {
                 if (e) return e;
             }
         }
-        if (a.dW) {
+        if (a.dW && few_rows(a, count)) {
+            if (a.dtype == TF_BF16) launch_few_rows<TF_BF16>(a, first, count, g_ld, st);
+            else launch_few_rows<TF_F16>(a, first, count, g_ld, st);
+            e = (int)hipGetLastError();
+            if (e) return e;
+        } else if (a.dW) {
             ProductLaunch q{};
             q.M = Side{a.s.x, a.s.ld, a.s.x_plane, 0, a.s.ld};
             q.N = Side{a.s.G, g_ld, a.s.g_cap, 0, piece};
