@@ -83,8 +83,12 @@ struct Side {
     int64_t ld, plane;            // elements: from row to row, from part to part
     int64_t rows, cols;           // what there is of it (cols: whole pieces of 16 bytes, unless `any`); further elements count as zeros
 };
-// Shares of a contraction: each has four steps of 64 at least.
-constexpr int shares_of(int most, int steps) { return most < steps / 4 ? most : steps / 4 < 1 ? 1 : steps / 4; }
+// Shares of a contraction: each has four steps at least, or one of numbers in parts, which takes six.
+constexpr int least_share(int parts) { return parts == 3 ? 1 : 4; }
+constexpr int shares_of(int most, int steps, int parts) {
+    const int shares = steps / least_share(parts);
+    return most < shares ? most : shares < 1 ? 1 : shares;
+}
 enum ProductEnd { kEndSums = 0, kEndGradient = 1, kEndSlab = 2, kEndOut = 3 };
 enum ProductTile { kTile256 = 0, kTile128 = 1, kTile64 = 2, kTile16 = 3 };
 struct ProductLaunch {

@@ -288,9 +288,9 @@ __global__ __launch_bounds__(WM * WN * 64, TM * TN > 32 ? 1 : 2) void k_product(
     const int kept = *a.n;
     // Tiles: a contiguous share for each XCD, in bands of eight rows of tiles, so that the 32 workgroups that an XCD runs at a time are eight by four
     // tiles and its L2 is asked for twelve pieces of operands a step, not 33.
-    // (Only as many as there are kept rows for; a share of K that would have under four steps is not made.)
+    // (Only as many as there are kept rows for; a share of K that would have too few steps is not made.)
     int steps = a.k_rows ? (kept + STEP - 1) / STEP : a.k_steps;
-    const int n_tiles = a.n_rows ? (kept + BN - 1) / BN : a.n_tiles, splits = shares_of(a.splits, steps);
+    const int n_tiles = a.n_rows ? (kept + BN - 1) / BN : a.n_tiles, splits = shares_of(a.splits, steps, a.parts);
     const int tiles = a.m_tiles * n_tiles, all = tiles * splits;
     int b = blockIdx.x;
     if (b >= all) return;

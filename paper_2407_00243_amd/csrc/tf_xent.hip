@@ -313,6 +313,8 @@ template <int EL> __device__ __forceinline__ void finish_row(const float *slab, 
 constexpr int kManySlabs = 8;
 // Columns of a step of the products.
 __host__ __device__ constexpr int step_of(const XentLaunch &a) { return a.native ? 32 : 64; }
+// Parts of a number.
+__host__ __device__ constexpr int parts_of(const XentLaunch &a) { return a.dtype == TF_F32 && !a.native ? 3 : 1; }
 
 // dX: the shares' sums of each row that counts, zeros in the others.
 template <int EL> __global__ __launch_bounds__(256) void k_finish_rows(const XentLaunch a, const int splits, const int64_t size) {      // (the same for every piece)
@@ -329,7 +331,7 @@ template <int EL> __global__ __launch_bounds__(256) void k_finish_rows(const Xen
 }
 // Rows first .. first + count of dW.
 template <int EL> __global__ __launch_bounds__(256) void k_finish_classes(const XentLaunch a, const int64_t first, const int64_t count, const int most, const int64_t size) {
-    const int splits = shares_of(most, (int)ceil_div(*a.s.n, step_of(a)));
+    const int splits = shares_of(most, (int)ceil_div(*a.s.n, step_of(a)), parts_of(a));
     const float unit = *a.s.unit;
     const int per_row = threads_of_row(a.n_in);
     const bool by_slab = splits >= kManySlabs;
@@ -455,7 +457,6 @@ bool whole_pieces(const XentLaunch &a) {
 // fp32 numbers that are multiplied in parts are always packed.
 bool through_registers(const XentLaunch &a) { return !whole_pieces(a) && (a.dtype == TF_F32 ? a.native : a.n_rows <= (a.loss ? 1023 : 64)); }
 bool in_place(const XentLaunch &a) { return a.dtype == TF_F32 ? a.native : whole_pieces(a) || through_registers(a); }
-int parts_of(const XentLaunch &a) { return a.dtype == TF_F32 && !a.native ? 3 : 1; }
 
 // Numbers and copies the rows that count.  (Also without rows: it sets the unit.)  Up to 8192 rows every block counts the rows before it.  Packs the
 // first `classes` of W as well, where it has to be.
@@ -516,7 +517,7 @@ double tenths(ProductTile t, int64_t tiles, double steps, bool native, bool slow
     }
 }
 Cut cut_product(int64_t m, int64_t n, int64_t steps, int pairs, bool native, bool slow, bool rows, int64_t most) {
-    most = std::max<int64_t>(1, std::min(most, steps / 4));       // (a share has four steps at least)
+    most = std::max<int64_t>(1, std::min<int64_t>(most, steps / least_share(pairs == 6 ? 3 : 1)));
     n = std::max<int64_t>(n, 1);
     if (rows && n <= 16) return Cut{kTile16, std::max<int64_t>(1, std::min(1024 / ceil_div(m, m_side(kTile16)), most))};
     const bool few = rows && (n <= 64 || m <= 128);

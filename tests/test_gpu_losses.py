@@ -294,11 +294,31 @@ def test_xent_around_borders(T, d, dtype):
     check_xent(*xent_case(T, 1100, d, dtype, T + d, unlabelled=0.0), what=f"T{T} d{d} {dtype}")
 
 
-def test_xent_few_rows_of_a_plan_for_many():
+@pytest.mark.parametrize("T,V,d", [(33, 9000, 1000), (64, 20000, 515), (50, 40003, 257), (32, 3000, 64), (31, 70, 3)])
+@pytest.mark.parametrize("dtype", [BF, HF, F])
+def test_xent_gradient_of_few_rows(T, V, d, dtype):
+    """W's gradient of up to 64 rows, its rows strided and beginning anywhere; NaN in what an earlier call left of other rows' G."""
+    print(f"T{T} V{V} d{d} {dtype}", flush=True)
+    plan = tf.XentPlan(V, d, dtype, max_rows=64)
+    X, W, labels, dloss = xent_case(64, V, d, dtype, 3, unlabelled=0.0)
+    dloss[:] = math.nan
+    plan.grad(X, W, labels, torch.zeros(64, device="cuda"), dloss, None, torch.empty_like(W), stream())
+    X, W, labels, dloss = xent_case(T, V, d, dtype, T)
+    check_xent(X, W, labels, dloss, plan=plan, what=f"T{T} V{V} d{d} {dtype}")
+    loss, lse = torch.empty(T, device="cuda"), torch.empty(T, device="cuda")
+    plan.loss(X, W, labels, loss, lse, stream())
+    out = torch.full((V, d + 5), 7.0, device="cuda", dtype=dtype)
+    plan.grad(X, W, labels, lse, dloss, None, out[:, 2:2 + d], stream())
+    lu.check(out[:, 2:2 + d], *lu.xent(X, W, labels, dloss)["dW"], dtype)
+    assert (out[:, :2] == 7).all() and (out[:, 2 + d:] == 7).all()
+
+
+@pytest.mark.parametrize("T", [70, 20])
+def test_xent_few_rows_of_a_plan_for_many(T):
     """Such a plan has room for more columns of few rows' gradients than are taken at a time."""
     V, d = (1 << 22) + 1000, 8
     plan = tf.XentPlan(V, d, BF, max_rows=3500000)
-    check_xent(*xent_case(70, V, d, BF, 5), plan=plan, what="plan for many")
+    check_xent(*xent_case(T, V, d, BF, 5), plan=plan, what="plan for many")
 
 
 @pytest.mark.parametrize("dtype,d", [(BF, 8), (F, 7)])
