@@ -1,4 +1,11 @@
-// Products of the cross entropy: C = M N^T, a tile of C by each workgroup, 16-bit operands, sums in 32 bits.
+// Products of the cross entropy: C = M N^T, a tile of C by each workgroup, 16-bit operands (fp32 ones as they are or in three parts), sums in 32 bits.
+//   logits  l = W X^T      ended by their largest, the sum of exponentials and the label's (loss), or by g = dloss (exp(l - lse) - [label]) (gradient)
+//   dX^T    = W^T G^T      W by columns
+//   dW^T    = X^T G        both by columns, K goes over the rows that count
+// Bound by the matrix cores where there are many rows: 8192 rows, 4096 -> 32768 classes, bf16, tiles of 256 x 256: logits to sums 1.63 ms (1.35 PFLOP/s), to G
+// 1.71, dX 1.58, dW 1.54.  A wave's 128 x 128 sums fill the accumulation registers, so 64 products follow 16 reads of LDS and one workgroup a compute unit
+// suffices.  Instructions of 32 x 32 x 16 took 1.39 ms on zeros (these 1.41) but 1.79 on normal
+// numbers, where the card's clock gives way.  With few rows bound by reading W: 1 row of 4096 -> 65536, tiles of 64 x 16: 99 us, 5.4 TB/s.
 #pragma once
 #include <algorithm>
 #include <type_traits>

@@ -149,6 +149,7 @@ template <int EL> __global__ __launch_bounds__(256) void k_pack_classes(const Xe
 // Numbers the rows that have a label in their order and copies them, one after the other, to x, where columns up to a multiple of 64 are zeros behind
 // the last one; rows without a label get their zeros.  A block of rows a workgroup, which sums up the counts of the blocks before
 // it; where there are few rows (`counted` 0) it counts them itself, which saves a launch.  Workgroups behind the `blocks` first ones pack W's first rows.
+// 8192 rows of 4096 bf16 numbers 38 us, 3.5 TB/s; one row 4.7 us, a chain of three loads.
 template <int EL> __global__ __launch_bounds__(256) void k_pack_rows(const XentLaunch a, const int block, const int blocks, const int counted, const int64_t classes) {
     __shared__ int n_of[4], rows[256], ats[256];
     __shared__ float top_of[4];
@@ -235,7 +236,8 @@ template <int EL> __global__ __launch_bounds__(256) void k_pack_rows(const XentL
 // ------------------------------------------------------------------------------------------- ends
 
 // Adds the sums of `blocks` blocks of classes to those of the classes before them (unless `first`).  ROWS rows a workgroup: 64 / ROWS lanes of each of
-// its 16 waves take a row, and all of them every block once.  The last call writes the results.
+// its 16 waves take a row, and all of them every block once.  The last call writes the results.  Bound by reading: 8192 rows with 2048 sums each 26 us, 5.1 TB/s; one
+// row with 1024 sums 6 us, latency.
 template <int ROWS> __global__ __launch_bounds__(1024) void k_merge(const XentLaunch a, const int64_t blocks, const int64_t ld, const int first, const int last) {
     __shared__ Float2 of_wave[16][ROWS];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
@@ -266,12 +268,12 @@ template <int ROWS> __global__ __launch_bounds__(1024) void k_merge(const XentLa
 }
 
 // Rows `row` of an output from the sums of `splits` slabs, `none` for zeros.  A row's columns lie in `per_row` threads; the others of a workgroup take
-// other rows, or, where there are many slabs, other slabs (`by_slab`), added up in their order.
+// other rows, or, where there are many slabs, other slabs (`by_slab`), added up in their order.  Bound by reading: one slab of 8192 x 4096 to bf16 39 us, 5.1 TB/s.
 template <int EL> __device__ __forceinline__ void finish_row(const float *slab, int64_t size, int splits, void *out, int64_t n_in, bool none, float unit,
                                                              int per_row, bool by_slab, bool is) {
     __shared__ float part[256][9];
     const int tid = threadIdx.x, slices = by_slab ? 256 / per_row : 1, slice = by_slab ? tid / per_row : 0;
-    for (int64_t k0 = 0; k0 < n_in; k0 += per_row * 8) {
+    for (int64_t k0 = (int64_t)blockIdx.y * per_row * 8; k0 < n_in; k0 += (int64_t)gridDim.y * per_row * 8) {
         const int64_t k = k0 + tid % per_row * 8;
         float x[8] = {};
         if (is && !none && k < n_in)
@@ -319,8 +321,8 @@ __host__ __device__ constexpr int parts_of(const XentLaunch &a) { return a.dtype
 // dX: the shares' sums of each row that counts, zeros in the others.
 template <int EL> __global__ __launch_bounds__(256) void k_finish_rows(const XentLaunch a, const int splits, const int64_t size) {      // (the same for every piece)
     const float unit = *a.s.unit;
-    const int per_row = threads_of_row(a.n_in);
     const bool by_slab = splits >= kManySlabs;
+    const int per_row = min(threads_of_row(a.n_in), by_slab ? 32 : 256);
     const int at_once = by_slab ? 1 : 256 / per_row;
     for (int64_t t0 = (int64_t)blockIdx.x * at_once; t0 < a.n_rows; t0 += (int64_t)gridDim.x * at_once) {
         const int64_t t = t0 + (by_slab ? 0 : threadIdx.x / per_row);
@@ -333,8 +335,8 @@ template <int EL> __global__ __launch_bounds__(256) void k_finish_rows(const Xen
 template <int EL> __global__ __launch_bounds__(256) void k_finish_classes(const XentLaunch a, const int64_t first, const int64_t count, const int most, const int64_t size) {
     const int splits = shares_of(most, (int)ceil_div(*a.s.n, step_of(a)), parts_of(a));
     const float unit = *a.s.unit;
-    const int per_row = threads_of_row(a.n_in);
     const bool by_slab = splits >= kManySlabs;
+    const int per_row = min(threads_of_row(a.n_in), by_slab ? 32 : 256);
     const int at_once = by_slab ? 1 : 256 / per_row;
     for (int64_t i0 = (int64_t)blockIdx.x * at_once; i0 < count; i0 += (int64_t)gridDim.x * at_once) {
         const int64_t i = i0 + (by_slab ? 0 : threadIdx.x / per_row);
@@ -345,7 +347,8 @@ template <int EL> __global__ __launch_bounds__(256) void k_finish_classes(const 
 
 // dW of few rows, 32 KH at most: dW = G^T X has as little as one step of K then, and is bound by writing it.  A wave holds its 64 columns of X as
 // operands and goes over classes, 64 at a time, the next ones' G on its way.  Which rows of an operand are which columns and classes is free: with
-// those below a lane reads four classes of G at once and writes eight columns of dW.
+// those below a lane reads four classes of G at once and writes eight columns of dW.  4096 -> 65536 classes, bf16, one row 93 us, 5.8 TB/s; 64 rows of
+// 4096 -> 20000 50 us, 3.3 TB/s (registers for three waves a SIMD).
 template <int EL, int KH> __global__ __launch_bounds__(256, KH > 1 ? 3 : 4) void k_few_rows(const XentLaunch a, const int64_t first, const int64_t count, const int64_t g_ld,
                                                                                             const int64_t each) {
     typedef typename El<EL>::T T;
@@ -427,9 +430,9 @@ dim3 row_grid(int64_t rows, int64_t columns) {
     const int64_t per_row = std::min<int64_t>(256, ceil_div(columns, 8));
     return dim3((unsigned)std::max<int64_t>(1, std::min<int64_t>(ceil_div(rows * per_row, 256), 8192)));
 }
-// The same for rows that are summed from slabs.
+// The same for rows that are summed from slabs; of many slabs 256 columns a workgroup.
 dim3 slab_grid(int64_t rows, int64_t columns, int64_t splits) {
-    return splits >= kManySlabs ? dim3((unsigned)std::min<int64_t>(rows, 8192)) : row_grid(rows, columns);
+    return splits >= kManySlabs ? dim3((unsigned)std::min<int64_t>(rows, 8192), (unsigned)std::min<int64_t>(ceil_div(columns, 256), 64)) : row_grid(rows, columns);
 }
 #define TF_BY_TYPE(dtype, kernel, grid, ...)                                                                           \
     do {                                                                                                               \
