@@ -196,6 +196,8 @@ __device__ __forceinline__ float numerators(float (&n)[R::N], float (&slope)[R::
 }
 
 __device__ __forceinline__ float over(float x, float total) { return total == 0.0f ? 0.0f : x / total; }
+// 1 / total, good to a unit of 2^-23: a division is a dozen instructions, of which a row of gradients takes two.
+__device__ __forceinline__ float inverse(float total) { return total == 0.0f ? 0.0f : __builtin_amdgcn_rcpf(total); }
 
 // ---------------------------------------------------------------------------------------- balance
 
@@ -335,7 +337,7 @@ template <int EL, int L, int NV, bool SIGMOIDS> __global__ __launch_bounds__(102
         float n[R::N], slope[R::N];
         bool scaled;
         const float total = numerators<R, SIGMOIDS>(n, slope, raw, lane, E, scaled);
-        const float each = named ? over(1.0f, total) : 0.0f;
+        const float each = named ? inverse(total) : 0.0f;
         if (named)
 #pragma unroll
             for (int i = 0; i < R::N; ++i) mass[i] += n[i] * each;
@@ -473,7 +475,7 @@ template <int EL, int L, int NV, bool SIGMOIDS> __global__ __launch_bounds__(256
         float n[R::N], slope[R::N];
         bool scaled;
         const float total = numerators<R, SIGMOIDS>(n, slope, raw, lane, E, scaled);
-        const float over_all = named ? over(1.0f, total) : 0.0f;
+        const float over_all = named ? inverse(total) : 0.0f;
         float fs = 0.0f, gs = 0.0f, some = 0.0f;
         if (a.dloss) {
 #pragma unroll
@@ -500,7 +502,7 @@ template <int EL, int L, int NV, bool SIGMOIDS> __global__ __launch_bounds__(256
         }
         // (`again`: numerators that say little; with plain sigmoids, slopes that are over an exponential)
         const bool again = a.dvals && named && (top_only ? some < kSmall : sigmoid_only && scaled);
-        const float A = factor * over_all, B = !a.dvals ? 0.0f : sigmoid_only ? 1.0f : top_only ? over(1.0f, some) : over_all;
+        const float A = factor * over_all, B = !a.dvals ? 0.0f : sigmoid_only ? 1.0f : top_only ? inverse(some) : over_all;
         gs *= sigmoid_only ? 0.0f : B;
         // what is taken off: A sum p f, B sum q g for the experts that are named or, with shares over all experts, for all of them
         const float Afs = A * fs, Bgs = B * gs, off = Afs + (top_only ? 0.0f : Bgs), off_named = top_only ? Bgs : 0.0f;

@@ -181,7 +181,7 @@ template <int EL> __global__ __launch_bounds__(256) void k_pack_rows(const XentL
     // gradients are divided by the largest one, so that no size of dloss is lost in 16 bits
     const float scale = a.dtype == TF_F16 ? 32768.0f : 1.0f;
     if (top == 0.0f) top = 1.0f;
-    if (a.dloss && blockIdx.x == 0 && tid == 0) *a.s.unit = top / scale;
+    if (!a.loss && blockIdx.x == 0 && tid == 0) *a.s.unit = top / scale;       // (without rows there is no dloss)
     const int64_t columns = round_up(a.n_in, 64);
     const int per_row = threads_of_row(columns), at_once = 256 / per_row;
     for (int64_t r0 = first; r0 < end; r0 += 256) {

@@ -387,6 +387,20 @@ def test_rows_without_a_label_are_not_read(dtype):
 
 
 @pytest.mark.parametrize("dtype", [BF, HF, F])
+def test_no_rows_at_first(dtype):
+    """A plan's first call has no rows, and its workspace lies where NaN was."""
+    V, d = 300, 64
+    for size in (1 << 16, 1 << 21, 1 << 24):
+        torch.full((size,), math.nan, device="cuda")
+    torch.cuda.empty_cache()
+    plan = tf.XentPlan(V, d, dtype, max_rows=100)
+    W, dW = torch.randn(V, d, device="cuda").to(dtype), torch.full((V, d), math.nan, device="cuda", dtype=dtype)
+    e, none = torch.empty(0, device="cuda"), torch.empty(0, device="cuda", dtype=torch.int32)
+    plan.grad(W[:0], W, none, e, e, None, dW, stream())
+    assert not dW.any()
+
+
+@pytest.mark.parametrize("dtype", [BF, HF, F])
 def test_one_gradient_alone_and_fewer_rows(dtype):
     V, d = 400, 96
     plan = tf.XentPlan(V, d, dtype, max_rows=500)
