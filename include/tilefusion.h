@@ -453,7 +453,7 @@ tf_status tf_moe_route_grad(const void *scores, int64_t ld, int32_t dtype, int32
  * lse and rows of dX are 0.
  *     lse[t] = log sum_v exp(l_tv)                                 loss[t] = lse[t] - l_t,labels[t]
  *     g_tv   = dloss[t] (exp(l_tv - lse[t]) - [v = labels[t]])     dX = g W      dW = g^T X
- * The logits are made for a piece of the classes at a time, by both calls; g is held for a piece, rounded to 16 bits (bf16: to bf16; fp16: to
+ * A loss below 2^-126 may be 0.  The logits are made for a piece of the classes at a time, by both calls; g is held for a piece, rounded to 16 bits (bf16: to bf16; fp16: to
  * fp16 after division by the largest |dloss|, so that no size of dloss is lost; fp32: in 32 bits for few rows, else as three bf16 numbers, which
  * hold 24 bits). */
 typedef struct tf_xent_desc {

@@ -100,7 +100,9 @@ template <int EL, int W, bool TR, int WAVES> struct Loader {
     // Where the next step lies, what lies behind its end counting as zeros; goes on to the one after it.
     __device__ __forceinline__ Words4 next(int lane) {
         const uint32_t n = !TR || left >= STEP ? records : left <= 0 ? 0u : (uint32_t)(left - 1) * row + tail;
-        const Words4 w{(uint32_t)at, (uint32_t)(at >> 32), n, 0x00020000u};
+        // (the same for all lanes, which the compiler does not always see)
+        const auto one = [](uint32_t x) { return (uint32_t)__builtin_amdgcn_readfirstlane((int)x); };
+        const Words4 w{one((uint32_t)at), one((uint32_t)(at >> 32)), one(n), 0x00020000u};
         if (!TR && left < STEP) {
             // The last step, which ends inside of its columns.  (A lane's columns are the same ones in every instruction; numbers in parts have
             // whole steps, so that this is the end of all steps.)
@@ -275,6 +277,30 @@ template <int THREADS> __device__ __forceinline__ void join_sums(const ProductLa
     for (int s = max(rows, 64); s < THREADS; s += max(rows, 64)) x = add_sums(x, sums[s + threadIdx.x]);
     const int64_t to = a.out_row[first + threadIdx.x];
     write_loss(x, __hip_atomic_load(a.hit + first + threadIdx.x, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT), a.loss + to, a.lse_out + to);
+}
+
+// Four 16-bit numbers.
+typedef uint32_t Words2 __attribute__((ext_vector_type(2), aligned(2)));
+template <int EL> __device__ __forceinline__ Words2 pack4(float a, float b, float c, float d) {
+    return Words2{El<EL>::put(a) | (uint32_t)El<EL>::put(b) << 16, El<EL>::put(c) | (uint32_t)El<EL>::put(d) << 16};
+}
+// Two neighbouring tiles of results lie in a lane as four columns of each; exchanged between rows of sixteen lanes, as eight columns of one (those that
+// columns_of(number of the first tile, lane / 16) tells): stores of 16 bytes, 64 in a line.
+__device__ __forceinline__ int columns_of(int x, int g) { return 16 * (x + (g & 1)) + 8 * (g >> 1); }
+__device__ __forceinline__ AnyWords4 eight_columns(Words2 a, Words2 b) {
+    const auto lo = __builtin_amdgcn_permlane16_swap(a[0], b[0], false, false), hi = __builtin_amdgcn_permlane16_swap(a[1], b[1], false, false);
+    return AnyWords4{(uint32_t)lo[0], (uint32_t)hi[0], (uint32_t)lo[1], (uint32_t)hi[1]};
+}
+// N of them to columns c, c + 1, ... of a row, those behind its last one left out.
+template <int N> __device__ __forceinline__ void put_columns(uint16_t *row, int64_t c, int64_t columns, AnyWords4 w) {
+    if (c + N <= columns) {
+        if constexpr (N == 8) *reinterpret_cast<AnyWords4 *>(row + c) = w;
+        else *reinterpret_cast<Words2 *>(row + c) = Words2{w[0], w[1]};
+    } else {
+#pragma unroll
+        for (int v = 0; v < N; ++v)
+            if (c + v < columns) row[c + v] = (uint16_t)(w[v / 2] >> (16 * (v & 1)));
+    }
 }
 
 // f(0), f(1), ... f(N - 1), the number known when the code is made.
@@ -481,6 +507,7 @@ __global__ __launch_bounds__(WM * WN * 64, TM * TN > 32 ? 1 : 2) void k_product(
                 typedef typename El<EL>::T T;
                 T *out = static_cast<T *>(a.G) + row * a.g_ld + mw + 4 * g;
                 typedef uint16_t U4 __attribute__((ext_vector_type(4)));
+                Words2 before;
 #pragma unroll
                 for (int x = 0; x < TM; ++x) {
                     float d[4];
@@ -503,8 +530,12 @@ __global__ __launch_bounds__(WM * WN * 64, TM * TN > 32 ? 1 : 2) void k_product(
                         for (int v = 0; v < 4; ++v) split3<EL>(d[v], p[v]);
 #pragma unroll
                         for (int i = 0; i < 3; ++i) *reinterpret_cast<U4 *>(out + i * a.g_plane + 16 * x) = U4{p[0][i], p[1][i], p[2][i], p[3][i]};
+                    } else if constexpr (TM % 2 == 0) {
+                        const Words2 w = pack4<EL>(d[0], d[1], d[2], d[3]);
+                        if (x % 2) *reinterpret_cast<AnyWords4 *>(static_cast<T *>(a.G) + row * a.g_ld + mw + columns_of(x - 1, g)) = eight_columns(before, w);
+                        else before = w;
                     } else {
-                        *reinterpret_cast<U4 *>(out + 16 * x) = U4{El<EL>::put(d[0]), El<EL>::put(d[1]), El<EL>::put(d[2]), El<EL>::put(d[3])};
+                        *reinterpret_cast<Words2 *>(out + 16 * x) = pack4<EL>(d[0], d[1], d[2], d[3]);
                     }
                 }
             }
@@ -534,6 +565,7 @@ __global__ __launch_bounds__(WM * WN * 64, TM * TN > 32 ? 1 : 2) void k_product(
             int64_t row = nw + 16 * y;
             if (row >= rows) continue;
             if (a.out_row) row = a.out_row[row];
+            Words2 before;
 #pragma unroll
             for (int x = 0; x < TM; ++x) {
                 const int64_t m = mw + 16 * x + 4 * g;
@@ -547,16 +579,16 @@ __global__ __launch_bounds__(WM * WN * 64, TM * TN > 32 ? 1 : 2) void k_product(
                     else
                         for (int v = 0; v < 4; ++v)
                             if (m + v < a.m_count) to[v] = f[v];
-                } else {
-                    uint16_t *to = static_cast<uint16_t *>(a.out) + row * a.ldo + m;
-                    typedef uint16_t U4 __attribute__((ext_vector_type(4), aligned(2)));
-                    U4 d;
-#pragma unroll
-                    for (int v = 0; v < 4; ++v) d[v] = El<EL == TF_F32 ? TF_BF16 : EL>::put(f[v]);
-                    if (m + 4 <= a.m_count) *reinterpret_cast<U4 *>(to) = d;
-                    else
-                        for (int v = 0; v < 4; ++v)
-                            if (m + v < a.m_count) to[v] = d[v];
+                } else if constexpr (EL != TF_F32) {
+                    uint16_t *to = static_cast<uint16_t *>(a.out) + row * a.ldo;
+                    const Words2 w = pack4<EL>(f[0], f[1], f[2], f[3]);
+                    if constexpr (TM % 2 == 0) {
+                        const int64_t c = mw + columns_of(x - 1, g);
+                        if (x % 2) put_columns<8>(to, c, a.m_count, eight_columns(before, w));
+                        else before = w;
+                    } else {
+                        put_columns<4>(to, m, a.m_count, Words4{w[0], w[1], 0, 0});
+                    }
                 }
             }
         }
