@@ -298,7 +298,7 @@ template <typename R, bool GRADIENTS> struct Input {
 // mass_e = sum over rows of n_te / sum_j n_tj.  Every wave takes ROWS tokens at a time and adds up their shares in registers; entries are counted in LDS
 // (whole numbers: their order does not matter).  LDS holds the counts, and at the end a line of sums for each wave.  Two sets of rows are on their way
 // from memory while a third is worked on.  131072 rows of 256 bf16 experts, 8 entries each: 20 us, 3.6 TB/s (the launch after it 8); sigmoids 24.
-// Of 1 Mi rows 139 us, 4.1 TB/s: bound by its instructions, an exponential and about ten others a score.
+// Of 1 Mi rows 135 us, 4.2 TB/s: bound by its instructions, an exponential and about ten others a score.
 template <int EL, int L, int NV, bool SIGMOIDS> __global__ __launch_bounds__(1024) void k_balance(const RouterLaunch a) {
     typedef Row<EL, L, NV> R;
     extern __shared__ __attribute__((aligned(16))) int shared[];
@@ -387,7 +387,7 @@ template <int EL, int L, int NV, bool SIGMOIDS> __global__ __launch_bounds__(102
 // The entries of a row meet its scores in LDS: each puts its gradient and a one where its expert's are, and the lanes that hold the scores find
 // them there, or zeros.  (They read them, and f, twice: registers hold two numbers a score and what comes from memory next.)  Where a row names an
 // expert more than once one lane adds its entries up instead.  A wave has no barrier: its instructions of LDS are done in their order.
-// 131072 rows of 256 bf16 experts, 8 entries each, both parts, sigmoid shares: 51 us, 2.8 TB/s; softmax 47.  Bound by its instructions: one or two of a quarter of
+// 131072 rows of 256 bf16 experts, 8 entries each, both parts, sigmoid shares: 50 us, 2.8 TB/s; softmax 47.  Bound by its instructions: one or two of a quarter of
 // the others' rate a score, and about twenty others.
 __device__ __forceinline__ void in_order() { asm volatile("" ::: "memory"); }
 

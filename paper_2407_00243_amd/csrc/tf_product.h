@@ -285,7 +285,8 @@ template <int EL> __device__ __forceinline__ Words2 pack4(float a, float b, floa
     return Words2{El<EL>::put(a) | (uint32_t)El<EL>::put(b) << 16, El<EL>::put(c) | (uint32_t)El<EL>::put(d) << 16};
 }
 // Two neighbouring tiles of results lie in a lane as four columns of each; exchanged between rows of sixteen lanes, as eight columns of one (those that
-// columns_of(number of the first tile, lane / 16) tells): stores of 16 bytes, 64 in a line.
+// columns_of(number of the first tile, lane / 16) tells): stores of 16 bytes, 64 in a line.  dW of 128 rows, 4096 -> 20000, 62 us; with stores of 8 bytes,
+// 32 in a line, 73.
 __device__ __forceinline__ int columns_of(int x, int g) { return 16 * (x + (g & 1)) + 8 * (g >> 1); }
 __device__ __forceinline__ AnyWords4 eight_columns(Words2 a, Words2 b) {
     const auto lo = __builtin_amdgcn_permlane16_swap(a[0], b[0], false, false), hi = __builtin_amdgcn_permlane16_swap(a[1], b[1], false, false);

@@ -347,8 +347,8 @@ template <int EL> __global__ __launch_bounds__(256) void k_finish_classes(const 
 
 // dW of few rows, 32 KH at most: dW = G^T X has as little as one step of K then, and is bound by writing it.  A wave holds its 64 columns of X as
 // operands and goes over classes, 64 at a time, the next ones' G on its way.  Which rows of an operand are which columns and classes is free: with
-// those below a lane reads four classes of G at once and writes eight columns of dW.  4096 -> 65536 classes, bf16, one row 93 us, 5.8 TB/s; 64 rows of
-// 4096 -> 20000 50 us, 3.3 TB/s (registers for three waves a SIMD).
+// those below a lane reads four classes of G at once and writes eight columns of dW.  4096 -> 65536 classes, bf16, one row 96 us, 5.6 TB/s; 64 rows of
+// 4096 -> 20000 51 us, 3.2 TB/s (registers for three waves a SIMD).
 template <int EL, int KH> __global__ __launch_bounds__(256, KH > 1 ? 3 : 4) void k_few_rows(const XentLaunch a, const int64_t first, const int64_t count, const int64_t g_ld,
                                                                                             const int64_t each) {
     typedef typename El<EL>::T T;
@@ -540,8 +540,8 @@ Cut cut_product(int64_t m, int64_t n, int64_t steps, int pairs, bool native, boo
     return best;
 }
 
-// Up to 32 rows, and up to 64 where that fills the card.  Columns -> classes, us, and as a product of tiles of 128 x 128: 4096 -> 65536 1 row 93 / 210,
-// 16 rows 122 / 216; 4096 -> 20000 32 rows 35 / 70, 64 rows 50 / 70; 777 -> 50000 20 rows 35 / 42; 512 -> 1000 64 rows 10.4 / 5.7.
+// Up to 32 rows, and up to 64 where that fills the card.  Columns -> classes, us, and as a product of tiles of 128 x 128: 4096 -> 65536 1 row 96 / 180,
+// 16 rows 125 / 199; 4096 -> 20000 32 rows 36 / 60, 64 rows 51 / 60; 777 -> 50000 20 rows 35 / 42; 512 -> 1000 64 rows 10.4 / 5.7.
 bool few_rows(const XentLaunch &a, int64_t count) {
     return a.dtype != TF_F32 && (a.n_rows <= 32 || (a.n_rows <= 64 && count * a.n_in >= (int64_t)1 << 23));
 }
