@@ -433,7 +433,7 @@ template <int EL, int L, int NV, bool SIGMOIDS> __global__ __launch_bounds__(256
     in[0].load(a, t, lane);
     in[1].load(a, t + step, lane);
     auto row = [&](Input<R, true> &in) {
-        const typename R::Raw raw = in.raw;
+        typename R::Raw raw = in.raw;
         bool named = false, twice = false;
         for (int first = 0;;) {
 #pragma unroll
@@ -472,6 +472,12 @@ template <int EL, int L, int NV, bool SIGMOIDS> __global__ __launch_bounds__(256
             each_entry(true);
         }
         in_order();
+        // (a row without an entry gets zeros whatever its scores are: a softmax of +inf is NaN, which no factor of zero takes away)
+        if (__ballot(!named))
+#pragma unroll
+            for (int c = 0; c < NV; ++c)
+#pragma unroll
+                for (int w = 0; w < 4; ++w) raw.c[c][w] = named ? raw.c[c][w] : 0u;
         float n[R::N], slope[R::N];
         bool scaled;
         const float total = numerators<R, SIGMOIDS>(n, slope, raw, lane, E, scaled);
@@ -502,7 +508,7 @@ template <int EL, int L, int NV, bool SIGMOIDS> __global__ __launch_bounds__(256
         }
         // (`again`: numerators that say little; with plain sigmoids, slopes that are over an exponential)
         const bool again = a.dvals && named && (top_only ? some < kSmall : sigmoid_only && scaled);
-        const float A = factor * over_all, B = !a.dvals ? 0.0f : sigmoid_only ? 1.0f : top_only ? inverse(some) : over_all;
+        const float A = named ? factor * over_all : 0.0f, B = !a.dvals ? 0.0f : sigmoid_only ? 1.0f : top_only ? inverse(some) : over_all;
         gs *= sigmoid_only ? 0.0f : B;
         // what is taken off: A sum p f, B sum q g for the experts that are named or, with shares over all experts, for all of them
         const float Afs = A * fs, Bgs = B * gs, off = Afs + (top_only ? 0.0f : Bgs), off_named = top_only ? Bgs : 0.0f;
