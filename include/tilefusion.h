@@ -483,6 +483,12 @@ tf_status tf_xent_loss(const tf_xent *plan, const void *X, int64_t ldx, const vo
  * tf_xent_loss made and the gradient of each row's loss.  dX and dW are overwritten; they must not overlap X, W or each other. */
 tf_status tf_xent_grad(const tf_xent *plan, const void *X, int64_t ldx, const void *W, int64_t ldw, const int32_t *labels, const float *lse,
                        const float *dloss, int64_t n_rows, void *dX, int64_t lddx, void *dW, int64_t lddw, void *hip_stream);
+/* The same from the loss that tf_xent_loss made as well: the label's part of g is then dloss[t] (exp(-loss[t]) - 1), which keeps its precision in rows that
+ * are nearly certain of their label.  From lse alone it is off by 2^-24 |lse[t]| of dloss[t], more than itself where the loss is as small as that.
+ * loss NULL: tf_xent_grad. */
+tf_status tf_xent_grad_by_loss(const tf_xent *plan, const void *X, int64_t ldx, const void *W, int64_t ldw, const int32_t *labels, const float *loss,
+                               const float *lse, const float *dloss, int64_t n_rows, void *dX, int64_t lddx, void *dW, int64_t lddw,
+                               void *hip_stream);
 
 /* Message for the most recent failure on the calling thread ("" if none). */
 const char *tf_last_error(void);

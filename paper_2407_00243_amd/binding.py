@@ -110,7 +110,7 @@ EXPORTS = ["tf_plan_create", "tf_plan_destroy", "tf_plan_schedule", "tf_plan_wor
            "tf_csr_validate", "tf_q4_sizes", "tf_q4_pack", "tf_q4_quantize", "tf_q4_unpack", "tf_q4_matvec",
            "tf_moe_route", "tf_moe_create", "tf_moe_destroy", "tf_moe_layer", "tf_moe_layer_q4",
            "tf_moe_balance_size", "tf_moe_balance", "tf_moe_route_grad", "tf_xent_create", "tf_xent_destroy",
-           "tf_xent_device", "tf_xent_loss", "tf_xent_grad",
+           "tf_xent_device", "tf_xent_loss", "tf_xent_grad", "tf_xent_grad_by_loss",
            "tf_last_error", "tf_version"]
 _INT_RETURNS = [e for e in EXPORTS if e not in ("tf_last_error", "tf_version")]
 
@@ -163,6 +163,7 @@ def load_library():
     lib.tf_xent_device.argtypes = [vp, ctypes.POINTER(i32)]
     lib.tf_xent_loss.argtypes = [vp, vp, i64, vp, i64, vp, i64, vp, vp, vp]
     lib.tf_xent_grad.argtypes = [vp, vp, i64, vp, i64, vp, vp, vp, i64, vp, i64, vp, i64, vp]
+    lib.tf_xent_grad_by_loss.argtypes = [vp, vp, i64, vp, i64, vp, vp, vp, vp, i64, vp, i64, vp, i64, vp]
     for name in _INT_RETURNS:
         getattr(lib, name).restype = ctypes.c_int
     lib.tf_last_error.restype = ctypes.c_char_p
@@ -703,6 +704,11 @@ def tf_xent_loss(plan: int, X, W, labels, loss, lse, stream=None) -> None:
 
 
 def tf_xent_grad(plan: int, X, W, labels, lse, dloss, dX=None, dW=None, stream=None) -> None:
+    tf_xent_grad_by_loss(plan, X, W, labels, None, lse, dloss, dX, dW, stream)
+
+
+def tf_xent_grad_by_loss(plan: int, X, W, labels, loss, lse, dloss, dX=None, dW=None, stream=None) -> None:
+    """loss: that of tf_xent_loss, with which the gradients of rows that are nearly certain of their label keep their precision, or None."""
     rows, n, ldx = _matrix(X, "X")
     classes, _, ldw = _matrix(W, "W", n)
     _xent_types(X, W, dX, dW)
@@ -714,9 +720,9 @@ def tf_xent_grad(plan: int, X, W, labels, lse, dloss, dX=None, dW=None, stream=N
             if have != want:
                 raise ValueError(f"{what} must have {want} rows, not {have}")
             lddx, lddw = (step, lddw) if what == "dX" else (lddx, step)
-    status = load_library().tf_xent_grad(
+    status = load_library().tf_xent_grad_by_loss(
         plan, X.data_ptr(), ldx, W.data_ptr(), ldw, _vector(labels, "labels", rows, "torch.int32", device),
-        _vector(lse, "lse", rows, "torch.float32", device), _vector(dloss, "dloss", rows, "torch.float32", device), rows,
+        None if loss is None else _vector(loss, "loss", rows, "torch.float32", device), _vector(lse, "lse", rows, "torch.float32", device), _vector(dloss, "dloss", rows, "torch.float32", device), rows,
         _addr(dX), lddx, _addr(dW), lddw, stream)
     if status:
         _check(status)
@@ -757,10 +763,11 @@ class XentPlan:
         self._look(X, W)
         tf_xent_loss(self.handle, X, W, labels, loss, lse, stream)
 
-    def grad(self, X, W, labels, lse, dloss, dX=None, dW=None, stream=None) -> None:
-        """Writes dX and dW (like X and W; None: not wanted) from lse and the gradient of each row's loss (float32)."""
+    def grad(self, X, W, labels, lse, dloss, dX=None, dW=None, stream=None, loss=None) -> None:
+        """Writes dX and dW (like X and W; None: not wanted) from lse and the gradient of each row's loss (float32).  loss: what the call of that
+        name wrote; with it the gradients of rows that are nearly certain of their label keep their precision."""
         self._look(X, W)
-        tf_xent_grad(self.handle, X, W, labels, lse, dloss, dX, dW, stream)
+        tf_xent_grad_by_loss(self.handle, X, W, labels, loss, lse, dloss, dX, dW, stream)
 
     def close(self) -> None:
         if self.handle:

@@ -46,7 +46,7 @@ struct XentSpace {
     unsigned *arrived;            // for blocks of rows: workgroups that have left their sums
     float *unit;                  // what sums of gradients are multiplied by at the end
     int32_t *label;
-    float *lse, *g, *hit;         // log of the sum, gradient over the unit, logit of the label
+    float *lse, *g, *hit;         // log of the sum, gradient over the unit, logit of the label (or, where the loss is given, its gradient over dloss)
     float *top, *sum;             // running maximum and sum of exponentials
     Float2 *part;                 // both for blocks of classes, block after block
     void *x, *w, *G;              // operands: rows that count, a copy of W where there has to be one, gradient of the logits; planes of 16-bit
@@ -69,7 +69,7 @@ struct XentLaunch {
     const int32_t *labels;
     int32_t n_rows, n_classes, n_in, dtype;
     float *loss, *lse;
-    const float *lse_in, *dloss;
+    const float *lse_in, *dloss, *loss_in;   // loss_in: NULL or the rows' losses
     void *dX, *dW;
     int32_t native;               // fp32 operands are multiplied as they are, not in parts
     int32_t direct_dx;            // dX is written by its product; rows without a label get their zeros first
@@ -107,7 +107,7 @@ struct ProductLaunch {
     int32_t first_class;
     const int32_t *label;
     const float *lse, *g, *unit;
-    float *hit;
+    float *hit;                   // (gradient: NULL or what exp(l - lse) - 1 is at the label)
     Float2 *part;                 // largest logit and sum of exponentials over it
     int64_t part_ld;
     int32_t join;                 // 1: the last workgroup of a block of rows adds up its sums and writes

@@ -244,6 +244,11 @@ tf_status tf_xent_loss(const tf_xent *p, const void *X, int64_t ldx, const void 
 
 tf_status tf_xent_grad(const tf_xent *p, const void *X, int64_t ldx, const void *W, int64_t ldw, const int32_t *labels, const float *lse,
                        const float *dloss, int64_t n_rows, void *dX, int64_t lddx, void *dW, int64_t lddw, void *stream) {
+    return tf_xent_grad_by_loss(p, X, ldx, W, ldw, labels, nullptr, lse, dloss, n_rows, dX, lddx, dW, lddw, stream);
+}
+
+tf_status tf_xent_grad_by_loss(const tf_xent *p, const void *X, int64_t ldx, const void *W, int64_t ldw, const int32_t *labels, const float *loss,
+                               const float *lse, const float *dloss, int64_t n_rows, void *dX, int64_t lddx, void *dW, int64_t lddw, void *stream) {
     const tf_status st = check_xent(p, X, ldx, W, ldw, labels, n_rows);
     if (st != TF_OK) return st;
     if (!p->d.gradients) return report(TF_EMISMATCH, "the plan was made without gradients");
@@ -251,11 +256,13 @@ tf_status tf_xent_grad(const tf_xent *p, const void *X, int64_t ldx, const void 
     if (n_rows > 0 && (!lse || !dloss)) return report(TF_EINVAL, "null argument");
     if ((dX && lddx < p->d.n_in) || (dW && lddw < p->d.n_in)) return report(TF_EINVAL, "rows of dX or dW are closer together than they are wide");
     const int64_t es = bytes_of(p->d.dtype);
-    if (!aligned(dX, es) || !aligned(dW, es) || !aligned(lse, 4) || !aligned(dloss, 4)) return report(TF_EINVAL, "arrays must be aligned to their elements");
+    if (!aligned(dX, es) || !aligned(dW, es) || !aligned(loss, 4) || !aligned(lse, 4) || !aligned(dloss, 4))
+        return report(TF_EINVAL, "arrays must be aligned to their elements");
     if (n_rows == 0 && !dW) return TF_OK;
     tf::XentLaunch a = xent_args(p, X, ldx, W, ldw, labels, n_rows);
     a.lse_in = lse;
     a.dloss = dloss;
+    a.loss_in = loss;
     a.dX = dX;
     a.lddx = lddx;
     a.dW = dW;

@@ -504,7 +504,8 @@ __global__ __launch_bounds__(WM * WN * 64, TM * TN > 32 ? 1 : 2) void k_product(
                     }
                 }
             } else if (is) {
-                const float from = a.lse[row] * LOG2E, scale = a.g[row];
+                // The label's is exp(l - lse) - 1, which for rows that are nearly certain of it cancels to 2^-24 of lse; exp(-loss) - 1 does not.
+                const float from = a.lse[row] * LOG2E, scale = a.g[row], own = any && a.hit ? a.hit[row] : -1.0f, times = a.hit ? 0.0f : 1.0f;
                 typedef typename El<EL>::T T;
                 T *out = static_cast<T *>(a.G) + row * a.g_ld + mw + 4 * g;
                 typedef uint16_t U4 __attribute__((ext_vector_type(4)));
@@ -516,7 +517,8 @@ __global__ __launch_bounds__(WM * WN * 64, TM * TN > 32 ? 1 : 2) void k_product(
                     for (int v = 0; v < 4; ++v) d[v] = __builtin_amdgcn_exp2f(fmaf(value(x, y, v), LOG2E, -from));
                     if (any)
 #pragma unroll
-                        for (int v = 0; v < 4; ++v) d[v] -= at == 16 * x + v ? 1.0f : 0.0f;
+                        for (int v = 0; v < 4; ++v)
+                            if (at == 16 * x + v) d[v] = fmaf(d[v], times, own);
 #pragma unroll
                     for (int v = 0; v < 4; ++v) d[v] *= scale;
                     if (!whole)

@@ -206,6 +206,7 @@ template <int EL> __global__ __launch_bounds__(256) void k_pack_rows(const XentL
                 if (a.dloss) {
                     a.s.lse[n + at] = a.lse_in[r];
                     a.s.g[n + at] = a.dloss[r] / top * scale;
+                    if (a.loss_in) a.s.hit[n + at] = expm1f(-a.loss_in[r]);
                 }
             } else if (a.loss) {
                 a.loss[r] = a.lse[r] = 0.0f;
@@ -621,6 +622,7 @@ int launch_xent_grad(const XentLaunch &call, void *stream) {
             p.end = kEndGradient;
             p.lse = a.s.lse;
             p.g = a.s.g;
+            p.hit = a.loss_in ? a.s.hit : nullptr;
             p.G = a.s.G;
             p.g_ld = g_ld;
             p.g_plane = a.s.g_cap;

@@ -55,3 +55,88 @@ def test_rows_without_an_entry_get_zeros_whatever_they_hold(E, dtype, scoring):
         if d is None or math.isfinite(d):
             ref, bound = lu.route_grad(clean, c, k, scoring, 1.5, v, n, dloss)
             lu.check(out, ref, bound, dtype, f"E{E} {dtype} scoring {scoring}")
+
+
+# ----------------------------------------------------------------------------------- cross entropy
+
+def run_xent(plan, X, W, labels, dloss, given=False, grads="XW"):
+    """loss, lse, dX and dW of one plan; `given`: the gradients are made from the loss as well."""
+    T = X.shape[0]
+    loss, lse = torch.full((T,), math.nan, device="cuda"), torch.full((T,), math.nan, device="cuda")
+    dX = torch.full(X.shape, math.nan, device="cuda", dtype=X.dtype) if "X" in grads else None
+    dW = torch.full(W.shape, math.nan, device="cuda", dtype=W.dtype) if "W" in grads else None
+    plan.loss(X, W, labels, loss, lse, stream())
+    more = {"loss": loss} if given else {}
+    plan.grad(X, W, labels, lse, dloss, dX, dW, stream(), **more)
+    return loss, lse, dX, dW
+
+
+def grad_bounds(X, W, labels, dloss, given=False):
+    """dX and dW in 64 bits and the bounds of loss_util.xent with two of its terms made finer (every row has a label).
+
+    What fp16 loses below its range is 2^-25 of 2^15 in numbers over the row's own |dloss| for dX, over the largest for dW: 2^-40 of them.
+    `given`: the label's part is exp(-loss) - 1, off by exp(-loss) of the loss's own bound and 2^-22 of itself.
+    """
+    dtype, T, V = X.dtype, X.shape[0], W.shape[0]
+    parts = 6 if dtype == F else 1
+    ref = lu.xent(X, W, labels, dloss)
+    x, w, y, c, at = X.double(), W.double(), labels.long(), dloss.double()[:, None], torch.arange(T, device="cuda")
+    wt = w.t().contiguous()
+    l, dl = x @ wt, lu.sum_bound(X.shape[1], x.abs() @ wt.abs(), parts)
+    lse, dlse = (t[:, None] for t in ref["lse"])
+    p = torch.exp(l - lse)
+    g = p.clone()
+    g[at, y] = torch.expm1(-ref["loss"][0])
+    off = p * (dl + dlse + 2.0 ** -20) + 2.0 ** -23 * (p + 1e-9)
+    if given:
+        off[at, y] = torch.exp(-ref["loss"][0]) * ref["loss"][1]
+    off += (lu.UNIT[dtype] + 2.0 ** -22) * g.abs()
+    g *= c
+    out = []
+    for row, what in ((c.abs(), "dX"), (c.abs().max(), "dW")):
+        dg = off * c.abs() + (2.0 ** -40 if dtype == HF else 2.0 ** -126) * row
+        ga = g.abs() + dg
+        if what == "dX":
+            out.append((g @ w, dg @ w.abs() + lu.sum_bound(V, ga @ w.abs(), parts)))
+        else:
+            out.append((g.t().contiguous() @ x, dg.t().contiguous() @ x.abs() + lu.sum_bound(T, ga.t().contiguous() @ x.abs(), parts)))
+    return out
+
+
+@pytest.mark.parametrize("dtype", [BF, HF, F])
+@pytest.mark.parametrize("T,size", [(33, 40.0), (33, 200.0), (500, 40.0), (1500, 200.0)])
+def test_gradients_of_nearly_certain_rows(T, size, dtype):
+    """Losses of 1e-6 to 1 at logits of `size`, where 2^-24 of lse is as large as the label's gradient: with the loss given it keeps its precision."""
+    print(f"T{T} size {size} {dtype}", flush=True)
+    V, d = 64, 40
+    g = gen(T)
+    # classes in pairs that differ in the last column only; a row lies along its pair's first columns, and its last one tells the two apart
+    half = torch.randn(V // 2, d, device="cuda", generator=g) / 4
+    W = half.repeat_interleave(2, 0)
+    W[:, d - 1] = torch.tensor([0.0, 1.0], device="cuda").repeat(V // 2)
+    W = W.to(dtype)
+    labels = torch.randint(0, V // 2, (T,), device="cuda", generator=g) * 2
+    along = W[labels].float()
+    X = along * (size / (along * along).sum(1, keepdim=True))
+    X[:, d - 1] = -torch.linspace(0.5, 14, T, device="cuda")
+    X, labels = X.to(dtype), labels.to(torch.int32)
+    dloss = torch.rand(T, device="cuda", generator=g) + 0.5
+    plan = tf.XentPlan(V, d, dtype, max_rows=T)
+    loss, lse, dX, dW = run_xent(plan, X, W, labels, dloss, given=True)
+    ref = lu.xent(X, W, labels, dloss)
+    assert ref["loss"][0].min() < 1e-5 and ref["loss"][0].max() > 0.1
+    lu.check(loss, *ref["loss"], what="loss")
+    for got, want, what in zip((dX, dW), grad_bounds(X, W, labels, dloss, given=True), ("dX", "dW")):
+        lu.check(got, *want, dtype, what)
+    torch.cuda.synchronize()
+
+
+def test_refusals_of_the_loss():
+    T, V, d = 8, 20, 16
+    X, W = torch.randn(T, d, device="cuda").to(BF), torch.randn(V, d, device="cuda").to(BF)
+    labels, v = torch.zeros(T, device="cuda", dtype=torch.int32), torch.zeros(T + 1, device="cuda")
+    plan = tf.XentPlan(V, d, BF, max_rows=T)
+    for bad in (v, v[:T].double(), v[:T].cpu(), torch.zeros(2 * T, device="cuda")[::2]):
+        with pytest.raises((TypeError, ValueError)):
+            plan.grad(X, W, labels, v[:T], v[:T], torch.empty_like(X), None, stream(), loss=bad)
+    torch.cuda.synchronize()
