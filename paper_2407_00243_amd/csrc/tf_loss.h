@@ -46,11 +46,12 @@ struct XentSpace {
     unsigned *arrived;            // for blocks of rows: workgroups that have left their sums
     float *unit;                  // what sums of gradients are multiplied by at the end
     int32_t *label;
-    float *lse, *g, *hit;         // log of the sum, gradient over the unit, logit of the label (or, where the loss is given, its gradient over dloss)
+    float *lse, *g, *hit;         // log of the sum, gradient over the unit, logit of the label (or, where the loss is given, minus that)
+    float *dloss;                 // gradient of the row's loss (fp16)
     float *top, *sum;             // running maximum and sum of exponentials
     Float2 *part;                 // both for blocks of classes, block after block
     void *x, *w, *G;              // operands: rows that count, a copy of W where there has to be one, gradient of the logits; planes of 16-bit
-                                  // numbers, or (native) fp32
+                                  // numbers, or (native) fp32.  fp16 has two planes of G: see kRowUnit
     float *dx, *dw;               // sums in 32 bits, one slab for each share of a contraction
     int64_t ld;                   // row length of x and w: n_in rounded up to 256, and kRowPad
     int64_t x_plane;              // elements
@@ -59,6 +60,9 @@ struct XentSpace {
 constexpr int64_t kMostBlocks = 1024;      // of rows
 constexpr int kMostJoins = 1024;           // blocks of rows whose sums the last workgroup adds up
 constexpr int kJoinApart = 32;             // their counters: a line of memory each, else all workgroups would count in one
+// G in fp16.  Its first plane is what dX is made of: each row is over its own dloss times kRowUnit, so that a row keeps its precision whatever the others'
+// dloss is.  The second is what dW, a sum over the rows, is made of: all rows over the largest |dloss| times 2^-15.
+constexpr float kRowUnit = 1.0f / 32768.0f;
 // Elements between the rows of x, w and G: rows a power of two apart would all lie in one channel of an XCD's L2.
 constexpr int64_t kRowPad = 64;
 
@@ -107,7 +111,8 @@ struct ProductLaunch {
     int32_t first_class;
     const int32_t *label;
     const float *lse, *g, *unit;
-    float *hit;                   // (gradient: NULL or what exp(l - lse) - 1 is at the label)
+    const float *row_unit;        // NULL or, for each row of N, what its results are multiplied by besides kRowUnit, in the unit's place
+    float *hit;                   // (gradient: NULL or the logarithm of the label's exp(l - lse))
     Float2 *part;                 // largest logit and sum of exponentials over it
     int64_t part_ld;
     int32_t join;                 // 1: the last workgroup of a block of rows adds up its sums and writes
@@ -115,6 +120,7 @@ struct ProductLaunch {
     float *loss, *lse_out;        // (at out_row)
     void *G;
     int64_t g_ld, g_plane;
+    int32_t for_dx, for_dw;       // fp16: which planes of G are wanted
     float *slab;
     int64_t slab_ld, slab_size;
     int32_t add;                  // to what the slab holds

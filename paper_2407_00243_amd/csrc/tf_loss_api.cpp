@@ -77,18 +77,18 @@ struct Cut {
 
 // Sizes of the workspace: G (the gradient of the logits) and a copy of W are held for as many classes at a time as 2^28 numbers allow (256 at
 // least), partial sums for as many as leave 2^25 of them, slabs of the shares of dX up to 2^26 numbers, or what one share needs, of dW 2^25.  fp32 numbers
-// take three planes of 16 bits, in which they also lie as they are.
+// take three planes of 16 bits, in which they also lie as they are; G in fp16 has two.
 int64_t lay_out(tf_xent &p, char *base) {
     const tf_xent_desc &d = p.d;
     tf::XentSpace &s = p.s;
     const int64_t rows = round_up(d.max_rows, 256), classes = round_up(d.n_classes, 256);
-    const int64_t planes = d.dtype == TF_F32 ? 3 : 1;
+    const int64_t planes = d.dtype == TF_F32 ? 3 : 1, g_planes = d.dtype == TF_F16 ? 2 : planes;
     s.ld = round_up(d.n_in, 256) + tf::kRowPad;
     s.x_plane = rows * s.ld;
     s.part_cap = std::max(std::min(classes / 64 * rows, (int64_t)1 << 25), 4 * rows);
-    const auto piece = [&](int64_t row) { return std::max<int64_t>(256, std::min(classes, ((int64_t)1 << 28) / row / 256 * 256)); };
-    s.w_cap = piece(s.ld) * s.ld;
-    s.g_cap = d.gradients ? (piece(rows) + tf::kRowPad) * rows : 0;
+    const auto piece = [&](int64_t row, int64_t most) { return std::max<int64_t>(256, std::min(classes, most / row / 256 * 256)); };
+    s.w_cap = piece(s.ld, (int64_t)1 << 28) * s.ld;
+    s.g_cap = d.gradients ? (piece(rows, ((int64_t)1 << 28) / (d.dtype == TF_F16 ? 2 : 1)) + tf::kRowPad) * rows : 0;
     s.dx_cap = d.gradients ? std::max({rows * s.ld, std::min((int64_t)1 << 26, 4 * rows * s.ld), std::min((int64_t)1 << 24, 512 * 64 * s.ld)}) : 0;
     s.dw_cap = d.gradients ? (int64_t)1 << 25 : 0;
     Cut c{base};
@@ -103,13 +103,14 @@ int64_t lay_out(tf_xent &p, char *base) {
     c.take(s.lse, d.max_rows);
     c.take(s.g, d.max_rows);
     c.take(s.hit, d.max_rows);
+    c.take(s.dloss, d.dtype == TF_F16 ? d.max_rows : 0);
     c.take(s.top, d.max_rows);
     c.take(s.sum, d.max_rows);
     c.take(s.part, s.part_cap);
     uint16_t *x, *w, *G;
     c.take(x, planes * s.x_plane);
     c.take(w, planes * s.w_cap);
-    c.take(G, planes * s.g_cap);
+    c.take(G, g_planes * s.g_cap);
     s.x = x;
     s.w = w;
     s.G = G;

@@ -505,11 +505,23 @@ __global__ __launch_bounds__(WM * WN * 64, TM * TN > 32 ? 1 : 2) void k_product(
                 }
             } else if (is) {
                 // The label's is exp(l - lse) - 1, which for rows that are nearly certain of it cancels to 2^-24 of lse; exp(-loss) - 1 does not.
-                const float from = a.lse[row] * LOG2E, scale = a.g[row], own = any && a.hit ? a.hit[row] : -1.0f, times = a.hit ? 0.0f : 1.0f;
+                const float from = a.lse[row] * LOG2E, scale = a.g[row], own = any && a.hit ? expm1f(a.hit[row]) : -1.0f, times = a.hit ? 0.0f : 1.0f;
                 typedef typename El<EL>::T T;
-                T *out = static_cast<T *>(a.G) + row * a.g_ld + mw + 4 * g;
+                T *row_of_G = static_cast<T *>(a.G) + row * a.g_ld + mw, *out = row_of_G + 4 * g;
                 typedef uint16_t U4 __attribute__((ext_vector_type(4)));
-                Words2 before;
+                Words2 before[2];
+                // four columns, times `by`, to one of the planes
+                auto put = [&](const float (&d)[4], float by, T *plane, int x, Words2 &before) __attribute__((always_inline)) {
+                    if constexpr (EL != TF_F32) {
+                        const Words2 w = pack4<EL>(d[0] * by, d[1] * by, d[2] * by, d[3] * by);
+                        if constexpr (TM % 2 == 0) {
+                            if (x % 2) *reinterpret_cast<AnyWords4 *>(plane + columns_of(x - 1, g)) = eight_columns(before, w);
+                            else before = w;
+                        } else {
+                            *reinterpret_cast<Words2 *>(plane + 16 * x + 4 * g) = w;
+                        }
+                    }
+                };
 #pragma unroll
                 for (int x = 0; x < TM; ++x) {
                     float d[4];
@@ -519,8 +531,9 @@ __global__ __launch_bounds__(WM * WN * 64, TM * TN > 32 ? 1 : 2) void k_product(
 #pragma unroll
                         for (int v = 0; v < 4; ++v)
                             if (at == 16 * x + v) d[v] = fmaf(d[v], times, own);
+                    if constexpr (EL != TF_F16)
 #pragma unroll
-                    for (int v = 0; v < 4; ++v) d[v] *= scale;
+                        for (int v = 0; v < 4; ++v) d[v] *= scale;
                     if (!whole)
 #pragma unroll
                         for (int v = 0; v < 4; ++v)
@@ -533,12 +546,11 @@ __global__ __launch_bounds__(WM * WN * 64, TM * TN > 32 ? 1 : 2) void k_product(
                         for (int v = 0; v < 4; ++v) split3<EL>(d[v], p[v]);
 #pragma unroll
                         for (int i = 0; i < 3; ++i) *reinterpret_cast<U4 *>(out + i * a.g_plane + 16 * x) = U4{p[0][i], p[1][i], p[2][i], p[3][i]};
-                    } else if constexpr (TM % 2 == 0) {
-                        const Words2 w = pack4<EL>(d[0], d[1], d[2], d[3]);
-                        if (x % 2) *reinterpret_cast<AnyWords4 *>(static_cast<T *>(a.G) + row * a.g_ld + mw + columns_of(x - 1, g)) = eight_columns(before, w);
-                        else before = w;
+                    } else if constexpr (EL == TF_F16) {
+                        if (a.for_dx) put(d, 1.0f / kRowUnit, row_of_G, x, before[0]);
+                        if (a.for_dw) put(d, scale, row_of_G + a.g_plane, x, before[1]);
                     } else {
-                        *reinterpret_cast<Words2 *>(out + 16 * x) = pack4<EL>(d[0], d[1], d[2], d[3]);
+                        put(d, 1.0f, row_of_G, x, before[0]);
                     }
                 }
             }
@@ -567,6 +579,7 @@ __global__ __launch_bounds__(WM * WN * 64, TM * TN > 32 ? 1 : 2) void k_product(
         for (int y = 0; y < TN; ++y) {
             int64_t row = nw + 16 * y;
             if (row >= rows) continue;
+            const float times = EL == TF_F16 && a.row_unit ? a.row_unit[row] * kRowUnit : unit;
             if (a.out_row) row = a.out_row[row];
             Words2 before;
 #pragma unroll
@@ -574,7 +587,7 @@ __global__ __launch_bounds__(WM * WN * 64, TM * TN > 32 ? 1 : 2) void k_product(
                 const int64_t m = mw + 16 * x + 4 * g;
                 Float4 f;
 #pragma unroll
-                for (int v = 0; v < 4; ++v) f[v] = value(x, y, v) * unit;
+                for (int v = 0; v < 4; ++v) f[v] = value(x, y, v) * times;
                 if (EL == TF_F32 || a.out_dtype == TF_F32) {
                     float *to = static_cast<float *>(a.out) + row * a.ldo + m;
                     typedef float F4 __attribute__((ext_vector_type(4), aligned(4)));

@@ -178,7 +178,7 @@ template <int EL> __global__ __launch_bounds__(256) void k_pack_rows(const XentL
     __syncthreads();
     n = n_of[0] + n_of[1] + n_of[2] + n_of[3];
     top = fmaxf(fmaxf(top_of[0], top_of[1]), fmaxf(top_of[2], top_of[3]));
-    // gradients are divided by the largest one, so that no size of dloss is lost in 16 bits
+    // gradients are divided by the largest one: what dW, their sum, can hold is not lost in 16 bits
     const float scale = a.dtype == TF_F16 ? 32768.0f : 1.0f;
     if (top == 0.0f) top = 1.0f;
     if (!a.loss && blockIdx.x == 0 && tid == 0) *a.s.unit = top / scale;       // (without rows there is no dloss)
@@ -206,7 +206,8 @@ template <int EL> __global__ __launch_bounds__(256) void k_pack_rows(const XentL
                 if (a.dloss) {
                     a.s.lse[n + at] = a.lse_in[r];
                     a.s.g[n + at] = a.dloss[r] / top * scale;
-                    if (a.loss_in) a.s.hit[n + at] = expm1f(-a.loss_in[r]);
+                    if (EL == TF_F16) a.s.dloss[n + at] = a.dloss[r];
+                    if (a.loss_in) a.s.hit[n + at] = -a.loss_in[r];
                 }
             } else if (a.loss) {
                 a.loss[r] = a.lse[r] = 0.0f;
@@ -321,7 +322,7 @@ __host__ __device__ constexpr int parts_of(const XentLaunch &a) { return a.dtype
 
 // dX: the shares' sums of each row that counts, zeros in the others.
 template <int EL> __global__ __launch_bounds__(256) void k_finish_rows(const XentLaunch a, const int splits, const int64_t size) {      // (the same for every piece)
-    const float unit = *a.s.unit;
+    const float all = *a.s.unit;
     const bool by_slab = splits >= kManySlabs;
     const int per_row = min(threads_of_row(a.n_in), by_slab ? 32 : 256);
     const int at_once = by_slab ? 1 : 256 / per_row;
@@ -329,6 +330,7 @@ template <int EL> __global__ __launch_bounds__(256) void k_finish_rows(const Xen
         const int64_t t = t0 + (by_slab ? 0 : threadIdx.x / per_row);
         const bool is = t < a.n_rows;
         const int64_t i = is ? a.s.pos[t] : -1;
+        const float unit = EL == TF_F16 && i >= 0 ? a.s.dloss[i] * kRowUnit : all;
         finish_row<EL>(a.s.dx + i * a.s.ld, size, splits, static_cast<typename El<EL>::T *>(a.dX) + t * a.lddx, a.n_in, i < 0, unit, per_row, by_slab, is);
     }
 }
@@ -359,6 +361,7 @@ template <int EL, int KH> __global__ __launch_bounds__(256, KH > 1 ? 3 : 4) void
     const int64_t c0 = (int64_t)blockIdx.x * 256 + wave * 64, v_end = min(count, ((int64_t)blockIdx.y + 1) * each);
     if (c0 >= a.n_in) return;
     const float unit = *a.s.unit;
+    const uint16_t *G = static_cast<const uint16_t *>(a.s.G) + (EL == TF_F16 ? a.s.g_cap : 0);
     V x[4][KH];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
@@ -383,7 +386,7 @@ template <int EL, int KH> __global__ __launch_bounds__(256, KH > 1 ? 3 : 4) void
             for (int k = 0; k < 8; ++k) {
                 const int64_t t = 32 * h + 8 * g + k;
                 next[h][k] = U4{0, 0, 0, 0};
-                if (t < kept) next[h][k] = *reinterpret_cast<const U4 *>(static_cast<const uint16_t *>(a.s.G) + t * g_ld + v + 4 * r);
+                if (t < kept) next[h][k] = *reinterpret_cast<const U4 *>(G + t * g_ld + v + 4 * r);
             }
     };
     int64_t v0 = blockIdx.y * each;
@@ -626,6 +629,8 @@ int launch_xent_grad(const XentLaunch &call, void *stream) {
             p.G = a.s.G;
             p.g_ld = g_ld;
             p.g_plane = a.s.g_cap;
+            p.for_dx = a.dX != nullptr;
+            p.for_dw = a.dW != nullptr;
             e = launch_product(p, a, stream);
             if (e) return e;
             if (a.dX) {
@@ -641,6 +646,7 @@ int launch_xent_grad(const XentLaunch &call, void *stream) {
                 q.n_count = a.n_rows;
                 q.end = a.direct_dx ? kEndOut : kEndSlab;
                 q.unit = a.s.unit;
+                q.row_unit = a.dtype == TF_F16 ? a.s.dloss : nullptr;
                 q.out = a.dX;
                 q.ldo = a.lddx;
                 q.out_row = a.s.list;
@@ -663,7 +669,7 @@ int launch_xent_grad(const XentLaunch &call, void *stream) {
         } else if (a.dW) {
             ProductLaunch q{};
             q.M = Side{a.s.x, a.s.ld, a.s.x_plane, 0, a.s.ld};
-            q.N = Side{a.s.G, g_ld, a.s.g_cap, 0, piece};
+            q.N = Side{static_cast<uint16_t *>(a.s.G) + (a.dtype == TF_F16 ? a.s.g_cap : 0), g_ld, a.s.g_cap, 0, piece};
             q.parts = parts;
             q.n = a.s.n;
             q.k_rows = 1;

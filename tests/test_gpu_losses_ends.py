@@ -140,3 +140,26 @@ def test_refusals_of_the_loss():
         with pytest.raises((TypeError, ValueError)):
             plan.grad(X, W, labels, v[:T], v[:T], torch.empty_like(X), None, stream(), loss=bad)
     torch.cuda.synchronize()
+
+
+@pytest.mark.parametrize("T,V", [(12, 50000), (60, 50000), (60, 300), (700, 5000)])
+def test_gradients_of_very_different_rows_of_many_classes(T, V):
+    """fp16, dloss over nine decades: each row of dX keeps its precision though all classes but the label's are small numbers in it.
+
+    W's numbers have a common part that adds up to nothing over a row's gradients, so that classes that are lost show."""
+    print(f"T{T} V{V}", flush=True)
+    d = 64
+    g = gen(V)
+    W = (64 * (1 + torch.randn(V, d, device="cuda", generator=g) / 2)).to(HF)
+    X = (torch.randn(T, d, device="cuda", generator=g) / 256).to(HF)
+    labels = torch.randint(0, V, (T,), device="cuda", generator=g).to(torch.int32)
+    dloss = 10.0 ** torch.linspace(-7, 2, T, device="cuda")
+    dloss[::2] *= -1
+    plan = tf.XentPlan(V, d, HF, max_rows=T)
+    want = grad_bounds(X, W, labels, dloss)
+    for grads in ("XW", "X", "W"):
+        loss, lse, dX, dW = run_xent(plan, X, W, labels, dloss, grads=grads)
+        for got, ref, what in zip((dX, dW), want, ("dX", "dW")):
+            if got is not None:
+                lu.check(got, *ref, HF, f"{what} of {grads}")
+    torch.cuda.synchronize()
