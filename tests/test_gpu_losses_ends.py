@@ -163,3 +163,29 @@ def test_gradients_of_very_different_rows_of_many_classes(T, V):
             if got is not None:
                 lu.check(got, *ref, HF, f"{what} of {grads}")
     torch.cuda.synchronize()
+
+
+@pytest.mark.parametrize("T", [40])
+def test_the_largest_fp32_numbers(T):
+    """Numbers beside the largest one."""
+    V, d = 90, 24
+    g = gen(T)
+    most, least = torch.finfo(F).max, 2.0 ** -126
+    X, W = torch.randn(T, d, device="cuda", generator=g), torch.randn(V, d, device="cuda", generator=g) / 4
+    sign = torch.randint(0, 2, (T,), device="cuda", generator=g) * 2.0 - 1
+    X[:, 3] = most * sign * (1 - torch.rand(T, device="cuda", generator=g) * 2.0 ** -10)
+    W[:, 3] = least * (torch.arange(V, device="cuda") % 3 - 1)
+    X[:, 17] = least * sign
+    W[:, 17] = most * (1 - torch.rand(V, device="cuda", generator=g) * 2.0 ** -10) * (torch.arange(V, device="cuda") % 2)
+    labels = torch.randint(0, V, (T,), device="cuda", generator=g).to(torch.int32)
+    dloss = torch.rand(T, device="cuda", generator=g) / T
+    plan = tf.XentPlan(V, d, F, max_rows=T)
+    loss, lse, dX, dW = run_xent(plan, X, W, labels, dloss)
+    ref = lu.xent(X, W, labels, dloss)
+    lu.check(loss, *ref["loss"], what="loss")
+    lu.check(lse, *ref["lse"], what="lse")
+    # (column 3 of dX and 17 of dW are sums of products with the smallest number: below what fp32 holds)
+    rest = torch.arange(d, device="cuda")
+    lu.check(dX[:, rest != 3], *(t[:, rest != 3] for t in ref["dX"]), what="dX")
+    lu.check(dW[:, rest != 17], *(t[:, rest != 17] for t in ref["dW"]), what="dW")
+    torch.cuda.synchronize()
