@@ -58,6 +58,13 @@ template <int EL> __device__ __forceinline__ void write8(const float (&x)[8], vo
     }
 }
 
+// The first part of a finite number is finite: beside the largest ones rounding would give infinity, and NaN in the parts behind it.
+__device__ __forceinline__ uint16_t first_part(float x) {
+    constexpr float MOST = 0x1.fep127f;        // of bf16
+    const float size = fabsf(x);
+    return El<TF_BF16>::put(size > MOST && size < __builtin_inff() ? copysignf(MOST, x) : x);
+}
+
 // Eight columns as an operand of the products: 16-bit numbers as they are, fp32 ones as three bf16 numbers that add up to them.
 template <int EL> __device__ __forceinline__ void put8(const float (&x)[8], void *to_row, int64_t k, int64_t plane) {
     uint16_t *to = static_cast<uint16_t *>(to_row) + k;
@@ -68,7 +75,7 @@ template <int EL> __device__ __forceinline__ void put8(const float (&x)[8], void
             float a = x[2 * i], b = x[2 * i + 1];
 #pragma unroll
             for (int p = 0; p < 3; ++p) {
-                const uint16_t ha = El<TF_BF16>::put(a), hb = El<TF_BF16>::put(b);
+                const uint16_t ha = p ? El<TF_BF16>::put(a) : first_part(a), hb = p ? El<TF_BF16>::put(b) : first_part(b);
                 w[p][i] = ha | (uint32_t)hb << 16;
                 a -= El<TF_BF16>::get(ha);
                 b -= El<TF_BF16>::get(hb);
@@ -179,9 +186,9 @@ template <int EL> __global__ __launch_bounds__(256) void k_pack_rows(const XentL
     n = n_of[0] + n_of[1] + n_of[2] + n_of[3];
     top = fmaxf(fmaxf(top_of[0], top_of[1]), fmaxf(top_of[2], top_of[3]));
     // fp16: gradients are divided by the largest one, so that what dW, their sum, can hold is not lost in 16 bits.  The other types' range is that of the
-    // results: only gradients that are all very small are made larger (of others the sums could pass the largest number though dX and dW do not).
+    // results: only gradients that are all very small or some very large are divided (of others the sums could pass the largest number though dX and dW do not).
     const float scale = a.dtype == TF_F16 ? 32768.0f : 1.0f;
-    if (top == 0.0f || (a.dtype != TF_F16 && top > 0x1p-64f)) top = 1.0f;
+    if (top == 0.0f || (a.dtype != TF_F16 && top > 0x1p-64f && top < 0x1p64f)) top = 1.0f;
     if (!a.loss && blockIdx.x == 0 && tid == 0) *a.s.unit = top / scale;       // (without rows there is no dloss)
     const int64_t columns = round_up(a.n_in, 64);
     const int per_row = threads_of_row(columns), at_once = 256 / per_row;

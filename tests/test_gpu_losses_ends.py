@@ -165,9 +165,9 @@ def test_gradients_of_very_different_rows_of_many_classes(T, V):
     torch.cuda.synchronize()
 
 
-@pytest.mark.parametrize("T", [40])
+@pytest.mark.parametrize("T", [40, 500])
 def test_the_largest_fp32_numbers(T):
-    """Numbers beside the largest one."""
+    """Numbers beside the largest one, which rounded to bf16 would be infinite, of few and of many rows."""
     V, d = 90, 24
     g = gen(T)
     most, least = torch.finfo(F).max, 2.0 ** -126
@@ -188,4 +188,23 @@ def test_the_largest_fp32_numbers(T):
     rest = torch.arange(d, device="cuda")
     lu.check(dX[:, rest != 3], *(t[:, rest != 3] for t in ref["dX"]), what="dX")
     lu.check(dW[:, rest != 17], *(t[:, rest != 17] for t in ref["dW"]), what="dW")
+    torch.cuda.synchronize()
+
+
+@pytest.mark.parametrize("T", [40, 500])
+def test_an_fp32_row_of_nan_or_infinity_stays_a_row(T):
+    """Of few and of many rows: their loss and dX are not finite, the others' as they are without them."""
+    V, d = 90, 24
+    g = gen(T)
+    X, W = torch.randn(T, d, device="cuda", generator=g), torch.randn(V, d, device="cuda", generator=g) / 4
+    labels = torch.randint(0, V, (T,), device="cuda", generator=g).to(torch.int32)
+    dloss = torch.rand(T, device="cuda", generator=g) / T
+    ref = lu.xent(X, W, labels, dloss)
+    X[11, 5], X[12, 6], X[13, 0] = math.nan, math.inf, -math.inf
+    loss, lse, dX, dW = run_xent(tf.XentPlan(V, d, F, max_rows=T), X, W, labels, dloss)
+    rest = torch.ones(T, dtype=torch.bool, device="cuda")
+    rest[11:14] = False
+    assert not torch.isfinite(loss[11:14]).any() and not torch.isfinite(dX[11:14]).any()
+    for name, got in (("loss", loss), ("lse", lse), ("dX", dX)):
+        lu.check(got[rest], *(t[rest] for t in ref[name]), what=name)
     torch.cuda.synchronize()
