@@ -9,6 +9,7 @@ namespace {
 
 constexpr float kLow = -__builtin_inff();
 typedef int Int4 __attribute__((ext_vector_type(4)));
+typedef double Double4 __attribute__((ext_vector_type(4)));
 
 // Sums and maxima over 2, 4, 8 or 16 neighbouring lanes take one instruction for each doubling (the neighbours' values come with it: lane ^ 1,
 // lane ^ 2, then mirror images of eight and sixteen lanes); 32 and 64 lanes exchange rows of sixteen and halves.
@@ -202,16 +203,16 @@ __device__ __forceinline__ float inverse(float total) { return total == 0.0f ? 0
 // ---------------------------------------------------------------------------------------- balance
 
 // The end of it: thread e has the sum of expert e's shares and its count, `rows` are the rows of this thread's.  loss = E sum_e f_e mass_e.
-__device__ __forceinline__ int wave_total(int x) {
+template <typename T> __device__ __forceinline__ T wave_total(T x) {
 #pragma unroll
     for (int d = 32; d; d >>= 1) x += __shfl_xor(x, d, 64);
     return x;
 }
-__device__ void write_balance(const RouterLaunch &a, float m, int c, int rows) {
-    __shared__ float part[16];
+__device__ void write_balance(const RouterLaunch &a, double m, int c, int rows) {
+    __shared__ double part[16];
     __shared__ int named_of[16], rows_of[16];
     const int E = a.n_experts, tid = threadIdx.x;
-    const float x = over_lanes<64, Plus>(m * (float)c);
+    const double x = wave_total(m * c);
     const int named = wave_total(c), r = wave_total(rows);
     if ((tid & 63) == 0) {
         part[tid >> 6] = x;
@@ -219,7 +220,7 @@ __device__ void write_balance(const RouterLaunch &a, float m, int c, int rows) {
         rows_of[tid >> 6] = r;
     }
     __syncthreads();
-    float sum = 0.0f;
+    double sum = 0.0;
     int n = 0, all = 0;
     for (int w = 0; w < (int)blockDim.x / 64; ++w) {
         sum += part[w];
@@ -228,30 +229,30 @@ __device__ void write_balance(const RouterLaunch &a, float m, int c, int rows) {
     }
     if (tid < E) {
         a.counts[tid] = c;
-        a.mass[tid] = n ? m / (float)n : 0.0f;
+        a.mass[tid] = n ? (float)(m / n) : 0.0f;
     }
     if (tid == 0) {
         a.counts[E] = n;
-        a.loss[0] = n ? (float)E * sum / ((float)all * (float)n) : 0.0f;
+        a.loss[0] = n ? (float)(E * sum / ((double)all * n)) : 0.0f;
     }
 }
 
 // Adds up the sums of `groups` workgroups in a fixed order: 1024 threads, each four experts and every (1024 / (experts / 4))-th workgroup.  256 of 256 experts: 8 us,
 // a launch and three trips to memory.  (A last workgroup of the launch before would need a counter that somebody clears, and the workspace is the caller's.)
 __global__ __launch_bounds__(1024) void k_balance_finish(const RouterLaunch a, const int groups) {
-    __shared__ Float4 masses[1024];
+    __shared__ Double4 masses[1024];
     __shared__ Int4 counts[1024];
     const int tid = threadIdx.x, fours = balance_row(a.n_experts) / 4, slices = min(1024 / fours, 16);
     const Float4 *mass = static_cast<const Float4 *>(a.workspace);
     const Int4 *count = reinterpret_cast<const Int4 *>(mass + (int64_t)kBalanceGroups * fours);
     const int *rows = reinterpret_cast<const int *>(count + (int64_t)kBalanceGroups * fours);
-    Float4 m = {0, 0, 0, 0};
+    Double4 m = {0, 0, 0, 0};
     Int4 c = {0, 0, 0, 0};
     if (tid < slices * fours) {
         const int e = tid % fours;
 #pragma unroll 8
         for (int g = tid / fours; g < groups; g += slices) {
-            m += mass[g * fours + e];
+            m += __builtin_convertvector(mass[g * fours + e], Double4);
             c += count[g * fours + e];
         }
     }
@@ -259,7 +260,7 @@ __global__ __launch_bounds__(1024) void k_balance_finish(const RouterLaunch a, c
     masses[tid] = m;
     counts[tid] = c;
     __syncthreads();
-    float me = 0.0f;
+    double me = 0.0;
     int ce = 0;
     if (tid < a.n_experts)
         for (int s = 0; s < slices; ++s) {
@@ -296,9 +297,10 @@ template <typename R, bool GRADIENTS> struct Input {
 };
 
 // mass_e = sum over rows of n_te / sum_j n_tj.  Every wave takes ROWS tokens at a time and adds up their shares in registers; entries are counted in LDS
-// (whole numbers: their order does not matter).  LDS holds the counts, and at the end a line of sums for each wave.  Two sets of rows are on their way
-// from memory while a third is worked on.  131072 rows of 256 bf16 experts, 8 entries each: 20 us, 3.6 TB/s (the launch after it 8); sigmoids 24.
+// (whole numbers: their order does not matter).  LDS holds the counts, and at the end a line of sums for each wave.  In 32 bits a lane adds up kSteps rows at most, in 64 what
+// those come to; its own sum and a workgroup's are rounded once, so that what mass is off by does not grow with the number of rows.  Two sets of rows are on their way from memory while a third is worked on.  131072 rows of 256 bf16 experts, 8 entries each: 20 us, 3.6 TB/s (the launch after it 8); sigmoids 24.
 // Of 1 Mi rows 135 us, 4.2 TB/s: bound by its instructions, an exponential and about ten others a score.
+constexpr int kSteps = 8;
 template <int EL, int L, int NV, bool SIGMOIDS> __global__ __launch_bounds__(1024) void k_balance(const RouterLaunch a) {
     typedef Row<EL, L, NV> R;
     extern __shared__ __attribute__((aligned(16))) int shared[];
@@ -309,6 +311,7 @@ template <int EL, int L, int NV, bool SIGMOIDS> __global__ __launch_bounds__(102
     for (int e = threadIdx.x; e < line; e += blockDim.x) counted[e] = 0;
     __syncthreads();
     float mass[R::N] = {};
+    double before[R::N] = {};
     int rows = 0;
     const int64_t step = (int64_t)gridDim.x * waves * R::ROWS;
     int64_t t = ((int64_t)blockIdx.x * waves + wave) * R::ROWS + sub;
@@ -342,15 +345,24 @@ template <int EL, int L, int NV, bool SIGMOIDS> __global__ __launch_bounds__(102
 #pragma unroll
             for (int i = 0; i < R::N; ++i) mass[i] += n[i] * each;
     };
+    int steps = 0;
     for (int64_t base = t - sub; base < a.n_tokens; base += 2 * step) {
         row(in[0]);
         t += step;
         if (base + step < a.n_tokens) row(in[1]);
         t += step;
+        if ((steps += 2) == kSteps) {
+#pragma unroll
+            for (int i = 0; i < R::N; ++i) {
+                before[i] += mass[i];
+                mass[i] = 0.0f;
+            }
+            steps = 0;
+        }
     }
     // rows of a wave, then waves in their order
 #pragma unroll
-    for (int i = 0; i < R::N; ++i) mass[i] = over_groups<L>(mass[i]);
+    for (int i = 0; i < R::N; ++i) mass[i] = over_groups<L>((float)(before[i] + mass[i]));
     rows = wave_total(at == 0 ? rows : 0);
     if (sub == 0) {
 #pragma unroll
@@ -362,7 +374,7 @@ template <int EL, int L, int NV, bool SIGMOIDS> __global__ __launch_bounds__(102
     }
     __syncthreads();
     const int e = threadIdx.x;
-    float m = 0.0f;
+    double m = 0.0;
     if (e < E)
         for (int w = 0; w < waves; ++w) m += masses[w * line + e];
     const int c = e < E ? counted[e] : 0, r = e < waves ? rows_of[e] : 0;
@@ -370,7 +382,7 @@ template <int EL, int L, int NV, bool SIGMOIDS> __global__ __launch_bounds__(102
     float *out = static_cast<float *>(a.workspace);
     int *count = reinterpret_cast<int *>(out + (int64_t)kBalanceGroups * line);
     if (e < line) {
-        out[blockIdx.x * line + e] = m;
+        out[blockIdx.x * line + e] = (float)m;
         count[blockIdx.x * line + e] = c;
     }
     if (wave == 0) {

@@ -208,3 +208,24 @@ def test_an_fp32_row_of_nan_or_infinity_stays_a_row(T):
     for name, got in (("loss", loss), ("lse", lse), ("dX", dX)):
         lu.check(got[rest], *(t[rest] for t in ref[name]), what=name)
     torch.cuda.synchronize()
+
+
+def test_mass_of_very_many_rows():
+    """Shares of 2^-24.5 after one of 1 in every lane's rows: sums of 32 bits that go over all of a lane's rows would lose them all."""
+    step, rounds, E = 262144, 128, 2
+    T = step * rounds
+    scores = torch.zeros(T, E, device="cuda")
+    scores[step:, 1] = -17.0
+    scores[:step, 0] = -40.0
+    c = torch.zeros(T, dtype=torch.int32, device="cuda")
+    counts = torch.empty(E + 1, dtype=torch.int32, device="cuda")
+    mass, loss = torch.empty(E, device="cuda"), torch.empty(1, device="cuda")
+    work = torch.empty(tf.tf_moe_balance_size(T, E), dtype=torch.uint8, device="cuda")
+    tf.tf_moe_balance(scores, matrix(T, E, 1, c), counts, mass, loss, work, lu.SOFTMAX, stream())
+    assert counts.tolist() == [T, 0, T]
+    small = 1 / (1 + math.exp(17.0))
+    want = (1 + (rounds - 1) * small) / rounds
+    # a reciprocal (2^-23), sums of at most eight rows in a lane (2^-24 each) and of two lanes, the result; the small shares' own errors are nothing beside it
+    assert abs(mass[1].item() / want - 1) <= (2 + 8 + 6 + 1) * 2.0 ** -24
+    assert abs(mass.double().sum().item() - 1) <= 32 * 2.0 ** -24
+    assert abs(loss.item() / (E * mass[0].item()) - 1) <= 4 * 2.0 ** -24
