@@ -297,8 +297,9 @@ template <typename R, bool GRADIENTS> struct Input {
 };
 
 // mass_e = sum over rows of n_te / sum_j n_tj.  Every wave takes ROWS tokens at a time and adds up their shares in registers; entries are counted in LDS
-// (whole numbers: their order does not matter).  LDS holds the counts, and at the end a line of sums for each wave.  In 32 bits a lane adds up kSteps rows at most, in 64 what
-// those come to; its own sum and a workgroup's are rounded once, so that what mass is off by does not grow with the number of rows.  Two sets of rows are on their way from memory while a third is worked on.  131072 rows of 256 bf16 experts, 8 entries each: 20 us, 3.6 TB/s (the launch after it 8); sigmoids 24.
+// (whole numbers: their order does not matter).  In 32 bits a lane adds up kSteps rows at most, in 64 what
+// those come to; its own sum and a workgroup's are rounded once, so that what mass is off by does not grow with the number of rows.  LDS holds the counts,
+// the lanes' sums in 64 bits (which registers have no room for) and at the end, in their place, a line of sums for each wave.  Two sets of rows are on their way from memory while a third is worked on.  131072 rows of 256 bf16 experts, 8 entries each: 20 us, 3.6 TB/s (the launch after it 8); sigmoids 24.
 // Of 1 Mi rows 135 us, 4.2 TB/s: bound by its instructions, an exponential and about ten others a score.
 constexpr int kSteps = 8;
 template <int EL, int L, int NV, bool SIGMOIDS> __global__ __launch_bounds__(1024) void k_balance(const RouterLaunch a) {
@@ -310,8 +311,8 @@ template <int EL, int L, int NV, bool SIGMOIDS> __global__ __launch_bounds__(102
     const int sub = lane / L, at = lane & (L - 1);
     for (int e = threadIdx.x; e < line; e += blockDim.x) counted[e] = 0;
     __syncthreads();
+    double *before = reinterpret_cast<double *>(masses) + threadIdx.x;       // blockDim.x apart
     float mass[R::N] = {};
-    double before[R::N] = {};
     int rows = 0;
     const int64_t step = (int64_t)gridDim.x * waves * R::ROWS;
     int64_t t = ((int64_t)blockIdx.x * waves + wave) * R::ROWS + sub;
@@ -346,24 +347,28 @@ template <int EL, int L, int NV, bool SIGMOIDS> __global__ __launch_bounds__(102
             for (int i = 0; i < R::N; ++i) mass[i] += n[i] * each;
     };
     int steps = 0;
+    bool more = false;
     for (int64_t base = t - sub; base < a.n_tokens; base += 2 * step) {
         row(in[0]);
         t += step;
         if (base + step < a.n_tokens) row(in[1]);
         t += step;
-        if ((steps += 2) == kSteps) {
+        if ((steps += 2) == kSteps && base + 2 * step < a.n_tokens) {
 #pragma unroll
             for (int i = 0; i < R::N; ++i) {
-                before[i] += mass[i];
+                double *to = before + i * blockDim.x;
+                *to = more ? *to + mass[i] : mass[i];
                 mass[i] = 0.0f;
             }
+            more = true;
             steps = 0;
         }
     }
     // rows of a wave, then waves in their order
 #pragma unroll
-    for (int i = 0; i < R::N; ++i) mass[i] = over_groups<L>((float)(before[i] + mass[i]));
+    for (int i = 0; i < R::N; ++i) mass[i] = over_groups<L>(more ? (float)(before[i * blockDim.x] + mass[i]) : mass[i]);
     rows = wave_total(at == 0 ? rows : 0);
+    __syncthreads();
     if (sub == 0) {
 #pragma unroll
         for (int i = 0; i < R::N; ++i) {
@@ -600,14 +605,16 @@ template <int EL, int L, int NV, bool SIGMOIDS> int balance_of(const RouterLaunc
     const bool few = (int64_t)a.n_tokens * a.n_experts <= 16384;
     const int waves = a.n_experts <= 256 && (few ? sets <= 8 : sets <= 8 * kBalanceGroups) ? 4 : 16;
     const int64_t groups = few ? 1 : std::min<int64_t>(kBalanceGroups, ceil_div(sets, waves));
-    const int line = balance_row(a.n_experts), lds = (line * (waves + 1) + 16) * 4;
+    const bool many = sets > groups * waves * kSteps;       // of a lane's rows
+    const int line = balance_row(a.n_experts), sums = Row<EL, L, NV>::N * waves * 64 * 8;
+    const int lds = (line + 16) * 4 + std::max(line * waves * 4, many ? sums : 0);
     if (lds > 65536) {
         static DoneOnDevices done;
         int device = 0;
         hipError_t e = hipGetDevice(&device);
         if (e != hipSuccess) return (int)e;
         if (!done.has(device)) {
-            e = hipFuncSetAttribute(reinterpret_cast<const void *>(k_balance<EL, L, NV, SIGMOIDS>), hipFuncAttributeMaxDynamicSharedMemorySize, 17 * 4096 + 64);
+            e = hipFuncSetAttribute(reinterpret_cast<const void *>(k_balance<EL, L, NV, SIGMOIDS>), hipFuncAttributeMaxDynamicSharedMemorySize, 4096 + 64 + 16 * 8192);
             if (e != hipSuccess) return (int)e;
             done.add(device);
         }
