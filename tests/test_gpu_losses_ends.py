@@ -229,3 +229,77 @@ def test_mass_of_very_many_rows():
     assert abs(mass[1].item() / want - 1) <= (2 + 8 + 6 + 1) * 2.0 ** -24
     assert abs(mass.double().sum().item() - 1) <= 32 * 2.0 ** -24
     assert abs(loss.item() / (E * mass[0].item()) - 1) <= 4 * 2.0 ** -24
+
+
+def odd(shape, bits, g):
+    """Odd whole numbers of so many bits, as fp32: of more than eight they need more than one bf16 number, of more than sixteen three."""
+    low = torch.rand(*shape, device="cuda", generator=g, dtype=torch.float64)
+    top = 2.0 ** (bits - 1)
+    n = torch.floor(top + low * top)
+    return torch.where(bits == 1, torch.ones_like(n), 2 * torch.floor(n / 2) + 1).float()
+
+
+BITS = (1, 4, 8, 11, 12, 13, 16, 20, 23)      # of one factor; the other has 24 less these, so that their product is a number of 32 bits
+
+
+@pytest.mark.parametrize("T,V", [(449, 1), (500, 300), (2100, 2500), (3000, 70)])
+def test_products_of_fp32_parts_are_whole_logits(T, V):
+    """One product in each sum, of all of its 24 bits: each pair of parts is needed.  (Large tiles, and few classes.)"""
+    print(f"T{T} V{V}", flush=True)
+    d, g = 99, gen(T)
+    bits = torch.tensor(BITS, device="cuda", dtype=torch.float64).repeat(d // 9)
+    W, X = torch.zeros(V, d + 1, device="cuda"), torch.zeros(T, d + 1, device="cuda")
+    W[0, :d] = odd((d,), bits, g) * 2.0 ** -12
+    W[1:, d] = -2.0 ** 40
+    X[:, d] = 1.0
+    at = torch.arange(T, device="cuda") % d
+    X[torch.arange(T, device="cuda"), at] = odd((T,), 24 - bits[at], g) * 2.0 ** -4
+    labels = torch.zeros(T, dtype=torch.int32, device="cuda")
+    loss, lse = torch.empty(T, device="cuda"), torch.empty(T, device="cuda")
+    plan = tf.XentPlan(V, d + 1, F, max_rows=T, gradients=False)
+    plan.loss(X, W, labels, loss, lse, stream())
+    assert not loss.any()
+    assert torch.equal(lse.double(), X[torch.arange(T, device="cuda"), at].double() * W[0, at].double())
+    torch.cuda.synchronize()
+
+
+@pytest.mark.parametrize("T,n", [(193, 63), (500, 1008), (2500, 63), (2000, 1998)])
+def test_products_of_fp32_parts_are_whole_gradients(T, n):
+    """Rows that are certain of a class that is not theirs: g is dloss there, minus that at the label, and each of dX and dW one product of 24 bits."""
+    print(f"T{T} n{n}", flush=True)
+    more, g = 40, gen(T)
+    rows = torch.arange(T, device="cuda")
+    o = rows % n
+    bits = torch.tensor(BITS, device="cuda", dtype=torch.float64).repeat(n // 9)
+    dloss = odd((T,), 24 - bits[o], g)
+    dloss[0] = 2.0 ** 23          # (row 0's: a power of two, by which the others are divided)
+    V = n + 1
+    labels = torch.full((T,), n, dtype=torch.int32, device="cuda")
+
+    def operands(d):
+        """Logits of -1024 but for each row's own class, whose is 0; columns n + 1 .. d - 1 are free."""
+        W, X = torch.zeros(V, d, device="cuda"), torch.zeros(T, d, device="cuda")
+        X[:, 0] = 1.0
+        W[:, 0] = -1024.0
+        X[rows, 1 + o] = 1.0
+        W[torch.arange(n), 1 + torch.arange(n)] = 1024.0
+        return X, W
+
+    lse = torch.zeros(T, device="cuda")
+    X, W = operands(n + 1 + more)
+    W[:n, n + 1:] = odd((n, more), bits[:, None], g)
+    dX, dW = torch.full_like(X, math.nan), torch.full_like(W, math.nan)
+    tf.XentPlan(V, X.shape[1], F, max_rows=T).grad(X, W, labels, lse, dloss, dX, dW, stream())
+    want = dloss.double()[:, None] * W[o, n + 1:].double()
+    assert torch.equal(dX[:, n + 1:].double(), want)
+    assert not dW[:, n + 1:].any()
+    # one row in each of the free columns
+    X, W = operands(n + 1 + T)
+    X[rows, n + 1 + rows] = odd((T,), bits[o], g)
+    dW = torch.full_like(W, math.nan)
+    tf.XentPlan(V, X.shape[1], F, max_rows=T).grad(X, W, labels, lse, dloss, None, dW, stream())
+    want = torch.zeros(V, T, device="cuda", dtype=torch.float64)
+    want[o, rows] = dloss.double() * X[rows, n + 1 + rows].double()
+    want[n] = -want[:n].sum(0)
+    assert torch.equal(dW[:, n + 1:].double(), want)
+    torch.cuda.synchronize()
