@@ -433,7 +433,8 @@ tf_status tf_moe_layer_q4(const tf_moe *plan, const tf_csr *A, const void *X, in
  * which is 1 where experts are met evenly.  All are 0 where n is.  A is a matrix as tf_moe_route makes it: the same number of entries in
  * each row (at most 64, for at most 1024 columns), columns that are not an expert's (-1) are passed over; rowptr and vals are not read.
  * counts (n_cols + 1), mass, loss and the workspace (16-byte aligned) are device arrays; the workspace has the size that tf_moe_balance_size
- * tells (at most 4 MiB) and may be used by one call at a time.  A score of +inf makes the shares of its row, and so mass and loss, NaN. */
+ * tells (at most 4 MiB) and may be used by one call at a time.  With softmax scorings a score of +inf makes the shares of
+ * its row, and so mass and loss, NaN (if the row has an entry); with sigmoid scorings its sigma is 1. */
 tf_status tf_moe_balance_size(int64_t n_tokens, int64_t n_experts, int64_t *bytes);
 tf_status tf_moe_balance(const void *scores, int64_t ld, int32_t dtype, int32_t scoring, const tf_csr *A, int32_t *counts, float *mass,
                          float *loss, void *workspace, void *hip_stream);

@@ -303,3 +303,47 @@ def test_products_of_fp32_parts_are_whole_gradients(T, n):
     want[n] = -want[:n].sum(0)
     assert torch.equal(dW[:, n + 1:].double(), want)
     torch.cuda.synchronize()
+
+
+@pytest.mark.parametrize("scoring", range(4))
+def test_the_router_makes_the_weights_whose_gradient_is_taken(scoring):
+    """tf_moe_route's values against the weights that test_router_gradient_against_differences differentiates, with the same scale."""
+    T, E, k = 40, 24, 3
+    scores = 2 * torch.randn(T, E, device="cuda", generator=gen(scoring))
+    A = matrix(T, E, k, torch.empty(T * k, dtype=torch.int32, device="cuda"))
+    tf.tf_moe_route(scores, A, scoring, scale=1.5, stream=stream())
+    z = torch.sigmoid(scores.double()) if scoring >= lu.SIGMOID else torch.exp(scores.double())
+    chosen = torch.gather(z, 1, A.colidx.long().reshape(T, k))
+    want = 1.5 * chosen / {0: z.sum(1, keepdim=True), 1: chosen.sum(1, keepdim=True), 2: 1.0, 3: chosen.sum(1, keepdim=True)}[scoring]
+    # shares as loss_util bounds them: 40 and the difference under the exponential, below 16 here, in steps of 2^-23
+    assert (A.vals.double().reshape(T, k) / want - 1).abs().max().item() <= 56 * 2.0 ** -23
+
+
+@pytest.mark.parametrize("scoring", range(4))
+@pytest.mark.parametrize("T", [30, 5000])
+def test_a_score_of_infinity(T, scoring):
+    """Softmax scorings: its row's shares, and so mass and loss, are NaN.  Sigmoid scorings: sigma is 1, and all stays as it is defined.  Gradients of
+    the other rows are not touched."""
+    E, k = 16, 2
+    scores = 2 * torch.randn(T, E, device="cuda", generator=gen(scoring))
+    scores[7, 3] = math.inf
+    c = scores.topk(k, 1).indices.to(torch.int32).reshape(-1).contiguous()
+    A = matrix(T, E, k, c)
+    counts = torch.empty(E + 1, dtype=torch.int32, device="cuda")
+    mass, loss = torch.empty(E, device="cuda"), torch.empty(1, device="cuda")
+    work = torch.empty(tf.tf_moe_balance_size(T, E), dtype=torch.uint8, device="cuda")
+    tf.tf_moe_balance(scores, A, counts, mass, loss, work, scoring, stream())
+    if scoring < lu.SIGMOID:
+        assert torch.isnan(mass).all() and torch.isnan(loss).all()
+    else:
+        ref = lu.balance(scores.clamp_max(1e30), c, k, scoring)
+        lu.check(mass, ref[1], ref[2])
+        lu.check(loss, ref[3].reshape(1), ref[4].reshape(1))
+    dvals, one = torch.randn(T * k, device="cuda", generator=gen(1)), torch.ones(1, device="cuda")
+    out = torch.empty_like(scores)
+    tf.tf_moe_route_grad(scores, A, out, scoring, 1.0, dvals, counts, one, stream())
+    ref, bound = lu.route_grad(scores.clamp_max(1e30), c, k, scoring, 1.0, dvals, counts, one)
+    rest = torch.arange(T, device="cuda") != 7
+    if scoring >= lu.SIGMOID:
+        rest[7] = True
+    lu.check(out[rest], ref[rest], bound[rest])
