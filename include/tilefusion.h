@@ -468,6 +468,9 @@ typedef struct tf_xent_desc {
 
 typedef struct tf_xent tf_xent; /* opaque, library-owned: the sizes above and a workspace */
 
+/* Bytes of the workspace that tf_xent_create allocates: a copy of X's rows, at most 2^29 of g (and 256 classes of it at least), 2^28 of W where its rows
+ * have to be copied, sums of shares of long contractions. */
+tf_status tf_xent_size(const tf_xent_desc *desc, int64_t *bytes);
 /* Allocates the workspace on the current device.  On failure *out is NULL. */
 tf_status tf_xent_create(const tf_xent_desc *desc, tf_xent **out);
 /* Frees it.  NULL is accepted. */

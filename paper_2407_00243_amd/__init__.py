@@ -15,6 +15,6 @@ from .binding import (  # noqa: F401
     TF_ACT_IDENTITY, TF_ACT_RELU, TF_ACT_SILU, TF_ACT_GELU, Q4Matrix, MoePlan,
     tf_q4_sizes, tf_q4_pack, tf_q4_quantize, tf_q4_unpack, tf_q4_matvec, tf_moe_route, tf_moe_create,
     tf_moe_destroy, tf_moe_layer, tf_moe_layer_q4,
-    tf_moe_balance_size, tf_moe_balance, tf_moe_route_grad, XentPlan, tf_xent_create, tf_xent_destroy, tf_xent_device,
+    tf_moe_balance_size, tf_moe_balance, tf_moe_route_grad, XentPlan, tf_xent_size, tf_xent_create, tf_xent_destroy, tf_xent_device,
     tf_xent_loss, tf_xent_grad, tf_xent_grad_by_loss,
 )

@@ -109,7 +109,7 @@ EXPORTS = ["tf_plan_create", "tf_plan_destroy", "tf_plan_schedule", "tf_plan_wor
            "tf_unfused_spmm_spmm", "tf_run_wavefront", "tf_plan_prepare_unfused", "tf_plan_workspace_unfused",
            "tf_csr_validate", "tf_q4_sizes", "tf_q4_pack", "tf_q4_quantize", "tf_q4_unpack", "tf_q4_matvec",
            "tf_moe_route", "tf_moe_create", "tf_moe_destroy", "tf_moe_layer", "tf_moe_layer_q4",
-           "tf_moe_balance_size", "tf_moe_balance", "tf_moe_route_grad", "tf_xent_create", "tf_xent_destroy",
+           "tf_moe_balance_size", "tf_moe_balance", "tf_moe_route_grad", "tf_xent_size", "tf_xent_create", "tf_xent_destroy",
            "tf_xent_device", "tf_xent_loss", "tf_xent_grad", "tf_xent_grad_by_loss",
            "tf_last_error", "tf_version"]
 _INT_RETURNS = [e for e in EXPORTS if e not in ("tf_last_error", "tf_version")]
@@ -158,6 +158,7 @@ def load_library():
     lib.tf_moe_balance_size.argtypes = [i64, i64, ctypes.POINTER(i64)]
     lib.tf_moe_balance.argtypes = [vp, i64, i32, i32, csr, vp, vp, vp, vp, vp]
     lib.tf_moe_route_grad.argtypes = [vp, i64, i32, i32, ctypes.c_float, csr, vp, vp, vp, vp, i64, vp]
+    lib.tf_xent_size.argtypes = [ctypes.POINTER(tf_xent_desc), ctypes.POINTER(i64)]
     lib.tf_xent_create.argtypes = [ctypes.POINTER(tf_xent_desc), ctypes.POINTER(vp)]
     lib.tf_xent_destroy.argtypes = [vp]
     lib.tf_xent_device.argtypes = [vp, ctypes.POINTER(i32)]
@@ -670,6 +671,13 @@ def tf_moe_route_grad(scores, A: DeviceCsr, dscores, scoring: int = TF_ROUTE_SOF
         None if dloss is None else _vector(dloss, "dloss", 1, "torch.float32", device), dscores.data_ptr(), ldd, stream)
     if status:
         _check(status)
+
+
+def tf_xent_size(n_classes: int, n_in: int, dtype, max_rows: int, gradients: bool = True) -> int:
+    """Bytes of device memory that a plan for these sizes holds."""
+    d, out = tf_xent_desc(n_classes, n_in, max_rows, _routed_code(dtype), 1 if gradients else 0), ctypes.c_int64()
+    _check(load_library().tf_xent_size(ctypes.byref(d), ctypes.byref(out)))
+    return out.value
 
 
 def tf_xent_create(n_classes: int, n_in: int, dtype, max_rows: int, gradients: bool = True) -> int:

@@ -53,7 +53,8 @@ struct XentSpace {
     void *x, *w, *G;              // operands: rows that count, a copy of W where there has to be one, gradient of the logits; planes of 16-bit
                                   // numbers, or (native) fp32.  fp16 has two planes of G: see kRowUnit
     float *dx, *dw;               // sums in 32 bits, one slab for each share of a contraction
-    int64_t ld;                   // row length of x and w: n_in rounded up to 256, and kRowPad
+    int64_t ld;                   // row length of x and w: n_in rounded up to 64, and kRowPad
+    int64_t slab_ld;              // of dx and dw: rounded up to 256
     int64_t x_plane;              // elements
     int64_t part_cap, g_cap, w_cap, dx_cap, dw_cap;     // elements that there is room for (of a plane)
 };
@@ -65,6 +66,11 @@ constexpr int kJoinApart = 32;             // their counters: a line of memory e
 constexpr float kRowUnit = 1.0f / 32768.0f;
 // Elements between the rows of x, w and G: rows a power of two apart would all lie in one channel of an XCD's L2.
 constexpr int64_t kRowPad = 64;
+// Up to so many rows (of the loss, of its gradients) fp32 numbers are multiplied as they are, and rows of W that begin anywhere go through registers:
+// W is not copied.  (Measured where the rules are: tf_xent.hip.)
+constexpr int64_t kNativeRows[2] = {448, 192}, kRegisterRows[2] = {1023, 64};
+// 256 rows of G stay below 2^32 bytes, as the products' loads count them.  (A plan for very many rows has room for more columns of few.)
+constexpr int64_t kMostColumnsOfG = (int64_t)1 << 22;
 
 struct XentLaunch {
     XentSpace s;

@@ -75,22 +75,37 @@ struct Cut {
     }
 };
 
-// Sizes of the workspace: G (the gradient of the logits) and a copy of W are held for as many classes at a time as 2^28 numbers allow (256 at
-// least), partial sums for as many as leave 2^25 of them, slabs of the shares of dX up to 2^26 numbers, or what one share needs, of dW 2^25.  fp32 numbers
-// take three planes of 16 bits, in which they also lie as they are; G in fp16 has two.
+// Sizes of the workspace.  G (the gradient of the logits) is held for as many classes at a time as 2^29 bytes allow (256 at least), a copy of W for as many
+// as 2^28 do, partial sums for as many as leave 2^25 of them, slabs of the shares of dX up to 2^26 numbers, or what one share needs, of dW 2^25; and
+// nothing of it for which the plan's sizes leave no use.  fp32 numbers take three planes of 16 bits, in which they also lie as they are; G in fp16 has two.
 int64_t lay_out(tf_xent &p, char *base) {
     const tf_xent_desc &d = p.d;
     tf::XentSpace &s = p.s;
+    const bool f32 = d.dtype == TF_F32;
     const int64_t rows = round_up(d.max_rows, 256), classes = round_up(d.n_classes, 256);
-    const int64_t planes = d.dtype == TF_F32 ? 3 : 1, g_planes = d.dtype == TF_F16 ? 2 : planes;
-    s.ld = round_up(d.n_in, 256) + tf::kRowPad;
+    const int64_t planes = f32 ? 3 : 1, g_planes = d.dtype == TF_F16 ? 2 : planes;
+    s.ld = round_up(d.n_in, 64) + tf::kRowPad;
+    s.slab_ld = round_up(d.n_in, 256) + tf::kRowPad;
     s.x_plane = rows * s.ld;
     s.part_cap = std::max(std::min(classes / 64 * rows, (int64_t)1 << 25), 4 * rows);
     const auto piece = [&](int64_t row, int64_t most) { return std::max<int64_t>(256, std::min(classes, most / row / 256 * 256)); };
-    s.w_cap = piece(s.ld, (int64_t)1 << 28) * s.ld;
-    s.g_cap = d.gradients ? (piece(rows, ((int64_t)1 << 28) / (d.dtype == TF_F16 ? 2 : 1)) + tf::kRowPad) * rows : 0;
-    s.dx_cap = d.gradients ? std::max({rows * s.ld, std::min((int64_t)1 << 26, 4 * rows * s.ld), std::min((int64_t)1 << 24, 512 * 64 * s.ld)}) : 0;
-    s.dw_cap = d.gradients ? (int64_t)1 << 25 : 0;
+    // W is copied by calls of more rows than kNativeRows or kRegisterRows only; 16-bit rows of whole pieces of 16 bytes only where they do not begin at
+    // such pieces, for which a small piece at a time will do.
+    const int64_t least_rows = (f32 ? tf::kNativeRows : tf::kRegisterRows)[d.gradients], w_most = f32 || d.n_in % 8 ? ((int64_t)1 << 27) / planes : (int64_t)1 << 24;
+    const int64_t w_piece = piece(s.ld, w_most), g_piece = piece(rows, ((int64_t)1 << 28) / g_planes);
+    s.w_cap = d.max_rows > least_rows ? w_piece * s.ld : 0;
+    s.g_cap = d.gradients ? (g_piece + tf::kRowPad) * rows : 0;
+    // shares that contractions over so many classes or rows can be cut into
+    const auto most_shares = [&](int64_t k) {
+        const int whole = tf::shares_of(1 << 30, (int)ceil_div(k, 64), (int)planes);
+        return (int64_t)(f32 ? std::max(whole, tf::shares_of(1 << 30, (int)ceil_div(k, 32), 1)) : whole);
+    };
+    const int64_t dx_shares = most_shares(d.n_classes), dw_shares = most_shares(d.max_rows), dx_size = rows * s.slab_ld;
+    const bool one_piece = g_piece >= classes && classes <= tf::kMostColumnsOfG && (s.w_cap == 0 || w_piece >= classes);
+    s.dx_cap = !d.gradients || (one_piece && dx_shares == 1)
+                   ? 0
+                   : std::min(dx_shares * dx_size, std::max({dx_size, std::min((int64_t)1 << 26, 4 * dx_size), std::min((int64_t)1 << 24, 512 * 64 * s.slab_ld)}));
+    s.dw_cap = !d.gradients || dw_shares == 1 ? 0 : std::min((int64_t)1 << 25, dw_shares * classes * s.slab_ld);
     Cut c{base};
     c.take(s.list, d.max_rows);
     c.take(s.pos, d.max_rows);
@@ -119,6 +134,15 @@ int64_t lay_out(tf_xent &p, char *base) {
     return c.bytes;
 }
 
+tf_status check_desc(const tf_xent_desc *desc) {
+    if (!desc) return report(TF_EINVAL, "null argument");
+    if (desc->n_classes < 1 || desc->n_in < 1 || desc->max_rows < 1) return report(TF_EINVAL, "sizes must be positive");
+    if (!loss_dtype(desc->dtype)) return report(TF_EUNSUPPORTED, "element type must be fp32, bf16 or fp16");
+    if (desc->gradients != 0 && desc->gradients != 1) return report(TF_EINVAL, "gradients must be 0 or 1");
+    if (desc->n_in > tf::kXentMaxColumns) return report(TF_EUNSUPPORTED, "weights have rows of at most 2^22 columns");
+    if (desc->n_classes > tf::kXentMaxClasses || desc->max_rows > tf::kXentMaxRows) return report(TF_EUNSUPPORTED, "a size is too large");
+    return TF_OK;
+}
 tf_status check_xent(const tf_xent *p, const void *X, int64_t ldx, const void *W, int64_t ldw, const int32_t *labels, int64_t n_rows) {
     if (!p || !W) return report(TF_EINVAL, "null argument");
     if (n_rows < 0) return report(TF_EINVAL, "number of rows");
@@ -200,15 +224,21 @@ tf_status tf_moe_route_grad(const void *scores, int64_t ld, int32_t dtype, int32
     return e ? report_hip(e, "launching the router's gradient") : TF_OK;
 }
 
+tf_status tf_xent_size(const tf_xent_desc *desc, int64_t *bytes) {
+    if (!bytes) return report(TF_EINVAL, "null argument");
+    const tf_status st = check_desc(desc);
+    if (st != TF_OK) return st;
+    tf_xent p;
+    p.d = *desc;
+    *bytes = lay_out(p, nullptr);
+    return TF_OK;
+}
+
 tf_status tf_xent_create(const tf_xent_desc *desc, tf_xent **out) {
     if (!out) return report(TF_EINVAL, "null argument");
     *out = nullptr;
-    if (!desc) return report(TF_EINVAL, "null argument");
-    if (desc->n_classes < 1 || desc->n_in < 1 || desc->max_rows < 1) return report(TF_EINVAL, "sizes must be positive");
-    if (!loss_dtype(desc->dtype)) return report(TF_EUNSUPPORTED, "element type must be fp32, bf16 or fp16");
-    if (desc->gradients != 0 && desc->gradients != 1) return report(TF_EINVAL, "gradients must be 0 or 1");
-    if (desc->n_in > tf::kXentMaxColumns) return report(TF_EUNSUPPORTED, "weights have rows of at most 2^22 columns");
-    if (desc->n_classes > tf::kXentMaxClasses || desc->max_rows > tf::kXentMaxRows) return report(TF_EUNSUPPORTED, "a size is too large");
+    const tf_status st = check_desc(desc);
+    if (st != TF_OK) return st;
     tf_xent *p = new (std::nothrow) tf_xent;
     if (!p) return report(TF_ENOMEM, "out of host memory");
     p->d = *desc;

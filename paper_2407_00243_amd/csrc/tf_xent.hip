@@ -339,7 +339,7 @@ template <int EL> __global__ __launch_bounds__(256) void k_finish_rows(const Xen
         const bool is = t < a.n_rows;
         const int64_t i = is ? a.s.pos[t] : -1;
         const float unit = EL == TF_F16 && i >= 0 ? a.s.dloss[i] * kRowUnit : all;
-        finish_row<EL>(a.s.dx + i * a.s.ld, size, splits, static_cast<typename El<EL>::T *>(a.dX) + t * a.lddx, a.n_in, i < 0, unit, per_row, by_slab, is);
+        finish_row<EL>(a.s.dx + i * a.s.slab_ld, size, splits, static_cast<typename El<EL>::T *>(a.dX) + t * a.lddx, a.n_in, i < 0, unit, per_row, by_slab, is);
     }
 }
 // Rows first .. first + count of dW.
@@ -351,7 +351,7 @@ template <int EL> __global__ __launch_bounds__(256) void k_finish_classes(const 
     const int at_once = by_slab ? 1 : 256 / per_row;
     for (int64_t i0 = (int64_t)blockIdx.x * at_once; i0 < count; i0 += (int64_t)gridDim.x * at_once) {
         const int64_t i = i0 + (by_slab ? 0 : threadIdx.x / per_row);
-        finish_row<EL>(a.s.dw + i * a.s.ld, size, splits, static_cast<typename El<EL>::T *>(a.dW) + (first + i) * a.lddw, a.n_in, false, unit, per_row, by_slab,
+        finish_row<EL>(a.s.dw + i * a.s.slab_ld, size, splits, static_cast<typename El<EL>::T *>(a.dW) + (first + i) * a.lddw, a.n_in, false, unit, per_row, by_slab,
                        i < count);
     }
 }
@@ -460,7 +460,7 @@ int launch_product(const ProductLaunch &p, const XentLaunch &a, void *stream) {
 // Few fp32 rows are multiplied by the fp32 instructions, W where it lies: as parts its numbers would be written and read again several times.
 // 4096 -> 100000 classes, fp32 instructions / parts, us: loss of 1 row 320 / 1666, 128 948 / 1976, 600 3706 / 4077, 1024 5766 / 5153; gradients
 // of 128 2757 / 3801, 300 6560 / 6357.
-bool is_native(const XentLaunch &a) { return a.dtype == TF_F32 && a.n_rows <= (a.loss ? 448 : 192); }
+bool is_native(const XentLaunch &a) { return a.dtype == TF_F32 && a.n_rows <= kNativeRows[a.loss ? 0 : 1]; }
 
 // Whether W's rows are whole 16-byte pieces, as the products load them.
 bool whole_pieces(const XentLaunch &a) {
@@ -470,7 +470,7 @@ bool whole_pieces(const XentLaunch &a) {
 // Otherwise they go through registers while there are few rows, and are copied first where the products take long enough to pay for that.
 // 1023 -> 40000 classes, bf16, through registers / copied, us: loss of 64 rows 37 / 60, 300 64 / 78, 1024 135 / 133; gradients of 64 126 / 140, 300 226 / 201.
 // fp32 numbers that are multiplied in parts are always packed.
-bool through_registers(const XentLaunch &a) { return !whole_pieces(a) && (a.dtype == TF_F32 ? a.native : a.n_rows <= (a.loss ? 1023 : 64)); }
+bool through_registers(const XentLaunch &a) { return !whole_pieces(a) && (a.dtype == TF_F32 ? a.native : a.n_rows <= kRegisterRows[a.loss ? 0 : 1]); }
 bool in_place(const XentLaunch &a) { return a.dtype == TF_F32 ? a.native : whole_pieces(a) || through_registers(a); }
 
 // Numbers and copies the rows that count.  (Also without rows: it sets the unit.)  Up to 8192 rows every block counts the rows before it.  Packs the
@@ -564,9 +564,6 @@ template <int EL> void launch_few_rows(const XentLaunch &a, int64_t first, int64
     else hipLaunchKernelGGL((k_few_rows<EL, 2>), grid, dim3(256), 0, st, a, first, count, g_ld, each);
 }
 
-// 256 rows of G stay below 2^32 bytes, as the products' loads count them.  (A plan for very many rows has room for more columns of few.)
-constexpr int64_t kMostColumnsOfG = (int64_t)1 << 22;
-
 // Whether the last workgroup of a block of rows adds up its `sums` sums: the workgroups count themselves in one after the other, 20 ns each.
 // (65536 classes of one row, 1024 workgroups: 125 us, by another launch 99 + 7.)
 bool joins(int64_t m_tiles, int64_t n_tiles, int64_t sums) { return m_tiles == 1 || (m_tiles <= 1024 && n_tiles <= kMostJoins && sums <= 8192); }
@@ -618,7 +615,7 @@ int launch_xent_grad(const XentLaunch &call, void *stream) {
     if (!in_place(a)) piece = std::min(piece, a.s.w_cap / a.s.ld);
     const int64_t g_ld = piece + kRowPad;
     const int parts = parts_of(a), pairs = parts == 3 ? 6 : 1, step = step_of(a);
-    const int64_t dx_size = rows * a.s.ld;
+    const int64_t dx_size = rows * a.s.slab_ld;
     // (the same shares for every piece: the slabs are added to)
     const Cut dx = cut_product(a.n_in, a.n_rows, ceil_div(std::min<int64_t>(piece, a.n_classes), step), pairs, a.native, true, true, a.s.dx_cap / dx_size);
     a.direct_dx = piece >= a.n_classes && dx.shares == 1;
@@ -662,7 +659,7 @@ int launch_xent_grad(const XentLaunch &call, void *stream) {
                 q.tile = dx.tile;
                 q.splits = (int32_t)dx.shares;
                 q.slab = a.s.dx;
-                q.slab_ld = a.s.ld;
+                q.slab_ld = a.s.slab_ld;
                 q.slab_size = dx_size;
                 q.add = first != 0;
                 e = launch_product(q, a, stream);
@@ -683,7 +680,7 @@ int launch_xent_grad(const XentLaunch &call, void *stream) {
             q.k_rows = 1;
             q.m_count = a.n_in;
             q.n_count = (int32_t)count;
-            const int64_t size = round_up(count, 256) * a.s.ld;
+            const int64_t size = round_up(count, 256) * a.s.slab_ld;
             const Cut dw = cut_product(a.n_in, count, ceil_div(a.n_rows, step), pairs, a.native, false, false, a.s.dw_cap / size);
             q.tile = dw.tile;
             q.splits = (int32_t)dw.shares;
@@ -692,7 +689,7 @@ int launch_xent_grad(const XentLaunch &call, void *stream) {
             q.ldo = a.lddw;
             q.out_dtype = a.dtype;
             q.slab = a.s.dw;
-            q.slab_ld = a.s.ld;
+            q.slab_ld = a.s.slab_ld;
             q.slab_size = size;
             q.end = q.splits > 1 ? kEndSlab : kEndOut;
             e = launch_product(q, a, stream);

@@ -347,3 +347,53 @@ def test_a_score_of_infinity(T, scoring):
     if scoring >= lu.SIGMOID:
         rest[7] = True
     lu.check(out[rest], ref[rest], bound[rest])
+
+
+# ------------------------------------------------------------------------------------------- plans
+
+def check_plan(plan, T, V, d, dtype, grads="XW", ldw=0, what=""):
+    """W's rows are ldw further apart than they are wide, with NaN in between."""
+    g = gen(T + V)
+    W = torch.full((V, d + ldw), math.nan, device="cuda", dtype=dtype)[:, :d]
+    W.copy_(3 / math.sqrt(d) * torch.randn(V, d, device="cuda", generator=g))
+    labels = torch.randint(0, V, (T,), device="cuda", generator=g).to(torch.int32)
+    X = (torch.randn(T, d, device="cuda", generator=g) + W[labels.long()].float()).to(dtype)
+    dloss = torch.randn(T, device="cuda", generator=g) / T
+    loss, lse = torch.full((T,), math.nan, device="cuda"), torch.full((T,), math.nan, device="cuda")
+    plan.loss(X, W, labels, loss, lse, stream())
+    got = {"loss": loss, "lse": lse}
+    if grads:
+        got["dX"], got["dW"] = torch.full_like(X, math.nan), torch.full((V, d), math.nan, device="cuda", dtype=dtype)
+        plan.grad(X, W, labels, lse, dloss, got["dX"], got["dW"], stream(), loss=loss)
+    ref = lu.xent(X, W, labels, dloss)
+    for name, x in got.items():
+        lu.check(x, *ref[name], x.dtype, f"{what} {name}")
+    torch.cuda.synchronize()
+
+
+@pytest.mark.parametrize("T,V,d,dtype,ldw", [(1100, 33000, 1000, BF, 3), (70, 33000, 1000, HF, 1), (500, 11100, 4000, F, 0), (200, 11100, 4000, F, 1)])
+def test_copies_of_W_in_pieces(T, V, d, dtype, ldw):
+    """More classes than a plan holds a copy of: 16-bit rows of whole pieces that begin anywhere, fp32 rows."""
+    print(f"T{T} V{V} d{d} {dtype}", flush=True)
+    check_plan(tf.XentPlan(V, d, dtype, max_rows=T), T, V, d, dtype, ldw=ldw)
+
+
+@pytest.mark.parametrize("T,dtype,gradients", [(1023, BF, False), (1024, BF, False), (64, HF, True), (65, HF, True), (448, F, False), (449, F, False), (192, F, True),
+                                               (193, F, True)])
+def test_plans_that_never_copy_W(T, dtype, gradients):
+    """The largest numbers of rows whose plans have no room for a copy, and the smallest that do; rows of W that begin anywhere and that do not."""
+    print(f"T{T} {dtype} {gradients}", flush=True)
+    for V, d, ldw in ((700, 64, 0), (700, 64, 1), (700, 65, 0), (5000, 33, 6)):
+        plan = tf.XentPlan(V, d, dtype, max_rows=T, gradients=gradients)
+        for rows in (T, 7):
+            check_plan(plan, rows, V, d, dtype, "XW" if gradients else "", ldw, f"V{V} d{d} {ldw} rows {rows}")
+
+
+@pytest.mark.parametrize("dtype", [BF, HF, F])
+@pytest.mark.parametrize("T,V,d", [(300, 64, 40), (300, 64, 500), (20, 300, 2000), (3000, 30, 100), (5000, 4000, 70), (90, 9000, 257)])
+def test_plans_of_exactly_their_rows(T, V, d, dtype):
+    """Slabs are as many as the sizes can be cut into: few and many classes, rows and columns, and fewer rows than the plan's."""
+    print(f"T{T} V{V} d{d} {dtype}", flush=True)
+    plan = tf.XentPlan(V, d, dtype, max_rows=T)
+    for rows in (T, 1, max(1, T // 3)):
+        check_plan(plan, rows, V, d, dtype, what=f"rows {rows}")
