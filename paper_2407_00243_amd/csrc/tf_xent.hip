@@ -457,9 +457,10 @@ int launch_product(const ProductLaunch &p, const XentLaunch &a, void *stream) {
     return a.dtype == TF_F16 ? launch_product_f16(p, stream) : a.native ? launch_product_f32(p, stream) : launch_product_bf16(p, stream);
 }
 
-// Few fp32 rows are multiplied by the fp32 instructions, W where it lies: as parts its numbers would be written and read again several times.
-// 4096 -> 100000 classes, fp32 instructions / parts, us: loss of 1 row 320 / 1666, 128 948 / 1976, 600 3706 / 4077, 1024 5766 / 5153; gradients
-// of 128 2757 / 3801, 300 6560 / 6357.
+// Few fp32 rows are multiplied by the fp32 instructions, W where it lies: as parts its numbers would be written and read again several times.  How many are
+// few depends on the sizes; up to kNativeRows the instructions are ahead at all that were tried but 192 rows of 47 classes.  fp32 instructions / parts, us,
+// loss of 448, 600, 1024 rows: 4096 -> 100000 2675 / 3563, 3729 / 3862, 5862 / 6232; 2048 -> 20000 326 / 394, 451 / 362, 600 / 554; 1000 -> 5000
+// 60 / 73, 78 / 76, 111 / 89.  Gradients of 192, 256, 448 rows: 3709 / 4749, 4784 / 5831, 8391 / 8286; 404 / 482, 534 / 517, 913 / 870; 86 / 89, 108 / 97, 163 / 150.
 bool is_native(const XentLaunch &a) { return a.dtype == TF_F32 && a.n_rows <= kNativeRows[a.loss ? 0 : 1]; }
 
 // Whether W's rows are whole 16-byte pieces, as the products load them.
