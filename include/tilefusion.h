@@ -421,7 +421,8 @@ tf_status tf_moe_layer_q4(const tf_moe *plan, const tf_csr *A, const void *X, in
                           const tf_q4 *W2, void *D, int64_t ldd, void *hip_stream);
 
 /* ------------------------------------------------------------------------------------------------
- * Losses and their gradients: what trains a routed network or a classifier (of a graph's nodes, of tokens).
+ * Losses and their gradients: what trains a router and a classifier (of a graph's nodes, of tokens).  The mixture-of-experts layer has no gradient of its
+ * own here: that of A's values (dvals below) is the caller's to make.
  * The conventions of the routed operators hold: fp32, bf16 and fp16, 32-bit sums rounded once, rows that may be further apart
  * than they are wide, calls that allocate nothing and may be captured.
  */

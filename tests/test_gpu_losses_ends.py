@@ -397,3 +397,33 @@ def test_plans_of_exactly_their_rows(T, V, d, dtype):
     plan = tf.XentPlan(V, d, dtype, max_rows=T)
     for rows in (T, 1, max(1, T // 3)):
         check_plan(plan, rows, V, d, dtype, what=f"rows {rows}")
+
+
+@pytest.mark.parametrize("dtype", [BF, HF, F])
+def test_pieces_of_classes_by_the_loss(dtype):
+    """So many rows that three pieces of the classes are taken one after the other, their labels in each of them."""
+    check_plan(tf.XentPlan(700, 8, dtype, max_rows=600000), 600000, 700, 8, dtype)
+
+
+@pytest.mark.parametrize("T", [40, 300])
+def test_an_fp16_row_of_nan_or_infinity_stays_a_row(T):
+    """In X and in dloss; and gradients that are all zero, or all too small for the type."""
+    V, d = 400, 64
+    g = gen(T)
+    X, W = torch.randn(T, d, device="cuda", generator=g).to(HF), (torch.randn(V, d, device="cuda", generator=g) / 4).to(HF)
+    labels = torch.randint(0, V, (T,), device="cuda", generator=g).to(torch.int32)
+    dloss = torch.rand(T, device="cuda", generator=g) + 0.5
+    want = grad_bounds(X, W, labels, dloss)[0]
+    plan = tf.XentPlan(V, d, HF, max_rows=T)
+    bad = X.clone()
+    bad[11, 5], bad[12, 6] = math.nan, math.inf
+    spoilt = dloss.clone()
+    spoilt[13], spoilt[14] = math.nan, -math.inf
+    _, _, dX, _ = run_xent(plan, bad, W, labels, spoilt)
+    rest = torch.ones(T, dtype=torch.bool, device="cuda")
+    rest[11:15] = False
+    lu.check(dX[rest], want[0][rest], want[1][rest], HF)
+    assert not torch.isfinite(dX[11:15].float()).any()
+    for by in (0.0, 1e-30):
+        _, _, dX, dW = run_xent(plan, X, W, labels, dloss * by)
+        assert not dX.any() and not dW.any()
