@@ -427,3 +427,34 @@ def test_an_fp16_row_of_nan_or_infinity_stays_a_row(T):
     for by in (0.0, 1e-30):
         _, _, dX, dW = run_xent(plan, X, W, labels, dloss * by)
         assert not dX.any() and not dW.any()
+
+
+@pytest.mark.parametrize("T,dtype,d", [(3, BF, 4096), (40, HF, 4096), (70, BF, 4097), (300, BF, 4096), (70, F, 2048), (500, F, 2048)])
+def test_W_of_more_than_2_to_the_32_bytes(T, dtype, d):
+    """Rows that are certain of a class near W's beginning, middle or end, which is not theirs: loss, dX and dW are single numbers."""
+    print(f"T{T} {dtype} d{d}", flush=True)
+    V = 540000
+    g = gen(T)
+    W, X = torch.zeros(V, d, device="cuda", dtype=dtype), torch.zeros(T, d, device="cuda", dtype=dtype)
+    assert W.numel() * W.element_size() > 2 ** 32
+    W[:, 0], X[:, 0] = -1024.0, 1.0
+    at = torch.tensor([1, V // 2, V - 2], device="cuda")
+    rows = torch.arange(T, device="cuda")
+    o = at[rows % 3]
+    W[at, torch.tensor([1, 2, 3], device="cuda")] = 1024.0
+    X[rows, 1 + rows % 3] = 1.0
+    W[at, 10:] = torch.randn(3, d - 10, device="cuda", generator=g).to(dtype)
+    labels = torch.full((T,), V - 1, device="cuda", dtype=torch.int32)
+    dloss = 2.0 ** -(rows % 5).float()
+    loss, lse, dX, dW = run_xent(tf.XentPlan(V, d, dtype, max_rows=T), X, W, labels, dloss, given=True)
+    assert (loss == 1024).all() and not lse.any()
+    # (column 0 is -1024 in both classes of a row)
+    want = dloss[:, None] * W[o].float()
+    want[:, 0] = 0.0
+    assert torch.equal(dX, want.to(dtype))        # (one product, rounded to the type: W's small numbers over 16 are below the normal ones of fp16)
+    sums = torch.zeros(V, 4, device="cuda", dtype=torch.float64)
+    for j in range(3):
+        sums[at[j], 0] = sums[at[j], 1 + j] = dloss[rows % 3 == j].double().sum()
+    sums[V - 1] = -sums[at].sum(0)
+    assert torch.equal(dW[:, :4].double(), sums.to(dtype).double()) and not dW[:, 4:].any()
+    torch.cuda.synchronize()
