@@ -237,7 +237,7 @@ __device__ void write_balance(const RouterLaunch &a, double m, int c, int rows) 
     }
 }
 
-// Adds up the sums of `groups` workgroups in a fixed order: 1024 threads, each four experts and every (1024 / (experts / 4))-th workgroup.  256 of 256 experts: 8 us,
+// Adds up the sums of `groups` workgroups in a fixed order: 1024 threads, each four experts and every (1024 / (experts / 4))-th workgroup.  256 of 256 experts: 9 us,
 // a launch and three trips to memory.  (A last workgroup of the launch before would need a counter that somebody clears, and the workspace is the caller's.)
 __global__ __launch_bounds__(1024) void k_balance_finish(const RouterLaunch a, const int groups) {
     __shared__ Double4 masses[1024];
@@ -297,10 +297,11 @@ template <typename R, bool GRADIENTS> struct Input {
 };
 
 // mass_e = sum over rows of n_te / sum_j n_tj.  Every wave takes ROWS tokens at a time and adds up their shares in registers; entries are counted in LDS
-// (whole numbers: their order does not matter).  In 32 bits a lane adds up kSteps rows at most, in 64 what
-// those come to; its own sum and a workgroup's are rounded once, so that what mass is off by does not grow with the number of rows.  LDS holds the counts,
-// the lanes' sums in 64 bits (which registers have no room for) and at the end, in their place, a line of sums for each wave.  Two sets of rows are on their way from memory while a third is worked on.  131072 rows of 256 bf16 experts, 8 entries each: 20 us, 3.6 TB/s (the launch after it 8); sigmoids 24.
-// Of 1 Mi rows 135 us, 4.2 TB/s: bound by its instructions, an exponential and about ten others a score.
+// (whole numbers: their order does not matter).  In 32 bits a lane adds up kSteps rows at most, in 64 what those come to; its own sum and a workgroup's
+// are rounded once, so that what mass is off by does not grow with the number of rows.  LDS holds the counts, the lanes' sums in 64 bits (registers have
+// no room for them) and at the end, in their place, a line of sums for each wave.  Two sets of rows are on their way from memory while a third is
+// worked on.  131072 rows of 256 bf16 experts, 8 entries each: 20 us, 3.6 TB/s (the launch after it 9); sigmoids 25.  Of 1 Mi rows 120 to 125 us,
+// 4.6 TB/s: bound by its instructions, an exponential and about ten others a score.
 constexpr int kSteps = 8;
 template <int EL, int L, int NV, bool SIGMOIDS> __global__ __launch_bounds__(1024) void k_balance(const RouterLaunch a) {
     typedef Row<EL, L, NV> R;
@@ -404,7 +405,7 @@ template <int EL, int L, int NV, bool SIGMOIDS> __global__ __launch_bounds__(102
 // The entries of a row meet its scores in LDS: each puts its gradient and a one where its expert's are, and the lanes that hold the scores find
 // them there, or zeros.  (They read them, and f, twice: registers hold two numbers a score and what comes from memory next.)  Where a row names an
 // expert more than once one lane adds its entries up instead.  A wave has no barrier: its instructions of LDS are done in their order.
-// 131072 rows of 256 bf16 experts, 8 entries each, both parts, sigmoid shares: 50 us, 2.8 TB/s; softmax 47.  Bound by its instructions: one or two of a quarter of
+// 131072 rows of 256 bf16 experts, 8 entries each, both parts, sigmoid shares: 50 us, 2.8 TB/s; softmax 48.  Bound by its instructions: one or two of a quarter of
 // the others' rate a score, and about twenty others.
 __device__ __forceinline__ void in_order() { asm volatile("" ::: "memory"); }
 
@@ -634,7 +635,7 @@ template <int EL, int L, int NV> int grad_with(const RouterLaunch &a, hipStream_
 }
 // Sixteen experts a lane (eight for the gradient, which holds more of each, while there are lanes for that), in as few lanes as they need: what goes on
 // between lanes is then shared by as many rows as there can be.
-// Balance with 16 / 8 a lane, us: 131072 rows of 256 bf16 experts 27.5 / 32, 1 Mi rows 138 / 179 (fp32 36 / 34).  Gradient with 8 / 16: 32768 rows
+// Balance with 16 / 8 a lane, us: 131072 rows of 256 bf16 experts 27.6 / 32.1, 1 Mi rows 128 / 176 (fp32, 131072 rows: 36 / 36).  Gradient with 8 / 16: 32768 rows
 // 19.7 / 26.6, 131072 rows 47 / 50, 1 Mi rows 356 / 314 (fp32, 131072 rows: 58 / 58).
 template <int EL, bool GRAD> int router_el(const RouterLaunch &a, hipStream_t st) {
     constexpr int NV = (EL == TF_F32 ? 4 : 2) / (GRAD ? 2 : 1);
