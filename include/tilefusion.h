@@ -455,10 +455,11 @@ tf_status tf_moe_route_grad(const void *scores, int64_t ld, int32_t dtype, int32
  * lse and rows of dX are 0.
  *     lse[t] = log sum_v exp(l_tv)                                 loss[t] = lse[t] - l_t,labels[t]
  *     g_tv   = dloss[t] (exp(l_tv - lse[t]) - [v = labels[t]])     dX = g W      dW = g^T X
- * A loss below 2^-126 may be 0.  The logits are made for a piece of the classes at a time, by both calls; g is held for a piece, rounded to 16 bits (bf16: to bf16; fp16: to
- * fp16, for dX over the row's own dloss, so that rows of every size of it keep their precision, and for dW, a sum over the rows, over the largest
- * |dloss|, both with 2^-40 of it as the smallest number; fp32: in 32 bits for few rows, else as three bf16 numbers, which hold 24
- * bits of X, W and g from 2^-110 on, and of smaller numbers those above 2^-126.  Infinite fp32 numbers may give NaN where they are held so). */
+ * A loss below 2^-126 may be 0. The logits are made for a piece of the classes at a time, by both calls; g is held for a piece, rounded to 16 bits
+ * (bf16: to bf16; fp16: to fp16, for dX over the row's own dloss, so that rows of every size of it keep their precision, and for dW, a sum over the
+ * rows, over the largest |dloss|, both with 2^-40 of it as the smallest number; a caller who needs more bits of it makes a plan for fp32 and converts
+ * the operands; fp32: in 32 bits for few rows, else as three bf16 numbers, which hold 24 bits of X, W and g from 2^-110 on, and of smaller numbers
+ * those above 2^-126. Infinite fp32 numbers may give NaN where they are held so). */
 typedef struct tf_xent_desc {
     int64_t n_classes;    /* rows of W, at most 2^30                                       */
     int64_t n_in;         /* columns of X and W, at most 2^22                              */
