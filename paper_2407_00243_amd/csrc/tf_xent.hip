@@ -186,9 +186,9 @@ template <int EL> __global__ __launch_bounds__(256) void k_pack_rows(const XentL
     n = n_of[0] + n_of[1] + n_of[2] + n_of[3];
     top = fmaxf(fmaxf(top_of[0], top_of[1]), fmaxf(top_of[2], top_of[3]));
     // fp16: gradients are divided by the largest one, so that what dW, their sum, can hold is not lost in 16 bits.  The other types' range is that of the
-    // results: only gradients that are all very small or some very large are divided (of others the sums could pass the largest number though dX and dW do not).
+    // results: only gradients that are all very small, or one as large as the type, are divided (others would pass the range that their sums stay in).
     const float scale = a.dtype == TF_F16 ? 32768.0f : 1.0f;
-    if (top == 0.0f || (a.dtype != TF_F16 && top > 0x1p-64f && top < 0x1p64f)) top = 1.0f;
+    if (top == 0.0f || (a.dtype != TF_F16 && top > 0x1p-64f && top < 0x1p126f)) top = 1.0f;
     if (!a.loss && blockIdx.x == 0 && tid == 0) *a.s.unit = top / scale;       // (without rows there is no dloss)
     const int64_t columns = round_up(a.n_in, 64);
     const int per_row = threads_of_row(columns), at_once = 256 / per_row;

@@ -458,3 +458,18 @@ def test_W_of_more_than_2_to_the_32_bytes(T, dtype, d):
     sums[V - 1] = -sums[at].sum(0)
     assert torch.equal(dW[:, :4].double(), sums.to(dtype).double()) and not dW[:, 4:].any()
     torch.cuda.synchronize()
+
+
+@pytest.mark.parametrize("T,dtype", [(60, BF), (60, F), (300, BF), (300, F)])
+def test_rows_of_very_large_and_very_small_gradients(T, dtype):
+    """dloss over fifty decades: each row of dX keeps its precision beside the largest one."""
+    V, d = 150, 64
+    g = gen(T)
+    W = (torch.randn(V, d, device="cuda", generator=g) / 4).to(dtype)
+    X = torch.randn(T, d, device="cuda", generator=g).to(dtype)
+    labels = torch.randint(0, V, (T,), device="cuda", generator=g).to(torch.int32)
+    dloss = 10.0 ** torch.linspace(-25, 25, T, device="cuda")
+    _, _, dX, dW = run_xent(tf.XentPlan(V, d, dtype, max_rows=T), X, W, labels, dloss)
+    for got, want, what in zip((dX, dW), grad_bounds(X, W, labels, dloss), ("dX", "dW")):
+        lu.check(got, *want, dtype, f"T{T} {dtype} {what}")
+    torch.cuda.synchronize()
