@@ -42,9 +42,11 @@ struct XentSpace {
     int32_t *list, *pos;          // row of X of a kept row; number of a row or -1
     int32_t *block_rows;          // kept rows of each block of rows
     float *block_top;             // largest |dloss| there
+    float *block_low, *block_high;       // smallest and largest dloss (fp16)
     int32_t *n;                   // kept rows
     unsigned *arrived;            // for blocks of rows: workgroups that have left their sums
     float *unit;                  // what sums of gradients are multiplied by at the end
+    int32_t *same;                // 1: all kept rows have the same dloss (fp16)
     int32_t *label;
     float *lse, *g, *hit;         // log of the sum, gradient over the unit, logit of the label (or, where the loss is given, minus that)
     float *dloss;                 // gradient of the row's loss (fp16)
@@ -62,7 +64,8 @@ constexpr int64_t kMostBlocks = 1024;      // of rows
 constexpr int kMostJoins = 1024;           // blocks of rows whose sums the last workgroup adds up
 constexpr int kJoinApart = 32;             // their counters: a line of memory each, else all workgroups would count in one
 // G in fp16.  Its first plane is what dX is made of: each row is over its own dloss times kRowUnit, so that a row keeps its precision whatever the others'
-// dloss is.  The second is what dW, a sum over the rows, is made of: all rows over the largest |dloss| times 2^-15.
+// dloss is.  The second is what dW, a sum over the rows, is made of: all rows over the largest |dloss| times 2^-15.  Where all rows have the same dloss, as a
+// mean's have, the first one serves both.
 constexpr float kRowUnit = 1.0f / 32768.0f;
 // Elements between the rows of x, w and G: rows a power of two apart would all lie in one channel of an XCD's L2.
 constexpr int64_t kRowPad = 64;
@@ -126,7 +129,8 @@ struct ProductLaunch {
     float *loss, *lse_out;        // (at out_row)
     void *G;
     int64_t g_ld, g_plane;
-    int32_t for_dx, for_dw;       // fp16: which planes of G are wanted
+    int32_t for_dx, for_dw;       // fp16: what G is wanted for
+    const int32_t *same;          // fp16: which plane is dW's
     float *slab;
     int64_t slab_ld, slab_size;
     int32_t add;                  // to what the slab holds

@@ -111,9 +111,12 @@ int64_t lay_out(tf_xent &p, char *base) {
     c.take(s.pos, d.max_rows);
     c.take(s.block_rows, tf::kMostBlocks);
     c.take(s.block_top, tf::kMostBlocks);
+    c.take(s.block_low, tf::kMostBlocks);
+    c.take(s.block_high, tf::kMostBlocks);
     c.take(s.n, 1);
     c.take(s.arrived, tf::kMostJoins * tf::kJoinApart);
     c.take(s.unit, 1);
+    c.take(s.same, 1);
     c.take(s.label, d.max_rows);
     c.take(s.lse, d.max_rows);
     c.take(s.g, d.max_rows);

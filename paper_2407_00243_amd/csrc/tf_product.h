@@ -337,7 +337,10 @@ __global__ __launch_bounds__(WM * WN * 64, TM * TN > 32 ? 1 : 2) void k_product(
     const int mt = 8 * band + in_band % high, nt = in_band / high;
     const int64_t m0 = (int64_t)mt * BM, n0 = (int64_t)nt * BN;
     Side M = a.M, N = a.N;
-    if (a.k_rows) M.rows = N.rows = kept;
+    if (a.k_rows) {
+        M.rows = N.rows = kept;
+        if (EL == TF_F16 && !*a.same) N.p = static_cast<const uint16_t *>(N.p) + a.g_plane;
+    }
     const int s0 = (int)((int64_t)steps * split / splits), s1 = (int)((int64_t)steps * (split + 1) / splits);
     const int pairs = a.parts == 3 ? 6 : 1, total = pairs * (s1 - s0);
     int pair = a.parts == 3 ? 0 : 5, in_pair = s1 - s0, to_load = total;
@@ -447,6 +450,7 @@ __global__ __launch_bounds__(WM * WN * 64, TM * TN > 32 ? 1 : 2) void k_product(
         // logit, 256 of them a lane.  What c = fl(top log2(e)) is off by scales all terms alike, by less than 2^-24 |top|.
         constexpr float LOG2E = 1.44269504088896340736f;
         const bool whole = mw + TM * 16 <= a.m_count;
+        const bool same = EL == TF_F16 && END == kEndGradient && *a.same, first_plane = a.for_dx || same, second_plane = a.for_dw && !same;
 #pragma unroll
         for (int y = 0; y < TN; ++y) {
             const int64_t row = nw + 16 * y;
@@ -547,8 +551,8 @@ __global__ __launch_bounds__(WM * WN * 64, TM * TN > 32 ? 1 : 2) void k_product(
 #pragma unroll
                         for (int i = 0; i < 3; ++i) *reinterpret_cast<U4 *>(out + i * a.g_plane + 16 * x) = U4{p[0][i], p[1][i], p[2][i], p[3][i]};
                     } else if constexpr (EL == TF_F16) {
-                        if (a.for_dx) put(d, 1.0f / kRowUnit, row_of_G, x, before[0]);
-                        if (a.for_dw) put(d, scale, row_of_G + a.g_plane, x, before[1]);
+                        if (first_plane) put(d, 1.0f / kRowUnit, row_of_G, x, before[0]);
+                        if (second_plane) put(d, scale, row_of_G + a.g_plane, x, before[1]);
                     } else {
                         put(d, 1.0f, row_of_G, x, before[0]);
                     }

@@ -105,36 +105,70 @@ __device__ __forceinline__ float wave_max(float x) {
     return x;
 }
 
-// What a row adds to a count of the rows that have a label; the largest finite |dloss| of those goes to `top`.
-__device__ __forceinline__ bool counts(const XentLaunch &a, int64_t row, float &top) {
-    const int y = a.labels[row];
-    const bool keep = y >= 0 && y < a.n_classes;
-    if (keep && a.dloss) {
-        const float g = fabsf(a.dloss[row]);
-        if (g < __builtin_inff()) top = fmaxf(top, g);
+// dloss of the rows that have a label: the largest finite size, and (fp16) the smallest and the largest number, +-infinity where one is not finite.
+template <bool BOTH> struct Gradients {
+    float top, low, high;
+    static __device__ __forceinline__ Gradients none() { return Gradients{0.0f, __builtin_inff(), kLow}; }
+    __device__ __forceinline__ void add(float g) {
+        const float size = fabsf(g);
+        const bool finite = size < __builtin_inff();
+        if (finite) top = fmaxf(top, size);
+        if constexpr (BOTH) {
+            low = fminf(low, finite ? g : kLow);
+            high = fmaxf(high, finite ? g : __builtin_inff());
+        }
     }
+    __device__ __forceinline__ void add(Gradients x) {
+        top = fmaxf(top, x.top);
+        if constexpr (BOTH) {
+            low = fminf(low, x.low);
+            high = fmaxf(high, x.high);
+        }
+    }
+    __device__ __forceinline__ void over_wave() {
+        top = wave_max(top);
+        if constexpr (BOTH) {
+            low = -wave_max(-low);
+            high = wave_max(high);
+        }
+    }
+};
+// Whether a row has a label.
+__device__ __forceinline__ bool counts(const XentLaunch &a, int64_t row) {
+    const int y = a.labels[row];
+    return y >= 0 && y < a.n_classes;
+}
+// The same, and what it adds to the gradients.
+template <bool BOTH> __device__ __forceinline__ bool counts(const XentLaunch &a, int64_t row, Gradients<BOTH> &g) {
+    const bool keep = counts(a, row);
+    if (keep && a.dloss) g.add(a.dloss[row]);
     return keep;
 }
 
 // Count and largest gradient of a block of rows a workgroup.
-__global__ __launch_bounds__(256) void k_count_rows(const XentLaunch a, const int block) {
+template <bool BOTH> __global__ __launch_bounds__(256) void k_count_rows(const XentLaunch a, const int block) {
     __shared__ int n_of[4];
-    __shared__ float top_of[4];
+    __shared__ Gradients<BOTH> g_of[4];
     const int tid = threadIdx.x;
     const int64_t first = (int64_t)blockIdx.x * block, end = min(first + block, (int64_t)a.n_rows);
     int n = 0;
-    float top = 0.0f;
-    for (int64_t r = first + tid; r < end; r += 256) n += counts(a, r, top);
+    Gradients<BOTH> g = Gradients<BOTH>::none();
+    for (int64_t r = first + tid; r < end; r += 256) n += counts(a, r, g);
     n = wave_sum(n);
-    top = wave_max(top);
+    g.over_wave();
     if ((tid & 63) == 0) {
         n_of[tid >> 6] = n;
-        top_of[tid >> 6] = top;
+        g_of[tid >> 6] = g;
     }
     __syncthreads();
     if (tid == 0) {
+        for (int w = 1; w < 4; ++w) g.add(g_of[w]);
         a.s.block_rows[blockIdx.x] = n_of[0] + n_of[1] + n_of[2] + n_of[3];
-        a.s.block_top[blockIdx.x] = fmaxf(fmaxf(top_of[0], top_of[1]), fmaxf(top_of[2], top_of[3]));
+        a.s.block_top[blockIdx.x] = g.top;
+        if constexpr (BOTH) {
+            a.s.block_low[blockIdx.x] = g.low;
+            a.s.block_high[blockIdx.x] = g.high;
+        }
     }
 }
 
@@ -158,44 +192,49 @@ template <int EL> __global__ __launch_bounds__(256) void k_pack_classes(const Xe
 // it; where there are few rows (`counted` 0) it counts them itself, which saves a launch.  Workgroups behind the `blocks` first ones pack W's first rows.
 // 8192 rows of 4096 bf16 numbers 38 us, 3.5 TB/s; one row 4.7 us, a chain of three loads.
 template <int EL> __global__ __launch_bounds__(256) void k_pack_rows(const XentLaunch a, const int block, const int blocks, const int counted, const int64_t classes) {
+    typedef Gradients<EL == TF_F16> Of;
     __shared__ int n_of[4], rows[256], ats[256];
-    __shared__ float top_of[4];
+    __shared__ Of g_of[4];
     if ((int)blockIdx.x >= blocks) return pack_classes<EL>(a, 0, classes, blockIdx.x - blocks, gridDim.x - blocks);
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int64_t first = (int64_t)blockIdx.x * block, end = min(first + block, (int64_t)a.n_rows);
     int n = 0;
-    float top = 0.0f;
+    Of g = Of::none();
     if (counted) {
         for (int b = tid; b < blocks; b += 256) {
             if (b < (int)blockIdx.x) n += a.s.block_rows[b];
-            top = fmaxf(top, a.s.block_top[b]);
+            if (a.dloss) g.add(EL == TF_F16 ? Of{a.s.block_top[b], a.s.block_low[b], a.s.block_high[b]} : Of{a.s.block_top[b], 0.0f, 0.0f});
         }
     } else {
         for (int64_t r = tid; r < (a.dloss ? (int64_t)a.n_rows : first); r += 256) {
-            const bool keep = counts(a, r, top);
+            const bool keep = counts(a, r, g);
             n += keep && r < first;
         }
     }
     n = wave_sum(n);
-    top = wave_max(top);
+    if (a.dloss) g.over_wave();
     if (lane == 0) {
         n_of[wave] = n;
-        top_of[wave] = top;
+        g_of[wave] = g;
     }
     __syncthreads();
     n = n_of[0] + n_of[1] + n_of[2] + n_of[3];
-    top = fmaxf(fmaxf(top_of[0], top_of[1]), fmaxf(top_of[2], top_of[3]));
+    for (int w = 0; w < 4; ++w) g.add(g_of[w]);
+    float top = g.top;
     // fp16: gradients are divided by the largest one, so that what dW, their sum, can hold is not lost in 16 bits.  The other types' range is that of the
     // results: only gradients that are all very small, or one as large as the type, are divided (others would pass the range that their sums stay in).
     const float scale = a.dtype == TF_F16 ? 32768.0f : 1.0f;
     if (top == 0.0f || (a.dtype != TF_F16 && top > 0x1p-64f && top < 0x1p126f)) top = 1.0f;
-    if (!a.loss && blockIdx.x == 0 && tid == 0) *a.s.unit = top / scale;       // (without rows there is no dloss)
+    if (!a.loss && blockIdx.x == 0 && tid == 0) {        // (without rows there is no dloss)
+        const bool same = EL == TF_F16 && g.low == g.high;
+        if (EL == TF_F16) *a.s.same = same;
+        *a.s.unit = (same ? g.high : top) / scale;
+    }
     const int64_t columns = round_up(a.n_in, 64);
     const int per_row = threads_of_row(columns), at_once = 256 / per_row;
     for (int64_t r0 = first; r0 < end; r0 += 256) {
         const int64_t r = r0 + tid;
-        float unused = 0.0f;
-        const bool keep = r < end && counts(a, r, unused);
+        const bool keep = r < end && counts(a, r);
         const uint64_t kept = __ballot(keep);
         __syncthreads();        // (the last round's lists have been read)
         if (lane == 0) n_of[wave] = __popcll(kept);
@@ -369,7 +408,7 @@ template <int EL, int KH> __global__ __launch_bounds__(256, KH > 1 ? 3 : 4) void
     const int64_t c0 = (int64_t)blockIdx.x * 256 + wave * 64, v_end = min(count, ((int64_t)blockIdx.y + 1) * each);
     if (c0 >= a.n_in) return;
     const float unit = *a.s.unit;
-    const uint16_t *G = static_cast<const uint16_t *>(a.s.G) + (EL == TF_F16 ? a.s.g_cap : 0);
+    const uint16_t *G = static_cast<const uint16_t *>(a.s.G) + (EL == TF_F16 && !*a.s.same ? a.s.g_cap : 0);
     V x[4][KH];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
@@ -479,7 +518,8 @@ bool in_place(const XentLaunch &a) { return a.dtype == TF_F32 ? a.native : whole
 int begin(const XentLaunch &a, int64_t classes, hipStream_t st) {
     const int counted = a.n_rows > 8192;
     const int64_t block = std::max<int64_t>(1, ceil_div(a.n_rows, kMostBlocks)), blocks = std::max<int64_t>(1, ceil_div(a.n_rows, block));
-    if (counted) hipLaunchKernelGGL(k_count_rows, dim3((unsigned)blocks), dim3(256), 0, st, a, (int)block);
+    if (counted && a.dtype == TF_F16) hipLaunchKernelGGL(k_count_rows<true>, dim3((unsigned)blocks), dim3(256), 0, st, a, (int)block);
+    else if (counted) hipLaunchKernelGGL(k_count_rows<false>, dim3((unsigned)blocks), dim3(256), 0, st, a, (int)block);
     const int64_t others = a.n_rows && !in_place(a) ? row_grid(classes, round_up(a.n_in, 64)).x : 0;
     TF_BY_TYPE(a.dtype, k_pack_rows, dim3((unsigned)(blocks + others)), a, (int)block, (int)blocks, counted, classes);
     return (int)hipGetLastError();
@@ -638,6 +678,7 @@ int launch_xent_grad(const XentLaunch &call, void *stream) {
             p.g_plane = a.s.g_cap;
             p.for_dx = a.dX != nullptr;
             p.for_dw = a.dW != nullptr;
+            p.same = a.s.same;
             e = launch_product(p, a, stream);
             if (e) return e;
             if (a.dX) {
@@ -676,7 +717,9 @@ int launch_xent_grad(const XentLaunch &call, void *stream) {
         } else if (a.dW) {
             ProductLaunch q{};
             q.M = Side{a.s.x, a.s.ld, a.s.x_plane, 0, a.s.ld};
-            q.N = Side{static_cast<uint16_t *>(a.s.G) + (a.dtype == TF_F16 ? a.s.g_cap : 0), g_ld, a.s.g_cap, 0, piece};
+            q.N = Side{a.s.G, g_ld, a.s.g_cap, 0, piece};
+            q.g_plane = a.s.g_cap;
+            q.same = a.s.same;
             q.parts = parts;
             q.n = a.s.n;
             q.k_rows = 1;

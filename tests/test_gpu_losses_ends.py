@@ -473,3 +473,33 @@ def test_rows_of_very_large_and_very_small_gradients(T, dtype):
     for got, want, what in zip((dX, dW), grad_bounds(X, W, labels, dloss), ("dX", "dW")):
         lu.check(got, *want, dtype, f"T{T} {dtype} {what}")
     torch.cuda.synchronize()
+
+
+@pytest.mark.parametrize("T,V,d", [(20, 300, 64), (60, 300, 64), (300, 2000, 100), (9000, 700, 24), (300000, 600, 8)])
+def test_fp16_gradients_that_are_all_the_same(T, V, d):
+    """Where all labelled rows have one dloss (of either sign, or zero) G has one plane; one other among them, and it has two.  On one plan, by turns."""
+    print(f"T{T} V{V} d{d}", flush=True)
+    g = gen(T)
+    W = (torch.randn(V, d, device="cuda", generator=g) / 4).to(HF)
+    X = torch.randn(T, d, device="cuda", generator=g).to(HF)
+    labels = torch.randint(0, V, (T,), device="cuda", generator=g).to(torch.int32)
+    plan = tf.XentPlan(V, d, HF, max_rows=T)
+    size = 1.0 / T if T < 1000 else 100.0 / T
+    for value, other in ((size, size), (-3 * size, -3 * size), (size, 5 * size), (0.0, 0.0), (-size, size), (2 * size, 2 * size)):
+        dloss = torch.full((T,), value, device="cuda")
+        dloss[T // 2] = other
+        want = grad_bounds(X, W, labels, dloss)
+        for grads in ("W", "XW", "X"):
+            _, _, dX, dW = run_xent(plan, X, W, labels, dloss, grads=grads)
+            for got, ref, what in zip((dX, dW), want, ("dX", "dW")):
+                if got is not None:
+                    lu.check(got, *ref, HF, f"{what} of {grads}, {value} {other}")
+    # what unlabelled rows have counts for nothing
+    labels[::3] = -1
+    dloss = torch.full((T,), size, device="cuda")
+    dloss[::3] = math.nan
+    ref = lu.xent(X, W, labels, dloss)
+    _, _, dX, dW = run_xent(plan, X, W, labels, dloss)
+    lu.check(dX, *ref["dX"], HF)
+    lu.check(dW, *ref["dW"], HF)
+    torch.cuda.synchronize()
